@@ -25,6 +25,12 @@
  *   hs_tree_attention_paged, hs_kv_commit_paged   the same two on caches made of pages
  *   hs_tree_attention_shared_tree   hs_tree_attention on batch entries that all verify one tree
  *
+ * and a step on a quantised cache, which holds a third to a half of what the bfloat16 cache holds in the same bytes:
+ *
+ *   hs_rotary, hs_tree_rotary   rotary positions of query and key rows; tree rows find theirs from the tree
+ *   hs_kv_append_mx, hs_kv_commit_mx, hs_kv_read_mx   prompt rows and accepted paths join the cache, and are read back
+ *   hs_tree_attention_mx        tree-masked attention over it
+ *
  * Conventions that hold for every call
  *   - Pointers are DEVICE pointers unless the parameter name starts with host_.  The caller owns
  *     every buffer; the library allocates and frees nothing, and keeps nothing after a call.
@@ -79,9 +85,31 @@ typedef enum {
   HS_PSTAR_LOCAL = 1       /* ... with the largest confidence of its own (final) token                 */
 } hs_pstar_mode;
 
+/* Element format of a quantised cache (see hs_kv_append_mx) */
+typedef enum {
+  HS_MX_E4M3 = 0, /* 8 bits: sign, 4 exponent and 3 mantissa bits, largest value 448 */
+  HS_MX_E2M1 = 1  /* 4 bits: 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives          */
+} hs_mx_format;
+
+typedef enum {
+  HS_ROTARY_HALF = 0,      /* pair j: elements j and j + rot_dim / 2 */
+  HS_ROTARY_NEIGHBOURS = 1 /* pair j: elements 2 j and 2 j + 1       */
+} hs_rotary_pairs;
+
+typedef enum { /* see hs_rotary_frequencies */
+  HS_ROTARY_PLAIN = 0,
+  HS_ROTARY_LINEAR = 1,
+  HS_ROTARY_BASE = 2,
+  HS_ROTARY_WAVELENGTH = 3,
+  HS_ROTARY_YARN = 4
+} hs_rotary_scaling;
+
 typedef void* hs_stream; /* a hipStream_t */
 
 #define HS_MAX_TOPK 64
+#define HS_MX_PAGE 64              /* tokens of a page of a quantised cache                      */
+#define HS_MX_BLOCK 32             /* neighbours of a row that share a scale                     */
+#define HS_MX_MAX_TOKENS 16777216  /* prefix tokens of a sequence that hs_tree_attention_mx takes */
 #define HS_MAX_CHILDREN 256 /* children of one node that the sampling accept rules try (see hs_verify_accept) */
 
 /* Static description of a status code; never NULL, never freed. */
@@ -452,6 +480,117 @@ hs_status hs_kv_commit_paged(const void* k_tree, const void* v_tree, const int32
                              void* k_pages, void* v_pages, const int32_t* block_table, int32_t max_blocks,
                              int32_t page_tokens, int64_t* cache_lens,
                              int32_t B, int32_t Hkv, int32_t D, hs_dtype dt, hs_stream stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * hs_rotary, hs_tree_rotary  (what the attention calls leave to their caller: "no positional encoding is applied")
+ *
+ * The first rot_dim elements of every head's row are turned, pair by pair: row n at position p, pair j, angle
+ *   t = p * inv_freq[j]          (double precision: exact to 2^-50 of a turn for every position below 2^24 or so)
+ *   (a, b) -> mscale * (a cos t - b sin t, b cos t + a sin t)
+ * with (a, b) = elements (j, j + rot_dim / 2) (HS_ROTARY_HALF) or (2 j, 2 j + 1) (HS_ROTARY_NEIGHBOURS) of the head.  The
+ * elements behind rot_dim are copied as they are.
+ *   q [N,Hq,D] and k [N,Hkv,D] of element type dt, computed in float32 and rounded once; row n begins at
+ *   base + n * stride (elements, at least heads * D: a slice of a fused projection, say), its heads are dense.
+ *   Hkv = 0: no k.  q_out / k_out likewise; an output may be its input itself (same base and stride), other overlaps
+ *   are not allowed.
+ *   inv_freq [rot_dim / 2] double (device; hs_rotary_frequencies makes it).
+ * hs_rotary: positions [N] int64.
+ * hs_tree_rotary: the rows of B draft trees (node_offsets [B+1], parent [N] local, as everywhere): the root is at position
+ *   prefix_lens[s] (int64 [B]: the tokens in the cache, the root's own not among them), a row at that plus its depth.
+ *   Trees of any size; parents of a sequence's rows beyond the 1024th are followed one by one.  B = 0 with N = 0 only.
+ * A rotation's gradient, and its undoing where mscale is 1, is the rotation by the opposite angles: the same call with
+ * inv_freq negated.
+ * Requires rot_dim even, 2 <= rot_dim <= D <= 1024, (Hq + Hkv) * D <= 2^24.  No workspace.  Rows that begin at
+ * multiples of 16 bytes, strides, D and rot_dim / 2 (HS_ROTARY_NEIGHBOURS: rot_dim) that are multiples of eight take the faster path.
+ */
+hs_status hs_rotary(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const int64_t* positions,
+                    int32_t N, int32_t Hq, int32_t Hkv, int32_t D, hs_dtype dt,
+                    const double* inv_freq, int32_t rot_dim, hs_rotary_pairs pairs, float mscale,
+                    void* q_out, int64_t q_out_stride, void* k_out, int64_t k_out_stride, hs_stream stream);
+hs_status hs_tree_rotary(const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                         const int32_t* parent, const int32_t* node_offsets, const int64_t* prefix_lens, int32_t B,
+                         int32_t N, int32_t Hq, int32_t Hkv, int32_t D, hs_dtype dt,
+                         const double* inv_freq, int32_t rot_dim, hs_rotary_pairs pairs, float mscale,
+                         void* q_out, int64_t q_out_stride, void* k_out, int64_t k_out_stride, hs_stream stream);
+
+/* hs_rotary_frequencies: the table inv_freq of a rotation, and the factor on its result, written to HOST memory
+ * (host_inv_freq [rot_dim / 2] double, host_mscale).  With f_j = base^(-2 j / rot_dim):
+ *   HS_ROTARY_PLAIN       f_j
+ *   HS_ROTARY_LINEAR      f_j / factor
+ *   HS_ROTARY_BASE        base * factor^(rot_dim / (rot_dim - 2)) in the place of base  (rot_dim > 2)
+ *   HS_ROTARY_WAVELENGTH  (1 - t) f_j / factor + t f_j,  t = (turns - low) / (high - low) within [0, 1], turns = context * f_j / (2 pi):
+ *                         waves that turn less than `low` times within the context are stretched, those that turn
+ *                         more than `high` times are not
+ *   HS_ROTARY_YARN        the same blend with 1 - t a ramp over the pairs, from floor(c(high)) to ceil(c(low)),
+ *                         c(turns) = rot_dim ln(context / (2 pi turns)) / (2 ln base), both within [0, rot_dim - 1];
+ *                         mscale = 0.1 ln(factor) + 1
+ * mscale is 1 but for HS_ROTARY_YARN.  factor >= 1; context, low, high are looked at by the last two only.  No device work. */
+hs_status hs_rotary_frequencies(int32_t rot_dim, double base, hs_rotary_scaling scaling, double factor,
+                                double context, double low, double high, double* host_inv_freq, float* host_mscale);
+
+/* ------------------------------------------------------------------------------------------------
+ * hs_kv_append_mx, hs_kv_commit_mx, hs_kv_read_mx  (a KV cache of 8- or 4-bit elements)
+ *
+ * The cache is paged: k_codes / v_codes are pools [n_pages, Hkv, HS_MX_PAGE, D] of elements (HS_MX_E4M3: a byte each;
+ * HS_MX_E2M1: two to a byte, the even one in the low half), k_scales / v_scales bytes [n_pages, Hkv, HS_MX_PAGE, D / HS_MX_BLOCK].
+ * block_table [B, max_blocks] int32 names the page of each 64 tokens of a sequence.  The 32 neighbours of a row that
+ * share a scale have an exponent e: the least for which the largest of their magnitudes is at most 448 * 2^e (6 * 2^e), and
+ * -100 at least.  An element is x / 2^e rounded to the format (nearest, ties to even; nothing saturates), the scale byte is
+ * e + 127, and an element read back is code * 2^e, which a bfloat16 holds exactly (magnitudes beyond 1.875 * 2^127 may round to
+ * 2^128, which reads as infinity).  A block with a NaN or an infinity in it has scale byte 255 and reads back as NaN.
+ *
+ * hs_kv_append_mx: rows node_offsets[s] .. node_offsets[s+1] - 1 of k and v (element type dt; row n begins at
+ *   base + n * stride, a row is [Hkv, D]) become tokens cache_lens[s], cache_lens[s] + 1, ... of sequence s.  NN = node_offsets[B].
+ * hs_kv_commit_mx: the rows of the tree's root and of the accepted path, as in hs_kv_commit.
+ * Both leave cache_lens (int64 [B]) alone, so that the layers of a model share it; new_lens (int64 [B], may be NULL, must not overlap
+ *   cache_lens) receives cache_lens[s] plus the rows that sequence s took.  A sequence takes at most max_blocks * 64 tokens: the
+ *   leading rows that fit.  Rows whose block-table entry is not a page (0 .. n_pages - 1) are dropped.
+ * hs_kv_read_mx: tokens first[s] .. (int64 [B], device; NULL: from 0) of sequence s as rows out_offsets[s] .. out_offsets[s+1] - 1
+ *   (int64 [B+1], device; total = out_offsets[B]) of k_out / v_out [total, Hkv, D] of element type dt.  The tokens must have been stored.
+ *   Rows beyond the table, or of entries that are no page, are left as they were.
+ * Requires D to be a multiple of 32 and rows that begin at multiples of 16 bytes.  No workspace.
+ */
+hs_status hs_kv_append_mx(const void* k, int64_t k_stride, const void* v, int64_t v_stride, const int32_t* node_offsets, int32_t NN,
+                          void* k_codes, void* k_scales, void* v_codes, void* v_scales, hs_mx_format fmt,
+                          const int32_t* block_table, int32_t max_blocks, int32_t n_pages,
+                          const int64_t* cache_lens, int64_t* new_lens,
+                          int32_t B, int32_t Hkv, int32_t D, hs_dtype dt, hs_stream stream);
+hs_status hs_kv_commit_mx(const void* k_tree, int64_t k_stride, const void* v_tree, int64_t v_stride,
+                          const int32_t* node_offsets, const int32_t* accept_path, const int32_t* accept_len, int32_t max_depth,
+                          void* k_codes, void* k_scales, void* v_codes, void* v_scales, hs_mx_format fmt,
+                          const int32_t* block_table, int32_t max_blocks, int32_t n_pages,
+                          const int64_t* cache_lens, int64_t* new_lens,
+                          int32_t B, int32_t Hkv, int32_t D, hs_dtype dt, hs_stream stream);
+hs_status hs_kv_read_mx(const void* k_codes, const void* k_scales, const void* v_codes, const void* v_scales, hs_mx_format fmt,
+                        const int32_t* block_table, int32_t max_blocks, int32_t n_pages,
+                        const int64_t* first, const int64_t* out_offsets, int64_t total, void* k_out, void* v_out,
+                        int32_t B, int32_t Hkv, int32_t D, hs_dtype dt, hs_stream stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * hs_tree_attention_mx  (hs_tree_attention_paged on a quantised cache; decoding of single tokens: trees of one row)
+ *
+ * o[i,h,:] = softmax_j( scale * <q[i,h,:], k[j,g,:]> ) . v[j,g,:] over j = the prefix_lens[s] stored tokens of sequence s, with the
+ * values that hs_kv_read_mx reads back, and the tree rows on the root path of i, which come from k_tree / v_tree as they are.
+ *   q [NN,Hq,D], k_tree, v_tree [NN,Hkv,D] bfloat16, row n at base + n * stride (elements); o [NN,Hq,D] bfloat16, dense.
+ *   parent, node_offsets, host_node_offsets, prefix_lens, host_prefix_lens, lse as in hs_tree_attention_paged: the host copies are what
+ *   the launch is planned from, they must equal the device arrays, and a captured launch keeps them.
+ * Float32 sums and softmax; P is rounded to bfloat16 for the second product, the output once.  A token with a NaN block makes
+ * the rows that see it NaN.  Block-table entries behind a sequence's last token are not looked at.
+ * Requires dt = HS_BF16, D in {64, 128}, Hq % Hkv == 0, at most 1024 tree rows per sequence, scale > 0, rows that begin at
+ * multiples of 16 bytes.
+ * Workspace: one record of D + 4 floats per (tree row, query head, key split); the query gives what a call with these host arrays
+ * needs (0: none; also for arrays that the call would refuse), at most 2^18 records.
+ */
+size_t hs_tree_attention_mx_workspace(const int32_t* host_node_offsets, const int64_t* host_prefix_lens,
+                                      int32_t B, int32_t Hq, int32_t Hkv, int32_t D);
+hs_status hs_tree_attention_mx(const void* q, int64_t q_stride,
+                               const void* k_codes, const void* k_scales, const void* v_codes, const void* v_scales,
+                               hs_mx_format fmt, const void* k_tree, int64_t k_stride, const void* v_tree, int64_t v_stride,
+                               const int32_t* parent, const int32_t* node_offsets, const int32_t* host_node_offsets,
+                               const int32_t* block_table, int32_t max_blocks, int32_t n_pages,
+                               const int64_t* prefix_lens, const int64_t* host_prefix_lens,
+                               int32_t B, int32_t Hq, int32_t Hkv, int32_t D, hs_dtype dt, float scale,
+                               void* o, float* lse, void* workspace, size_t workspace_bytes, hs_stream stream);
 
 /* ------------------------------------------------------------------------------------------------
  * hs_time_next_attention  (measurement aid, not a step of the method)

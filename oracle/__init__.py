@@ -25,6 +25,10 @@ Pin status (see tests/test_oracle_*.py):
                       commits equals dense causal attention (torch) over the whole sequence; the
                       paged forms (kv_commit_paged, gather_pages) by scatter / gather identity and
                       equality with the dense commit.
+  rotary              pinned (tests/test_oracle_mx.py): lengths of pairs, scores that depend on the distance alone,
+                      hand-worked quarter turns, differences.
+  mx_cache            pinned: hand-worked codes and ties, every code a fixed point, the least scale, brute force over
+                      all values of the format.
 """
 from .entropy_topk import draft_entropy_topk
 from .tree_prune import tree_prune
@@ -33,5 +37,8 @@ from .verify_accept import verify_accept
 from .adaptive_control import adaptive_control
 from .tree_expand import tree_expand
 from .kv_commit import kv_commit
+from . import mx_cache
+from .rotary import rotary, tree_positions
 
-__all__ = ["draft_entropy_topk", "tree_prune", "tree_attention", "verify_accept", "adaptive_control", "tree_expand", "kv_commit"]
+__all__ = ["draft_entropy_topk", "tree_prune", "tree_attention", "verify_accept", "adaptive_control", "tree_expand", "kv_commit", "mx_cache",
+           "rotary", "tree_positions"]

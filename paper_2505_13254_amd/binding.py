@@ -22,6 +22,10 @@ HS_ERR_WORKSPACE = 4
 HS_ACCEPT_GREEDY, HS_ACCEPT_STOCHASTIC, HS_ACCEPT_STOCHASTIC_POINTMASS = 0, 1, 2
 HS_PSTAR_CUMULATIVE, HS_PSTAR_LOCAL = 0, 1
 HS_MAX_TOPK = 64
+HS_MX_E4M3, HS_MX_E2M1 = 0, 1
+HS_MX_PAGE, HS_MX_BLOCK = 64, 32
+HS_ROTARY_HALF, HS_ROTARY_NEIGHBOURS = 0, 1
+HS_ROTARY_SCALINGS = {"none": 0, "linear": 1, "base": 2, "wavelength": 3, "yarn": 4}
 
 _c = ctypes
 _vp, _i32, _i64, _f32, _sz = _c.c_void_p, _c.c_int32, _c.c_int64, _c.c_float, _c.c_size_t
@@ -58,6 +62,20 @@ _SIGNATURES = {
     "hs_kv_commit_paged": (_c.c_int, [_vp, _vp, _vp, _vp, _vp, _i32, _vp, _vp, _vp, _i32, _i32, _vp, _i32, _i32, _i32,
                                       _c.c_int, _vp]),
     "hs_kv_commit": (_c.c_int, [_vp, _vp, _vp, _vp, _vp, _i32, _vp, _vp, _vp, _vp, _i32, _i32, _i32, _c.c_int, _vp]),
+    "hs_rotary": (_c.c_int, [_vp, _i64, _vp, _i64, _vp, _i32, _i32, _i32, _i32, _c.c_int, _vp, _i32, _c.c_int, _f32, _vp, _i64,
+                             _vp, _i64, _vp]),
+    "hs_tree_rotary": (_c.c_int, [_vp, _i64, _vp, _i64, _vp, _vp, _vp, _i32, _i32, _i32, _i32, _i32, _c.c_int, _vp, _i32,
+                                  _c.c_int, _f32, _vp, _i64, _vp, _i64, _vp]),
+    "hs_rotary_frequencies": (_c.c_int, [_i32, _c.c_double, _c.c_int, _c.c_double, _c.c_double, _c.c_double, _c.c_double, _vp, _vp]),
+    "hs_kv_append_mx": (_c.c_int, [_vp, _i64, _vp, _i64, _vp, _i32, _vp, _vp, _vp, _vp, _c.c_int, _vp, _i32, _i32, _vp, _vp, _i32,
+                                   _i32, _i32, _c.c_int, _vp]),
+    "hs_kv_commit_mx": (_c.c_int, [_vp, _i64, _vp, _i64, _vp, _vp, _vp, _i32, _vp, _vp, _vp, _vp, _c.c_int, _vp, _i32, _i32, _vp,
+                                   _vp, _i32, _i32, _i32, _c.c_int, _vp]),
+    "hs_kv_read_mx": (_c.c_int, [_vp, _vp, _vp, _vp, _c.c_int, _vp, _i32, _i32, _vp, _vp, _i64, _vp, _vp, _i32, _i32, _i32,
+                                 _c.c_int, _vp]),
+    "hs_tree_attention_mx_workspace": (_sz, [_vp, _vp, _i32, _i32, _i32, _i32]),
+    "hs_tree_attention_mx": (_c.c_int, [_vp, _i64, _vp, _vp, _vp, _vp, _c.c_int, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _vp, _i32, _i32,
+                                        _vp, _vp, _i32, _i32, _i32, _i32, _c.c_int, _f32, _vp, _vp, _vp, _sz, _vp]),
     "hs_tree_validate": (_c.c_int, [_vp, _vp, _vp, _i32, _i32, _vp, _vp]),
     "hs_time_next_attention": (_c.c_int, [_vp, _vp]),
     "hs_tree_attention_last_kernel": (_c.c_int32, []),
@@ -394,6 +412,165 @@ def hs_kv_commit(k_tree, v_tree, node_offsets, accept_path, accept_len, k_cache,
                              cache_offsets, cache_lens, B, Hkv, D, stream)
     _check(st, "hs_kv_commit")
     return cache_lens
+
+
+def hs_rotary_frequencies(rot_dim: int, base: float = 10000.0, *, scaling: str = "none", factor: float = 1.0, context: float = 0.0,
+                          low: float = 1.0, high: float = 4.0, device=None):
+    """The table of a rotation: (inv_freq float64 [rot_dim / 2] on `device`, mscale).  scaling: "none", "linear", "base",
+    "wavelength" or "yarn" (whose usual low and high are 1 and 32)."""
+    if scaling not in HS_ROTARY_SCALINGS:
+        raise ValueError("scaling must be one of %s" % ", ".join(HS_ROTARY_SCALINGS))
+    table = torch.empty(max(0, int(rot_dim)) // 2, dtype=torch.float64)
+    m = _f32(1.0)
+    _check(lib().hs_rotary_frequencies(int(rot_dim), float(base), HS_ROTARY_SCALINGS[scaling], float(factor), float(context), float(low),
+                                       float(high), table.data_ptr(), _c.byref(m)), "hs_rotary_frequencies")
+    return table if device is None else table.to(device), float(m.value)
+
+
+def _rotary_args(q, k, inv_freq, q_out, k_out):
+    if q.dim() != 3 or (k is not None and (k.dim() != 3 or k.shape[0] != q.shape[0] or k.shape[2] != q.shape[2])):
+        raise ValueError("q and k must be [N, heads, D] with the same N and D")
+    if q_out is None:
+        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    if k_out is None and k is not None:
+        k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
+    if q_out.shape != q.shape or (k_out is None) != (k is None) or (k is not None and k_out.shape != k.shape):
+        raise ValueError("outputs must have their inputs' shapes")
+    return q_out, k_out, (0 if k is None else k.shape[1])
+
+
+def hs_rotary(q, k, positions, inv_freq, *, interleaved: bool = False, mscale: float = 1.0, q_out=None, k_out=None, stream=None):
+    """q [N,Hq,D], k [N,Hkv,D] or None (float32 or bfloat16, GPU; rows may have a stride of their own, e.g. slices of a fused
+    projection), positions int64 [N], inv_freq float64 [rot_dim / 2] on the GPU (hs_rotary_frequencies).  interleaved: pairs
+    are neighbours, otherwise halves.  q_out / k_out may be q / k themselves.  Returns (q_out, k_out)."""
+    q_out, k_out, Hkv = _rotary_args(q, k, inv_freq, q_out, k_out)
+    N, Hq, D = q.shape
+    if positions.numel() != N:
+        raise ValueError("positions must hold N values")
+    _check(_calls.hs_rotary(q, k, positions, N, Hq, Hkv, D, inv_freq, 2 * inv_freq.numel(),
+                            HS_ROTARY_NEIGHBOURS if interleaved else HS_ROTARY_HALF, mscale, q_out, k_out, stream), "hs_rotary")
+    return q_out, k_out
+
+
+def hs_tree_rotary(q, k, parent, node_offsets, prefix_lens, inv_freq, *, interleaved: bool = False, mscale: float = 1.0, q_out=None,
+                   k_out=None, stream=None):
+    """hs_rotary of the rows of draft trees (parent int32 [N], node_offsets int32 [B+1], GPU): a row's position is
+    prefix_lens[s] (int64 [B], GPU) plus its depth."""
+    q_out, k_out, Hkv = _rotary_args(q, k, inv_freq, q_out, k_out)
+    N, Hq, D = q.shape
+    B = node_offsets.numel() - 1
+    if parent.numel() != N or prefix_lens.numel() != B:
+        raise ValueError("parent must hold N values, prefix_lens B")
+    _check(_calls.hs_tree_rotary(q, k, parent, node_offsets, prefix_lens, B, N, Hq, Hkv, D, inv_freq, 2 * inv_freq.numel(),
+                                 HS_ROTARY_NEIGHBOURS if interleaved else HS_ROTARY_HALF, mscale, q_out, k_out, stream), "hs_tree_rotary")
+    return q_out, k_out
+
+
+def new_mx_cache(n_pages: int, Hkv: int, D: int, fmt: int = HS_MX_E4M3, device="cuda:0") -> Dict[str, torch.Tensor]:
+    """Pools of a quantised cache (uninitialised): k_codes, v_codes [n_pages, Hkv, 64, D] float8_e4m3fn, or
+    [n_pages, Hkv, 64, D / 2] uint8 (two 4-bit elements to a byte), and k_scales, v_scales uint8 [n_pages, Hkv, 64, D / 32]."""
+    if fmt not in (HS_MX_E4M3, HS_MX_E2M1) or D % HS_MX_BLOCK != 0:
+        raise ValueError("fmt must be HS_MX_E4M3 or HS_MX_E2M1, D a multiple of %d" % HS_MX_BLOCK)
+    wide, kind = (D, torch.float8_e4m3fn) if fmt == HS_MX_E4M3 else (D // 2, torch.uint8)
+    c = {}
+    for n in ("k", "v"):
+        c[n + "_codes"] = torch.empty((n_pages, Hkv, HS_MX_PAGE, wide), dtype=kind, device=device)
+        c[n + "_scales"] = torch.empty((n_pages, Hkv, HS_MX_PAGE, D // HS_MX_BLOCK), dtype=torch.uint8, device=device)
+    return c
+
+
+def _mx_cache(cache, block_table, B):
+    """(k_codes, k_scales, v_codes, v_scales, format), pages, Hkv, D of a cache as new_mx_cache makes it."""
+    kc, ks, vc, vs = cache["k_codes"], cache["k_scales"], cache["v_codes"], cache["v_scales"]
+    fmt = HS_MX_E4M3 if kc.dtype == torch.float8_e4m3fn else HS_MX_E2M1
+    if kc.dim() != 4 or ks.dim() != 4 or kc.shape[2] != HS_MX_PAGE:
+        raise ValueError("a cache's codes must be [n_pages, Hkv, %d, D] and its scales [n_pages, Hkv, %d, D / %d]" % (HS_MX_PAGE, HS_MX_PAGE, HS_MX_BLOCK))
+    n_pages, Hkv, _, wide = kc.shape
+    D = wide if fmt == HS_MX_E4M3 else 2 * wide
+    if vc.dtype != kc.dtype or vc.shape != kc.shape or vs.shape != ks.shape or tuple(ks.shape) != (n_pages, Hkv, HS_MX_PAGE, D // HS_MX_BLOCK):
+        raise ValueError("the cache's four tensors do not fit each other")
+    if block_table.dim() != 2 or block_table.shape[0] != B:
+        raise ValueError("block_table must be [B, max_blocks]")
+    return (kc, ks, vc, vs, fmt), n_pages, Hkv, D
+
+
+def _mx_store_args(k, v, cache, block_table, cache_lens, new_lens, B):
+    pool, n_pages, Hkv, D = _mx_cache(cache, block_table, B)
+    if k.dim() != 3 or k.shape != v.shape or k.shape[1] != Hkv or k.shape[2] != D:
+        raise ValueError("k and v must be [NN, Hkv, D] of the cache's Hkv and D")
+    if cache_lens.numel() != B or (new_lens is not None and new_lens.numel() != B):
+        raise ValueError("cache_lens and new_lens must hold B values")
+    return pool, (block_table, block_table.shape[1], n_pages, cache_lens, new_lens, B, Hkv, D)
+
+
+def hs_kv_append_mx(k, v, node_offsets, cache, block_table, cache_lens, *, new_lens=None, stream=None) -> None:
+    """k, v [NN,Hkv,D] (float32 or bfloat16, GPU; rows may have a stride of their own): rows node_offsets[s] .. of sequence s
+    (int32 [B+1]) become its tokens cache_lens[s] .. (int64 [B], left alone) in `cache` (new_mx_cache) through block_table int32
+    [B, max_blocks].  new_lens (int64 [B] or None) receives the lengths afterwards."""
+    pool, rest = _mx_store_args(k, v, cache, block_table, cache_lens, new_lens, node_offsets.numel() - 1)
+    _check(_calls.hs_kv_append_mx(k, v, node_offsets, k.shape[0], *pool, *rest, stream), "hs_kv_append_mx")
+
+
+def hs_kv_commit_mx(k_tree, v_tree, node_offsets, accept_path, accept_len, cache, block_table, cache_lens, *, new_lens=None,
+                    stream=None) -> None:
+    """As hs_kv_append_mx, with the tree's root and the accepted rows (accept_path int32 [B, max_depth], accept_len int32 [B], as
+    hs_verify_accept writes them)."""
+    B = node_offsets.numel() - 1
+    pool, rest = _mx_store_args(k_tree, v_tree, cache, block_table, cache_lens, new_lens, B)
+    if accept_path.dim() != 2 or accept_path.shape[0] != B or accept_len.numel() != B:
+        raise ValueError("accept_path must be [B, max_depth], accept_len [B]")
+    _check(_calls.hs_kv_commit_mx(k_tree, v_tree, node_offsets, accept_path, accept_len, accept_path.shape[1], *pool, *rest, stream),
+           "hs_kv_commit_mx")
+
+
+def hs_kv_read_mx(cache, block_table, out_offsets, total: int, *, first=None, dtype=torch.bfloat16, out=None, stream=None):
+    """Tokens first[s] .. (int64 [B], GPU; None: from 0) of sequence s as rows out_offsets[s] .. out_offsets[s+1] - 1 (int64 [B+1],
+    GPU; total = the last) of two tensors [total, Hkv, D], `out` or new ones of `dtype`.  Returns (k, v)."""
+    B = out_offsets.numel() - 1
+    pool, n_pages, Hkv, D = _mx_cache(cache, block_table, B)
+    if out is None:
+        out = tuple(torch.empty((total, Hkv, D), dtype=dtype, device=block_table.device) for _ in range(2))
+    if any(tuple(t.shape) != (total, Hkv, D) for t in out) or (first is not None and first.numel() != B):
+        raise ValueError("out must be two tensors [total, Hkv, D], first must hold B values")
+    _check(_calls.hs_kv_read_mx(*pool, block_table, block_table.shape[1], n_pages, first, out_offsets, total, out[0], out[1], B, Hkv, D,
+                                stream), "hs_kv_read_mx")
+    return out[0], out[1]
+
+
+def hs_tree_attention_mx_workspace(host_node_offsets, host_prefix_lens, Hq: int, Hkv: int, D: int, device) -> Optional[torch.Tensor]:
+    """A workspace for hs_tree_attention_mx calls of these row counts and lengths (CPU tensors); None where none is needed."""
+    no, pl = host_node_offsets.to(torch.int32).contiguous(), host_prefix_lens.to(torch.int64).contiguous()
+    n = lib().hs_tree_attention_mx_workspace(no.data_ptr(), pl.data_ptr(), no.numel() - 1, int(Hq), int(Hkv), int(D))
+    return workspace(n, device)
+
+
+def hs_tree_attention_mx(q, cache, k_tree, v_tree, parent, node_offsets, host_node_offsets, block_table, prefix_lens,
+                         host_prefix_lens, scale: float, *, want_lse: bool = False, out: Optional[torch.Tensor] = None,
+                         lse: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None, stream=None):
+    """hs_tree_attention_paged on a quantised cache (new_mx_cache): q [NN,Hq,D], k_tree, v_tree [NN,Hkv,D] bfloat16 (GPU; rows may
+    have a stride of their own).  Returns (o [NN,Hq,D], lse [NN,Hq] or None)."""
+    if q.dim() != 3:
+        raise ValueError("q must be [NN, Hq, D]")
+    NN, Hq, D = q.shape
+    B = host_node_offsets.numel() - 1
+    pool, n_pages, Hkv, cache_D = _mx_cache(cache, block_table, B)
+    if cache_D != D or tuple(k_tree.shape) != (NN, Hkv, D) or v_tree.shape != k_tree.shape:
+        raise ValueError("k_tree and v_tree must be [NN, Hkv, D] of the cache's Hkv, and D that of q")
+    if parent.numel() != NN or node_offsets.numel() != B + 1 or prefix_lens.numel() != B or host_prefix_lens.numel() != B or \
+            (B > 0 and int(host_node_offsets[B]) != NN):
+        raise ValueError("parent must hold NN values, the offsets B + 1 (the last one NN), the lengths B")
+    if out is None:
+        out = torch.empty((NN, Hq, D), dtype=q.dtype, device=q.device)
+    if want_lse and lse is None:
+        lse = torch.empty((NN, Hq), dtype=torch.float32, device=q.device)
+    if out.shape != q.shape or (lse is not None and lse.numel() != NN * Hq):
+        raise ValueError("out must be [NN, Hq, D], lse [NN, Hq]")
+    if ws is None:
+        ws = hs_tree_attention_mx_workspace(host_node_offsets, host_prefix_lens, Hq, Hkv, D, q.device)
+    _check(_calls.hs_tree_attention_mx(q, *pool, k_tree, v_tree, parent, node_offsets, host_node_offsets, block_table,
+                                       block_table.shape[1], n_pages, prefix_lens, host_prefix_lens, B, Hq, Hkv, D, scale, out, lse, ws,
+                                       stream), "hs_tree_attention_mx")
+    return out, lse
 
 
 def hs_verify_accept(target_logits, draft_logits, token, parent, node_offsets, mode: int, temperature: float,

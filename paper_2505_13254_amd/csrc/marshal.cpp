@@ -28,6 +28,9 @@ namespace {
 // One code to a parameter of the C function.  Tensors: on the GPU and contiguous, of the type that the code says.
 //   i l f u   int32, int64, float32, uint8        (I F: may be None)
 //   t         float32 or bfloat16, all of a call of one type; D: that type's code (takes no argument)
+//   r         like t, but [rows, heads, D] with a row stride of its own, which follows as the next parameter (code R, takes no argument);
+//             O: may be None
+//   x         float64; c: the elements of a quantised cache (float8_e4m3fn or uint8), L: int64 that may be None
 //   o         an address only, not looked at any further (may be None)
 //   h H       on the host, int32 or int64, whatever its layout (converted where needed)
 //   w W       a workspace tensor (may be None) and, without an argument of its own, its size
@@ -35,8 +38,9 @@ namespace {
 struct Entry {
   const char* name;
   const char* codes;
-  const char* names;  // of the arguments that are checked (codes i l f u I F t), in order
+  const char* names;  // of the arguments that are checked (codes i l f u I F t r O x c L), in order
   PyObject* (*call)(const Entry&, void*, PyObject* const*, Py_ssize_t);
+  bool one_device;    // every checked tensor has to be on the current device (whose stream the call takes by default)
 };
 
 struct Failed {};  // a Python error is set
@@ -48,6 +52,7 @@ const char* type_name(at::ScalarType t) {
     case at::kFloat: return "torch.float32";
     case at::kByte: return "torch.uint8";
     case at::kBFloat16: return "torch.bfloat16";
+    case at::kDouble: return "torch.float64";
     default: return "torch";
   }
 }
@@ -62,6 +67,8 @@ struct Call {
   bool typed = false;
   at::ScalarType type = at::kFloat;
   size_t ws_bytes = 0;
+  int64_t row_stride = 0;
+  int device = -1;
   std::vector<at::Tensor> keep;             // converted host arrays, until the call has returned
   std::vector<std::vector<float>> floats;
 
@@ -88,6 +95,53 @@ struct Call {
     }
     return THPVariable_Unpack(o);
   }
+  void on_device(const at::Tensor& t) {
+    if (!e.one_device) return;
+    if (device < 0) device = c10::impl::getDeviceGuardImpl(c10::DeviceType::CUDA)->getDevice().index();
+    if (t.device().index() == device) return;
+    PyErr_Format(PyExc_ValueError, "%s is on another device than the current one (%d)", next_name().c_str(), device);
+    throw Failed{};
+  }
+  // one type for all tensors of codes t, r, O
+  void of_type(PyObject* o) {
+    if (!typed) {
+      type = tensor(o).scalar_type();
+      if (type != at::kFloat && type != at::kBFloat16) {
+        PyErr_SetString(PyExc_ValueError, "q/k/v must be float32 or bfloat16");
+        throw Failed{};
+      }
+      typed = true;
+    }
+  }
+  void* strided(bool optional) {
+    PyObject* o = next();
+    if (optional && o == Py_None) {
+      next_name();
+      row_stride = 0;
+      return nullptr;
+    }
+    of_type(o);
+    const at::Tensor& t = tensor(o);
+    if (!t.is_cuda() || t.scalar_type() != type || t.dim() != 3 || (t.size(2) > 1 && t.stride(2) != 1) ||
+        (t.size(1) > 1 && t.stride(1) != t.size(2)) || t.stride(0) < 0) {
+      PyErr_Format(PyExc_ValueError, "%s must be a %s tensor [rows, heads, D] on the GPU whose heads are dense", next_name().c_str(), type_name(type));
+      throw Failed{};
+    }
+    on_device(t);
+    next_name();
+    row_stride = t.size(0) > 1 ? t.stride(0) : t.size(1) * t.size(2);
+    return t.data_ptr();
+  }
+  void* elements() {
+    const at::Tensor& t = tensor(next());
+    if (!t.is_cuda() || (t.scalar_type() != at::kFloat8_e4m3fn && t.scalar_type() != at::kByte) || !t.is_contiguous()) {
+      PyErr_Format(PyExc_ValueError, "%s must be a contiguous float8_e4m3fn or uint8 tensor on the GPU", next_name().c_str());
+      throw Failed{};
+    }
+    on_device(t);
+    next_name();
+    return t.data_ptr();
+  }
   void* checked(at::ScalarType want, bool optional) {
     PyObject* o = next();
     if (optional && o == Py_None) {
@@ -99,6 +153,7 @@ struct Call {
       PyErr_Format(PyExc_ValueError, "%s must be a contiguous %s tensor on the GPU", next_name().c_str(), type_name(want));
       throw Failed{};
     }
+    on_device(t);
     next_name();
     return t.data_ptr();
   }
@@ -134,16 +189,14 @@ struct Call {
       case 'F': return checked(at::kFloat, true);
       case 'u': return checked(at::kByte, false);
       case 't': {
-        if (!typed) {
-          if (at < n_args) type = tensor(args[at]).scalar_type();
-          if (type != at::kFloat && type != at::kBFloat16) {
-            PyErr_SetString(PyExc_ValueError, "q/k/v must be float32 or bfloat16");
-            throw Failed{};
-          }
-          typed = true;
-        }
+        if (at < n_args) of_type(args[at]);
         return checked(type, false);
       }
+      case 'r': return strided(false);
+      case 'O': return strided(true);
+      case 'x': return checked(at::kDouble, false);
+      case 'c': return elements();
+      case 'L': return checked(at::kLong, true);
       case 'o': {
         PyObject* o = next();
         return o == Py_None ? nullptr : tensor(o).data_ptr();
@@ -154,6 +207,10 @@ struct Call {
         PyObject* o = next();
         if (o == Py_None) return nullptr;
         const at::Tensor& t = tensor(o);
+        if (e.one_device && (!t.is_cuda() || t.scalar_type() != at::kByte || !t.is_contiguous() || (device >= 0 && t.device().index() != device))) {
+          PyErr_SetString(PyExc_ValueError, "ws must be a contiguous torch.uint8 tensor on the current device");
+          throw Failed{};
+        }
         ws_bytes = (size_t)t.numel();
         return t.data_ptr();
       }
@@ -181,6 +238,7 @@ struct Call {
       return (P)v;
     } else {
       if (code == 'W') return static_cast<P>(ws_bytes);
+      if (code == 'R') return static_cast<P>(row_stride);
       if (code == 'D') return static_cast<P>(type == at::kBFloat16 ? HS_BF16 : HS_F32);
       const long long v = PyLong_AsLongLong(next());
       if (v == -1 && PyErr_Occurred()) throw Failed{};
@@ -235,9 +293,11 @@ template <typename... P>
 constexpr int n_params<hs_status(P...)> = sizeof...(P);
 constexpr int length(const char* s) { return *s == '\0' ? 0 : 1 + length(s + 1); }
 
-#define HS_ENTRY(fn, codes, names)                                                                   \
+#define HS_ENTRY_ON(fn, codes, names, one_device)                                                    \
   (static_cast<void>(std::integral_constant<int, 1 / (n_params<decltype(fn)> == length(codes) ? 1 : 0)>{}), \
-   Entry{#fn, codes, names, &Wrap<decltype(fn)>::call})
+   Entry{#fn, codes, names, &Wrap<decltype(fn)>::call, one_device})
+#define HS_ENTRY(fn, codes, names) HS_ENTRY_ON(fn, codes, names, false)
+#define HS_MX_CACHE "k_codes k_scales v_codes v_scales"
 #define HS_TREE "parent logc node_offsets"
 const Entry TABLE[] = {
     HS_ENTRY(hs_draft_entropy_topk, "onnnndooooowWs", ""),
@@ -258,6 +318,15 @@ const Entry TABLE[] = {
     HS_ENTRY(hs_kv_commit, "ttiiinttllnnnDs", "k_tree v_tree node_offsets accept_path accept_len k_cache v_cache cache_offsets cache_lens"),
     HS_ENTRY(hs_kv_commit_paged, "ttiiinttinnlnnnDs",
              "k_tree v_tree node_offsets accept_path accept_len k_pages v_pages block_table cache_lens"),
+    HS_ENTRY_ON(hs_rotary, "rROR" "lnnnnD" "xnnd" "rROR" "s", "q k positions inv_freq q_out k_out", true),
+    HS_ENTRY_ON(hs_tree_rotary, "rROR" "iilnnnnnD" "xnnd" "rROR" "s", "q k parent node_offsets prefix_lens inv_freq q_out k_out", true),
+    HS_ENTRY_ON(hs_kv_append_mx, "rRrRin" "cucun" "innlL" "nnnDs",
+                "k v node_offsets " HS_MX_CACHE " block_table cache_lens new_lens", true),
+    HS_ENTRY_ON(hs_kv_commit_mx, "rRrRiiin" "cucun" "innlL" "nnnDs",
+                "k_tree v_tree node_offsets accept_path accept_len " HS_MX_CACHE " block_table cache_lens new_lens", true),
+    HS_ENTRY_ON(hs_kv_read_mx, "cucun" "innLlnttnnnDs", HS_MX_CACHE " block_table first out_offsets k_out v_out", true),
+    HS_ENTRY_ON(hs_tree_attention_mx, "rRcucunrRrR" "iihinnlH" "nnnnDd" "tFwWs",
+                "q " HS_MX_CACHE " k_tree v_tree parent node_offsets block_table prefix_lens out lse", true),
 };
 
 // A bound function: self is a tuple (capsule of the entry, capsule of the address).
