@@ -14,7 +14,8 @@ LIB = os.path.join(PKG, "libheterospec.so")
 MARSHAL = os.path.join(PKG, "_marshal.so")  # host only: Python tensors -> the library's calls (csrc/marshal.cpp)
 SOURCES = ["api.cpp", "entropy_topk.hip", "tree_prune.hip", "tree_attention.hip", "tree_attention_mfma.hip",
            "verify_accept.hip", "tree_expand.hip", "adaptive_control.hip", "kv_commit.hip", "tree_validate.hip",
-           "rotary.hip", "kv_cache_mx.hip", "tree_attention_mx.hip"]
+           "rotary.hip", "kv_cache_mx.hip", "tree_attention_mx.hip",
+           "tree_attention_mx_e4m3.hip", "tree_attention_mx_e2m1.hip"]
 FLAGS = ["-O3", "-std=c++17", "-fPIC", "--offload-arch=gfx950", "-x", "hip",
          # packed-fp32 instruction selection is switched off for every device function of the library
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
