@@ -18,9 +18,70 @@ typedef __attribute__((address_space(3))) shortx4* lds_s4_ptr;
 constexpr int MXA_THREADS = 512;
 constexpr int MXA_WAVES = 8;
 constexpr int MXA_MAX_M = 1024;       // tree rows of a sequence
-constexpr float MX_LIMIT = 0x1p40f;   // a denominator (of a half-wave's keys) that reaches it moves the maximum
+constexpr float MX_LIMIT = 0x1p80f;   // a denominator (of a half-wave's keys) that reaches it moves the maximum
 constexpr float MXA_FLOOR = -3.402823466e38f;
 constexpr float MXA_LOG2E = 1.4426950408889634f, MXA_LN2 = 0.6931471805599453f;
+
+// How the sequences of a call are cut, on the host (the plan) and on the device (every workgroup finds its item).  A
+// sequence's rows of a KV head, in blocks of 32, are spread evenly over as few row groups of up to `blocks_most` blocks as hold
+// them; the size of a group decides how the eight waves of its workgroup share the work:
+//   one or two blocks    every wave by itself, on every eighth (fourth) 32 keys
+//   three or four        tiles of 64 keys shared through LDS, two waves to a block, each with half of a tile
+//   five to eight        the same, a wave to a block
+// Its keys are cut into splits of equal numbers of 64-token pages, at most pages[form] each; the tree's own rows go with the last
+// split, or are a split of their own where they would not fit it.
+enum MxForm { MX_PRIVATE_1 = 0, MX_PRIVATE_2 = 1, MX_SHARED_4 = 2, MX_SHARED_8 = 3 };
+constexpr int MXA_SPLITS = 64;  // of a sequence at most (a lane each where they meet)
+struct MxCuts {
+  int blocks_most;  // 1, 2, 4 or 8
+  int pages[4];
+};
+// x / d, exact, for 0 <= x < 2^23 and 1 <= d: a float product and one correction.
+__host__ __device__ __forceinline__ int mx_div(int x, int d) {
+#ifdef __HIP_DEVICE_COMPILE__
+  int q = (int)((float)x * __builtin_amdgcn_rcpf((float)d));
+  const int r = x - q * d;
+  q += r < 0 ? -1 : r >= d ? 1 : 0;
+  return q;
+#else
+  return x / d;
+#endif
+}
+struct MxCut {
+  int n_blk, n_rg, form, pages, n_sp;  // pages: of a split
+};
+__host__ __device__ __forceinline__ MxCut mx_cut(int M, int G, int L, const MxCuts& cuts) {
+  MxCut c;
+  c.n_blk = (G * M + 31) >> 5;
+  const int shift = cuts.blocks_most == 8 ? 3 : cuts.blocks_most == 4 ? 2 : cuts.blocks_most == 2 ? 1 : 0;
+  c.n_rg = (c.n_blk + cuts.blocks_most - 1) >> shift;
+  const bool over4 = c.n_blk > 4 * c.n_rg, over2 = c.n_blk > 2 * c.n_rg, over1 = c.n_blk > c.n_rg;
+  c.form = over4 ? MX_SHARED_8 : over2 ? MX_SHARED_4 : over1 ? MX_PRIVATE_2 : MX_PRIVATE_1;
+  int per = over4 ? cuts.pages[3] : over2 ? cuts.pages[2] : over1 ? cuts.pages[1] : cuts.pages[0];
+  const int pages = (L + MX_PAGE - 1) >> 6, tiles = (M + MX_PAGE - 1) >> 6, all = pages + tiles;
+  const int least = mx_div(all + MXA_SPLITS - 2, MXA_SPLITS - 1);
+  per = per < least ? least : per < 1 ? 1 : per;
+  const int even = mx_div(all + per - 1, per);
+  c.pages = mx_div(all + even - 1, even < 1 ? 1 : even);
+  c.pages = c.pages < 1 ? 1 : c.pages;
+  c.n_sp = mx_div(pages + c.pages - 1, c.pages);
+  if (c.n_sp > 0 && tiles > c.n_sp * c.pages - pages) ++c.n_sp;
+  c.n_sp = c.n_sp < 1 ? 1 : c.n_sp;
+  return c;
+}
+
+// A sequence as the host cut it.  The entries of up to MXA_ENTRIES sequences travel in the kernel's arguments: a workgroup then
+// knows its item after one trip to memory instead of two (2000 cycles).  Longer batches cut on the device.
+struct MxEntry {
+  int first;       // its first item
+  int n0, M, L;
+  int pages;       // of a split
+  int n_sp_form;   // splits | form << 8
+  int groups;      // row blocks | row groups << 16
+  int rec0;        // records of the sequences before
+};
+static_assert(sizeof(MxEntry) == 32, "two 16-byte loads");
+constexpr int MXA_ENTRIES = 64;
 
 struct MxAttnArgs {
   const void* q;
@@ -32,58 +93,51 @@ struct MxAttnArgs {
   const int32_t* node_offsets;
   const int64_t* lens;
   int B, Hq, G;
-  int blocks_most;       // row blocks of a work item at most: 1, 2, 4 or 8
-  int target;            // what an item may cost (mx_cut)
+  MxCuts cuts;
+  float inv_G;           // 1 / G
   float c2;              // scale * log2(e)
   void* o;
   float* lse;
   float* part;           // records of D + 4 floats: o (not normalised), maximum (in octaves), denominator
+  int n_entries;         // 0: more sequences than entries
+  alignas(16) MxEntry entries[MXA_ENTRIES];
 };
-
-// How a sequence is cut, on the host (the plan) and on the device (every workgroup finds its item).  Its rows of a KV head, in
-// blocks of 32, are spread evenly over as few row groups of up to `blocks_most` blocks as hold them; the size of a group decides
-// how the eight waves of its workgroup share the work:
-//   one or two blocks    every wave by itself, on every eighth (fourth) 32 keys
-//   three or four        tiles of 64 keys shared through LDS, two waves to a block, each with half of a tile
-//   five to eight        the same, a wave to a block
-// and with that what a page of 64 keys costs; the keys are cut into splits of as many pages as `target` pays for (64 splits at most).
-enum MxForm { MX_PRIVATE_1 = 0, MX_PRIVATE_2 = 1, MX_SHARED_4 = 2, MX_SHARED_8 = 3 };
-constexpr int MXA_SPLITS = 64;  // (a lane each where they meet)
-// Costs of a page in the four forms, in sixteenths of a microsecond, by format: see mx_plan.
-constexpr int MX_PAGE_COST[2][4] = {{8, 10, 16, 28}, {6, 9, 16, 28}};
-struct MxCut {
-  int n_blk, n_rg, form, pages, n_sp;  // pages: of a split
-};
-__host__ __device__ __forceinline__ MxCut mx_cut(int rows, int64_t L, int fmt, int blocks_most, int target) {
-  MxCut c;
-  c.n_blk = (rows + 31) >> 5;
-  const int shift = blocks_most == 8 ? 3 : blocks_most == 4 ? 2 : blocks_most == 2 ? 1 : 0;
-  c.n_rg = (c.n_blk + blocks_most - 1) >> shift;
-  const bool over4 = c.n_blk > 4 * c.n_rg, over2 = c.n_blk > 2 * c.n_rg, over1 = c.n_blk > c.n_rg;
-  c.form = over4 ? MX_SHARED_8 : over2 ? MX_SHARED_4 : over1 ? MX_PRIVATE_2 : MX_PRIVATE_1;
-  const int cost = over4 ? MX_PAGE_COST[fmt][3] : over2 ? MX_PAGE_COST[fmt][2] : over1 ? MX_PAGE_COST[fmt][1] : MX_PAGE_COST[fmt][0];
-  const int all = (int)((L + MX_PAGE - 1) / MX_PAGE), least = (all + MXA_SPLITS - 1) / MXA_SPLITS;
-  c.pages = (int)((unsigned)target / (unsigned)cost);
-  c.pages = c.pages < least ? least : c.pages;
-  c.pages = c.pages < 1 ? 1 : c.pages;
-  c.n_sp = (int)((unsigned)(all + c.pages - 1) / (unsigned)c.pages);
-  c.n_sp = c.n_sp < 1 ? 1 : c.n_sp;
-  c.pages = (int)((unsigned)(all + c.n_sp - 1) / (unsigned)c.n_sp);  // (splits of equal size)
-  c.pages = c.pages < 1 ? 1 : c.pages;
-  return c;
-}
 
 // The work item of this workgroup: items are numbered sequence by sequence, in a sequence
 // (split * row groups + row group) * Hkv + KV head.  Every wave finds it by a prefix sum over the sequences.
 struct MxItem {
-  int s, n0, M, g, sp, n_sp, pages, form;
-  int blk0, blk_n;  // row blocks
-  int64_t L;
-  int64_t rec0;     // records of the sequences before
+  int s, n0, M, L, g, form;
+  int blk0, blk_n;      // row blocks
+  int sp, n_sp, pages;  // its split, of how many, of how many pages
+  int64_t rec0;         // records of the sequences before
 };
-template <int FMT>
+// Fields that several ways of finding an item share; `local` is the item's number in its sequence.
+__device__ __forceinline__ void mx_place(const MxAttnArgs& a, int local, int n_blk, int n_rg, MxItem& w) {
+  const int x = __builtin_amdgcn_readfirstlane(mx_div(local, a.pool.Hkv));
+  w.g = local - x * a.pool.Hkv;
+  w.sp = n_rg == 1 ? x : __builtin_amdgcn_readfirstlane(mx_div(x, n_rg));
+  const int rg = x - w.sp * n_rg;
+  const int each = n_rg == 1 ? n_blk : __builtin_amdgcn_readfirstlane(mx_div(n_blk, n_rg)), more = n_blk - each * n_rg;
+  w.blk0 = rg * each + (rg < more ? rg : more);  // (the first `more` groups hold one block more)
+  w.blk_n = each + (rg < more ? 1 : 0);
+}
 __device__ __forceinline__ bool mx_item(const MxAttnArgs& a, int item, MxItem& w) {
   const int lane = (int)(threadIdx.x & 63);
+  if (a.n_entries > 0) {
+    const int4 lo = *reinterpret_cast<const int4*>(&a.entries[lane]), hi = *(reinterpret_cast<const int4*>(&a.entries[lane]) + 1);
+    const int e = __builtin_popcountll(__ballot(lane < a.n_entries && lo.x <= item)) - 1;  // (sequences without rows share their successor's first item)
+    w.s = e;
+    w.n0 = __builtin_amdgcn_readlane(lo.y, e);
+    w.M = __builtin_amdgcn_readlane(lo.z, e);
+    w.L = __builtin_amdgcn_readlane(lo.w, e);
+    w.pages = __builtin_amdgcn_readlane(hi.x, e);
+    const int nf = __builtin_amdgcn_readlane(hi.y, e), groups = __builtin_amdgcn_readlane(hi.z, e);
+    w.n_sp = nf & 255;
+    w.form = nf >> 8;
+    w.rec0 = __builtin_amdgcn_readlane(hi.w, e);
+    mx_place(a, item - __builtin_amdgcn_readlane(lo.x, e), groups & 0xffff, (int)((unsigned)groups >> 16), w);
+    return true;
+  }
   int done = 0;
   int64_t recs = 0;
   for (int base = 0; base < a.B; base += 64) {
@@ -94,7 +148,7 @@ __device__ __forceinline__ bool mx_item(const MxAttnArgs& a, int item, MxItem& w
       M = a.node_offsets[s + 1] - n0;
       L = (int)a.lens[s];
     }
-    const MxCut c = mx_cut(a.G * M, L, FMT, a.blocks_most, a.target);
+    const MxCut c = mx_cut(M, a.G, L, a.cuts);
     const int items = M > 0 ? c.n_sp * c.n_rg * a.pool.Hkv : 0;
     const int rec = M > 0 && c.n_sp > 1 ? M * a.Hq * c.n_sp : 0;
     const int upto = done + wave_prefix_sum(items), rec_upto = wave_prefix_sum(rec);
@@ -108,17 +162,9 @@ __device__ __forceinline__ bool mx_item(const MxAttnArgs& a, int item, MxItem& w
       w.n_sp = __builtin_amdgcn_readlane(c.n_sp, e);
       w.pages = __builtin_amdgcn_readlane(c.pages, e);
       w.form = __builtin_amdgcn_readlane(c.form, e);
-      const int n_blk = __builtin_amdgcn_readlane(c.n_blk, e), n_rg = __builtin_amdgcn_readlane(c.n_rg, e);
       w.rec0 = recs + __builtin_amdgcn_readlane(rec_upto, e) - __builtin_amdgcn_readlane(rec, e);
-      unsigned local = (unsigned)(item - (__builtin_amdgcn_readlane(upto, e) - __builtin_amdgcn_readlane(items, e)));
-      const unsigned hkv = (unsigned)a.pool.Hkv;
-      w.g = (int)(local % hkv);
-      local /= hkv;
-      const int rg = (int)(local % (unsigned)n_rg);
-      w.sp = (int)(local / (unsigned)n_rg);
-      const int each = n_blk / n_rg, more = n_blk - each * n_rg;  // the first `more` groups hold one block more
-      w.blk0 = rg * each + (rg < more ? rg : more);
-      w.blk_n = each + (rg < more ? 1 : 0);
+      mx_place(a, item - (__builtin_amdgcn_readlane(upto, e) - __builtin_amdgcn_readlane(items, e)), __builtin_amdgcn_readlane(c.n_blk, e),
+               __builtin_amdgcn_readlane(c.n_rg, e), w);
       return true;
     }
     done = __builtin_amdgcn_readlane(upto, 63);
@@ -195,13 +241,20 @@ struct MxState {
           if (((word >> j) & 1u) != 0u && !(fabsf(x) < HS_INF)) acc[t][e] += x;
         }
   }
-  // The maximum of the rows whose denominator reaches MX_LIMIT (or is a NaN) moves to the largest of a block's scores; the
+  // The first scores of an item (accumulators and sum are zero): their maximum is the row's.
+  __device__ __forceinline__ void start(const floatx16& S, float c2) {
+    float top = fmaxf(S[0], S[1]);
+#pragma unroll
+    for (int v = 2; v < 16; ++v) top = fmaxf(top, S[v]);
+    m = fmaxf(MXA_FLOOR, half_max(top) * c2);
+  }
+  // The maximum of the rows whose denominator reaches MX_LIMIT moves to the largest of a block's scores; the
   // other rows keep theirs, so that no row's rounding depends on its neighbours.
   __device__ __forceinline__ void move(const floatx16& S, float c2, float sum) {
     float top = fmaxf(S[0], S[1]);
 #pragma unroll
     for (int v = 2; v < 16; ++v) top = fmaxf(top, S[v]);
-    const bool moves = half_max(sum < MX_LIMIT ? 0.f : 1.f) > 0.f;
+    const bool moves = half_max(sum >= MX_LIMIT ? 1.f : 0.f) > 0.f;
     const float up = moves ? fmaxf(m, half_max(top) * c2) : m, alpha = exp2_fast(m - up);
     m = up;
     l *= alpha;
@@ -209,13 +262,6 @@ struct MxState {
     for (int t = 0; t < NT; ++t)
 #pragma unroll
       for (int v = 0; v < 16; ++v) acc[t][v] *= alpha;
-  }
-  // The first scores of a pass (accumulators and sum are zero): their maximum is the row's.
-  __device__ __forceinline__ void start(const floatx16& S, float c2) {
-    float top = fmaxf(S[0], S[1]);
-#pragma unroll
-    for (int v = 2; v < 16; ++v) top = fmaxf(top, S[v]);
-    m = fmaxf(MXA_FLOOR, half_max(top) * c2);
   }
   __device__ __forceinline__ floatx2 exps(const floatx16& S, float c2, int j) const {  // scores 2j, 2j + 1
     return floatx2{exp2_fast(__builtin_fmaf(S[2 * j], c2, -m)), exp2_fast(__builtin_fmaf(S[2 * j + 1], c2, -m))};
@@ -231,7 +277,7 @@ struct MxState {
     }
     P = make_uint4(w[0], w[1], w[2], w[3]);
   }
-  __device__ __forceinline__ static bool over(float s) { return __ballot(!(s < MX_LIMIT)) != 0ull; }
+  __device__ __forceinline__ static bool over(float s) { return __ballot(s >= MX_LIMIT) != 0ull; }  // (a NaN stays one)
   // Scores (masked ones at -inf) to P: bfloat16 pairs of the first 16 and the second 16 keys.
   __device__ __forceinline__ void softmax(const floatx16& S, float c2, uint4& p0, uint4& p1) {
     float s = l;
@@ -247,10 +293,67 @@ struct MxState {
   }
 };
 
-// The tree's parents and hops in LDS, by the whole workgroup (a barrier inside and behind).
-__device__ __forceinline__ void mx_stage_tree(const MxAttnArgs& a, const MxItem& it, int* par, int2* hops) {
-  for (int j = threadIdx.x; j < it.M; j += MXA_THREADS) par[j] = a.parent[it.n0 + j];
-  __syncthreads();
+// Barrier of the workgroup for LDS; loads in flight stay in flight.
+__device__ __forceinline__ void mx_meet() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+// Tree row i and query head h of row r of a KV head (r < 2^16, G <= 1024: r / G by a float product is exact).
+struct MxOwn {
+  int i, h;
+};
+__device__ __forceinline__ MxOwn mx_own(const MxAttnArgs& a, const MxItem& it, int r) {
+  const int i = (int)(((float)r + 0.5f) * a.inv_G);
+  return MxOwn{i, it.g * a.G + (r - i * a.G)};
+}
+// Q: 32 rows from memory in whole rows into LDS (rows of 2 D + 16 bytes: 16 lanes that read a piece each, of 16 rows, meet 16
+// banks).  (Every lane its own row's pieces from memory: 32 lines to a load, 3000 cycles where eight waves read the same rows.)
+template <int D>
+constexpr int MX_Q_ROW = 2 * D + 16;
+template <int D>
+__device__ __forceinline__ void mx_stage_q(const MxAttnArgs& a, const MxItem& it, int row_base, char* to, int first, int step) {
+  const int Rh = a.G * it.M;
+  for (int id = first; id < 32 * (D / 8); id += step) {
+    const int r = id / (D / 8), c = id % (D / 8);
+    const MxOwn o = mx_own(a, it, row_base + r < Rh ? row_base + r : Rh - 1);  // (rows behind the last repeat it)
+    *reinterpret_cast<uint4*>(to + r * MX_Q_ROW<D> + c * 16) =
+        *reinterpret_cast<const uint4*>(static_cast<const bf16_t*>(a.q) + (int64_t)(it.n0 + o.i) * a.q_stride + (int64_t)o.h * D + c * 8);
+  }
+}
+
+// Root paths.  Trees of up to 64 rows: a wave finds all of them in registers, every row's mask of ancestors and pointer doubled
+// until the pointers have left the tree, and keeps its rows' masks: no LDS, no barrier, as many rounds as the depth has
+// binary digits (a walk through LDS took 3000 cycles for 8 rows and 6000 for 64).  Larger trees: hops in LDS (see mx_stage_tree),
+// which a lane follows from its row up, a word of 32 tree rows at a time, as the tree's key blocks fall from call to call.
+struct MxPath {
+  unsigned lo, hi;  // small trees: the lane's row's path
+  int cur;          // large ones: where it has got to
+};
+__device__ __forceinline__ void mx_small_paths(int parent, int M, int row, MxPath& path) {  // parent: of tree row `lane`
+  const int lane = (int)(threadIdx.x & 63);
+  unsigned lo = lane < 32 ? 1u << lane : 0u, hi = lane >= 32 ? 1u << (lane - 32) : 0u;
+  int up = lane < M && parent >= 0 && parent < lane ? parent : -1;
+  while (__ballot(up >= 0) != 0ull) {
+    const int from = up >= 0 ? up : lane;
+    lo |= (unsigned)__shfl((int)lo, from);
+    hi |= (unsigned)__shfl((int)hi, from);
+    const int next = __shfl(up, from);
+    up = up >= 0 ? next : -1;
+  }
+  path.lo = (unsigned)__shfl((int)lo, row);
+  path.hi = (unsigned)__shfl((int)hi, row);
+}
+// The tree's parents, requested early, and its hops in LDS, by the whole workgroup (a barrier inside and behind).
+struct MxParents {
+  int a, b;
+};
+__device__ __forceinline__ MxParents mx_request_parents(const MxAttnArgs& a, const MxItem& it) {
+  const int32_t* const from = a.parent + it.n0;
+  const int i = it.M <= 64 ? (int)(threadIdx.x & 63) : (int)threadIdx.x, j = i + MXA_THREADS;
+  return MxParents{from[i < it.M ? i : 0], from[j < it.M ? j : 0]};
+}
+__device__ __forceinline__ void mx_stage_tree(const MxItem& it, const MxParents& mine, int* par, int2* hops) {
+  if ((int)threadIdx.x < it.M) par[threadIdx.x] = mine.a;
+  if ((int)threadIdx.x + MXA_THREADS < it.M) par[threadIdx.x + MXA_THREADS] = mine.b;
+  mx_meet();
   for (int j = threadIdx.x; j < it.M; j += MXA_THREADS) {
     unsigned bits = 1u << (j & 31);
     int x = j;
@@ -262,13 +365,14 @@ __device__ __forceinline__ void mx_stage_tree(const MxAttnArgs& a, const MxItem&
     }
     hops[j] = make_int2((int)bits, x < 0 ? -1 : x);
   }
-  __syncthreads();
+  mx_meet();
 }
-// The part of a row's root path in tree rows 32 b .. 32 b + 31; b falls from call to call.
-__device__ __forceinline__ unsigned mx_path_word(const int2* hops, int& cur, int b) {
-  if (cur < 0 || (cur >> 5) != b) return 0u;
-  const int2 hop = hops[cur];
-  cur = hop.y;
+// The part of the path in tree rows 32 b .. 32 b + 31; b falls from call to call.
+__device__ __forceinline__ unsigned mx_path_word(bool small, const int2* hops, MxPath& path, int b) {
+  if (small) return b == 0 ? path.lo : path.hi;
+  if (path.cur < 0 || (path.cur >> 5) != b) return 0u;
+  const int2 hop = hops[path.cur];
+  path.cur = hop.y;
   return (unsigned)hop.x;
 }
 

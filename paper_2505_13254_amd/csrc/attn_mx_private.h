@@ -1,15 +1,15 @@
 // Attention over a quantised cache, work items of one or two row blocks: every wave by itself (internal).
 //
-// Wave w works for row block w % R on every (8 / R)-th 32 keys of the item's split, alone: its keys go from memory into its
+// Wave w works for row block w % R (R = 1 or 2) on every (8 / R)-th 32 keys of the item's split, alone: its keys go from memory into its
 // registers, its softmax state is its own, and the waves of a row block meet once, at the end.
 //
 // K needs no LDS: which 8 elements of a row a lane's operand register holds is free as long as Q's agree, so a lane
 // loads 16 bytes of codes of its own key and converts them in place.  V is converted in the order it is
 // loaded, written to the wave's 8 KB of LDS and fetched from there with the transposing read.
 //
-// A row's maximum stays that of the wave's first 32 keys: weights above one cost no precision (P, sums and accumulators are
-// floating point) until a denominator reaches 2^40 (a score 27 above the first ones, or a NaN); the wave then takes its
-// keys again, with the maximum following.  So neither a block's maximum nor a rescaling is computed in almost every step.
+// A row's maximum stays that of the tree's rows and the wave's first 32 keys: neither a block's maximum nor a rescaling is
+// computed in almost every step.  Weights above one cost no precision (P, sums and accumulators are floating point) until
+// a denominator reaches 2^80 (a score 55 above the first ones): attn_mx_follow then takes the item.
 #pragma once
 #include <type_traits>
 
@@ -17,8 +17,9 @@
 
 namespace hs {
 
+// Returns whether the fixed maximum held; nothing is written where it did not.
 template <int FMT, int D, int R>
-__device__ __forceinline__ void attn_mx_private(const MxAttnArgs& a, const MxItem& it, MxLds<D>& mem) {
+__device__ __forceinline__ bool attn_mx_private(const MxAttnArgs& a, const MxItem& it, MxLds<D>& mem) {
   constexpr int W = MXA_WAVES / R;       // ways: waves that share a row block's keys
   constexpr int NK = D / 16;             // matrix instructions of a 32-key score block
   constexpr int NT = D / 32;
@@ -42,28 +43,72 @@ __device__ __forceinline__ void attn_mx_private(const MxAttnArgs& a, const MxIte
   const int Rh = a.G * it.M;
   const int row_base = (it.blk0 + rb) * 32;
   const bool active = rb < it.blk_n;
-  const int r_own = row_base + col < Rh ? row_base + col : Rh - 1;
-  const int i_own = r_own / a.G, h_own = it.g * a.G + (r_own - i_own * a.G);
-  const int64_t L = it.L;
+  const MxOwn own = mx_own(a, it, row_base + col < Rh ? row_base + col : Rh - 1);
   const bool last_split = it.sp == it.n_sp - 1;
-  const int64_t k_lo = (int64_t)it.sp * it.pages * MX_PAGE;
-  const int64_t k_hi = last_split ? L : k_lo + (int64_t)it.pages * MX_PAGE;
-  const int n_blocks = (int)((k_hi - k_lo + 31) >> 5);  // 32-key blocks of the prefix part
+  const int k_lo = it.sp * it.pages * MX_PAGE, k_hi = last_split || k_lo + it.pages * MX_PAGE > it.L ? it.L : k_lo + it.pages * MX_PAGE;
+  const int keys = k_hi > k_lo ? k_hi - k_lo : 0;  // of the prefix part
+  const int n_blocks = (keys + 31) >> 5;
 
-  if (last_split) mx_stage_tree(a, it, par, hops);
+  // ---- what the first steps wait for is requested first, all of it: the pages, the tree's parents, Q, a block of the tree
+  const int32_t* const table = a.pool.table + (int64_t)it.s * a.pool.max_blocks + (k_lo >> 6);
+  const int mine = active && n_blocks > way ? (n_blocks - way + W - 1) / W : 0;
+  auto pages_from = [&](int j) {  // lane l: the page of this wave's block j + l
+    const int b = way + (j + lane) * W, p = table[b < n_blocks ? b >> 1 : 0];
+    return p < 0 || p >= a.pool.n_pages ? 0 : p;  // (a page outside the pool would be a caller's error)
+  };
+  int page_of = mine > 0 ? pages_from(0) : 0;
+  MxParents parents = {};
+  MxPath path = {0u, 0u, own.i};
+  const bool small = it.M <= 64;
+  if (last_split) parents = mx_request_parents(a, it);
+  char* const q_lds = lds + MXA_WAVES * TILE + rb * 32 * MX_Q_ROW<D>;
+  static_assert(MXA_WAVES * TILE + 2 * 32 * MX_Q_ROW<D> <= (int)sizeof(mem.tiles), "Q behind the V tiles");
+  if (active) mx_stage_q<D>(a, it, row_base, q_lds, way * 64 + lane, W * 64);
+
+  // ---- prefix: 32-key blocks way, way + W, ... of the split
+  uint4 kc[KC], vc[VC];
+  unsigned ks = 0, vs[VC];
+  // (keys behind the last of a block repeat it; they are masked.  Scalar bases, 32 bits to a lane.)
+  // The loop's requests are unconditional (behind the last block it again): a wait can then count the younger ones, where a
+  // branch around them makes it a wait for all.
+  int64_t base = 0;
+  unsigned last = 0;
+  int page_j = 0;
+  auto request_k = [&](int j) {
+    const int b = way + j * W;
+    base = ((int64_t)__builtin_amdgcn_readlane(page_of, j - page_j) * a.pool.Hkv + it.g) * MX_PAGE + (b & 1) * 32;
+    last = (unsigned)(keys - b * 32 < 32 ? keys - b * 32 - 1 : 31);
+    const unsigned kr = (unsigned)col < last ? (unsigned)col : last;
+    mx_mem kp = (mx_mem)(a.pool.k_codes + base * ROW), kp_s = (mx_mem)(a.pool.k_scales + base * NS);
+    asm volatile("" : "+s"(kp), "+s"(kp_s));
+#pragma unroll
+    for (int n = 0; n < KC; ++n) kc[n] = mx_load16(kp + (kr * ROW + half * 16 + n * 32));
+    if constexpr (NS == 4) ks = *reinterpret_cast<const __attribute__((address_space(1))) unsigned*>(kp_s + kr * NS);
+    else ks = *reinterpret_cast<const __attribute__((address_space(1))) unsigned short*>(kp_s + kr * NS);
+  };
+  auto request_v = [&]() {  // of the block that request_k was called for last
+    mx_mem vp = (mx_mem)(a.pool.v_codes + base * ROW), vp_s = (mx_mem)(a.pool.v_scales + base * NS);
+    asm volatile("" : "+s"(vp), "+s"(vp_s));
+#pragma unroll
+    for (int n = 0; n < VC; ++n) {
+      const unsigned id = n * 64 + lane, key = id / CPR, c = id % CPR, vr = key < last ? key : last;
+      vc[n] = mx_load16(vp + (vr * ROW + c * 16));
+      vs[n] = vp_s[vr * NS + c * EPC / MX_BLOCK];
+    }
+  };
+  if (last_split && !small) mx_stage_tree(it, parents, par, hops);
+  if (mine > 0) request_k(0);
+  mx_meet();  // Q is there
+  if (last_split && small) mx_small_paths(parents.a, it.M, own.i, path);
 
   MxState<D> st;
   st.clear();
   char* const tile = lds + wave * TILE;
   if (active) {
-    // ---- Q: element order of step kk as K's (see below)
-    bf16x8 qf[NK];
-    {
-      const bf16_t* const src = static_cast<const bf16_t*>(a.q) + (int64_t)(it.n0 + i_own) * a.q_stride + (int64_t)h_own * D;
+    bf16x8 qf[NK];  // element order of step kk as K's (see below)
 #pragma unroll
-      for (int kk = 0; kk < NK; ++kk)
-        qf[kk] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(src + (kk / SPC) * 2 * EPC + half * EPC + (kk % SPC) * 8));
-    }
+    for (int kk = 0; kk < NK; ++kk)
+      qf[kk] = *reinterpret_cast<const bf16x8*>(q_lds + col * MX_Q_ROW<D> + ((kk / SPC) * 2 * EPC + half * EPC + (kk % SPC) * 8) * 2);
     // ---- V^T fragments: the transposing read returns, to lane l of a 16-lane group, element l % 4 of the 8-byte pieces
     // addressed by lanes l / 4 + {0, 4, 8, 12} of the group
     const int tr_a = lane & 3, tr_j = (lane >> 2) & 3, tr_dh = (lane >> 4) & 1;
@@ -88,41 +133,8 @@ __device__ __forceinline__ void attn_mx_private(const MxAttnArgs& a, const MxIte
     };
     const floatx16 zero = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 
-    // ---- prefix: 32-key blocks way, way + W, ... of the split
-    const int32_t* const table = a.pool.table + (int64_t)it.s * a.pool.max_blocks + (k_lo >> 6);
-    const int mine = n_blocks > way ? (n_blocks - way + W - 1) / W : 0;
-    int page_of = 0;  // lane j: the page of this wave's block j of the present 64
-    uint4 kc[KC], vc[VC];
-    unsigned ks = 0, vs[VC];
-    auto request = [&](int j) {
-      if ((j & 63) == 0) {
-        const int b = way + (j + lane) * W;
-        int p = b < n_blocks ? table[b >> 1] : 0;
-        page_of = p < 0 || p >= a.pool.n_pages ? 0 : p;  // (a page outside the pool would be a caller's error)
-      }
-      const int b = way + j * W;
-      const int page = __builtin_amdgcn_readlane(page_of, j & 63);
-      const int64_t base = ((int64_t)page * a.pool.Hkv + it.g) * MX_PAGE;
-      const int s0 = (b & 1) * 32;
-      const int last = (int)(k_hi - k_lo - (int64_t)b * 32) - 1;  // last key of the block that exists (>= 0)
-      const int kr = s0 + (col < last ? col : last);              // (keys behind it repeat it; masked)
-      const unsigned char* const kp = a.pool.k_codes + (base + kr) * ROW + half * 16;
-#pragma unroll
-      for (int n = 0; n < KC; ++n) kc[n] = *reinterpret_cast<const uint4*>(kp + n * 32);
-      const unsigned char* const sp = a.pool.k_scales + (base + kr) * NS;
-      if constexpr (NS == 4) ks = *reinterpret_cast<const unsigned*>(sp);
-      else ks = *reinterpret_cast<const unsigned short*>(sp);
-#pragma unroll
-      for (int n = 0; n < VC; ++n) {
-        const int id = n * 64 + lane, key = id / CPR, c = id % CPR;
-        const int64_t vr = base + s0 + (key < last ? key : last);
-        vc[n] = *reinterpret_cast<const uint4*>(a.pool.v_codes + vr * ROW + c * 16);
-        vs[n] = a.pool.v_scales[vr * NS + c * EPC / MX_BLOCK];
-      }
-    };
-    auto step = [&](int j, auto safe) {
-      constexpr bool SAFE = decltype(safe)::value;
-      if (SAFE) request(j);
+    bool fresh = true;  // no scores yet
+    auto step = [&](int j, auto first) {
       floatx16 S = zero;
 #pragma unroll
       for (int n = 0; n < KC; ++n) {
@@ -136,6 +148,7 @@ __device__ __forceinline__ void attn_mx_private(const MxAttnArgs& a, const MxIte
           S = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, f), qf[n * SPC + e], S, 0, 0, 0);
         }
       }
+      request_k(j + 1 < mine ? j + 1 : j);
 #pragma unroll
       for (int n = 0; n < VC; ++n) {
         const int id = n * 64 + lane, key = id / CPR, c = id % CPR;
@@ -146,55 +159,52 @@ __device__ __forceinline__ void attn_mx_private(const MxAttnArgs& a, const MxIte
           *reinterpret_cast<uint4*>(tile + v_at<D>(key, c * SPC + e)) =
               FMT == HS_MX_E4M3 ? mx_eight<FMT>(w[(2 * e) & 3], w[(2 * e + 1) & 3], s) : mx_eight<FMT>(w[e & 3], 0u, s);
       }
-      if (!SAFE && j + 1 < mine) request(j + 1);
-      const int left = (int)(k_hi - k_lo - (int64_t)(way + j * W) * 32);  // keys of this block
+      request_v();
+      const int left = keys - (way + j * W) * 32;  // keys of this block
       if (left < 32) {
 #pragma unroll
         for (int v = 0; v < 16; ++v) S[v] = 8 * (v >> 2) + 4 * half + (v & 3) < left ? S[v] : -HS_INF;
       }
-      uint4 p0, p1;
-      if constexpr (SAFE) {
-        st.softmax(S, a.c2, p0, p1);
-      } else {
-        if (j == 0) st.start(S, a.c2);
-        st.exp_half(S, a.c2, 0, p0, st.l);
-        st.exp_half(S, a.c2, 1, p1, st.l);
+      if constexpr (decltype(first)::value) {
+        if (fresh) st.start(S, a.c2);
+        else st.move(S, a.c2, HS_INF);
       }
+      uint4 p0, p1;
+      st.exp_half(S, a.c2, 0, p0, st.l);
+      st.exp_half(S, a.c2, 1, p1, st.l);
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // the tile is read by other lanes than wrote it
       second(p0, p1);
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     };
-    if (mine > 0) {
-      request(0);
-      for (int j = 0; j < mine; ++j) step(j, std::false_type{});
-      if (st.over(st.l)) {  // the first block's maximum did not hold: again, with the maximum following
-        st.clear();
-        for (int j = 0; j < mine; ++j) step(j, std::true_type{});
-      }
-    }
-
-    // ---- the tree's own rows, block by block from the last that a row of this wave can see to the first
-    if (last_split) {
+    // ---- the tree's own rows, block by block (of large trees from the last that a row of this wave can see to the first), dealt to the
+    // ways from the last one on, which has the fewest keys
+    auto tree_rows = [&]() {
+      if (!last_split) return;
       const int r_top = row_base + 31 < Rh ? row_base + 31 : Rh - 1;
-      int cur = i_own;
-      for (int b = (r_top / a.G) >> 5; b >= 0; --b) {
-        const unsigned word = mx_path_word(hops, cur, b);
-        if (b % W != way || __ballot(word != 0u) == 0ull) continue;
+      const int top_blk = mx_own(a, it, r_top).i >> 5;
+      for (int x = 0; x <= top_blk; ++x) {
+        const int b = small ? x : top_blk - x;
+        const unsigned word = mx_path_word(small, hops, path, b);
+        if (W - 1 - b % W != way || __ballot(word != 0u) == 0ull) continue;
         const int last = it.M - 1 - 32 * b;  // >= 0
-        const int kr = it.n0 + 32 * b + (col < last ? col : last);
+        int ln = lane;
+        asm volatile("" : "+v"(ln));  // (no address of these is kept in registers from block to block)
+        const int lc = ln & 31, lh = ln >> 5;
+        const int kr = it.n0 + 32 * b + (lc < last ? lc : last);
         const bf16_t* const kp = static_cast<const bf16_t*>(a.k_tree) + (int64_t)kr * a.k_stride + it.g * D;
         floatx16 S = zero;
 #pragma unroll
         for (int kk = 0; kk < NK; ++kk) {
-          const uint4 f = *reinterpret_cast<const uint4*>(kp + (kk / SPC) * 2 * EPC + half * EPC + (kk % SPC) * 8);
+          const uint4 f = *reinterpret_cast<const uint4*>(kp + (kk / SPC) * 2 * EPC + lh * EPC + (kk % SPC) * 8);
           S = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, f), qf[kk], S, 0, 0, 0);
         }
+        __builtin_amdgcn_sched_barrier(0);  // (V behind K: there are no registers for both)
         constexpr int TC = 32 * (D / 8) / 64;
         const bf16_t* const vb = static_cast<const bf16_t*>(a.v_tree) + (int64_t)(it.n0 + 32 * b) * a.v_stride + it.g * D;
         ushort2v most = {0, 0};
 #pragma unroll
         for (int n = 0; n < TC; ++n) {
-          const int id = n * 64 + lane, key = id / (D / 8), c = id % (D / 8);
+          const int id = n * 64 + ln, key = id / (D / 8), c = id % (D / 8);
           const uint4 w = *reinterpret_cast<const uint4*>(vb + (key < last ? key : last) * a.v_stride + c * 8);
           note_bits(most, w);
           *reinterpret_cast<uint4*>(tile + v_at<D>(key, c)) = w;
@@ -202,27 +212,38 @@ __device__ __forceinline__ void attn_mx_private(const MxAttnArgs& a, const MxIte
         const bool odd = __ballot(has_odd(most)) != 0ull;
         if (odd)
           for (int n = 0; n < TC; ++n) {
-            const int id = n * 64 + lane;
+            const int id = n * 64 + ln;
             uint4* const at = reinterpret_cast<uint4*>(tile + v_at<D>(id / (D / 8), id % (D / 8)));
             *at = without_odd(*at);
           }
 #pragma unroll
         for (int v = 0; v < 16; ++v) S[v] = (word >> (8 * (v >> 2) + 4 * half + (v & 3))) & 1u ? S[v] : -HS_INF;
         uint4 p0, p1;
+        if (fresh) st.start(S, a.c2);
+        fresh = false;
         st.softmax(S, a.c2, p0, p1);
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         second(p0, p1);
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         if (odd) st.add_odd(vb, a.v_stride, last < 31 ? last + 1 : 32, word, half);
       }
+    };
+    tree_rows();
+    if (mine > 0) request_v();
+    if (mine > 0) step(0, std::true_type{});
+    for (int j = 1; j < mine;) {
+      if (j > 1) page_of = pages_from(page_j = j);
+      for (const int stop = page_j + 63; j < mine && j < stop; ++j) step(j, std::false_type{});  // (the last one requests page_j + 63)
     }
+    if (st.over(st.l)) mem.redo = 1;  // (lanes of a wave agree)
     st.l = half_sum(st.l);
     if (half == 0) {
       den[wave][0][col] = st.m;
       den[wave][1][col] = st.l;
     }
   }
-  __syncthreads();  // every wave has its sums (and no tile is read any more)
+  mx_meet();  // every wave has its sums (and no tile is read any more)
+  if (mem.redo != 0) return false;
 
   // ---- the ways of a row block meet: each leaves its accumulators, scaled to the common maximum, and adds up its share
   // of the columns
@@ -234,16 +255,17 @@ __device__ __forceinline__ void attn_mx_private(const MxAttnArgs& a, const MxIte
     for (int x = 0; x < W; ++x) total += den[x * R + rb][1][col] * exp2_fast(den[x * R + rb][0][col] - top);
     const float mine = exp2_fast(st.m - top);
     float4* const to = reinterpret_cast<float4*>(lds) + wave * (NT * 4 * 64) + lane;
+    if (row_base + col < Rh)
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
       for (int b = 0; b < 4; ++b)
         to[(t * 4 + b) * 64] = make_float4(st.acc[t][4 * b] * mine, st.acc[t][4 * b + 1] * mine, st.acc[t][4 * b + 2] * mine, st.acc[t][4 * b + 3] * mine);
   }
-  __syncthreads();
-  if (!active || row_base + col >= Rh) return;
-  const int64_t out_row = (int64_t)(it.n0 + i_own) * a.Hq + h_own;
-  float* const rec = a.part + (it.rec0 + ((int64_t)i_own * a.Hq + h_own) * it.n_sp + it.sp) * (D + ATTN_REC_PAD);
+  mx_meet();
+  if (!active || row_base + col >= Rh) return true;
+  const int64_t out_row = (int64_t)(it.n0 + own.i) * a.Hq + own.h;
+  float* const rec = a.part + (it.rec0 + ((int64_t)own.i * a.Hq + own.h) * it.n_sp + it.sp) * (D + ATTN_REC_PAD);
   const float inv = 1.f / total;
   for (int x = way; x < NT * 4; x += W) {
     float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -262,6 +284,7 @@ __device__ __forceinline__ void attn_mx_private(const MxAttnArgs& a, const MxIte
       rec[D + 1] = total;
     }
   }
+  return true;
 }
 
 }  // namespace hs

@@ -13,12 +13,10 @@
 //     barrier (tile t + 1 is there)
 //     scores of the first block of t + 1 | of the second block of t, second half
 //     product of the second block of t   | of the first block of t + 1, first half
-// (W = 2: one block a tile, two windows.)  The partial page at the end of the prefix and the tree's own rows go through the
+// (W = 2: one block a tile, two windows.)  The tree's own rows before, and the partial page behind them, go through the
 // same buffers without that overlap: they are a few tiles.
 //
-// In this pass a row's maximum stays that of its first 32 keys.  Weights above one do no harm (P, sums and accumulators are
-// floating point) until a denominator reaches 2^40 (a score 27 above the first ones, or a NaN): the workgroup then
-// takes its pages again without the overlap, with the maximum following.  Rows that were in bounds get the same bits either way.
+// A row's maximum stays that of the tree's rows and its first 32 keys, as in the other kind.
 #pragma once
 #include <type_traits>
 
@@ -26,8 +24,9 @@
 
 namespace hs {
 
+// Returns whether the fixed maximum held; nothing is written where it did not.
 template <int FMT, int D, int W>
-__device__ __forceinline__ void attn_mx_shared(const MxAttnArgs& a, const MxItem& it, MxLds<D>& mem) {
+__device__ __forceinline__ bool attn_mx_shared(const MxAttnArgs& a, const MxItem& it, MxLds<D>& mem) {
   constexpr int NK = D / 16, NT = D / 32, STEPS = NK / 2, EPS = 4 / STEPS;
   constexpr int ROW = mx_row_bytes(FMT, D);
   constexpr int SPC = 16 / Mx<FMT>::BITS;      // 16-byte pieces of bfloat16 that a 16-byte chunk of codes becomes
@@ -54,20 +53,16 @@ __device__ __forceinline__ void attn_mx_shared(const MxAttnArgs& a, const MxItem
   const int Rh = a.G * it.M;
   const int row_base = (it.blk0 + rb) * 32;
   const bool active = rb < it.blk_n;
-  // Tree row and query head of the lane's row (rows behind the last repeat it).  Found again where they are needed, which the
-  // empty statement keeps the compiler from doing once ahead of the loops, where there are no registers to keep them in.
-  struct Own {
-    int i, h;
-  };
+  // (the lane's row is found again where it is needed, which the empty statement keeps the compiler from doing once ahead of
+  // the loops, where there are no registers to keep it in)
   auto own = [&]() {
     int c = col;
     asm volatile("" : "+v"(c));
-    const int r = row_base + c < Rh ? row_base + c : Rh - 1, i = r / a.G;
-    return Own{i, it.g * a.G + (r - i * a.G)};
+    return mx_own(a, it, row_base + c < Rh ? row_base + c : Rh - 1);  // (rows behind the last repeat it)
   };
   const bool last_split = it.sp == it.n_sp - 1;
-  const int64_t k_lo = (int64_t)it.sp * it.pages * MX_PAGE;
-  const int keys = (int)((last_split ? it.L : k_lo + (int64_t)it.pages * MX_PAGE) - k_lo);  // of the prefix part
+  const int k_lo = it.sp * it.pages * MX_PAGE, k_hi = last_split || k_lo + it.pages * MX_PAGE > it.L ? it.L : k_lo + it.pages * MX_PAGE;
+  const int keys = k_hi > k_lo ? k_hi - k_lo : 0;  // of the prefix part
   const int n_full = keys / MX_PAGE;
 
   // ---- a thread's part of a tile of codes
@@ -83,29 +78,26 @@ __device__ __forceinline__ void attn_mx_shared(const MxAttnArgs& a, const MxItem
     uint4 k, v;
     unsigned ks, vs;
   };
-  int page_of = 0, page_base = -64;
-  auto page_at = [&](int t) {  // lane j holds the page of tile page_base + j
-    if (t - page_base >= 64) {
-      page_base = t;
-      const int p = (t + lane) * MX_PAGE < keys ? table[t + lane] : 0;
-      page_of = p < 0 || p >= a.pool.n_pages ? 0 : p;  // (a page outside the pool would be a caller's error)
-    }
-    return __builtin_amdgcn_readlane(page_of, t - page_base);
+  auto pages_from = [&](int t) {  // lane l: the page of tile t + l
+    const int p = keys > 0 ? table[(t + lane) * MX_PAGE < keys ? t + lane : t] : 0;
+    return p < 0 || p >= a.pool.n_pages ? 0 : p;  // (a page outside the pool would be a caller's error)
   };
+  int page_of = pages_from(0), page_base = 0;  // (moved on outside of the loop over the tiles: see every_tile)
+  auto page_at = [&](int t) { return __builtin_amdgcn_readlane(page_of, t - page_base); };
   auto load = [&](int t, int rows, Raw& r) {  // (rows behind the last repeat it; they are masked)
     const int64_t base = ((int64_t)page_at(t) * a.pool.Hkv + it.g) * MX_PAGE;
     const unsigned back = c_row < rows ? 0u : (unsigned)(c_row - (rows - 1));
     const unsigned co = (unsigned)code_off - back * ROW, so = (unsigned)scale_off - back * NS;  // (a scalar base and a lane's 32 bits)
     // (the statements keep the page's address in scalar registers: added to a lane's address ahead of the loop it takes
     // two registers to a tensor)
-    const unsigned char *kc = my_codes + base * ROW, *ks = my_scales + base * NS;
+    mx_mem kc = (mx_mem)(my_codes + base * ROW), ks = (mx_mem)(my_scales + base * NS);
     asm volatile("" : "+s"(kc), "+s"(ks));
-    r.k = *reinterpret_cast<const uint4*>(kc + co);
+    r.k = mx_load16(kc + co);
     r.ks = ks[so];
     if constexpr (BOTH) {
-      const unsigned char *vc = a.pool.v_codes + base * ROW, *vs = a.pool.v_scales + base * NS;
+      mx_mem vc = (mx_mem)(a.pool.v_codes + base * ROW), vs = (mx_mem)(a.pool.v_scales + base * NS);
       asm volatile("" : "+s"(vc), "+s"(vs));
-      r.v = *reinterpret_cast<const uint4*>(vc + co);
+      r.v = mx_load16(vc + co);
       r.vs = vs[so];
     }
   };
@@ -128,10 +120,43 @@ __device__ __forceinline__ void attn_mx_shared(const MxAttnArgs& a, const MxItem
       put(r.k, r.ks, my_one + slot * my_step, x);
     }
   };
-  // barrier of the workgroup; loads in flight stay in flight
-  auto meet = [&]() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
+  auto meet = [&]() { mx_meet(); };
 
-  if (tid == 0) odd_lds = redo = 0;
+  // ---- what the first steps wait for is requested first, all of it: the pages, the tree's parents and its last tile, Q, three
+  // tiles of codes
+  constexpr int PER = MX_PAGE * (D / 8) / MXA_THREADS;  // 16-byte pieces of K (and of V) of a tree tile to a thread
+  static_assert(PER <= 2, "two pieces");
+  const int row_last = (it.blk0 + it.blk_n) * 32 <= Rh ? (it.blk0 + it.blk_n) * 32 - 1 : Rh - 1;
+  const int tree_top = last_split ? mx_own(a, it, row_last).i / MX_PAGE : -1;  // the last tile that a row of this workgroup sees
+  uint4 k0, v0, k1, v1;  // (an array is given memory here, not registers)
+  auto load_tree = [&](int t) {
+    const int left = it.M - t * MX_PAGE;  // >= 1 rows of this tile exist; rows behind them repeat the last
+    const bf16_t* const kb = static_cast<const bf16_t*>(a.k_tree) + (int64_t)(it.n0 + t * MX_PAGE) * a.k_stride + it.g * D;
+    const bf16_t* const vb = static_cast<const bf16_t*>(a.v_tree) + (int64_t)(it.n0 + t * MX_PAGE) * a.v_stride + it.g * D;
+    int x = tid;
+    asm volatile("" : "+v"(x));  // (no address of these is kept in registers through the pages)
+    auto one = [&](int id, uint4& k, uint4& v) {
+      const int key = id / (D / 8), c = id % (D / 8), r = key < left ? key : left - 1;
+      k = *reinterpret_cast<const uint4*>(kb + r * a.k_stride + 8 * c);
+      v = *reinterpret_cast<const uint4*>(vb + r * a.v_stride + 8 * c);
+    };
+    one(x, k0, v0);
+    if constexpr (PER == 2) one(x + MXA_THREADS, k1, v1);
+  };
+  MxParents parents = {};
+  MxPath path = {0u, 0u, 0};
+  const bool small = it.M <= 64;
+  if (last_split) {
+    parents = mx_request_parents(a, it);
+    load_tree(tree_top);
+  }
+  // ---- Q (B operand): element 16 kk + 8 half + j of step kk; by way of the wave's part of the tile buffers
+  char* const q_lds = lds + wave * 32 * MX_Q_ROW<D>;
+  static_assert(MXA_WAVES * 32 * MX_Q_ROW<D> <= (int)sizeof(mem.tiles), "room for Q");
+  if (active) mx_stage_q<D>(a, it, row_base, q_lds, lane, 64);
+  bf16x8 qf[NK];
+  if (last_split && !small) mx_stage_tree(it, parents, par, hops);
+  if (tid == 0) odd_lds = 0;
   Raw ra, rb_, rc;
   if (n_full > 0) {
     load(0, MX_PAGE, ra);
@@ -139,14 +164,10 @@ __device__ __forceinline__ void attn_mx_shared(const MxAttnArgs& a, const MxItem
     load(n_full > 2 ? 2 : n_full - 1, MX_PAGE, rc);
   }
 
-  // ---- Q (B operand): element 16 kk + 8 half + j of step kk
-  bf16x8 qf[NK];
-  {
-    const Own o = own();
-    const bf16_t* const src = static_cast<const bf16_t*>(a.q) + (int64_t)(it.n0 + o.i) * a.q_stride + (int64_t)o.h * D + 8 * half;
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
-    for (int kk = 0; kk < NK; ++kk) qf[kk] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(src + 16 * kk));
-  }
+  for (int kk = 0; kk < NK; ++kk) qf[kk] = *reinterpret_cast<const bf16x8*>(q_lds + col * MX_Q_ROW<D> + 32 * kk + 16 * half);
+  meet();  // (the buffers are free)
   MxState<D> st;
   st.clear();
   const float c2 = a.c2;
@@ -236,6 +257,15 @@ __device__ __forceinline__ void attn_mx_shared(const MxAttnArgs& a, const MxItem
     return S;
   };
 
+  // ---- the tree's own rows, the full pages, the partial page
+  auto block = [&](int b, const floatx16& S) {
+    const int slot = 0;
+    uint4 p0, p1;
+    st.softmax(S, c2, p0, p1);
+    const bf16x8 b0 = __builtin_bit_cast(bf16x8, p0), b1 = __builtin_bit_cast(bf16x8, p1);
+#pragma unroll
+    for (int f = 0; f < NK; ++f) st.acc[f % NT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ldv(slot, b, f), f < NT ? b0 : b1, st.acc[f % NT], 0, 0, 0);
+  };
   // Tile t + 1 of buffer S1 is converted from r, tile t + 4 requested into it (the last tile again behind the end).
   auto next_tile = [&](int t, Raw& r) { load(t + 4 < n_full ? t + 4 : n_full - 1, MX_PAGE, r); };
   auto convert = [&](const Raw& r, int slot, int j) {  // a step's share
@@ -246,10 +276,15 @@ __device__ __forceinline__ void attn_mx_shared(const MxAttnArgs& a, const MxItem
   // f(t, buffer of t, registers of tile t + 1) for every full tile but the last
   auto every_tile = [&](auto f) {
     int t = 0;
-    for (; t + 3 < n_full; t += 3) {  // (the buffers spelled out: every LDS address is a register plus an immediate)
-      f(t, std::integral_constant<int, 0>{}, rb_);
-      f(t + 1, std::integral_constant<int, 1>{}, rc);
-      f(t + 2, std::integral_constant<int, 2>{}, ra);
+    while (t + 3 < n_full) {
+      // 57 tiles request up to the 62nd from here.  (With the look-up of the pages in the loop, under a branch, the waits for a tile
+      // could not count the younger ones.)
+      if (t > 0) page_of = pages_from(page_base = t);
+      for (const int stop = t + 57; t + 3 < n_full && t < stop; t += 3) {  // (the buffers spelled out: every LDS address is a register plus an immediate)
+        f(t, std::integral_constant<int, 0>{}, rb_);
+        f(t + 1, std::integral_constant<int, 1>{}, rc);
+        f(t + 2, std::integral_constant<int, 2>{}, ra);
+      }
     }
     if (t + 1 < n_full) {
       f(t, std::integral_constant<int, 0>{}, rb_);
@@ -260,6 +295,48 @@ __device__ __forceinline__ void attn_mx_shared(const MxAttnArgs& a, const MxItem
     }
     return t;
   };
+  if (tree_top >= 0) {
+    path.cur = own().i;
+    if (small) mx_small_paths(parents.a, it.M, path.cur, path);
+    bool fresh = true;
+    for (int t = tree_top; t >= 0; --t) {  // (a small tree is one tile)
+      const int left = it.M - t * MX_PAGE;
+      ushort2v most = {0, 0};
+      meet();  // (the buffer's last readers are done)
+      int own_id = tid;
+      asm volatile("" : "+v"(own_id));
+      auto put_one = [&](int id, const uint4& k, const uint4& v) {
+        const int key = id / (D / 8), c = id % (D / 8);
+        note_bits(most, v);
+        *reinterpret_cast<uint4*>(lds_k + key * KR + c * 16) = k;
+        *reinterpret_cast<uint4*>(lds_v + key * VR + c * 16) = without_odd(v);
+      };
+      put_one(own_id, k0, v0);
+      if constexpr (PER == 2) put_one(own_id + MXA_THREADS, k1, v1);
+      if (has_odd(most)) odd_lds = 1;
+      if (t > 0) load_tree(t - 1);
+      meet();
+      if (active) {
+        for (int x = 0; x < 2; ++x) {
+          const int b = small ? x : 1 - x;
+          const unsigned word = mx_path_word(small, hops, path, 2 * t + b);
+          if (W == 2 && b != way) continue;
+          if (__ballot(word != 0u) == 0ull) continue;
+          floatx16 S = scores(0, W == 2 ? 0 : b);
+#pragma unroll
+          for (int v = 0; v < 16; ++v) S[v] = (word >> (8 * (v >> 2) + 4 * half + (v & 3))) & 1u ? S[v] : -HS_INF;
+          if (fresh) st.start(S, c2);
+          fresh = false;
+          block(W == 2 ? 0 : b, S);
+          if (odd_lds != 0) {
+            const bf16_t* const vb = static_cast<const bf16_t*>(a.v_tree) + (int64_t)(it.n0 + t * MX_PAGE + 32 * b) * a.v_stride + it.g * D;
+            st.add_odd(vb, a.v_stride, left - 32 * b < 32 ? left - 32 * b : 32, word, half);
+          }
+        }
+      }
+    }
+    meet();
+  }
   if (n_full > 0) {
 #pragma unroll
     for (int x = 0; x < PIECES; ++x) put_piece(ra, 0, x);
@@ -269,7 +346,7 @@ __device__ __forceinline__ void attn_mx_shared(const MxAttnArgs& a, const MxItem
       floatx16 sA, sB;
       uint4 pa, pb, pc;
       sA = scores(0, 0);
-      st.start(sA, c2);  // the maximum of the whole pass over the full tiles
+      st.move(sA, c2, HS_INF);  // the maximum of the whole pass over the full tiles
       st.exp_half(sA, c2, 0, pa, st.l);
       const int last = every_tile([&](int t, auto slot, Raw& r) {
         const int S0 = slot, S1 = (S0 + 1) % MXS_BUF;
@@ -311,35 +388,14 @@ __device__ __forceinline__ void attn_mx_shared(const MxAttnArgs& a, const MxItem
       });
     }
   }
-
-  // ---- the partial page (all pages where the fixed maximum did not hold), and the tree's own rows from the last that a row of this workgroup sees to the first
-  auto block = [&](int b, const floatx16& S) {
-    const int slot = 0;
-    uint4 p0, p1;
-    st.softmax(S, c2, p0, p1);
-    const bf16x8 b0 = __builtin_bit_cast(bf16x8, p0), b1 = __builtin_bit_cast(bf16x8, p1);
-#pragma unroll
-    for (int f = 0; f < NK; ++f) st.acc[f % NT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ldv(slot, b, f), f < NT ? b0 : b1, st.acc[f % NT], 0, 0, 0);
-  };
-  int t0 = n_full;
-  if (n_full > 0) {
-    if (st.over(st.l)) redo = 1;  // (lanes of a wave agree)
-    meet();
-    if (redo != 0) {
-      t0 = 0;
-      page_base = -64;
-      st.clear();
-    }
-  }
-  for (int t = t0; t * MX_PAGE < keys; ++t) {
-    const int rest = keys - t * MX_PAGE;
-    load(t, rest < MX_PAGE ? rest : MX_PAGE, ra);
+  if (keys > n_full * MX_PAGE) {
+    const int rest = keys - n_full * MX_PAGE;
+    load(n_full, rest, ra);
     meet();  // (the buffer's last readers are done)
 #pragma unroll
     for (int x = 0; x < PIECES; ++x) put_piece(ra, 0, x);
     meet();
     if (active) {
-#pragma unroll
       for (int b = 0; b < 2; ++b) {
         if (W == 2 ? b != way : false) continue;
         if (32 * b >= rest) continue;
@@ -350,49 +406,9 @@ __device__ __forceinline__ void attn_mx_shared(const MxAttnArgs& a, const MxItem
       }
     }
   }
-  if (last_split) {
-    mx_stage_tree(a, it, par, hops);
-    const int last_blk = (it.blk0 + it.blk_n) * 32;
-    const int r_top = last_blk <= Rh ? last_blk - 1 : Rh - 1;
-    int cur = own().i;
-    constexpr int PER = MX_PAGE * (D / 8) / MXA_THREADS;  // 16-byte pieces of K (and of V) of a thread
-    for (int t = (r_top / a.G) / MX_PAGE; t >= 0; --t) {
-      const int left = it.M - t * MX_PAGE;  // >= 1 rows of this tile exist
-      const bf16_t* const kb = static_cast<const bf16_t*>(a.k_tree) + (int64_t)(it.n0 + t * MX_PAGE) * a.k_stride + it.g * D;
-      const bf16_t* const vb = static_cast<const bf16_t*>(a.v_tree) + (int64_t)(it.n0 + t * MX_PAGE) * a.v_stride + it.g * D;
-      uint4 kp[PER], vp[PER];
-      ushort2v most = {0, 0};
-#pragma unroll
-      for (int n = 0; n < PER; ++n) {
-        const int id = n * MXA_THREADS + tid, key = id / (D / 8), c = id % (D / 8), r = key < left ? key : left - 1;
-        kp[n] = *reinterpret_cast<const uint4*>(kb + r * a.k_stride + 8 * c);
-        vp[n] = *reinterpret_cast<const uint4*>(vb + r * a.v_stride + 8 * c);
-      }
-      meet();
-#pragma unroll
-      for (int n = 0; n < PER; ++n) {
-        const int id = n * MXA_THREADS + tid, key = id / (D / 8), c = id % (D / 8);
-        note_bits(most, vp[n]);
-        *reinterpret_cast<uint4*>(lds_k + key * KR + c * 16) = kp[n];
-        *reinterpret_cast<uint4*>(lds_v + key * VR + c * 16) = without_odd(vp[n]);
-      }
-      if (has_odd(most)) odd_lds = 1;
-      meet();
-      if (active) {
-#pragma unroll
-        for (int b = 1; b >= 0; --b) {
-          const unsigned word = mx_path_word(hops, cur, 2 * t + b);
-          if (W == 2 && b != way) continue;
-          if (__ballot(word != 0u) == 0ull) continue;
-          floatx16 S = scores(0, W == 2 ? 0 : b);
-#pragma unroll
-          for (int v = 0; v < 16; ++v) S[v] = (word >> (8 * (v >> 2) + 4 * half + (v & 3))) & 1u ? S[v] : -HS_INF;
-          block(W == 2 ? 0 : b, S);
-          if (odd_lds != 0) st.add_odd(vb + (int64_t)(32 * b) * a.v_stride, a.v_stride, left - 32 * b < 32 ? left - 32 * b : 32, word, half);
-        }
-      }
-    }
-  }
+  if (st.over(st.l)) redo = 1;  // (lanes of a wave agree)
+  meet();
+  if (redo != 0) return false;
 
   // ---- out
   st.l = half_sum(st.l);
@@ -416,8 +432,8 @@ __device__ __forceinline__ void attn_mx_shared(const MxAttnArgs& a, const MxItem
         to[(t * 4 + b) * 64] = make_float4(st.acc[t][4 * b] * mine, st.acc[t][4 * b + 1] * mine, st.acc[t][4 * b + 2] * mine, st.acc[t][4 * b + 3] * mine);
     meet();
   }
-  if (!active || row_base + col >= Rh) return;
-  const Own o = own();
+  if (!active || row_base + col >= Rh) return true;
+  const MxOwn o = own();
   const int64_t out_row = (int64_t)(it.n0 + o.i) * a.Hq + o.h;
   float* const rec = a.part + (it.rec0 + ((int64_t)o.i * a.Hq + o.h) * it.n_sp + it.sp) * (D + ATTN_REC_PAD);
   const float inv = 1.f / total;
@@ -443,6 +459,7 @@ __device__ __forceinline__ void attn_mx_shared(const MxAttnArgs& a, const MxItem
       rec[D + 1] = total;
     }
   }
+  return true;
 }
 
 }  // namespace hs

@@ -33,6 +33,14 @@ struct Mx<HS_MX_E2M1> {
 };
 __host__ __device__ constexpr int mx_row_bytes(int fmt, int D) { return fmt == HS_MX_E4M3 ? D : D / 2; }
 
+// Memory that a pointer out of an asm statement is known to be (of a generic one the loads would be waited for all together).
+typedef const __attribute__((address_space(1))) unsigned char* mx_mem;
+typedef __attribute__((ext_vector_type(4))) unsigned mx_u4;
+__device__ __forceinline__ uint4 mx_load16(mx_mem p) {
+  const mx_u4 v = *reinterpret_cast<const __attribute__((address_space(1))) mx_u4*>(p);
+  return make_uint4(v[0], v[1], v[2], v[3]);
+}
+
 // A cache as the kernels see it.
 struct MxPool {
   unsigned char* k_codes;

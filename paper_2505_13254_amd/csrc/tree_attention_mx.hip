@@ -25,23 +25,31 @@ void attn_mx_launch_e2m1(const MxAttnArgs& a, unsigned items, hipStream_t stream
 // The splits of a (row, head) meet: a wave each, whose lanes first find the splits' weights, a split to a lane, and then add up
 // the records, D / 4 lanes and four columns to a lane to each of 64 / (D / 4) records at a time.
 constexpr int MXM_THREADS = 256;
-template <int FMT, int D>
+template <int D>
 __global__ __launch_bounds__(MXM_THREADS) void k_attn_mx_merge(MxAttnArgs a, int64_t rows) {
   constexpr int LANES = D / 4, AT_ONCE = 64 / LANES;
   const int lane = (int)(threadIdx.x & 63);
   const int64_t x = __builtin_amdgcn_readfirstlane((int)((int64_t)blockIdx.x * (MXM_THREADS / 64) + (threadIdx.x >> 6)));  // n * Hq + h
   if (x >= rows) return;
   const int n = (int)(x / a.Hq);
-  // its sequence and the records before, by the prefix sums of the attention's items
+  // its sequence and the records before
   int64_t recs = 0, first = -1;
   int n_sp = 0;
-  for (int base = 0; base < a.B; base += 64) {
+  if (a.n_entries > 0) {
+    const int4 lo = *reinterpret_cast<const int4*>(&a.entries[lane]), hi = *(reinterpret_cast<const int4*>(&a.entries[lane]) + 1);
+    const unsigned long long mine = __ballot(lane < a.n_entries && lo.y <= n && n < lo.y + lo.z);
+    if (mine == 0ull) return;
+    const int e = __builtin_ctzll(mine);
+    n_sp = __builtin_amdgcn_readlane(hi.y, e) & 255;
+    first = __builtin_amdgcn_readlane(hi.w, e) + (x - (int64_t)__builtin_amdgcn_readlane(lo.y, e) * a.Hq) * n_sp;
+  }
+  for (int base = 0; a.n_entries == 0 && base < a.B; base += 64) {
     const int s = base + lane;
     int n0 = 0, M = 0, sp = 0;
     if (s < a.B) {
       n0 = a.node_offsets[s];
       M = a.node_offsets[s + 1] - n0;
-      sp = mx_cut(a.G * M, a.lens[s], FMT, a.blocks_most, a.target).n_sp;
+      sp = mx_cut(M, a.G, (int)a.lens[s], a.cuts).n_sp;
     }
     const int rec = M > 0 && sp > 1 ? M * a.Hq * sp : 0;
     const int upto = wave_prefix_sum(rec);
@@ -96,32 +104,34 @@ __global__ __launch_bounds__(MXM_THREADS) void k_attn_mx_merge(MxAttnArgs a, int
 // ---- the plan
 constexpr int64_t MXA_RECORDS = 1 << 18;  // records that a call uses at most
 struct MxPlan {
-  int blocks_most, target;
+  MxCuts cuts;
   int64_t items, records;
 };
-static MxPlan mx_plan(const int32_t* hno, const int64_t* hlens, int B, int Hq, int Hkv, int fmt) {
+// What a page of 64 keys costs a workgroup in the four forms, in microseconds.
+constexpr double MX_PAGE_US[4] = {0.45, 0.6, 1.0, 1.6};
+static MxPlan mx_plan(const int32_t* hno, const int64_t* hlens, int B, int Hq, int Hkv) {
   const int G = Hq / Hkv;
-  MxPlan best = {8, 1 << 24, 0, 0};
+  MxPlan best = {};
   double best_us = 1e30;
   for (int most = 1; most <= 8; most *= 2) {
     for (int t = 0; t < 12; ++t) {
-      const int target = t == 11 ? 1 << 24 : 8 << t;
-      MxPlan p = {most, target, 0, 0};
+      const double target = t == 11 ? 1e9 : (double)(1 << t);  // what an item may take
+      MxPlan p = {};
+      p.cuts.blocks_most = most;
+      for (int f = 0; f < 4; ++f) p.cuts.pages[f] = (int)std::min(1e6, std::max(1.0, target / MX_PAGE_US[f]));
       double total = 0.0, longest = 0.0;
       for (int s = 0; s < B; ++s) {
         const int M = hno[s + 1] - hno[s];
         if (M <= 0) continue;
-        const MxCut c = mx_cut(G * M, hlens[s], fmt, most, target);
+        const MxCut c = mx_cut(M, G, (int)hlens[s], p.cuts);
         const int64_t items = (int64_t)c.n_sp * c.n_rg * Hkv;
-        const int64_t pages = (hlens[s] + MX_PAGE - 1) / MX_PAGE;
+        const int64_t pages = (hlens[s] + MX_PAGE - 1) / MX_PAGE + (M + MX_PAGE - 1) / MX_PAGE;
         p.items += items;
         if (c.n_sp > 1) p.records += (int64_t)M * Hq * c.n_sp;
-        const double cost = MX_PAGE_COST[fmt][c.form] / 16.0;
-        const double tree = ((M + MX_PAGE - 1) / MX_PAGE) * (c.form < MX_SHARED_4 ? 0.5 : 2.0);
-        total += (double)c.n_rg * Hkv * (pages * cost + tree) + items * 3.0;
-        longest = std::max(longest, 3.0 + c.pages * cost + tree);
+        total += (double)c.n_rg * Hkv * pages * MX_PAGE_US[c.form] + items * 5.0;
+        longest = std::max(longest, 5.0 + c.pages * MX_PAGE_US[c.form]);
       }
-      if (p.records > MXA_RECORDS && target != 1 << 24) continue;
+      if (p.records > MXA_RECORDS && t < 11) continue;
       const double us = std::max(longest, total / 256.0) + (p.records > 0 ? 5.0 + p.records * 1e-4 : 0.0);
       if (us < best_us) {
         best_us = us;
@@ -140,6 +150,7 @@ static hs_status mx_attn_host_check(const int32_t* hno, const int64_t* hlens, in
   HS_REQUIRE(B >= 0 && Hq >= 1 && Hkv >= 1, HS_ERR_SHAPE, "hs_tree_attention_mx: B=%d Hq=%d Hkv=%d", B, Hq, Hkv);
   HS_REQUIRE(Hq % Hkv == 0, HS_ERR_SHAPE, "hs_tree_attention_mx: Hq=%d is not a multiple of Hkv=%d", Hq, Hkv);
   HS_REQUIRE(D == 64 || D == 128, HS_ERR_UNSUPPORTED, "hs_tree_attention_mx: D=%d (64 and 128 are built)", D);
+  HS_REQUIRE(Hq / Hkv <= 1024 && Hkv <= 4096, HS_ERR_UNSUPPORTED, "hs_tree_attention_mx: Hq=%d Hkv=%d", Hq, Hkv);
   if (B == 0) return HS_OK;
   HS_REQUIRE(hno && hlens, HS_ERR_NULL, "hs_tree_attention_mx: NULL host array");
   HS_REQUIRE(hno[0] == 0, HS_ERR_SHAPE, "hs_tree_attention_mx: node_offsets[0] = %d", hno[0]);
@@ -160,9 +171,7 @@ extern "C" size_t hs_tree_attention_mx_workspace(const int32_t* host_node_offset
                                                  int32_t Hq, int32_t Hkv, int32_t D) {
   clear_error();
   if (mx_attn_host_check(host_node_offsets, host_prefix_lens, B, Hq, Hkv, D) != HS_OK || B == 0) return 0;
-  size_t most = 0;  // (of either format)
-  for (int fmt = HS_MX_E4M3; fmt <= HS_MX_E2M1; ++fmt) most = std::max(most, mx_bytes(mx_plan(host_node_offsets, host_prefix_lens, B, Hq, Hkv, fmt), D));
-  return most;
+  return mx_bytes(mx_plan(host_node_offsets, host_prefix_lens, B, Hq, Hkv), D);
 }
 
 extern "C" hs_status hs_tree_attention_mx(const void* q, int64_t q_stride, const void* k_codes, const void* k_scales,
@@ -207,30 +216,33 @@ extern "C" hs_status hs_tree_attention_mx(const void* q, int64_t q_stride, const
              HS_ERR_UNSUPPORTED, "%s: rows must begin at multiples of 16 bytes", what);
   a.q = q, a.k_tree = k_tree, a.v_tree = v_tree, a.q_stride = q_stride, a.k_stride = k_stride, a.v_stride = v_stride;
   a.parent = parent, a.node_offsets = node_offsets, a.lens = prefix_lens;
-  a.B = B, a.Hq = Hq, a.G = Hq / Hkv;
+  a.B = B, a.Hq = Hq, a.G = Hq / Hkv, a.inv_G = 1.f / (float)(Hq / Hkv);
   a.c2 = scale * MXA_LOG2E;
   a.o = o, a.lse = lse, a.part = static_cast<float*>(workspace);
-  const MxPlan p = mx_plan(host_node_offsets, host_prefix_lens, B, Hq, Hkv, fmt);
+  const MxPlan p = mx_plan(host_node_offsets, host_prefix_lens, B, Hq, Hkv);
   HS_REQUIRE(p.items < ((int64_t)1 << 31), HS_ERR_UNSUPPORTED, "%s: too many rows for one call", what);
   const size_t need = mx_bytes(p, D);
   if (need > 0) {
     HS_REQUIRE(workspace && reinterpret_cast<uintptr_t>(workspace) % 256 == 0 && workspace_bytes >= need, HS_ERR_WORKSPACE,
                "%s: workspace of %zu bytes, %zu are needed (256-byte aligned)", what, workspace_bytes, need);
   }
-  a.blocks_most = p.blocks_most, a.target = p.target;
+  a.cuts = p.cuts;
+  if (B <= MXA_ENTRIES) {
+    a.n_entries = B;
+    int first = 0, rec0 = 0;
+    for (int s = 0; s < B; ++s) {
+      const int n0 = host_node_offsets[s], M = host_node_offsets[s + 1] - n0;
+      const MxCut c = mx_cut(M, a.G, (int)host_prefix_lens[s], p.cuts);
+      a.entries[s] = MxEntry{first, n0, M, (int)host_prefix_lens[s], c.pages, c.n_sp | c.form << 8, (int)((unsigned)c.n_blk | (unsigned)c.n_rg << 16), rec0};
+      if (M > 0) first += c.n_sp * c.n_rg * Hkv, rec0 += c.n_sp > 1 ? M * Hq * c.n_sp : 0;
+    }
+  }
   (fmt == HS_MX_E4M3 ? attn_mx_launch_e4m3 : attn_mx_launch_e2m1)(a, (unsigned)p.items, static_cast<hipStream_t>(stream));
   st = launch_status(what);
   if (st != HS_OK || p.records == 0) return st;
   const int64_t rows = (int64_t)NN * Hq;
   const dim3 merge_grid((unsigned)((rows + MXM_THREADS / 64 - 1) / (MXM_THREADS / 64)));
-#define MXM_LAUNCH(F, DD) hipLaunchKernelGGL((k_attn_mx_merge<F, DD>), merge_grid, dim3(MXM_THREADS), 0, static_cast<hipStream_t>(stream), a, rows)
-  if (fmt == HS_MX_E4M3) {
-    if (D == 128) MXM_LAUNCH(HS_MX_E4M3, 128);
-    else MXM_LAUNCH(HS_MX_E4M3, 64);
-  } else {
-    if (D == 128) MXM_LAUNCH(HS_MX_E2M1, 128);
-    else MXM_LAUNCH(HS_MX_E2M1, 64);
-  }
-#undef MXM_LAUNCH
+  if (D == 128) hipLaunchKernelGGL((k_attn_mx_merge<128>), merge_grid, dim3(MXM_THREADS), 0, static_cast<hipStream_t>(stream), a, rows);
+  else hipLaunchKernelGGL((k_attn_mx_merge<64>), merge_grid, dim3(MXM_THREADS), 0, static_cast<hipStream_t>(stream), a, rows);
   return launch_status(what);
 }
