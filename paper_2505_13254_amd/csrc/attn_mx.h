@@ -1,5 +1,7 @@
 // Shared pieces of the attention kernels on a quantised cache (internal).
 #pragma once
+#include <type_traits>
+
 #include "mx.h"
 
 namespace hs {
@@ -50,14 +52,16 @@ __host__ __device__ __forceinline__ int mx_div(int x, int d) {
 struct MxCut {
   int n_blk, n_rg, form, pages, n_sp;  // pages: of a split
 };
-__host__ __device__ __forceinline__ MxCut mx_cut(int M, int G, int L, const MxCuts& cuts) {
+__host__ __device__ __forceinline__ MxCut mx_groups(int M, int G, int blocks_most) {
   MxCut c;
   c.n_blk = (G * M + 31) >> 5;
-  const int shift = cuts.blocks_most == 8 ? 3 : cuts.blocks_most == 4 ? 2 : cuts.blocks_most == 2 ? 1 : 0;
-  c.n_rg = (c.n_blk + cuts.blocks_most - 1) >> shift;
+  const int shift = blocks_most == 8 ? 3 : blocks_most == 4 ? 2 : blocks_most == 2 ? 1 : 0;
+  c.n_rg = (c.n_blk + blocks_most - 1) >> shift;
   const bool over4 = c.n_blk > 4 * c.n_rg, over2 = c.n_blk > 2 * c.n_rg, over1 = c.n_blk > c.n_rg;
   c.form = over4 ? MX_SHARED_8 : over2 ? MX_SHARED_4 : over1 ? MX_PRIVATE_2 : MX_PRIVATE_1;
-  int per = over4 ? cuts.pages[3] : over2 ? cuts.pages[2] : over1 ? cuts.pages[1] : cuts.pages[0];
+  return c;
+}
+__host__ __device__ __forceinline__ void mx_splits(int M, int L, int per, MxCut& c) {
   const int pages = (L + MX_PAGE - 1) >> 6, tiles = (M + MX_PAGE - 1) >> 6, all = pages + tiles;
   const int least = mx_div(all + MXA_SPLITS - 2, MXA_SPLITS - 1);
   per = per < least ? least : per < 1 ? 1 : per;
@@ -67,16 +71,20 @@ __host__ __device__ __forceinline__ MxCut mx_cut(int M, int G, int L, const MxCu
   c.n_sp = mx_div(pages + c.pages - 1, c.pages);
   if (c.n_sp > 0 && tiles > c.n_sp * c.pages - pages) ++c.n_sp;
   c.n_sp = c.n_sp < 1 ? 1 : c.n_sp;
+}
+__host__ __device__ __forceinline__ MxCut mx_cut(int M, int G, int L, const MxCuts& cuts) {
+  MxCut c = mx_groups(M, G, cuts.blocks_most);
+  mx_splits(M, L, c.form == 3 ? cuts.pages[3] : c.form == 2 ? cuts.pages[2] : c.form == 1 ? cuts.pages[1] : cuts.pages[0], c);
   return c;
 }
 
-// A sequence as the host cut it.  The entries of up to MXA_ENTRIES sequences travel in the kernel's arguments: a workgroup then
+// A sequence with rows as the host cut it.  The entries of up to MXA_ENTRIES sequences, in the order of their items, travel in the kernel's arguments: a workgroup then
 // knows its item after one trip to memory instead of two (2000 cycles).  Longer batches cut on the device.
 struct MxEntry {
   int first;       // its first item
   int n0, M, L;
   int pages;       // of a split
-  int n_sp_form;   // splits | form << 8
+  int n_sp_form;   // splits | form << 8 | sequence << 16
   int groups;      // row blocks | row groups << 16
   int rec0;        // records of the sequences before
 };
@@ -123,17 +131,24 @@ __device__ __forceinline__ void mx_place(const MxAttnArgs& a, int local, int n_b
 }
 __device__ __forceinline__ bool mx_item(const MxAttnArgs& a, int item, MxItem& w) {
   const int lane = (int)(threadIdx.x & 63);
+  if (a.n_entries == 1) {  // (its entry comes with the other arguments)
+    const MxEntry& e = a.entries[0];
+    w.s = e.n_sp_form >> 16, w.n0 = e.n0, w.M = e.M, w.L = e.L, w.pages = e.pages, w.rec0 = 0;
+    w.n_sp = e.n_sp_form & 255, w.form = (e.n_sp_form >> 8) & 255;
+    mx_place(a, item, e.groups & 0xffff, (int)((unsigned)e.groups >> 16), w);
+    return true;
+  }
   if (a.n_entries > 0) {
     const int4 lo = *reinterpret_cast<const int4*>(&a.entries[lane]), hi = *(reinterpret_cast<const int4*>(&a.entries[lane]) + 1);
-    const int e = __builtin_popcountll(__ballot(lane < a.n_entries && lo.x <= item)) - 1;  // (sequences without rows share their successor's first item)
-    w.s = e;
+    const int e = __builtin_popcountll(__ballot(lane < a.n_entries && lo.x <= item)) - 1;
     w.n0 = __builtin_amdgcn_readlane(lo.y, e);
     w.M = __builtin_amdgcn_readlane(lo.z, e);
     w.L = __builtin_amdgcn_readlane(lo.w, e);
     w.pages = __builtin_amdgcn_readlane(hi.x, e);
     const int nf = __builtin_amdgcn_readlane(hi.y, e), groups = __builtin_amdgcn_readlane(hi.z, e);
     w.n_sp = nf & 255;
-    w.form = nf >> 8;
+    w.form = (nf >> 8) & 255;
+    w.s = nf >> 16;
     w.rec0 = __builtin_amdgcn_readlane(hi.w, e);
     mx_place(a, item - __builtin_amdgcn_readlane(lo.x, e), groups & 0xffff, (int)((unsigned)groups >> 16), w);
     return true;
@@ -195,6 +210,14 @@ template <int D>
 __device__ __forceinline__ int v_at(int r, int c) {
   const int x = D == 128 ? ((r & 3) << 2) | ((r >> 2) & 3) : (((r >> 1) & 1) << 2) | ((r >> 2) & 3);
   return r * (2 * D) + ((c ^ x) << 4);
+}
+
+// 16 bytes of each lane's own address straight into LDS, lane l's at `to` (the wave's) + 16 l.  The caller waits for them with vmcnt(0).
+// (As a builtin the compiler waits for every load in flight ahead of each loop's first read of LDS.)
+__device__ __forceinline__ void mx_to_lds(const void* from, char* to) {
+  const unsigned at = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)to);
+  unsigned saved;
+  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, off\n\ts_mov_b32 m0, %0" : "=&s"(saved) : "s"(at), "v"(from) : "memory");
 }
 
 // NaN and infinity among the values of tree rows: a row that does not see such a row must not take 0 x NaN from it.  The
@@ -386,6 +409,48 @@ __device__ __forceinline__ void mx_write4(const MxAttnArgs& a, bool whole, int64
     *reinterpret_cast<uint2*>(static_cast<bf16_t*>(a.o) + out * a.pool.D + d) = w;
   } else {
     *reinterpret_cast<float4*>(rec + d) = sum;
+  }
+}
+
+// Columns D / 2 x .. D / 2 x + D / 2 - 1 of a wave's 32 rows, by way of its part of the tile buffers (rows as Q's): whole lines leave, 16 bytes to
+// a lane.  (Every lane its own row's columns, 32 bytes to a line: 7000 cycles for 256 rows, this 3500.)
+template <int D>
+__device__ __forceinline__ void mx_write_half(const MxAttnArgs& a, const MxItem& it, int row_base, int x, const floatx16* acc, float inv, char* to, int lane) {
+  constexpr int NT = D / 64;  // of 32 columns
+  const int Rh = a.G * it.M, col = lane & 31, half = lane >> 5;
+  char* const mine = to + col * MX_Q_ROW<D>;
+  auto rows = [&](auto pieces, auto store) {
+    constexpr int PIECES = decltype(pieces)::value;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    for (int id = lane; id < 32 * PIECES; id += 64) {
+      const int r = id / PIECES, c = id % PIECES;
+      if (row_base + r < Rh) store(mx_own(a, it, row_base + r), c, *reinterpret_cast<const uint4*>(to + r * MX_Q_ROW<D> + c * 16));
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  };
+  if (it.n_sp == 1) {
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int b = 0; b < 4; ++b) {
+        const floatx2 lo = {acc[t][4 * b] * inv, acc[t][4 * b + 1] * inv}, hi = {acc[t][4 * b + 2] * inv, acc[t][4 * b + 3] * inv};
+        uint2 w;
+        w.x = __builtin_bit_cast(unsigned, __builtin_convertvector(lo, bf16x2));
+        w.y = __builtin_bit_cast(unsigned, __builtin_convertvector(hi, bf16x2));
+        *reinterpret_cast<uint2*>(mine + 64 * t + 16 * b + 8 * half) = w;
+      }
+    rows(std::integral_constant<int, D / 16>{}, [&](const MxOwn& o, int c, const uint4& w) {
+      *reinterpret_cast<uint4*>(static_cast<bf16_t*>(a.o) + ((int64_t)(it.n0 + o.i) * a.Hq + o.h) * D + x * (D / 2) + 8 * c) = w;
+    });
+  } else {
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int b = 0; b < 4; ++b)
+        *reinterpret_cast<float4*>(mine + 128 * t + 32 * b + 16 * half) = make_float4(acc[t][4 * b], acc[t][4 * b + 1], acc[t][4 * b + 2], acc[t][4 * b + 3]);
+    rows(std::integral_constant<int, D / 8>{}, [&](const MxOwn& o, int c, const uint4& w) {
+      *reinterpret_cast<uint4*>(a.part + (it.rec0 + ((int64_t)o.i * a.Hq + o.h) * it.n_sp + it.sp) * (D + ATTN_REC_PAD) + x * (D / 2) + 4 * c) = w;
+    });
   }
 }
 

@@ -12,7 +12,8 @@ __global__ __launch_bounds__(MXA_THREADS) void k_attn_mx(MxAttnArgs a) {
   // the arguments in one batch: left to itself the compiler fetches each where it is first used, one trip after another
   asm volatile("" ::"s"(a.q), "s"(a.k_tree), "s"(a.v_tree), "s"(a.q_stride), "s"(a.k_stride), "s"(a.v_stride), "s"(a.pool.k_codes),
                "s"(a.pool.k_scales), "s"(a.pool.v_codes), "s"(a.pool.v_scales), "s"(a.pool.table), "s"(a.pool.max_blocks), "s"(a.pool.n_pages),
-               "s"(a.pool.Hkv), "s"(a.parent), "s"(a.Hq), "s"(a.G), "s"(a.inv_G), "s"(a.c2), "s"(a.o), "s"(a.lse), "s"(a.part), "s"(a.n_entries));
+               "s"(a.pool.Hkv), "s"(a.parent), "s"(a.Hq), "s"(a.G), "s"(a.inv_G), "s"(a.c2), "s"(a.o), "s"(a.lse), "s"(a.part), "s"(a.n_entries),
+               "s"(a.entries[0].n0), "s"(a.entries[0].M), "s"(a.entries[0].L), "s"(a.entries[0].pages), "s"(a.entries[0].n_sp_form), "s"(a.entries[0].groups));
   MxItem it;
   if (!mx_item(a, blockIdx.x, it)) return;
   if (threadIdx.x == 0) mem.redo = 0;  // (set behind a barrier at the earliest)

@@ -96,14 +96,40 @@ __device__ __forceinline__ bool attn_mx_private(const MxAttnArgs& a, const MxIte
       vs[n] = vp_s[vr * NS + c * EPC / MX_BLOCK];
     }
   };
+  // The tree's own rows go straight into LDS, those of a small tree from here: they take no registers on the way.  Lane l's 16 bytes come to lie
+  // behind lane l - 1's, so each lane fetches the piece whose place that is.
+  constexpr int TC = 32 * (D / 8) / 64;
+  char* const tile = lds + wave * TILE;
+  auto request_tree = [&](const void* rows, int64_t stride, int b, char* to) {
+    const int end = it.M - 1 - 32 * b;  // >= 0; rows behind the last repeat it
+    int ln = lane;
+    asm volatile("" : "+v"(ln));  // (no address of these is kept in registers from block to block)
+    const bf16_t* const from = static_cast<const bf16_t*>(rows) + (int64_t)(it.n0 + 32 * b) * stride + it.g * D;
+#pragma unroll
+    for (int n = 0; n < TC; ++n) {
+      const int id = n * 64 + ln, key = id / (D / 8), c = (v_at<D>(key, id % (D / 8)) - key * (2 * D)) >> 4;
+      mx_to_lds(from + (key < end ? key : end) * stride + c * 8, to + n * 1024);
+    }
+  };
+  const int top_blk = last_split ? mx_own(a, it, row_base + 31 < Rh ? row_base + 31 : Rh - 1).i >> 5 : -1;
+  // (block b is the way's whose number is W - 1 - b % W: at most one, where the tree has two)
+  const int tree_first = W - 1 - way;
+  const bool has_tree = active && small && tree_first <= top_blk;
+  char* const tree_k = lds + MXA_WAVES * TILE + 2 * 32 * MX_Q_ROW<D> + (rb * 2 + (tree_first & 1)) * TILE;  // (behind Q)
+  static_assert(MXA_WAVES * TILE + 2 * 32 * MX_Q_ROW<D> + 4 * TILE <= (int)sizeof(mem.tiles), "tree rows behind Q");
+  if (has_tree) {
+    request_tree(a.k_tree, a.k_stride, tree_first, tree_k);
+    request_tree(a.v_tree, a.v_stride, tree_first, tile);
+  }
   if (last_split && !small) mx_stage_tree(it, parents, par, hops);
-  if (mine > 0) request_k(0);
+  if (mine > 0) {
+    request_k(0);
+  }
   mx_meet();  // Q is there
   if (last_split && small) mx_small_paths(parents.a, it.M, own.i, path);
 
   MxState<D> st;
   st.clear();
-  char* const tile = lds + wave * TILE;
   if (active) {
     bf16x8 qf[NK];  // element order of step kk as K's (see below)
 #pragma unroll
@@ -178,57 +204,63 @@ __device__ __forceinline__ bool attn_mx_private(const MxAttnArgs& a, const MxIte
     };
     // ---- the tree's own rows, block by block (of large trees from the last that a row of this wave can see to the first), dealt to the
     // ways from the last one on, which has the fewest keys
-    auto tree_rows = [&]() {
-      if (!last_split) return;
-      const int r_top = row_base + 31 < Rh ? row_base + 31 : Rh - 1;
-      const int top_blk = mx_own(a, it, r_top).i >> 5;
-      for (int x = 0; x <= top_blk; ++x) {
-        const int b = small ? x : top_blk - x;
-        const unsigned word = mx_path_word(small, hops, path, b);
+    auto tree_block = [&](int b, unsigned word, floatx16 S) {
+      const int last = it.M - 1 - 32 * b;  // >= 0
+      const int ln = lane;
+      const bf16_t* const vb = static_cast<const bf16_t*>(a.v_tree) + (int64_t)(it.n0 + 32 * b) * a.v_stride + it.g * D;
+      ushort2v most = {0, 0};
+#pragma unroll
+      for (int n = 0; n < TC; ++n) note_bits(most, *reinterpret_cast<const uint4*>(tile + n * 1024 + ln * 16));
+      const bool odd = __ballot(has_odd(most)) != 0ull;
+      if (odd)
+        for (int n = 0; n < TC; ++n) {
+          const int id = n * 64 + ln;
+          uint4* const at = reinterpret_cast<uint4*>(tile + id * 16);
+          *at = without_odd(*at);
+        }
+#pragma unroll
+      for (int v = 0; v < 16; ++v) S[v] = (word >> (8 * (v >> 2) + 4 * half + (v & 3))) & 1u ? S[v] : -HS_INF;
+      uint4 p0, p1;
+      if (fresh) st.start(S, a.c2);
+      fresh = false;
+      st.softmax(S, a.c2, p0, p1);
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      second(p0, p1);
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      if (odd) st.add_odd(vb, a.v_stride, last < 31 ? last + 1 : 32, word, half);
+    };
+    // (piece of a K row that step kk multiplies, and the step, are those of the cache's keys)
+    auto piece = [&](int kk) { return (kk / SPC) * 2 * SPC + half * SPC + kk % SPC; };
+    if (has_tree) {
+      const unsigned word = tree_first == 0 ? path.lo : path.hi;
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the tree's rows are there
+      if (__ballot(word != 0u) != 0ull) {
+        floatx16 S = zero;
+#pragma unroll
+        for (int kk = 0; kk < NK; ++kk)
+          S = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(tree_k + v_at<D>(col, piece(kk))), qf[kk], S, 0, 0, 0);
+        tree_block(tree_first, word, S);
+      }
+    } else if (!small) {
+      for (int b = top_blk; b >= 0; --b) {
+        const unsigned word = mx_path_word(false, hops, path, b);
         if (W - 1 - b % W != way || __ballot(word != 0u) == 0ull) continue;
-        const int last = it.M - 1 - 32 * b;  // >= 0
+        request_tree(a.v_tree, a.v_stride, b, tile);
+        const int end = it.M - 1 - 32 * b;
         int ln = lane;
-        asm volatile("" : "+v"(ln));  // (no address of these is kept in registers from block to block)
+        asm volatile("" : "+v"(ln));
         const int lc = ln & 31, lh = ln >> 5;
-        const int kr = it.n0 + 32 * b + (lc < last ? lc : last);
-        const bf16_t* const kp = static_cast<const bf16_t*>(a.k_tree) + (int64_t)kr * a.k_stride + it.g * D;
+        const bf16_t* const kp = static_cast<const bf16_t*>(a.k_tree) + (int64_t)(it.n0 + 32 * b + (lc < end ? lc : end)) * a.k_stride + it.g * D;
         floatx16 S = zero;
 #pragma unroll
         for (int kk = 0; kk < NK; ++kk) {
-          const uint4 f = *reinterpret_cast<const uint4*>(kp + (kk / SPC) * 2 * EPC + lh * EPC + (kk % SPC) * 8);
+          const uint4 f = *reinterpret_cast<const uint4*>(kp + 8 * ((kk / SPC) * 2 * SPC + lh * SPC + kk % SPC));
           S = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, f), qf[kk], S, 0, 0, 0);
         }
-        __builtin_amdgcn_sched_barrier(0);  // (V behind K: there are no registers for both)
-        constexpr int TC = 32 * (D / 8) / 64;
-        const bf16_t* const vb = static_cast<const bf16_t*>(a.v_tree) + (int64_t)(it.n0 + 32 * b) * a.v_stride + it.g * D;
-        ushort2v most = {0, 0};
-#pragma unroll
-        for (int n = 0; n < TC; ++n) {
-          const int id = n * 64 + ln, key = id / (D / 8), c = id % (D / 8);
-          const uint4 w = *reinterpret_cast<const uint4*>(vb + (key < last ? key : last) * a.v_stride + c * 8);
-          note_bits(most, w);
-          *reinterpret_cast<uint4*>(tile + v_at<D>(key, c)) = w;
-        }
-        const bool odd = __ballot(has_odd(most)) != 0ull;
-        if (odd)
-          for (int n = 0; n < TC; ++n) {
-            const int id = n * 64 + ln;
-            uint4* const at = reinterpret_cast<uint4*>(tile + v_at<D>(id / (D / 8), id % (D / 8)));
-            *at = without_odd(*at);
-          }
-#pragma unroll
-        for (int v = 0; v < 16; ++v) S[v] = (word >> (8 * (v >> 2) + 4 * half + (v & 3))) & 1u ? S[v] : -HS_INF;
-        uint4 p0, p1;
-        if (fresh) st.start(S, a.c2);
-        fresh = false;
-        st.softmax(S, a.c2, p0, p1);
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        second(p0, p1);
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        if (odd) st.add_odd(vb, a.v_stride, last < 31 ? last + 1 : 32, word, half);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // V is there
+        tree_block(b, word, S);
       }
-    };
-    tree_rows();
+    }
     if (mine > 0) request_v();
     if (mine > 0) step(0, std::true_type{});
     for (int j = 1; j < mine;) {

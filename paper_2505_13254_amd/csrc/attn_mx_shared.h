@@ -413,7 +413,7 @@ __device__ __forceinline__ bool attn_mx_shared(const MxAttnArgs& a, const MxItem
   // ---- out
   st.l = half_sum(st.l);
   float top = st.m, total = st.l;
-  if constexpr (W == 2) {
+  if constexpr (W == 2) {  // each way of a row block hands over the columns that the other one writes
     if (half == 0) {
       den[wave][0][col] = st.m;
       den[wave][1][col] = st.l;
@@ -424,40 +424,43 @@ __device__ __forceinline__ bool attn_mx_shared(const MxAttnArgs& a, const MxItem
     top = fmaxf(st.m, m2);
     const float mine = exp2_fast(st.m - top);
     total = st.l * mine + den[other][1][col] * exp2_fast(m2 - top);
-    float4* const to = reinterpret_cast<float4*>(lds) + wave * (NT * 4 * 64) + lane;
+    floatx16 keep[NT / 2];
+    float4* const to = reinterpret_cast<float4*>(lds) + wave * (NT / 2 * 4 * 64) + lane;
+    const float4* const from = reinterpret_cast<const float4*>(lds) + other * (NT / 2 * 4 * 64) + lane;
 #pragma unroll
-    for (int t = 0; t < NT; ++t)
+    for (int t = 0; t < NT / 2; ++t) {
+      keep[t] = way == 0 ? st.acc[t] : st.acc[NT / 2 + t];
+      const floatx16 give = way == 0 ? st.acc[NT / 2 + t] : st.acc[t];
 #pragma unroll
       for (int b = 0; b < 4; ++b)
-        to[(t * 4 + b) * 64] = make_float4(st.acc[t][4 * b] * mine, st.acc[t][4 * b + 1] * mine, st.acc[t][4 * b + 2] * mine, st.acc[t][4 * b + 3] * mine);
+        to[(t * 4 + b) * 64] = make_float4(give[4 * b] * mine, give[4 * b + 1] * mine, give[4 * b + 2] * mine, give[4 * b + 3] * mine);
+    }
     meet();
-  }
-  if (!active || row_base + col >= Rh) return true;
-  const MxOwn o = own();
-  const int64_t out_row = (int64_t)(it.n0 + o.i) * a.Hq + o.h;
-  float* const rec = a.part + (it.rec0 + ((int64_t)o.i * a.Hq + o.h) * it.n_sp + it.sp) * (D + ATTN_REC_PAD);
-  const float inv = 1.f / total;
-  const bool whole = it.n_sp == 1;
-  if constexpr (W == 1) {
 #pragma unroll
-    for (int t = 0; t < NT; ++t)
+    for (int t = 0; t < NT / 2; ++t)
 #pragma unroll
-      for (int b = 0; b < 4; ++b)
-        mx_write4(a, whole, out_row, rec, 32 * t + 8 * b + 4 * half, make_float4(st.acc[t][4 * b], st.acc[t][4 * b + 1], st.acc[t][4 * b + 2], st.acc[t][4 * b + 3]), inv);
+      for (int b = 0; b < 4; ++b) {
+        const float4 f = from[(t * 4 + b) * 64];
+        keep[t][4 * b] = keep[t][4 * b] * mine + f.x, keep[t][4 * b + 1] = keep[t][4 * b + 1] * mine + f.y;
+        keep[t][4 * b + 2] = keep[t][4 * b + 2] * mine + f.z, keep[t][4 * b + 3] = keep[t][4 * b + 3] * mine + f.w;
+      }
+    meet();
+    if (!active) return true;
+    mx_write_half<D>(a, it, row_base, way, keep, 1.f / total, q_lds, lane);
   } else {
-    const float4* const from = reinterpret_cast<const float4*>(lds) + rb * (NT * 4 * 64) + lane;
-    for (int x = way; x < NT * 4; x += 2) {
-      const float4 f = from[x * 64], g = from[BLOCKS * (NT * 4 * 64) + x * 64];
-      mx_write4(a, whole, out_row, rec, 8 * x + 4 * half, make_float4(f.x + g.x, f.y + g.y, f.z + g.z, f.w + g.w), inv);
-    }
+    if (!active) return true;
+    const float inv = 1.f / total;
+    mx_write_half<D>(a, it, row_base, 0, st.acc, inv, q_lds, lane);
+    mx_write_half<D>(a, it, row_base, 1, st.acc + NT / 2, inv, q_lds, lane);
   }
-  if (way == 0 && half == 0) {
-    if (whole) {
-      if (a.lse != nullptr) a.lse[out_row] = (top + __log2f(total)) * MXA_LN2;
-    } else {
-      rec[D] = top;
-      rec[D + 1] = total;
-    }
+  if (row_base + col >= Rh || way != 0 || half != 0) return true;
+  const MxOwn o = own();
+  if (it.n_sp == 1) {
+    if (a.lse != nullptr) a.lse[(int64_t)(it.n0 + o.i) * a.Hq + o.h] = (top + __log2f(total)) * MXA_LN2;
+  } else {
+    float* const rec = a.part + (it.rec0 + ((int64_t)o.i * a.Hq + o.h) * it.n_sp + it.sp) * (D + ATTN_REC_PAD);
+    rec[D] = top;
+    rec[D + 1] = total;
   }
   return true;
 }

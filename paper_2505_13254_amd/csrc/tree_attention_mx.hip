@@ -14,6 +14,7 @@
 // Ancestor masks: every lane walks its row's root path from the row up, a word of 32 tree rows at a time, with the
 // tree's key blocks taken from the last to the first.
 #include <algorithm>
+#include <cmath>
 
 #include "attn_mx.h"
 
@@ -64,27 +65,32 @@ __global__ __launch_bounds__(MXM_THREADS) void k_attn_mx_merge(MxAttnArgs a, int
   }
   if (n_sp <= 1) return;
   const float* const from = a.part + first * (D + ATTN_REC_PAD);
-  float m = MXA_FLOOR, l = 0.f;
-  if (lane < n_sp) {  // (at most 64 splits)
-    m = from[lane * (D + ATTN_REC_PAD) + D];
-    l = from[lane * (D + ATTN_REC_PAD) + D + 1];
-  }
-  const float top = wave_max(m), weight = exp2_fast(m - top), total = wave_sum(weight * l);
   const int d = 4 * (lane % LANES), k0 = lane / LANES;
-  float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int k = 0; k < n_sp; k += 4 * AT_ONCE) {
-    float4 f[4];
+  float4 f[4];
+  auto fetch = [&](int k) {  // (behind the last record: the last one again, at weight 0)
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {  // (behind the last record: the last one again, at weight 0)
+    for (int u = 0; u < 4; ++u) {
       const int at = k + u * AT_ONCE + k0;
-      f[u] = *reinterpret_cast<const float4*>(from + (at < n_sp ? at : n_sp - 1) * (D + ATTN_REC_PAD) + d);
+      f[u] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (k + u * AT_ONCE < n_sp) f[u] = *reinterpret_cast<const float4*>(from + (at < n_sp ? at : n_sp - 1) * (D + ATTN_REC_PAD) + d);
     }
+  };
+  const int sp = lane < n_sp ? lane : 0;  // (at most 64 splits)
+  const float2 ml = *reinterpret_cast<const float2*>(from + sp * (D + ATTN_REC_PAD) + D);
+  fetch(0);  // (the first records with their maxima: one trip to memory)
+  const float m = lane < n_sp ? ml.x : MXA_FLOOR, l = lane < n_sp ? ml.y : 0.f;
+  const float top = wave_max(m), weight = exp2_fast(m - top), total = wave_sum(weight * l);
+  float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int k = 0;;) {
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       const int at = k + u * AT_ONCE + k0;
       const float c = __shfl(weight, at & 63);
       if (at < n_sp) sum.x += c * f[u].x, sum.y += c * f[u].y, sum.z += c * f[u].z, sum.w += c * f[u].w;
     }
+    k += 4 * AT_ONCE;
+    if (k >= n_sp) break;
+    fetch(k);
   }
 #pragma unroll
   for (int o = LANES; o < 64; o *= 2) {
@@ -102,44 +108,106 @@ __global__ __launch_bounds__(MXM_THREADS) void k_attn_mx_merge(MxAttnArgs a, int
 }
 
 // ---- the plan
-constexpr int64_t MXA_RECORDS = 1 << 18;  // records that a call uses at most
+// A call's work is cut for the shortest estimated time.  What an item takes is a fixed part and one in proportion to its
+// pages, measured (D = 128) on 256 workgroups at once, where the memory and the clock give less to each, and on up to half as many.
+// Of a list of times that an item may take (a page less or more in it moves whole rounds of items) every sequence cuts itself
+// for the least total, and the best estimate of the call is taken: the total over the compute units, the longest item, and for every k
+// the k + 1 rounds that 256 k + 1 items of some size need at least; items run longest first.
+constexpr int64_t MXA_RECORDS = 1 << 18;  // records that a call uses at most, unless its sequences are longer than a split can be
+constexpr double MX_ITEM_US[4] = {5.5, 6.5, 9.0, 11.0};         // an item, by form
+constexpr double MX_PAGE_FREE_US[4] = {0.30, 0.60, 0.92, 1.27};  // a page of it, by form: up to 128 items
+constexpr double MX_PAGE_FULL_US[2][9] = {{0.0, 0.63, 0.89, 1.17, 1.34, 1.66, 1.79, 1.88, 1.99},   // 256 items, by row blocks, e4m3
+                                          {0.0, 0.37, 0.73, 0.94, 1.05, 1.29, 1.40, 1.52, 1.59}};  // e2m1
+struct MxSeqPlan {
+  MxCut cut;
+  int s;
+  int64_t items;
+  double free_us, full_us;  // its longest item
+};
 struct MxPlan {
-  MxCuts cuts;
+  MxCuts cuts;                  // B > MXA_ENTRIES: of all
+  MxSeqPlan seq[MXA_ENTRIES];   // otherwise: each, longest items first
+  int n_seq;
   int64_t items, records;
 };
-// What a page of 64 keys costs a workgroup in the four forms, in microseconds.
-constexpr double MX_PAGE_US[4] = {0.45, 0.6, 1.0, 1.6};
-static MxPlan mx_plan(const int32_t* hno, const int64_t* hlens, int B, int Hq, int Hkv) {
+static void mx_seq_plan(int M, int G, int L, int Hkv, int D, int fmt, int most, double us, MxSeqPlan& p, double& total) {
+  MxCut c = mx_groups(M, G, most);
+  const double per = D == 128 ? 1.0 : 0.5, fixed = MX_ITEM_US[c.form];
+  const double full = MX_PAGE_FULL_US[fmt][c.n_rg == 1 ? c.n_blk : (c.n_blk + c.n_rg - 1) / c.n_rg] * per;
+  mx_splits(M, L, us > 1e8 ? 1 << 20 : std::max(1, (int)((us - fixed) / full)), c);
+  const int all = (L + MX_PAGE - 1) / MX_PAGE + (M + MX_PAGE - 1) / MX_PAGE, longest = std::min(all, c.pages + (c.n_sp == 1 ? all : 0));
+  p.cut = c;
+  p.items = (int64_t)c.n_sp * c.n_rg * Hkv;
+  p.free_us = fixed + longest * MX_PAGE_FREE_US[c.form] * per;
+  p.full_us = fixed + longest * full;
+  total = (double)c.n_rg * Hkv * (c.n_sp * fixed + all * full);
+}
+static void mx_plan(const int32_t* hno, const int64_t* hlens, int B, int Hq, int Hkv, int D, int fmt, MxPlan& best) {
   const int G = Hq / Hkv;
-  MxPlan best = {};
-  double best_us = 1e30;
-  for (int most = 1; most <= 8; most *= 2) {
-    for (int t = 0; t < 12; ++t) {
-      const double target = t == 11 ? 1e9 : (double)(1 << t);  // what an item may take
-      MxPlan p = {};
+  const bool each = B <= MXA_ENTRIES;
+  MxPlan p;
+  double best_us = 1e30, most_work = 0.0;
+  best.items = best.records = 0, best.n_seq = 0;
+  const int tries = std::max(6, std::min(14, 256 / std::max(1, B)));
+  const double ratio = tries == 14 ? 1.154 : std::pow(5.6, 1.0 / (tries - 2));
+  double us = 1e9;
+  for (int t = 0; t < tries; ++t) {  // uncut, then from 1.4 times an equal share (or 11 us) down to a quarter
+    for (int most = each ? 8 : 1; most <= 8; most *= 2) {  // (sequences that are cut on the device share the size of their groups)
+      p.items = p.records = 0, p.n_seq = 0;
       p.cuts.blocks_most = most;
-      for (int f = 0; f < 4; ++f) p.cuts.pages[f] = (int)std::min(1e6, std::max(1.0, target / MX_PAGE_US[f]));
+      for (int f = 0; f < 4; ++f) p.cuts.pages[f] = us > 1e8 ? 1 << 20 : std::max(1, (int)((us - MX_ITEM_US[f]) / (MX_PAGE_FULL_US[fmt][1 << f] * (D == 128 ? 1.0 : 0.5))));
       double total = 0.0, longest = 0.0;
       for (int s = 0; s < B; ++s) {
         const int M = hno[s + 1] - hno[s];
         if (M <= 0) continue;
-        const MxCut c = mx_cut(M, G, (int)hlens[s], p.cuts);
-        const int64_t items = (int64_t)c.n_sp * c.n_rg * Hkv;
-        const int64_t pages = (hlens[s] + MX_PAGE - 1) / MX_PAGE + (M + MX_PAGE - 1) / MX_PAGE;
-        p.items += items;
-        if (c.n_sp > 1) p.records += (int64_t)M * Hq * c.n_sp;
-        total += (double)c.n_rg * Hkv * pages * MX_PAGE_US[c.form] + items * 5.0;
-        longest = std::max(longest, 5.0 + c.pages * MX_PAGE_US[c.form]);
+        MxSeqPlan now = {}, q;
+        double least = 1e30, one;
+        if (each) {
+          const int n_blk = (G * M + 31) >> 5;
+          for (int m = 1;; m *= 2) {
+            mx_seq_plan(M, G, (int)hlens[s], Hkv, D, fmt, m, us, q, one);
+            if (one < least) least = one, now = q;
+            if (m >= n_blk || m == 8) break;
+          }
+          now.s = s;
+          p.seq[p.n_seq++] = now;
+        } else {
+          mx_seq_plan(M, G, (int)hlens[s], Hkv, D, fmt, most, us, now, least);
+          const MxCut c = mx_cut(M, G, (int)hlens[s], p.cuts);
+          now.items = (int64_t)c.n_sp * c.n_rg * Hkv;
+          now.cut = c;
+        }
+        p.items += now.items;
+        if (now.cut.n_sp > 1) p.records += (int64_t)M * Hq * now.cut.n_sp;
+        total += least;
+        longest = std::max(longest, now.full_us);
       }
-      if (p.records > MXA_RECORDS && t < 11) continue;
-      const double us = std::max(longest, total / 256.0) + (p.records > 0 ? 5.0 + p.records * 1e-4 : 0.0);
-      if (us < best_us) {
-        best_us = us;
-        best = p;
+      if (us > 1e8 && most == 8) most_work = total / 256.0;
+      if (us < 1e8 && p.records > MXA_RECORDS) continue;
+      double took = std::max(total / 256.0, 0.0);
+      if (each) {
+        if (p.n_seq > 1) std::sort(p.seq, p.seq + p.n_seq, [](const MxSeqPlan& a, const MxSeqPlan& b) { return a.full_us > b.full_us || (a.full_us == b.full_us && a.s < b.s); });
+        const double load = std::min(1.0, std::max(0.0, (double)(p.items - 128) / 128.0));
+        int64_t at = 0, k = 0;
+        for (int i = 0; i < p.n_seq; ++i) {
+          const MxSeqPlan& q = p.seq[i];
+          if (i == 0) took = std::max(took, q.free_us + (q.full_us - q.free_us) * load);
+          at += q.items;
+          if (k == 0) k = 1;
+          while (at > 256 * k && k < 64) took = std::max(took, (double)(++k) * q.full_us);
+        }
+      } else {
+        took += longest * 0.5;
+      }
+      took += p.records > 0 ? 4.0 + p.records * 2.2e-4 : 0.0;
+      if (took < best_us) {
+        best_us = took;
+        best.cuts = p.cuts, best.n_seq = p.n_seq, best.items = p.items, best.records = p.records;
+        std::copy(p.seq, p.seq + p.n_seq, best.seq);
       }
     }
+    us = t == 0 ? std::max(8.0, most_work) * 1.4 : us / ratio;
   }
-  return best;
 }
 
 }  // namespace hs
@@ -171,7 +239,13 @@ extern "C" size_t hs_tree_attention_mx_workspace(const int32_t* host_node_offset
                                                  int32_t Hq, int32_t Hkv, int32_t D) {
   clear_error();
   if (mx_attn_host_check(host_node_offsets, host_prefix_lens, B, Hq, Hkv, D) != HS_OK || B == 0) return 0;
-  return mx_bytes(mx_plan(host_node_offsets, host_prefix_lens, B, Hq, Hkv), D);
+  size_t need = 0;  // of either format
+  MxPlan p;
+  for (int fmt = 0; fmt < 2; ++fmt) {
+    mx_plan(host_node_offsets, host_prefix_lens, B, Hq, Hkv, D, fmt, p);
+    need = std::max(need, mx_bytes(p, D));
+  }
+  return need;
 }
 
 extern "C" hs_status hs_tree_attention_mx(const void* q, int64_t q_stride, const void* k_codes, const void* k_scales,
@@ -219,7 +293,8 @@ extern "C" hs_status hs_tree_attention_mx(const void* q, int64_t q_stride, const
   a.B = B, a.Hq = Hq, a.G = Hq / Hkv, a.inv_G = 1.f / (float)(Hq / Hkv);
   a.c2 = scale * MXA_LOG2E;
   a.o = o, a.lse = lse, a.part = static_cast<float*>(workspace);
-  const MxPlan p = mx_plan(host_node_offsets, host_prefix_lens, B, Hq, Hkv);
+  MxPlan p;
+  mx_plan(host_node_offsets, host_prefix_lens, B, Hq, Hkv, D, (int)fmt, p);
   HS_REQUIRE(p.items < ((int64_t)1 << 31), HS_ERR_UNSUPPORTED, "%s: too many rows for one call", what);
   const size_t need = mx_bytes(p, D);
   if (need > 0) {
@@ -227,15 +302,12 @@ extern "C" hs_status hs_tree_attention_mx(const void* q, int64_t q_stride, const
                "%s: workspace of %zu bytes, %zu are needed (256-byte aligned)", what, workspace_bytes, need);
   }
   a.cuts = p.cuts;
-  if (B <= MXA_ENTRIES) {
-    a.n_entries = B;
-    int first = 0, rec0 = 0;
-    for (int s = 0; s < B; ++s) {
-      const int n0 = host_node_offsets[s], M = host_node_offsets[s + 1] - n0;
-      const MxCut c = mx_cut(M, a.G, (int)host_prefix_lens[s], p.cuts);
-      a.entries[s] = MxEntry{first, n0, M, (int)host_prefix_lens[s], c.pages, c.n_sp | c.form << 8, (int)((unsigned)c.n_blk | (unsigned)c.n_rg << 16), rec0};
-      if (M > 0) first += c.n_sp * c.n_rg * Hkv, rec0 += c.n_sp > 1 ? M * Hq * c.n_sp : 0;
-    }
+  a.n_entries = B <= MXA_ENTRIES ? p.n_seq : 0;
+  for (int e = 0, first = 0, rec0 = 0; e < a.n_entries; ++e) {
+    const MxCut& c = p.seq[e].cut;
+    const int s = p.seq[e].s, n0 = host_node_offsets[s], M = host_node_offsets[s + 1] - n0;
+    a.entries[e] = MxEntry{first, n0, M, (int)host_prefix_lens[s], c.pages, c.n_sp | c.form << 8 | s << 16, (int)((unsigned)c.n_blk | (unsigned)c.n_rg << 16), rec0};
+    first += c.n_sp * c.n_rg * Hkv, rec0 += c.n_sp > 1 ? M * Hq * c.n_sp : 0;
   }
   (fmt == HS_MX_E4M3 ? attn_mx_launch_e4m3 : attn_mx_launch_e2m1)(a, (unsigned)p.items, static_cast<hipStream_t>(stream));
   st = launch_status(what);

@@ -177,8 +177,12 @@ def test_refusals_need_no_gpu(hs):
                       (3, dict(scale=float("nan"))), (3, dict(scale=float("inf"))), (2, dict(no=(1, 3, 10))), (2, dict(no=(0, 5, 3))), (3, dict(no=(0, 3, 1028))), (2, dict(lens=(-1, 5))),
                       (2, dict(lens=(100, 257))), (3, dict(lens=(100, 1 << 40), blocks=2 ** 31 - 1)), (2, dict(pages=0)), (1, dict(q=None)), (1, dict(kt=None)), (1, dict(o=None)),
                       (1, dict(parent=None)), (1, dict(dno=None)), (1, dict(dlens=None)), (1, dict(table=None)), (1, dict(lens=None)), (2, dict(qs=100)), (2, dict(ks=1000)),
-                      (3, dict(qs=4100)), (3, dict(q=d + 8)), (4, dict(ws=None)), (4, dict(ws=d + 16)), (4, dict(ws_bytes=100))]:
+                      (3, dict(qs=4100)), (3, dict(q=d + 8))]:
         assert attend(**bad) == want, bad
+    long = dict(lens=(4096, 70), blocks=64, pages=64)  # (a call that splits its keys: one that does not needs no workspace)
+    assert lib.hs_tree_attention_mx_workspace((i32 * 3)(0, 3, 10), (i64 * 2)(4096, 70), 2, 32, 8, 128) > 100
+    for bad in (dict(ws=None), dict(ws=d + 16), dict(ws_bytes=100)):
+        assert attend(**long, **bad) == 4, bad
 
 
 def test_workspace_query_is_host_arithmetic(hs):
