@@ -1,14 +1,59 @@
 // hs_kv_append_mx, hs_kv_commit_mx, hs_kv_read_mx: rows join a quantised cache, and are read back.
 //
-// A lane takes eight neighbours of a row, four lanes a block of 32: the block's largest magnitude meets in two lane
-// exchanges (as an integer maximum of the bits, which puts NaN and infinity on top), its scale is a shift of that
-// maximum's exponent, and four conversion instructions round the eight elements.  Bound by memory: a bfloat16 row is read
-// once, 0.52 (e4m3) or 0.27 (e2m1) of it is written.
+// A workgroup takes a few rows and, of K's and V's columns side by side, as many eighths (units) as it has threads.  Its first
+// lanes look the rows up (sequence, token, page) into LDS, and a thread keeps its unit - which of K and V, head and columns - through
+// the rows, four of them at a time: what is left of a unit is an address of the row's and one of the thread's, a load, four
+// conversions and a store.  (Every lane by itself, a 64-bit division and a look-up each: 83 us instead of 52 for 36000 rows of
+// 8 heads out of e4m3, 16 instead of 12 for 8192 into it.)
+//
+// Storing, four lanes hold a block of 32: its largest magnitude meets in two lane exchanges (as an integer maximum of
+// the bits, which puts NaN and infinity on top), its scale is a shift of that maximum's exponent, and conversion instructions
+// round the elements.  Bound by memory: a bfloat16 row is read once, 0.52 (e4m3) or 0.27 (e2m1) of it is written.
 #include "mx.h"
 
 namespace hs {
 
 constexpr int MXC_THREADS = 256;
+constexpr int MXC_ROWS = 32;   // of a workgroup at most
+constexpr int MXC_AT_ONCE = 4;
+
+// Rows of a workgroup: four to a thread, whose loads then are in flight together, or fewer where that leaves less than 1024
+// workgroups.  (Rows of 256 units, us at 1 | 2 | 4 | 8 | 16 | 32 rows: 36000 read 71 | 55 | 52 | 55 | 62 | 61, 8192 stored 19 | 14 | 12 |
+// 12 | 14 | 23, 2000 read 5.8 | 6.2 | 6.2 | 6.3 | 8.5 | 15.)
+static int mxc_rows(int64_t rows, const MxPool& c) {
+  const int64_t units = 2ll * c.Hkv * (c.D >> 3), side = (units + MXC_THREADS - 1) / MXC_THREADS;
+  int64_t per = MXC_AT_ONCE * (units < MXC_THREADS ? MXC_THREADS / units : 1);
+  per = per < MXC_ROWS ? per : MXC_ROWS;
+  while (per > 1 && rows * side < 1024 * per) per /= 2;
+  return (int)per;
+}
+// The thread's unit of a row of `units` (gridDim.y workgroups side by side, or several rows to a workgroup): whether it has one,
+// its first row of the workgroup's and the step to the next.
+struct MxUnit {
+  bool any, is_v;
+  int row, step;
+  int g, d;
+};
+__device__ __forceinline__ MxUnit mx_unit(const MxPool& c) {
+  const int eights = c.D >> 3, half = c.Hkv * eights, units = 2 * half;
+  MxUnit t;
+  int u;
+  if (units >= MXC_THREADS) {
+    t.row = 0, t.step = 1;
+    u = blockIdx.y * MXC_THREADS + threadIdx.x;
+    t.any = u < units;
+  } else {
+    t.step = MXC_THREADS / units;
+    t.row = (int)threadIdx.x / units;
+    u = (int)threadIdx.x - t.row * units;
+    t.any = t.row < t.step;
+  }
+  t.is_v = u >= half;
+  if (t.is_v) u -= half;
+  t.g = u / eights;
+  t.d = 8 * (u - t.g * eights);
+  return t;
+}
 
 template <typename T>
 __device__ __forceinline__ void load8_bits(const T* p, unsigned* b);  // eight elements as float32 bits
@@ -73,6 +118,7 @@ struct MxStoreArgs {
   int64_t* new_lens;             // may be NULL
   int B;
   int64_t places;                // rows (append), or B * (1 + max_depth) (commit)
+  int per;                       // of a workgroup
   MxPool pool;
 };
 
@@ -87,57 +133,73 @@ __device__ __forceinline__ int64_t mx_rows(const MxStoreArgs& a, int s) {
 
 template <typename T, int FMT, bool PATH>
 __global__ __launch_bounds__(MXC_THREADS) void k_mx_store(MxStoreArgs a) {
-  const int64_t id = (int64_t)blockIdx.x * MXC_THREADS + threadIdx.x;
+  __shared__ int64_t from[MXC_ROWS], to[MXC_ROWS];  // row of k and v; row of head 0 in the pool (-1: none)
   const MxPool& c = a.pool;
   const int64_t cap = (int64_t)c.max_blocks * MX_PAGE;
-  if (a.new_lens != nullptr)
-    for (int64_t s = id; s < a.B; s += (int64_t)gridDim.x * MXC_THREADS) {
+  if (a.new_lens != nullptr && blockIdx.y == 0)
+    for (int64_t s = (int64_t)blockIdx.x * MXC_THREADS + threadIdx.x; s < a.B; s += (int64_t)gridDim.x * MXC_THREADS) {
       const int64_t used = a.lens[s], rows = mx_rows<PATH>(a, (int)s), room = used >= cap ? 0 : cap - used;
       a.new_lens[s] = used + (rows < room ? rows : room);
     }
-  const int eights = c.D >> 3;  // units of a head's row
-  const int half = c.Hkv * eights, per_place = 2 * half;
-  const int64_t place = id / per_place;
-  // the first place of this wave, whose sequence all lanes look up together
-  const int64_t place0 = __builtin_amdgcn_readfirstlane((int)place);  // (places are fewer than 2^31)
-  int s, t, row;
-  if constexpr (PATH) {
-    if (place >= a.places) return;
-    s = (int)place / (1 + a.max_depth);
-    t = (int)place - s * (1 + a.max_depth);
-    if (t >= mx_rows<true>(a, s)) return;
-    const int n0 = a.node_offsets[s], M = a.node_offsets[s + 1] - n0;
-    int r = t == 0 ? 0 : a.path[(int64_t)s * a.max_depth + t - 1];
-    r = r < 0 ? 0 : r >= M ? M - 1 : r;  // (an entry outside the tree would be a caller's error)
-    row = n0 + r;
-  } else {
-    s = seq_of_row(a.node_offsets, a.B, place0);
-    if (place >= a.places) return;
-    while (s + 1 < a.B && place >= a.node_offsets[s + 1]) ++s;
-    if (place >= a.node_offsets[s + 1]) return;
-    row = (int)place;
-    t = row - a.node_offsets[s];
+  const int64_t first = (int64_t)blockIdx.x * a.per;
+  if (threadIdx.x < 64) {
+    const int64_t place = first + threadIdx.x;
+    int64_t row = 0, at = -1;
+    int s = 0, t = -1;
+    if constexpr (PATH) {
+      if ((int)threadIdx.x < a.per && place < a.places) {
+        s = (int)place / (1 + a.max_depth);
+        t = (int)place - s * (1 + a.max_depth);
+        const int n0 = a.node_offsets[s], M = a.node_offsets[s + 1] - n0;
+        int r = t == 0 ? 0 : a.path[(int64_t)s * a.max_depth + t - 1];
+        r = r < 0 ? 0 : r >= M ? M - 1 : r;  // (an entry outside the tree would be a caller's error)
+        row = n0 + r;
+        if (t >= mx_rows<true>(a, s)) t = -1;
+      }
+    } else {
+      s = seq_of_row(a.node_offsets, a.B, first);
+      if ((int)threadIdx.x < a.per && place < a.places) {
+        while (s + 1 < a.B && place >= a.node_offsets[s + 1]) ++s;
+        row = place;
+        if (place < a.node_offsets[s + 1]) t = (int)(place - a.node_offsets[s]);
+      }
+    }
+    if (t >= 0) {
+      const int64_t tok = a.lens[s] + t;
+      if (tok >= 0 && tok < cap) {
+        const int page = c.table[(int64_t)s * c.max_blocks + tok / MX_PAGE];
+        if (page >= 0 && page < c.n_pages) at = (int64_t)page * c.Hkv * MX_PAGE + (tok & (MX_PAGE - 1));
+      }
+    }
+    if ((int)threadIdx.x < a.per) from[threadIdx.x] = row, to[threadIdx.x] = at;
   }
-  const int64_t tok = a.lens[s] + t;
-  if (tok < 0 || tok >= cap) return;
-  const int page = c.table[(int64_t)s * c.max_blocks + tok / MX_PAGE];
-  if (page < 0 || page >= c.n_pages) return;
-  int u = (int)(id - place * per_place);
-  const bool is_v = u >= half;
-  if (is_v) u -= half;
-  const int g = u / eights, d = 8 * (u - g * eights);
-  const T* const src = static_cast<const T*>(is_v ? a.v : a.k) + (int64_t)row * (is_v ? a.v_stride : a.k_stride) + (int64_t)g * c.D + d;
-  unsigned b[8];
-  load8_bits(src, b);
-  const int64_t at = ((int64_t)page * c.Hkv + g) * MX_PAGE + (tok & (MX_PAGE - 1));
-  mx_store8<FMT>(b, (is_v ? c.v_codes : c.k_codes) + at * mx_row_bytes(FMT, c.D) + d * Mx<FMT>::BITS / 8,
-                 (is_v ? c.v_scales : c.k_scales) + at * (c.D / MX_BLOCK) + d / MX_BLOCK, (d & (MX_BLOCK - 1)) == 0);
+  __syncthreads();
+  const MxUnit t = mx_unit(c);
+  if (!t.any) return;  // (units are whole blocks of four lanes)
+  const T* const src = static_cast<const T*>(t.is_v ? a.v : a.k) + (int64_t)t.g * c.D + t.d;
+  const int64_t stride = t.is_v ? a.v_stride : a.k_stride;
+  unsigned char* const codes = (t.is_v ? c.v_codes : c.k_codes) + ((int64_t)t.g * MX_PAGE * c.D + t.d) * Mx<FMT>::BITS / 8;
+  unsigned char* const scales = (t.is_v ? c.v_scales : c.k_scales) + (int64_t)t.g * MX_PAGE * (c.D / MX_BLOCK) + t.d / MX_BLOCK;
+  for (int i = t.row; i < a.per; i += MXC_AT_ONCE * t.step) {
+    unsigned b[MXC_AT_ONCE][8];
+    int64_t at[MXC_AT_ONCE];
+#pragma unroll
+    for (int x = 0; x < MXC_AT_ONCE; ++x) {
+      const int r = i + x * t.step;
+      at[x] = r < a.per ? to[r] : -1;
+      if (at[x] >= 0) load8_bits(src + from[r] * stride, b[x]);
+    }
+#pragma unroll
+    for (int x = 0; x < MXC_AT_ONCE; ++x)
+      if (at[x] >= 0) mx_store8<FMT>(b[x], codes + at[x] * mx_row_bytes(FMT, c.D), scales + at[x] * (c.D / MX_BLOCK), (t.d & (MX_BLOCK - 1)) == 0);
+  }
 }
 
 struct MxReadArgs {
   const int64_t* out_offsets;
   const int64_t* first;  // first token of each sequence; NULL: 0
   int B;
+  int per;  // rows of a workgroup
   int64_t total;
   void* k_out;
   void* v_out;
@@ -146,40 +208,60 @@ struct MxReadArgs {
 
 template <typename T, int FMT>
 __global__ __launch_bounds__(MXC_THREADS) void k_mx_read(MxReadArgs a) {
-  const int64_t id = (int64_t)blockIdx.x * MXC_THREADS + threadIdx.x;
+  __shared__ int64_t from[MXC_ROWS];  // row of head 0 in the pool (-1: none)
   const MxPool& c = a.pool;
-  const int eights = c.D >> 3;
-  const int half = c.Hkv * eights, per_row = 2 * half;
-  const int64_t row = id / per_row;
-  const int64_t row0 = ((int64_t)blockIdx.x * MXC_THREADS + (threadIdx.x & ~63)) / per_row;
-  int s = seq_of_row(a.out_offsets, a.B, row0);
-  if (row >= a.total) return;
-  while (s + 1 < a.B && row >= a.out_offsets[s + 1]) ++s;
-  if (row >= a.out_offsets[s + 1]) return;
-  const int64_t tok = row - a.out_offsets[s] + (a.first != nullptr ? a.first[s] : 0);
-  if (tok < 0 || tok >= (int64_t)c.max_blocks * MX_PAGE) return;
-  const int page = c.table[(int64_t)s * c.max_blocks + tok / MX_PAGE];
-  if (page < 0 || page >= c.n_pages) return;
-  int u = (int)(id - row * per_row);
-  const bool is_v = u >= half;
-  if (is_v) u -= half;
-  const int g = u / eights, d = 8 * (u - g * eights);
-  const int64_t at = ((int64_t)page * c.Hkv + g) * MX_PAGE + (tok & (MX_PAGE - 1));
-  const unsigned char* const codes = (is_v ? c.v_codes : c.k_codes) + at * mx_row_bytes(FMT, c.D) + d * Mx<FMT>::BITS / 8;
-  const float sc = mx_scale((is_v ? c.v_scales : c.k_scales)[at * (c.D / MX_BLOCK) + d / MX_BLOCK]);
-  uint4 e;
-  if constexpr (FMT == HS_MX_E4M3) {
-    const uint2 w = *reinterpret_cast<const uint2*>(codes);
-    e = mx_eight<FMT>(w.x, w.y, sc);
-  } else {
-    e = mx_eight<FMT>(*reinterpret_cast<const unsigned*>(codes), 0u, sc);
+  const int64_t first = (int64_t)blockIdx.x * a.per;
+  if (threadIdx.x < 64) {
+    const int64_t row = first + threadIdx.x;
+    int s = seq_of_row(a.out_offsets, a.B, first);
+    if ((int)threadIdx.x < a.per) {
+      int64_t at = -1;
+      if (row < a.total) {
+        while (s + 1 < a.B && row >= a.out_offsets[s + 1]) ++s;
+        if (row < a.out_offsets[s + 1]) {
+          const int64_t tok = row - a.out_offsets[s] + (a.first != nullptr ? a.first[s] : 0);
+          if (tok >= 0 && tok < (int64_t)c.max_blocks * MX_PAGE) {
+            const int page = c.table[(int64_t)s * c.max_blocks + tok / MX_PAGE];
+            if (page >= 0 && page < c.n_pages) at = (int64_t)page * c.Hkv * MX_PAGE + (tok & (MX_PAGE - 1));
+          }
+        }
+      }
+      from[threadIdx.x] = at;
+    }
   }
-  T* const dst = static_cast<T*>(is_v ? a.v_out : a.k_out) + (row * c.Hkv + g) * c.D + d;
-  if constexpr (sizeof(T) == 2) {
-    *reinterpret_cast<uint4*>(dst) = e;
-  } else {
-    *reinterpret_cast<uint4*>(dst) = make_uint4(e.x << 16, e.x & 0xffff0000u, e.y << 16, e.y & 0xffff0000u);
-    *reinterpret_cast<uint4*>(dst + 4) = make_uint4(e.z << 16, e.z & 0xffff0000u, e.w << 16, e.w & 0xffff0000u);
+  __syncthreads();
+  const MxUnit t = mx_unit(c);
+  if (!t.any) return;
+  const unsigned char* const codes = (t.is_v ? c.v_codes : c.k_codes) + ((int64_t)t.g * MX_PAGE * c.D + t.d) * Mx<FMT>::BITS / 8;
+  const unsigned char* const scales = (t.is_v ? c.v_scales : c.k_scales) + (int64_t)t.g * MX_PAGE * (c.D / MX_BLOCK) + t.d / MX_BLOCK;
+  T* const dst = static_cast<T*>(t.is_v ? a.v_out : a.k_out) + (first * c.Hkv + t.g) * c.D + t.d;
+  for (int i = t.row; i < a.per; i += MXC_AT_ONCE * t.step) {
+    uint2 w[MXC_AT_ONCE];
+    unsigned byte[MXC_AT_ONCE];
+    int64_t at[MXC_AT_ONCE];
+#pragma unroll
+    for (int x = 0; x < MXC_AT_ONCE; ++x) {
+      const int r = i + x * t.step;
+      at[x] = r < a.per ? from[r] : -1;
+      if (at[x] >= 0) {
+        const unsigned char* const p = codes + at[x] * mx_row_bytes(FMT, c.D);
+        if constexpr (FMT == HS_MX_E4M3) w[x] = *reinterpret_cast<const uint2*>(p);
+        else w[x].x = *reinterpret_cast<const unsigned*>(p), w[x].y = 0u;
+        byte[x] = scales[at[x] * (c.D / MX_BLOCK)];
+      }
+    }
+#pragma unroll
+    for (int x = 0; x < MXC_AT_ONCE; ++x) {
+      if (at[x] < 0) continue;
+      const uint4 e = mx_eight<FMT>(w[x].x, w[x].y, mx_scale(byte[x]));
+      T* const to = dst + (int64_t)(i + x * t.step) * c.Hkv * c.D;
+      if constexpr (sizeof(T) == 2) {
+        *reinterpret_cast<uint4*>(to) = e;
+      } else {
+        *reinterpret_cast<uint4*>(to) = make_uint4(e.x << 16, e.x & 0xffff0000u, e.y << 16, e.y & 0xffff0000u);
+        *reinterpret_cast<uint4*>(to + 4) = make_uint4(e.z << 16, e.z & 0xffff0000u, e.w << 16, e.w & 0xffff0000u);
+      }
+    }
   }
 }
 
@@ -231,10 +313,10 @@ static hs_status mx_store_impl(const char* what, MxStoreArgs a, hs_mx_format fmt
   } else if (a.new_lens == nullptr) {
     return HS_OK;
   }
-  const int64_t units = a.places * 2 * c.Hkv * (c.D / 8);
-  const int64_t blocks = any ? (units + MXC_THREADS - 1) / MXC_THREADS : 1;
-  HS_REQUIRE(blocks < ((int64_t)1 << 31), HS_ERR_UNSUPPORTED, "%s: %lld rows are too many for one call", what, (long long)a.places);
-  const dim3 grid((unsigned)blocks), block(MXC_THREADS);
+  a.per = mxc_rows(a.places, c);
+  const int64_t blocks = any ? (a.places + a.per - 1) / a.per : 1, units = 2ll * c.Hkv * (c.D / 8);
+  HS_REQUIRE(blocks < ((int64_t)1 << 24), HS_ERR_UNSUPPORTED, "%s: %lld rows are too many for one call", what, (long long)a.places);
+  const dim3 grid((unsigned)blocks, any ? (unsigned)((units + MXC_THREADS - 1) / MXC_THREADS) : 1u), block(MXC_THREADS);
 #define MXC_LAUNCH(T, F, P) hipLaunchKernelGGL((k_mx_store<T, F, P>), grid, block, 0, static_cast<hipStream_t>(stream), a)
 #define MXC_FMT(T, P)                                    \
   do {                                                   \
@@ -293,7 +375,7 @@ extern "C" hs_status hs_kv_read_mx(const void* k_codes, const void* k_scales, co
                                    const int64_t* first, const int64_t* out_offsets, int64_t total, void* k_out, void* v_out,
                                    int32_t B, int32_t Hkv, int32_t D, hs_dtype dt, hs_stream stream) {
   clear_error();
-  MxReadArgs a = {out_offsets, first, B, total, k_out, v_out, mx_pool(k_codes, k_scales, v_codes, v_scales, block_table, max_blocks, n_pages, Hkv, D)};
+  MxReadArgs a = {out_offsets, first, B, 1, total, k_out, v_out, mx_pool(k_codes, k_scales, v_codes, v_scales, block_table, max_blocks, n_pages, Hkv, D)};
   HS_REQUIRE(B >= 0 && total >= 0, HS_ERR_SHAPE, "hs_kv_read_mx: B=%d total=%lld", B, (long long)total);
   HS_REQUIRE(dt == HS_F32 || dt == HS_BF16, HS_ERR_SHAPE, "hs_kv_read_mx: unknown dtype %d", (int)dt);
   hs_status st = mx_pool_check("hs_kv_read_mx", a.pool, fmt);
@@ -305,10 +387,10 @@ extern "C" hs_status hs_kv_read_mx(const void* k_codes, const void* k_scales, co
   HS_REQUIRE(out_offsets && k_out && v_out, HS_ERR_NULL, "hs_kv_read_mx: NULL argument");
   HS_REQUIRE(((reinterpret_cast<uintptr_t>(k_out) | reinterpret_cast<uintptr_t>(v_out)) & 15) == 0, HS_ERR_UNSUPPORTED,
              "hs_kv_read_mx: outputs must be 16-byte aligned");
-  const int64_t per_row = 2ll * Hkv * (D / 8);
-  HS_REQUIRE(total < (((int64_t)1 << 31) - 1) * MXC_THREADS / per_row, HS_ERR_UNSUPPORTED, "hs_kv_read_mx: %lld rows are too many for one call",
-             (long long)total);
-  const dim3 grid((unsigned)((total * per_row + MXC_THREADS - 1) / MXC_THREADS)), block(MXC_THREADS);
+  a.per = mxc_rows(total, a.pool);
+  const int64_t blocks = (total + a.per - 1) / a.per, units = 2ll * Hkv * (D / 8);
+  HS_REQUIRE(blocks < ((int64_t)1 << 24), HS_ERR_UNSUPPORTED, "hs_kv_read_mx: %lld rows are too many for one call", (long long)total);
+  const dim3 grid((unsigned)blocks, (unsigned)((units + MXC_THREADS - 1) / MXC_THREADS)), block(MXC_THREADS);
 #define MXC_LAUNCH(T, F) hipLaunchKernelGGL((k_mx_read<T, F>), grid, block, 0, static_cast<hipStream_t>(stream), a)
   if (dt == HS_F32) {
     if (fmt == HS_MX_E4M3) MXC_LAUNCH(float, HS_MX_E4M3);

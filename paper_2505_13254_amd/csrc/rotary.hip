@@ -12,8 +12,8 @@
 namespace hs {
 
 constexpr int ROT_THREADS = 256;
-constexpr int ROT_TOKENS = 4;     // rows of a workgroup, where there are rows enough to fill the chip
-constexpr int ROT_MANY = 2048;    // rows from which on a workgroup takes ROT_TOKENS
+constexpr int ROT_MANY = 2048;    // rows from which on a workgroup takes as many as it has threads for (9 heads of 64, bfloat16: 5.9 us
+                                  // instead of 11.2 for 8192 rows, 36 instead of 80 for 65536; at 2048 either way 5)
 constexpr int ROT_STAGE = 1024;   // tree rows whose parents are staged in LDS
 
 struct RotaryArgs {
@@ -31,32 +31,24 @@ struct RotaryArgs {
   float mscale;
 };
 
+// 16 bytes: four float32 or eight bfloat16
 template <typename T>
-__device__ __forceinline__ void load8(const T* p, float* f);
-template <>
-__device__ __forceinline__ void load8<float>(const float* p, float* f) {
-  const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
-  f[0] = a.x, f[1] = a.y, f[2] = a.z, f[3] = a.w, f[4] = b.x, f[5] = b.y, f[6] = b.z, f[7] = b.w;
-}
-template <>
-__device__ __forceinline__ void load8<bf16_t>(const bf16_t* p, float* f) {
-  const uint4 a = *reinterpret_cast<const uint4*>(p);
+constexpr int ROT_WIDE = 16 / (int)sizeof(T);
+template <typename T>
+__device__ __forceinline__ void values(const uint4& a, float* f) {
   const unsigned w[4] = {a.x, a.y, a.z, a.w};
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    f[2 * i] = __builtin_bit_cast(float, w[i] << 16);
-    f[2 * i + 1] = __builtin_bit_cast(float, w[i] & 0xffff0000u);
+    if constexpr (sizeof(T) == 4) {
+      f[i] = __builtin_bit_cast(float, w[i]);
+    } else {
+      f[2 * i] = __builtin_bit_cast(float, w[i] << 16);
+      f[2 * i + 1] = __builtin_bit_cast(float, w[i] & 0xffff0000u);
+    }
   }
 }
-template <typename T>
-__device__ __forceinline__ void store8(T* p, const float* f);
-template <>
-__device__ __forceinline__ void store8<float>(float* p, const float* f) {
-  *reinterpret_cast<float4*>(p) = make_float4(f[0], f[1], f[2], f[3]);
-  *reinterpret_cast<float4*>(p + 4) = make_float4(f[4], f[5], f[6], f[7]);
-}
-template <>
-__device__ __forceinline__ void store8<bf16_t>(bf16_t* p, const float* f) {
+__device__ __forceinline__ void store16(float* p, const float* f) { *reinterpret_cast<float4*>(p) = make_float4(f[0], f[1], f[2], f[3]); }
+__device__ __forceinline__ void store16(bf16_t* p, const float* f) {
   unsigned w[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) w[i] = (unsigned)f32_to_bf16(f[2 * i]) | ((unsigned)f32_to_bf16(f[2 * i + 1]) << 16);
@@ -111,7 +103,7 @@ __device__ int tree_depth(const int32_t* parent, int i, int2* hop) {
   return found[0] + (found[1] >= 0 ? hop[found[1]].x : 0);
 }
 
-// PAIRS: 0 = halves, 1 = neighbours.  VEC: eight elements at a time (aligned rows, pairs in whole eights).
+// PAIRS: 0 = halves, 1 = neighbours.  VEC: 16 bytes at a time (aligned rows, pairs in whole eights).
 template <typename T, int PAIRS, bool TREE, bool VEC>
 __global__ __launch_bounds__(ROT_THREADS) void k_rotary(RotaryArgs a) {
   extern __shared__ __attribute__((aligned(16))) char lds_raw[];
@@ -121,79 +113,108 @@ __global__ __launch_bounds__(ROT_THREADS) void k_rotary(RotaryArgs a) {
   const int tid = threadIdx.x;
   const int n0 = blockIdx.x * a.tokens;
   const int n_here = a.N - n0 < a.tokens ? a.N - n0 : a.tokens;
-  int64_t tree_pos = 0;
-  if constexpr (TREE) {  // (one row to a workgroup)
-    const int s = seq_of_row(a.node_offsets, a.B, n0);
-    const int first = a.node_offsets[s];
-    tree_pos = a.prefix_lens[s] + tree_depth(a.parent + first, n0 - first, reinterpret_cast<int2*>(lds_raw + 8 * h));
-  }
-  for (int u = tid; u < n_here * h; u += ROT_THREADS) {
-    const int t = u / h, j = u - t * h;
-    const int64_t p = TREE ? tree_pos : a.positions[n0 + t];
-    const double turns = (double)p * (a.inv_freq[j] * 0.15915494309189533577);  // 1 / (2 pi)
-    const float rest = (float)(turns - rint(turns));
-    float sn, cs;
-    sincospif(2.f * rest, &sn, &cs);
-    c_lds[u] = cs * a.mscale;
-    s_lds[u] = sn * a.mscale;
-  }
-  __syncthreads();
   const int heads = a.heads[0] + a.heads[1];
   // what a head is made of: `turned` units that hold pairs, then units behind the turned part
-  const int width = VEC ? 8 : 1;
-  const int turned = VEC && PAIRS == 1 ? a.rot / 8 : h / width;
+  constexpr int WIDE = ROT_WIDE<T>, width = VEC ? WIDE : 1;
+  const int turned = VEC && PAIRS == 1 ? a.rot / WIDE : h / width;
   const int units = turned + (a.D - a.rot) / width;
+  // (row t, head, unit x) of this thread, and the step to its next one: the divisions are done once
   const int per_row = heads * units;
-  for (int u = tid; u < n_here * per_row; u += ROT_THREADS) {
-    const int t = u / per_row, w = u - t * per_row;
-    int head = w / units;
-    const int x = w - head * units;
-    const int which = head < a.heads[0] ? 0 : 1;
-    if (which) head -= a.heads[0];
-    const T* const src = static_cast<const T*>(a.in[which]) + (n0 + t) * a.in_stride[which] + (int64_t)head * a.D;
-    T* const dst = static_cast<T*>(a.out[which]) + (n0 + t) * a.out_stride[which] + (int64_t)head * a.D;
-    const float* const cs = c_lds + t * h;
-    const float* const sn = s_lds + t * h;
-    if (x >= turned) {  // behind the turned part: as it is
-      const int d = a.rot + (x - turned) * width;
-      if constexpr (VEC) {
-        if constexpr (sizeof(T) == 4) {
-          const float4 lo = *reinterpret_cast<const float4*>(src + d), hi = *reinterpret_cast<const float4*>(src + d + 4);
-          *reinterpret_cast<float4*>(dst + d) = lo;
-          *reinterpret_cast<float4*>(dst + d + 4) = hi;
-        } else {
-          *reinterpret_cast<uint4*>(dst + d) = *reinterpret_cast<const uint4*>(src + d);
-        }
+  int t = tid / per_row, head_t = (tid - t * per_row) / units, x = tid - t * per_row - head_t * units;
+  const int step_t = ROT_THREADS / per_row, step_h = (ROT_THREADS - step_t * per_row) / units, step_x = ROT_THREADS - step_t * per_row - step_h * units;
+  auto next = [&]() {
+    x += step_x, head_t += step_h, t += step_t;
+    if (x >= units) x -= units, ++head_t;
+    if (head_t >= heads) head_t -= heads, ++t;
+  };
+  auto angles = [&]() {
+    int64_t tree_pos = 0;
+    if constexpr (TREE) {  // (one row to a workgroup)
+      const int s = seq_of_row(a.node_offsets, a.B, n0);
+      const int first = a.node_offsets[s];
+      tree_pos = a.prefix_lens[s] + tree_depth(a.parent + first, n0 - first, reinterpret_cast<int2*>(lds_raw + 8 * h));
+    }
+    for (int u = tid; u < n_here * h; u += ROT_THREADS) {
+      const int t = u / h, j = u - t * h;
+      const int64_t p = TREE ? tree_pos : a.positions[n0 + t];
+      const double turns = (double)p * (a.inv_freq[j] * 0.15915494309189533577);  // 1 / (2 pi)
+      const float rest = (float)(turns - rint(turns));
+      float sn, cs;
+      sincospif(2.f * rest, &sn, &cs);
+      c_lds[u] = cs * a.mscale;
+      s_lds[u] = sn * a.mscale;
+    }
+    __syncthreads();
+  };
+  if constexpr (VEC) {
+    // A thread's first unit is read while the angles are computed, every later one ahead of the write of the one before, which a wait for it
+    // then need not cover.  (Behind that write: 52 us instead of 36 for 8192 rows of 40 heads.)
+    struct Unit {
+      uint4 p, q;
+      T* to;   // NULL: nothing
+      int at;  // of the angles; -1: behind the turned part, as it is
+    };
+    auto read = [&]() {
+      Unit r = {make_uint4(0u, 0u, 0u, 0u), make_uint4(0u, 0u, 0u, 0u), nullptr, -1};
+      if (t >= n_here) return r;
+      const int which = head_t < a.heads[0] ? 0 : 1, head = which ? head_t - a.heads[0] : head_t;
+      const bool turns = x < turned;
+      const int d = turns ? WIDE * x : a.rot + (x - turned) * WIDE;
+      const T* const src = static_cast<const T*>(a.in[which]) + (n0 + t) * a.in_stride[which] + (int64_t)head * a.D + d;
+      r.to = static_cast<T*>(a.out[which]) + (n0 + t) * a.out_stride[which] + (int64_t)head * a.D + d;
+      r.at = turns ? t * h + (PAIRS == 0 ? WIDE : WIDE / 2) * x : -1;
+      r.p = *reinterpret_cast<const uint4*>(src);
+      if (PAIRS == 0 && turns) r.q = *reinterpret_cast<const uint4*>(src + h);
+      next();
+      return r;
+    };
+    Unit ahead = read();
+    angles();
+    while (ahead.to != nullptr) {
+      const Unit now = ahead;
+      ahead = read();
+      if (now.at < 0) {
+        *reinterpret_cast<uint4*>(now.to) = now.p;
+        continue;
+      }
+      const float* const cs = c_lds + now.at;
+      const float* const sn = s_lds + now.at;
+      float f[WIDE], g[WIDE], r[WIDE];
+      values<T>(now.p, f);
+      if constexpr (PAIRS == 0) {
+        values<T>(now.q, g);
+#pragma unroll
+        for (int e = 0; e < WIDE; ++e) r[e] = f[e] * cs[e] - g[e] * sn[e];
+        store16(now.to, r);
+#pragma unroll
+        for (int e = 0; e < WIDE; ++e) r[e] = g[e] * cs[e] + f[e] * sn[e];
+        store16(now.to + h, r);
       } else {
+#pragma unroll
+        for (int e = 0; e < WIDE / 2; ++e) {
+          r[2 * e] = f[2 * e] * cs[e] - f[2 * e + 1] * sn[e];
+          r[2 * e + 1] = f[2 * e + 1] * cs[e] + f[2 * e] * sn[e];
+        }
+        store16(now.to, r);
+      }
+    }
+  } else {
+    angles();
+    while (t < n_here) {
+      const int which = head_t < a.heads[0] ? 0 : 1, head = which ? head_t - a.heads[0] : head_t;
+      const T* const src = static_cast<const T*>(a.in[which]) + (n0 + t) * a.in_stride[which] + (int64_t)head * a.D;
+      T* const dst = static_cast<T*>(a.out[which]) + (n0 + t) * a.out_stride[which] + (int64_t)head * a.D;
+      if (x >= turned) {
+        const int d = a.rot + (x - turned);
         dst[d] = src[d];
+      } else {
+        const float cs = c_lds[t * h + x], sn = s_lds[t * h + x];
+        const int d0 = PAIRS ? 2 * x : x, d1 = PAIRS ? 2 * x + 1 : x + h;
+        const float p = elem(src + d0), q = elem(src + d1);
+        store_elem(dst + d0, p * cs - q * sn);
+        store_elem(dst + d1, q * cs + p * sn);
       }
-    } else if constexpr (VEC && PAIRS == 0) {
-      const int j = 8 * x;
-      float p[8], q[8], f[8], g[8];
-      load8(src + j, p);
-      load8(src + j + h, q);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        f[e] = p[e] * cs[j + e] - q[e] * sn[j + e];
-        g[e] = q[e] * cs[j + e] + p[e] * sn[j + e];
-      }
-      store8(dst + j, f);
-      store8(dst + j + h, g);
-    } else if constexpr (VEC) {
-      const int j = 4 * x;
-      float p[8], f[8];
-      load8(src + 2 * j, p);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        f[2 * e] = p[2 * e] * cs[j + e] - p[2 * e + 1] * sn[j + e];
-        f[2 * e + 1] = p[2 * e + 1] * cs[j + e] + p[2 * e] * sn[j + e];
-      }
-      store8(dst + 2 * j, f);
-    } else {
-      const int d0 = PAIRS ? 2 * x : x, d1 = PAIRS ? 2 * x + 1 : x + h;
-      const float p = elem(src + d0), q = elem(src + d1);
-      store_elem(dst + d0, p * cs[x] - q * sn[x]);
-      store_elem(dst + d1, q * cs[x] + p * sn[x]);
+      next();
     }
   }
 }
@@ -227,7 +248,8 @@ static hs_status rotary_impl(RotaryArgs a, hs_dtype dt, hs_rotary_pairs pairs, b
   HS_REQUIRE(a.inv_freq, HS_ERR_NULL, "hs_rotary: NULL inv_freq");
   if (tree) HS_REQUIRE(a.parent && a.node_offsets && a.prefix_lens && a.B >= 1, HS_ERR_NULL, "hs_tree_rotary: NULL tree arrays, or rows of no sequence");
   else HS_REQUIRE(a.positions, HS_ERR_NULL, "hs_rotary: NULL positions");
-  a.tokens = !tree && a.N >= ROT_MANY ? ROT_TOKENS : 1;
+  const int wide = vec ? 16 / size : 1, units = (a.heads[0] + a.heads[1]) * ((pairs == HS_ROTARY_HALF || !vec ? a.rot / 2 : a.rot) + a.D - a.rot) / wide;
+  a.tokens = !tree && a.N >= ROT_MANY && units < ROT_THREADS ? ROT_THREADS / units : 1;
   const int h = a.rot / 2;
   const size_t lds = (size_t)a.tokens * h * 8 + (tree ? ROT_STAGE * 8 : 0);
   const dim3 grid((unsigned)((a.N + a.tokens - 1) / a.tokens)), block(ROT_THREADS);
