@@ -111,7 +111,7 @@ __global__ __launch_bounds__(MXM_THREADS) void k_attn_mx_merge(MxAttnArgs a, int
 // A call's work is cut for the shortest estimated time.  What an item takes is a fixed part and one in proportion to its
 // pages, measured (D = 128) on 256 workgroups at once, where the memory and the clock give less to each, and on up to half as many.
 // Of a list of times that an item may take (a page less or more in it moves whole rounds of items) every sequence cuts itself
-// for the least total, and the best estimate of the call is taken: the total over the compute units, the longest item, and for every k
+// for the least total, or, where the call does not fill the chip, for the shortest items, and the best estimate of the call is taken: the total over the compute units, the longest item, and for every k
 // the k + 1 rounds that 256 k + 1 items of some size need at least; items run longest first.
 constexpr int64_t MXA_RECORDS = 1 << 18;  // records that a call uses at most, unless its sequences are longer than a split can be
 constexpr double MX_ITEM_US[4] = {5.5, 6.5, 9.0, 11.0};         // an item, by form
@@ -133,7 +133,9 @@ struct MxPlan {
 static void mx_seq_plan(int M, int G, int L, int Hkv, int D, int fmt, int most, double us, MxSeqPlan& p, double& total) {
   MxCut c = mx_groups(M, G, most);
   const double per = D == 128 ? 1.0 : 0.5, fixed = MX_ITEM_US[c.form];
-  const double full = MX_PAGE_FULL_US[fmt][c.n_rg == 1 ? c.n_blk : (c.n_blk + c.n_rg - 1) / c.n_rg] * per;
+  // (the row groups of a sequence share what its keys cost the memory, which is what e4m3 takes longer than e2m1)
+  const int size = c.n_rg == 1 ? c.n_blk : (c.n_blk + c.n_rg - 1) / c.n_rg;
+  const double full = (MX_PAGE_FULL_US[1][size] + (MX_PAGE_FULL_US[fmt][size] - MX_PAGE_FULL_US[1][size]) / c.n_rg) * per;
   mx_splits(M, L, us > 1e8 ? 1 << 20 : std::max(1, (int)((us - fixed) / full)), c);
   const int all = (L + MX_PAGE - 1) / MX_PAGE + (M + MX_PAGE - 1) / MX_PAGE, longest = std::min(all, c.pages + (c.n_sp == 1 ? all : 0));
   p.cut = c;
@@ -148,10 +150,10 @@ static void mx_plan(const int32_t* hno, const int64_t* hlens, int B, int Hq, int
   MxPlan p;
   double best_us = 1e30, most_work = 0.0;
   best.items = best.records = 0, best.n_seq = 0;
-  const int tries = std::max(6, std::min(14, 256 / std::max(1, B)));
-  const double ratio = tries == 14 ? 1.154 : std::pow(5.6, 1.0 / (tries - 2));
+  const int tries = std::max(7, std::min(15, 256 / std::max(1, B)));
+  const double ratio = tries == 15 ? 1.154 : std::pow(5.6, 1.0 / (tries - 3));
   double us = 1e9;
-  for (int t = 0; t < tries; ++t) {  // uncut, then from 1.4 times an equal share (or 11 us) down to a quarter
+  for (int t = 0; t < tries; ++t) {  // uncut (twice: then the work is known), then from 1.4 times an equal share (or 11 us) down to a quarter
     for (int most = each ? 8 : 1; most <= 8; most *= 2) {  // (sequences that are cut on the device share the size of their groups)
       p.items = p.records = 0, p.n_seq = 0;
       p.cuts.blocks_most = most;
@@ -161,12 +163,13 @@ static void mx_plan(const int32_t* hno, const int64_t* hlens, int B, int Hq, int
         const int M = hno[s + 1] - hno[s];
         if (M <= 0) continue;
         MxSeqPlan now = {}, q;
-        double least = 1e30, one;
+        double least = 1e30, least_score = 1e30, one;
         if (each) {
           const int n_blk = (G * M + 31) >> 5;
           for (int m = 1;; m *= 2) {
             mx_seq_plan(M, G, (int)hlens[s], Hkv, D, fmt, m, us, q, one);
-            if (one < least) least = one, now = q;
+            const double score = std::max(most_work, t == 0 ? 0.0 : q.free_us) + one / 256.0;
+            if (score < least_score) least_score = score, least = one, now = q;
             if (m >= n_blk || m == 8) break;
           }
           now.s = s;
@@ -182,7 +185,7 @@ static void mx_plan(const int32_t* hno, const int64_t* hlens, int B, int Hq, int
         total += least;
         longest = std::max(longest, now.full_us);
       }
-      if (us > 1e8 && most == 8) most_work = total / 256.0;
+      if (t == 0 && most == 8) most_work = total / 256.0;
       if (us < 1e8 && p.records > MXA_RECORDS) continue;
       double took = std::max(total / 256.0, 0.0);
       if (each) {
@@ -206,7 +209,7 @@ static void mx_plan(const int32_t* hno, const int64_t* hlens, int B, int Hq, int
         std::copy(p.seq, p.seq + p.n_seq, best.seq);
       }
     }
-    us = t == 0 ? std::max(8.0, most_work) * 1.4 : us / ratio;
+    us = t == 0 ? us : t == 1 ? std::max(8.0, most_work) * 1.4 : us / ratio;
   }
 }
 
