@@ -19,24 +19,21 @@ def quantise(x, fmt):
     """x [..., D] -> (codes uint8 [..., D], one element each; scale bytes uint8 [..., D / 32])."""
     x = np.asarray(x, np.float64)
     mags = _magnitudes(fmt)
-    b = x.reshape(x.shape[:-1] + (-1, BLOCK))
-    flat = b.reshape(-1, BLOCK)
-    codes = np.zeros(flat.shape, np.uint8)
-    scales = np.zeros(len(flat), np.uint8)
-    for i, row in enumerate(flat):
-        if not np.isfinite(row).all():
-            scales[i] = 255
-            continue
-        e = LEAST
-        while np.abs(row).max() > mags[-1] * 2.0 ** e:
-            e += 1
-        scales[i] = e + 127
-        y = np.abs(row) / 2.0 ** e
-        hi = np.searchsorted(mags, y).clip(0, len(mags) - 1)
-        lo = (hi - 1).clip(0)
-        d_hi, d_lo = np.abs(mags[hi] - y), np.abs(y - mags[lo])
-        pick = np.where((d_lo < d_hi) | ((d_lo == d_hi) & (lo % 2 == 0)), lo, hi)
-        codes[i] = pick + (len(mags) + (fmt == "e4m3")) * np.signbit(row)
+    b = x.reshape(x.shape[:-1] + (x.shape[-1] // BLOCK, BLOCK))
+    flat = b.reshape(x.size // BLOCK, BLOCK)
+    finite = np.isfinite(flat).all(axis=1)
+    flat = np.where(finite[:, None], flat, 0.0)
+    top, e = np.abs(flat).max(axis=1, initial=0.0), np.full(len(flat), float(LEAST))
+    while (over := top > mags[-1] * 2.0 ** e).any():
+        e[over] += 1
+    y = np.abs(flat) / 2.0 ** e[:, None]
+    hi = np.searchsorted(mags, y).clip(0, len(mags) - 1)
+    lo = (hi - 1).clip(0)
+    d_hi, d_lo = np.abs(mags[hi] - y), np.abs(y - mags[lo])
+    pick = np.where((d_lo < d_hi) | ((d_lo == d_hi) & (lo % 2 == 0)), lo, hi)
+    codes = (pick + (len(mags) + (fmt == "e4m3")) * np.signbit(flat)).astype(np.uint8)
+    codes[~finite] = 0
+    scales = np.where(finite, e + 127, 255).astype(np.uint8)
     return codes.reshape(x.shape), scales.reshape(b.shape[:-1])
 
 
@@ -54,6 +51,7 @@ def store(k, rows_of, lens, table, n_pages, codes, scales, fmt):
     """Rows of k join a cache in place: rows_of[s] lists the rows that sequence s stores behind its lens[s] tokens; codes
     [n_pages, Hkv, 64, D] (one element each), scales [n_pages, Hkv, 64, D / 32].  Returns the lengths afterwards."""
     new = np.array(lens, np.int64)
+    k_codes, k_scales = quantise(k, fmt)
     for s, rows in enumerate(rows_of):
         for r in rows:
             t = int(new[s])
@@ -62,7 +60,7 @@ def store(k, rows_of, lens, table, n_pages, codes, scales, fmt):
             new[s] += 1
             page = int(table[s][t // PAGE])
             if 0 <= page < n_pages:
-                codes[page, :, t % PAGE], scales[page, :, t % PAGE] = quantise(k[r], fmt)
+                codes[page, :, t % PAGE], scales[page, :, t % PAGE] = k_codes[r], k_scales[r]
     return new
 
 

@@ -135,6 +135,80 @@ def test_matches_the_checker(hs, rows, lens, Hq, Hkv, back, D, fmt):
     assert torch.equal(o, again[0]) and torch.equal(lse, again[1])     # the same bits
 
 
+FULL = [  # calls that fill the chip: work items of two to eight row blocks, whose waves share their keys
+    ([5, 9, 16] * 20, [64, 200, 700] * 20, 32, 8, 9),                       # one and two blocks
+    ([17, 33, 33, 20] * 8, [400, 1, 64, 700] * 8, 32, 8, 9),                # three and five
+    ([12, 20, 33, 65, 97, 129] * 2, [700, 130, 64, 1, 300, 555] * 2, 64, 8, 9),  # up to 33, trees beyond 64 and 128 rows
+    ([64] * 24, [600, 64, 63, 0, 128, 191] * 4, 32, 8, 1),                  # eight, chains
+    ([20, 0, 41] * 24, [(29 * i) % 400 for i in range(72)], 24, 3, 9),      # more sequences than a wave has lanes
+    ([1] * 69 + [3], [(30 * i) % 200 for i in range(69)] + [9000], 8, 1, 1),
+]
+
+
+@pytest.mark.parametrize("fmt", [0, 1])
+@pytest.mark.parametrize("D", [128, 64])
+@pytest.mark.parametrize("rows,lens,Hq,Hkv,back", FULL)
+def test_full_chips(hs, rows, lens, Hq, Hkv, back, D, fmt):
+    test_matches_the_checker(hs, rows, lens, Hq, Hkv, back, D, fmt)
+
+
+@pytest.mark.parametrize("fmt", [0, 1])
+def test_scores_of_any_size_on_a_full_chip(hs, fmt):
+    for rows, lens in (([64] * 16, [300] * 16), ([20] * 32, [130, 64] * 16), ([9] * 48, [200] * 48)):
+        st = Step(hs, rows, lens, 32, 8, 128, fmt, gain=30.0, seed=3)
+        st.check(*st.run())
+
+
+def test_splits_of_shared_groups(hs):
+    """Long prefixes behind wide groups: items of eight blocks whose keys are cut, and the records' merge."""
+    st = Step(hs, [97, 61, 130], [2600, 2500, 2100], 64, 8, 128, 1, seed=4)
+    st.check(*st.run())
+    assert hs.hs_tree_attention_mx_workspace(torch.from_numpy(st.no), torch.from_numpy(st.lens), 64, 8, 128, DEV).numel() > 0
+
+
+@pytest.mark.parametrize("fmt", [0, 1])
+@pytest.mark.parametrize("n,L", [(33, 4500), (20, 4500), (9, 9000), (1, 17000)])
+def test_long_items(hs, n, L, fmt):
+    """Work items of more pages than a look-up of 64 covers: 32 sequences of the same rows and pages give the same bits, which are right."""
+    st, many = Step(hs, [n], [L], 32, 8, 128, fmt, seed=n), 32
+    host = [torch.arange(many + 1, dtype=torch.int32) * n, torch.full((many,), L, dtype=torch.int64)]
+    o, lse = st.run(q=st.q.repeat(many, 1, 1), k_tree=st.kt.repeat(many, 1, 1), v_tree=st.vt.repeat(many, 1, 1), parent=dev(np.tile(st.parent, many)),
+                    node_offsets=host[0].to(DEV), host_node_offsets=host[0], block_table=dev(st.table).repeat(many, 1), prefix_lens=host[1].to(DEV), host_prefix_lens=host[1])
+    st.check(o[:n], lse[:n])
+    assert torch.equal(o, o[:n].repeat(many, 1, 1)) and torch.equal(lse, lse[:n].repeat(many, 1))
+
+
+def test_the_same_rows_in_other_company(hs):
+    """A sequence's result alone and in a batch that takes its rows in other groups and splits: within both tolerances of the checker."""
+    st = Step(hs, [33] * 20, [700] * 20, 32, 8, 128, 0, seed=6)
+    st.check(*st.run())
+    one = dict(q=st.q[:33], k_tree=st.kt[:33], v_tree=st.vt[:33], parent=dev(st.parent[:33]), node_offsets=dev(st.no[:2]), host_node_offsets=torch.from_numpy(st.no[:2]),
+               block_table=dev(st.table[:1]), prefix_lens=dev(st.lens[:1]), host_prefix_lens=torch.from_numpy(st.lens[:1]))
+    o, lse = st.run(**one)
+    full, full_lse = st.run()
+    # both are within the checker's tolerance of the same value: |error| <= u |o| + (u + 5e-5 + ...) A with A <= max |V|
+    top = max(float(st.vt.abs().max()), float(np.abs(st.prefix()[1]).max()))
+    assert (np.abs(f64(o) - f64(full)[:33]) <= 4 * U * (1 + U) * top + 4e-4).all()
+    assert np.abs(f64(lse) - f64(full_lse)[:33]).max() < 1e-3
+
+
+def test_odd_tree_values_on_a_full_chip(hs):
+    """NaN and infinity in a tree row's value reach the rows below it, in groups whose waves share the tile, and leave the others' bits."""
+    for rows, lens in (([60] * 24, [130] * 24), ([70] * 12, [64] * 12)):
+        st = Step(hs, rows, lens, 32, 8, 128, 0, back=4, seed=9)
+        n = rows[0]
+        tree = np.concatenate([[-1, 0, 0, 1], np.where(np.arange(n - 4) % 2, 3, 2)])
+        st.parent[:] = np.tile(tree, len(rows))
+        o, _ = st.run()
+        below = np.zeros(len(rows) * n, bool)
+        below[5 * n + 2] = True
+        below[5 * n + 4:6 * n] = np.arange(n - 4) % 2 == 0
+        for bad in (float("nan"), float("inf")):
+            st.vt[5 * n + 2] = bad
+            o2, _ = st.run()
+            assert not o2[dev(below)].isfinite().any() and torch.equal(o2[dev(~below)], o[dev(~below)])
+
+
 @pytest.mark.parametrize("fmt", [0, 1])
 @pytest.mark.parametrize("gain", [30.0, 2.0 ** -20])
 def test_scores_of_any_size(hs, gain, fmt):

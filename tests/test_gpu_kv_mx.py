@@ -101,6 +101,14 @@ def test_append_and_read(hs, D, Hkv, sizes, lens, blocks, dtype, fmt):
                 assert np.array_equal(x[off[s]:off[s + 1]].float().cpu().numpy(), ref, equal_nan=True)
 
 
+@pytest.mark.parametrize("dtype,fmt", [(torch.bfloat16, "e4m3"), (torch.float32, "e2m1")])
+@pytest.mark.parametrize("D,Hkv,sizes,lens,blocks", [(32, 1, [5000, 0, 1, 3500, 800], [60, 5, 0, 3, 127], 80), (64, 3, [2049, 2, 1500], [1, 63, 0], 33),
+                                                     (128, 8, [3000, 0, 2, 1200], [61, 64, 190, 0], 48), (96, 5, [1300, 7, 900], [0, 1, 2], 21)])
+def test_append_and_read_many_rows(hs, D, Hkv, sizes, lens, blocks, dtype, fmt):
+    """Several rows to a workgroup, of sequences that begin and end inside it."""
+    test_append_and_read(hs, D, Hkv, sizes, lens, blocks, dtype, fmt)
+
+
 @pytest.mark.parametrize("fmt", ["e4m3", "e2m1"])
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("D,Hkv", [(128, 8), (64, 3)])
