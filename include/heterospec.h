@@ -548,7 +548,8 @@ hs_status hs_rotary_frequencies(int32_t rot_dim, double base, hs_rotary_scaling 
  * hs_kv_read_mx: tokens first[s] .. (int64 [B], device; NULL: from 0) of sequence s as rows out_offsets[s] .. out_offsets[s+1] - 1
  *   (int64 [B+1], device; total = out_offsets[B]) of k_out / v_out [total, Hkv, D] of element type dt.  The tokens must have been stored.
  *   Rows beyond the table, or of entries that are no page, are left as they were.
- * Requires D to be a multiple of 32 and rows that begin at multiples of 16 bytes.  No workspace.
+ * Requires D to be a multiple of 32, Hkv * D <= 2^24, rows that begin at multiples of 16 bytes, and fewer than 2^24 rows a call (several times as
+ * many where each is short).  No workspace.
  */
 hs_status hs_kv_append_mx(const void* k, int64_t k_stride, const void* v, int64_t v_stride, const int32_t* node_offsets, int32_t NN,
                           void* k_codes, void* k_scales, void* v_codes, void* v_scales, hs_mx_format fmt,
@@ -575,11 +576,13 @@ hs_status hs_kv_read_mx(const void* k_codes, const void* k_scales, const void* v
  *   parent, node_offsets, host_node_offsets, prefix_lens, host_prefix_lens, lse as in hs_tree_attention_paged: the host copies are what
  *   the launch is planned from, they must equal the device arrays, and a captured launch keeps them.
  * Float32 sums and softmax; P is rounded to bfloat16 for the second product, the output once.  A token with a NaN block makes
- * the rows that see it NaN.  Block-table entries behind a sequence's last token are not looked at.
- * Requires dt = HS_BF16, D in {64, 128}, Hq % Hkv == 0, at most 1024 tree rows per sequence, scale > 0, rows that begin at
- * multiples of 16 bytes.
+ * the rows that see it NaN.  Block-table entries behind a sequence's last token are not looked at.  The same call gives the same
+ * bits; how a sequence's keys are cut, and with it the order of its sums, depends on the others of the call.
+ * Requires dt = HS_BF16, D in {64, 128}, Hq % Hkv == 0, Hq / Hkv <= 1024, Hkv <= 4096, at most 1024 tree rows and HS_MX_MAX_TOKENS
+ * stored tokens per sequence, NN * Hq < 2^31, scale > 0, rows that begin at multiples of 16 bytes.
  * Workspace: one record of D + 4 floats per (tree row, query head, key split); the query gives what a call with these host arrays
- * needs (0: none; also for arrays that the call would refuse), at most 2^18 records.
+ * needs, of either format (0: none; also for arrays that the call would refuse), at most 2^18 records.  256-byte aligned; its content
+ * before a call does not matter.
  */
 size_t hs_tree_attention_mx_workspace(const int32_t* host_node_offsets, const int64_t* host_prefix_lens,
                                       int32_t B, int32_t Hq, int32_t Hkv, int32_t D);
