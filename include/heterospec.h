@@ -500,7 +500,7 @@ hs_status hs_kv_commit_paged(const void* k_tree, const void* v_tree, const int32
  *   Trees of any size; parents of a sequence's rows beyond the 1024th are followed one by one.  B = 0 with N = 0 only.
  * A rotation's gradient, and its undoing where mscale is 1, is the rotation by the opposite angles: the same call with
  * inv_freq negated.
- * Requires rot_dim even, 2 <= rot_dim <= D <= 1024, (Hq + Hkv) * D <= 2^24.  No workspace.  Rows that begin at
+ * Requires rot_dim even, 2 <= rot_dim <= D <= 1024, (Hq + Hkv) * D <= 2^24, hs_tree_rotary: N <= 2^23.  No workspace.  Rows that begin at
  * multiples of 16 bytes, strides, D and rot_dim / 2 (HS_ROTARY_NEIGHBOURS: rot_dim) that are multiples of eight take the faster path.
  */
 hs_status hs_rotary(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const int64_t* positions,
@@ -579,7 +579,8 @@ hs_status hs_kv_read_mx(const void* k_codes, const void* k_scales, const void* v
  * the rows that see it NaN.  Block-table entries behind a sequence's last token are not looked at.  The same call gives the same
  * bits; how a sequence's keys are cut, and with it the order of its sums, depends on the others of the call.
  * Requires dt = HS_BF16, D in {64, 128}, Hq % Hkv == 0, Hq / Hkv <= 1024, Hkv <= 4096, at most 1024 tree rows and HS_MX_MAX_TOKENS
- * stored tokens per sequence, NN * Hq < 2^31, scale > 0, rows that begin at multiples of 16 bytes.
+ * stored tokens per sequence, NN * Hq < 2^26, fewer than 2^23 blocks of 32 rows of a KV head, scale > 0, rows that begin at
+ * multiples of 16 bytes.
  * Workspace: one record of D + 4 floats per (tree row, query head, key split); the query gives what a call with these host arrays
  * needs, of either format (0: none; also for arrays that the call would refuse), at most 2^18 records.  256-byte aligned; its content
  * before a call does not matter.

@@ -539,7 +539,9 @@ def hs_kv_read_mx(cache, block_table, out_offsets, total: int, *, first=None, dt
 
 def hs_tree_attention_mx_workspace(host_node_offsets, host_prefix_lens, Hq: int, Hkv: int, D: int, device) -> Optional[torch.Tensor]:
     """A workspace for hs_tree_attention_mx calls of these row counts and lengths (CPU tensors); None where none is needed."""
-    no, pl = host_node_offsets.to(torch.int32).contiguous(), host_prefix_lens.to(torch.int64).contiguous()
+    if host_node_offsets.numel() != host_prefix_lens.numel() + 1:
+        raise ValueError("the offsets must hold B + 1 values, the lengths B")
+    no, pl = host_node_offsets.to("cpu", torch.int32).contiguous(), host_prefix_lens.to("cpu", torch.int64).contiguous()
     n = lib().hs_tree_attention_mx_workspace(no.data_ptr(), pl.data_ptr(), no.numel() - 1, int(Hq), int(Hkv), int(D))
     return workspace(n, device)
 

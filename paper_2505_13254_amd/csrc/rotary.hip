@@ -250,6 +250,8 @@ static hs_status rotary_impl(RotaryArgs a, hs_dtype dt, hs_rotary_pairs pairs, b
   else HS_REQUIRE(a.positions, HS_ERR_NULL, "hs_rotary: NULL positions");
   const int wide = vec ? 16 / size : 1, units = (a.heads[0] + a.heads[1]) * ((pairs == HS_ROTARY_HALF || !vec ? a.rot / 2 : a.rot) + a.D - a.rot) / wide;
   a.tokens = !tree && a.N >= ROT_MANY && units < ROT_THREADS ? ROT_THREADS / units : 1;
+  while (!tree && (a.N - 1) / a.tokens >= 1 << 23) a.tokens *= 2;  // (a launch has fewer than 2^32 threads)
+  HS_REQUIRE((a.N - 1) / a.tokens < 1 << 23, HS_ERR_UNSUPPORTED, "hs_tree_rotary: %d rows are too many for one call", a.N);
   const int h = a.rot / 2;
   const size_t lds = (size_t)a.tokens * h * 8 + (tree ? ROT_STAGE * 8 : 0);
   const dim3 grid((unsigned)((a.N + a.tokens - 1) / a.tokens)), block(ROT_THREADS);

@@ -155,6 +155,30 @@ static void mx_plan(const int32_t* hno, const int64_t* hlens, int B, int Hq, int
   MxPlan p;
   double best_us = 1e30, most_work = 0.0;
   best.items = best.records = 0, best.n_seq = 0;
+  // the sequences looked at: all, or of those that are cut on the device an even choice of 64, for the others too, and the one with the most work
+  int look[MXA_ENTRIES + 1], n_look = 0, most_blk = 0;
+  double others = 1.0;
+  if (each) {
+    for (int s = 0; s < B; ++s)
+      if (hno[s + 1] > hno[s]) look[n_look++] = s;
+  } else {
+    int n = 0, largest = 0;
+    double work = -1.0;
+    for (int s = 0; s < B; ++s) {
+      const int n_blk = (int)(((int64_t)G * (hno[s + 1] - hno[s]) + 31) >> 5);
+      if (n_blk == 0) continue;
+      ++n;
+      most_blk = std::max(most_blk, n_blk);
+      if ((double)n_blk * (double)(hlens[s] + MX_PAGE) > work) work = (double)n_blk * (double)(hlens[s] + MX_PAGE), largest = s;
+    }
+    const int step = (n + MXA_ENTRIES - 1) / MXA_ENTRIES;
+    for (int s = 0, at = 0; s < B; ++s)
+      if (hno[s + 1] > hno[s] && at++ % step == 0) look[n_look++] = s;
+    if (n_look > 0) {
+      others = (double)n / n_look;
+      look[n_look++] = largest;
+    }
+  }
   const int tries = std::max(7, std::min(15, 256 / std::max(1, B)));
   const double ratio = tries == 15 ? 1.154 : std::pow(5.6, 1.0 / (tries - 3));
   double us = 1e9;
@@ -164,9 +188,9 @@ static void mx_plan(const int32_t* hno, const int64_t* hlens, int B, int Hq, int
       p.cuts.blocks_most = most;
       for (int f = 0; f < 4; ++f) p.cuts.pages[f] = us > 1e8 ? 1 << 20 : std::max(1, (int)((us - MX_ITEM_US[f]) / (MX_PAGE_FULL_US[fmt][1 << f] * (D == 128 ? 1.0 : 0.5))));
       double total = 0.0, longest = 0.0;
-      for (int s = 0; s < B; ++s) {
-        const int M = hno[s + 1] - hno[s];
-        if (M <= 0) continue;
+      for (int i = 0; i < n_look; ++i) {
+        const int s = look[i], M = hno[s + 1] - hno[s];
+        const double share = each || i + 1 == n_look ? 1.0 : others;
         MxSeqPlan now = {}, q;
         double least = 1e30, least_score = 1e30, one;
         if (each) {
@@ -186,12 +210,15 @@ static void mx_plan(const int32_t* hno, const int64_t* hlens, int B, int Hq, int
           now.cut = c;
         }
         p.items += now.items;
-        if (now.cut.n_sp > 1) p.records += (int64_t)M * Hq * now.cut.n_sp;
-        total += least;
+        if (now.cut.n_sp > 1) p.records += (int64_t)(share * (double)((int64_t)M * Hq * now.cut.n_sp));
+        total += share * least;
         longest = std::max(longest, now.full_us);
       }
-      if (t == 0 && most == 8) most_work = total / 256.0;
-      if (us < 1e8 && p.records > MXA_RECORDS) continue;
+      if (t == 0) most_work = total / 256.0;
+      if (us < 1e8 && p.records > MXA_RECORDS) {
+        if (!each && most >= most_blk) break;
+        continue;
+      }
       double took = std::max(total / 256.0, 0.0);
       if (each) {
         if (p.n_seq > 1) std::sort(p.seq, p.seq + p.n_seq, [](const MxSeqPlan& a, const MxSeqPlan& b) { return a.full_us > b.full_us || (a.full_us == b.full_us && a.s < b.s); });
@@ -213,8 +240,24 @@ static void mx_plan(const int32_t* hno, const int64_t* hlens, int B, int Hq, int
         best.cuts = p.cuts, best.n_seq = p.n_seq, best.items = p.items, best.records = p.records;
         std::copy(p.seq, p.seq + p.n_seq, best.seq);
       }
+      if (!each && most >= most_blk) break;
     }
     us = t == 0 ? us : t == 1 ? std::max(8.0, most_work) * 1.4 : us / ratio;
+  }
+  for (bool again = !each && n_look > 0; again;) {  // what that cut comes to, of all
+    again = false;
+    best.items = best.records = 0;
+    for (int s = 0; s < B; ++s) {
+      const int M = hno[s + 1] - hno[s];
+      if (M <= 0) continue;
+      const MxCut c = mx_cut(M, G, (int)hlens[s], best.cuts);
+      best.items += (int64_t)c.n_sp * c.n_rg * Hkv;
+      if (c.n_sp > 1) best.records += (int64_t)M * Hq * c.n_sp;
+    }
+    if (best.records > MXA_RECORDS) {  // (the choice said fewer: uncut there are none)
+      for (int f = 0; f < 4; ++f) best.cuts.pages[f] = 1 << 20;
+      again = true;
+    }
   }
 }
 
@@ -237,7 +280,7 @@ static hs_status mx_attn_host_check(const int32_t* hno, const int64_t* hlens, in
     HS_REQUIRE(hlens[s] >= 0, HS_ERR_SHAPE, "hs_tree_attention_mx: prefix length %lld of sequence %d", (long long)hlens[s], s);
     HS_REQUIRE(hlens[s] <= HS_MX_MAX_TOKENS, HS_ERR_UNSUPPORTED, "hs_tree_attention_mx: sequence %d has %lld tokens", s, (long long)hlens[s]);
   }
-  HS_REQUIRE((int64_t)hno[B] * Hq < ((int64_t)1 << 31), HS_ERR_UNSUPPORTED, "hs_tree_attention_mx: %d rows of %d heads", hno[B], Hq);
+  HS_REQUIRE((int64_t)hno[B] * Hq < ((int64_t)1 << 26), HS_ERR_UNSUPPORTED, "hs_tree_attention_mx: %d rows of %d heads", hno[B], Hq);
   return HS_OK;
 }
 
@@ -303,7 +346,7 @@ extern "C" hs_status hs_tree_attention_mx(const void* q, int64_t q_stride, const
   a.o = o, a.lse = lse, a.part = static_cast<float*>(workspace);
   MxPlan p;
   mx_plan(host_node_offsets, host_prefix_lens, B, Hq, Hkv, D, (int)fmt, p);
-  HS_REQUIRE(p.items < ((int64_t)1 << 31), HS_ERR_UNSUPPORTED, "%s: too many rows for one call", what);
+  HS_REQUIRE(p.items < ((int64_t)1 << 23), HS_ERR_UNSUPPORTED, "%s: too many rows for one call", what);  // (2^32 threads)
   const size_t need = mx_bytes(p, D);
   if (need > 0) {
     HS_REQUIRE(workspace && reinterpret_cast<uintptr_t>(workspace) % 256 == 0 && workspace_bytes >= need, HS_ERR_WORKSPACE,

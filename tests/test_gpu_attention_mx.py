@@ -338,6 +338,18 @@ def test_refusals(hs):
             hs.hs_tree_attention_mx(**{**good, **bad})
 
 
+def test_host_arrays_are_converted(hs):
+    """Host copies of another integer type, or on the GPU, are copied, as the other attention calls do; with and without a workspace."""
+    st = Step(hs, [3, 2], [3000, 70], 8, 2, 128, 0, seed=1)
+    good = st.args()
+    want, _ = st.run()
+    ws = hs.hs_tree_attention_mx_workspace(good["host_node_offsets"], good["host_prefix_lens"], 8, 2, 128, DEV)
+    for other in (dict(host_node_offsets=good["node_offsets"]), dict(host_prefix_lens=good["prefix_lens"]),
+                  dict(host_node_offsets=good["host_node_offsets"].long(), host_prefix_lens=good["host_prefix_lens"].int())):
+        for w in (None, ws):
+            assert torch.equal(hs.hs_tree_attention_mx(**{**good, **other}, ws=w)[0], want)
+
+
 @pytest.mark.parametrize("fmt", [0, 1])
 def test_a_decoding_loop(hs, fmt):
     """Prompts are rotated and stored, then several steps of two sequences: rotary of the tree's rows, attention, the greedy walk, the

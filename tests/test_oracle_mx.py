@@ -196,3 +196,41 @@ def test_workspace_query_is_host_arithmetic(hs):
     for rows in (1, 61, 1024):
         for lens in (64, 5000, 10 ** 6):
             assert need([rows] * 20, [lens] * 20, 64, 8, 128) <= 2 ** 18 * 132 * 4 + 2 ** 16
+
+
+def test_workspace_query_checks_its_arrays(hs):
+    import torch
+    no, lens = torch.tensor([0, 1, 2], dtype=torch.int32), torch.tensor([5, 6], dtype=torch.int64)
+    for bad in ((no[:2], lens), (no, lens[:1]), (no[:0], lens[:0])):
+        with pytest.raises(ValueError):
+            hs.hs_tree_attention_mx_workspace(*bad, 8, 2, 128, "cpu")
+
+
+def test_plans_of_many_sequences(hs):
+    """The query's cost does not grow with the list of cuts it weighs beyond 64 sequences, and its records stay within their bound."""
+    import time
+
+    import torch
+    rs = np.random.RandomState(1)
+    for n, most in ((65, 300), (5000, 60), (3000, 1)):
+        rows, lens = rs.randint(0, most + 1, n), rs.randint(0, 9000, n)
+        lens[n // 2] = 10 ** 6
+        no, pl = torch.tensor([0] + list(np.cumsum(rows)), dtype=torch.int32), torch.tensor(lens, dtype=torch.int64)
+        hs.lib()
+        t = time.perf_counter()
+        bytes_ = hs.lib().hs_tree_attention_mx_workspace(no.data_ptr(), pl.data_ptr(), n, 64, 8, 128)
+        assert time.perf_counter() - t < 0.05
+        assert bytes_ % (4 * 132) == 0 and bytes_ // (4 * 132) <= 1 << 18
+
+
+def test_calls_beyond_a_launch_are_refused(hs):
+    """Host arithmetic alone refuses them: nothing is launched, no pointer is looked at."""
+    lib, d = hs.lib(), 0x100000
+    i32, i64 = ctypes.c_int32, ctypes.c_int64
+    n = 1 << 21                                       # sequences of one row, 32 KV heads: 2^26 work items
+    no, lens = (i32 * (n + 1))(*range(n + 1)), (i64 * n)()
+    args = [d, 4096, d, d, d, d, 0, d, 4096, d, 4096, d, d, no, d, 4, 9, d, lens, n, 32, 32, 128, 1, 0.1, d, None, d, 1 << 40, None]
+    assert lib.hs_tree_attention_mx(*args) == 3
+    args[19:22] = [n, 16, 16]                         # (2^25 rows of a head, 2^25 work items)
+    assert lib.hs_tree_attention_mx(*args) == 3
+    assert lib.hs_tree_rotary(d, 4096, None, 0, d, d, d, 1, (1 << 23) + 1, 4, 0, 128, 1, d, 128, 0, 1.0, d, 4096, None, 0, None) == 3
