@@ -15,7 +15,8 @@
 // path from the row up, a word of 32 tree rows at a time, with the tree's key blocks taken from the last to the first.
 //
 // What bounds it (D = 128, 8 KV heads, us of this kernel): one row to a sequence is a stream of the cache, 64 sequences of 512 to 16384
-// tokens in e4m3 (601 MB) 117, 5.1 TB/s, limited by the 67 KB that a compute unit has in flight; 776 rows to a KV head are matrix
+// tokens in e4m3 (601 MB) 117, 5.1 TB/s: three rounds of items, of whose time a sixth is their start and end, and 6.9 TB/s between (with
+// codes requested a whole step ahead, into LDS, it is no faster); 776 rows to a KV head are matrix
 // work, 4 x 8192 tokens in e2m1 122 (0.85 PFLOP/s; a full group of eight blocks runs at 1.35); one tree of 61 rows on 2048 tokens is a
 // chain of latencies, 13.7: 1 to know its item, 2 for Q and the pages, 1.5 for the tree, 0.3 a page, 2 to add up the waves, and 4 for the merge.
 #include <algorithm>
