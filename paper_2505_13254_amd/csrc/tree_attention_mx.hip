@@ -180,9 +180,9 @@ static void mx_plan(const int32_t* hno, const int64_t* hlens, int B, int Hq, int
       look[n_look++] = largest;
     }
   }
-  const int tries = std::max(7, std::min(15, 256 / std::max(1, B)));
+  const int tries = each ? std::max(11, std::min(15, 256 / std::max(1, B))) : 7;
   const double ratio = tries == 15 ? 1.154 : std::pow(5.6, 1.0 / (tries - 3));
-  double us = 1e9;
+  double us = 1e9, longest_item = 0.0;
   for (int t = 0; t < tries; ++t) {  // uncut (twice: then the work is known), then from 1.4 times an equal share (or 11 us) down to a quarter
     for (int most = each ? 8 : 1; most <= 8; most *= 2) {  // (sequences that are cut on the device share the size of their groups)
       p.items = p.records = 0, p.n_seq = 0;
@@ -235,6 +235,7 @@ static void mx_plan(const int32_t* hno, const int64_t* hlens, int B, int Hq, int
       } else {
         took += longest * 0.5;
       }
+      longest_item = longest;
       took += p.records > 0 ? 4.0 + p.records * 2.2e-4 : 0.0;
       if (took < best_us) {
         best_us = took;
@@ -243,6 +244,9 @@ static void mx_plan(const int32_t* hno, const int64_t* hlens, int B, int Hq, int
       }
       if (!each && most >= most_blk) break;
     }
+    // (where no item is longer than half of a share, or than a cut one and the merge, cuts gain little: not worth the host's time for many
+    // sequences; 64 short ones 33 -> 16 us a call)
+    if (t == 1 && n_look > 8 && longest_item <= std::max(0.5 * most_work, 10.0)) break;
     us = t == 0 ? us : t == 1 ? std::max(8.0, most_work) * 1.4 : us / ratio;
   }
   for (bool again = !each && n_look > 0; again;) {  // what that cut comes to, of all
