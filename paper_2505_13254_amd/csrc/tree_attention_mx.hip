@@ -117,9 +117,10 @@ __global__ __launch_bounds__(MXM_THREADS) void k_attn_mx_merge(MxAttnArgs a, int
 // A call's work is cut for the shortest estimated time.  What an item takes is a fixed part and one in proportion to its
 // pages, measured (D = 128) on 256 workgroups at once, where the memory and the clock give less to each, and on up to half as many.
 // Of a list of times that an item may take (a page less or more in it moves whole rounds of items) every sequence cuts itself
-// for the least total, or, where the call does not fill the chip, for the shortest items, and the best estimate of the call is taken: the total over the compute units, the longest item, and for every k
-// the k + 1 rounds that 256 k + 1 items of some size need at least; items run longest first.
-constexpr int64_t MXA_RECORDS = 1 << 18;  // records that a call uses at most, unless its sequences are longer than a split can be
+// for the least total, or, where the call does not fill the chip, for the shortest items, and the best estimate of the call is taken: the
+// total over the compute units, the longest item, and for every k the k + 1 rounds that 256 k + 1 items of some size need at least;
+// items run longest first.
+constexpr int64_t MXA_RECORDS = 1 << 18;  // records that a call uses at most
 constexpr double MX_ITEM_US[4] = {5.5, 6.5, 9.0, 11.0};         // an item, by form
 constexpr double MX_PAGE_FREE_US[4] = {0.30, 0.60, 0.92, 1.27};  // a page of it, by form: up to 128 items
 constexpr double MX_PAGE_FULL_US[2][9] = {{0.0, 0.63, 0.89, 1.17, 1.34, 1.66, 1.79, 1.88, 1.99},   // 256 items, by row blocks, e4m3
