@@ -388,6 +388,8 @@ __device__ __forceinline__ bool attn_mx_shared(const MxAttnArgs& a, const MxItem
       });
     }
   }
+  // (before the partial page, which may move a maximum: scaled down, a sum that has left its range could pass for one within it)
+  if (st.over(st.l)) redo = 1;  // (lanes of a wave agree)
   if (keys > n_full * MX_PAGE) {
     const int rest = keys - n_full * MX_PAGE;
     load(n_full, rest, ra);
@@ -406,7 +408,7 @@ __device__ __forceinline__ bool attn_mx_shared(const MxAttnArgs& a, const MxItem
       }
     }
   }
-  if (st.over(st.l)) redo = 1;  // (lanes of a wave agree)
+  if (st.over(st.l)) redo = 1;
   meet();
   if (redo != 0) return false;
 

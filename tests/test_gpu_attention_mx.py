@@ -229,6 +229,31 @@ def test_rising_scores(hs):
         st.check(*st.run())
 
 
+# Calls of one kind of work item each: (kind, rows of the trees)
+KINDS = [(0, [5] * 48), (1, [16] * 24), (2, [20] * 32), (2, [32] * 24), (3, [40] * 24), (3, [64] * 24)]
+
+
+@pytest.mark.parametrize("fmt", [0, 1])
+@pytest.mark.parametrize("L", [100, 230])
+@pytest.mark.parametrize("kind,rows", KINDS)
+def test_scores_that_jump_behind_the_first_keys(hs, kind, rows, L, fmt):
+    """Scores of 0 for the tree and the first 32 keys, then far above them in the full pages and again in the page that ends inside a
+    tile, by less and by more octaves than a float32 sum holds, with small and large values."""
+    st = Step(hs, rows, [L] * len(rows), 32, 8, 128, fmt, seed=5)
+    N = sum(st.lens)
+    st.kt.zero_()
+    st.q[..., 0] = 1.0
+    v = torch.randn((N, 8, 128), generator=torch.Generator(device=DEV).manual_seed(6), device=DEV)
+    token = torch.arange(N, device=DEV) % L
+    for full, rest in ((60, 60), (120, 120), (200, 200), (60, 200), (120, 260), (200, 60), (-60, 200)):
+        for gain in (1.0, 1000.0):
+            octaves = torch.where(token < 32, 0, torch.where(token < L // 64 * 64, full, rest))
+            k = torch.zeros((N, 8, 128), device=DEV)
+            k[..., 0] = (octaves * (math.log(2.0) / st.scale))[:, None]
+            hs.hs_kv_append_mx(k, v * gain, dev(st.po.astype(np.int32)), st.cache, dev(st.table), torch.zeros(len(rows), dtype=torch.int64, device=DEV))
+            st.check(*st.run())
+
+
 def test_strided_rows_and_outputs(hs):
     """q, k and v of the tree as slices of one projection; outputs into given tensors, no lse."""
     st = Step(hs, [20, 5], [300, 64], 8, 2, 128, 0, seed=7)
