@@ -229,7 +229,17 @@ def test_rising_scores(hs):
         st.check(*st.run())
 
 
-# Calls of one kind of work item each: (kind, rows of the trees)
+# Groups of four and of eight row blocks whose keys are cut into several splits, in either format (tests/test_attention_mx_plan.py)
+CUT = ([28, 64, 20, 40, 40, 20, 40, 40, 20], [3366, 3908, 4233, 4111, 2127, 2849, 3401, 3979, 4476])
+
+
+@pytest.mark.parametrize("fmt", [0, 1])
+def test_cut_groups_of_either_shared_kind(hs, fmt):
+    st = Step(hs, *CUT, 32, 8, 128, fmt, seed=4)
+    st.check(*st.run())
+
+
+# Calls of one kind of work item each (tests/test_attention_mx_plan.py holds them to it): (kind, rows of the trees)
 KINDS = [(0, [5] * 48), (1, [16] * 24), (2, [20] * 32), (2, [32] * 24), (3, [40] * 24), (3, [64] * 24)]
 
 
