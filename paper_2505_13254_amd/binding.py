@@ -1,7 +1,9 @@
 """Binding of libheterospec.so: argument marshalling only.
 
 Every function has the name and the arguments of the C entry point it calls (see
-include/heterospec.h); tensors are torch tensors on the GPU, used purely as device memory.
+include/heterospec.h); tensors are torch tensors on the GPU, used purely as device memory.  What a call makes
+for itself (outputs and a workspace that were not given) belongs to the stream that it runs on, `stream` or the
+current one, as tensors made under torch.cuda.stream(stream) do.
 There is no CPU path: if the library is not built, importing this module's functions raises.
 """
 from __future__ import annotations
@@ -158,11 +160,20 @@ def _stream(stream) -> int:
     return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
-def workspace(nbytes: int, device) -> Optional[torch.Tensor]:
-    """A 256-byte aligned scratch buffer (torch's allocator aligns to at least 512 bytes)."""
+def _empty(shape, dtype, device, stream) -> torch.Tensor:
+    """A tensor of the stream that uses it: its memory is free for that stream's next tensor alone once it is dropped, and what used
+    it before ran on that stream, too.  (Memory of the current stream could be written by both at once.)"""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(stream.cuda_stream)):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def workspace(nbytes: int, device, stream=None) -> Optional[torch.Tensor]:
+    """A 256-byte aligned scratch buffer (torch's allocator aligns to at least 512 bytes), for calls on `stream`."""
     if nbytes == 0:
         return None
-    return torch.empty(nbytes, dtype=torch.uint8, device=device)
+    return _empty(nbytes, torch.uint8, device, stream)
 
 
 def hs_workspace_prepare(ws: Optional[torch.Tensor], stream=None) -> None:
@@ -189,14 +200,14 @@ def hs_draft_entropy_topk(logits: torch.Tensor, K: int, temperature: float = 1.0
         R = row_index.numel()
     if out is None:
         dev = logits.device
-        out = dict(topk_idx=torch.empty((R, K), dtype=torch.int32, device=dev),
-                   topk_logp=torch.empty((R, K), dtype=torch.float32, device=dev),
-                   ent_topk=torch.empty(R, dtype=torch.float32, device=dev))
+        out = dict(topk_idx=_empty((R, K), torch.int32, dev, stream),
+                   topk_logp=_empty((R, K), torch.float32, dev, stream),
+                   ent_topk=_empty(R, torch.float32, dev, stream))
         if want_full:
-            out["ent_full"] = torch.empty(R, dtype=torch.float32, device=dev)
-            out["lse"] = torch.empty(R, dtype=torch.float32, device=dev)
+            out["ent_full"] = _empty(R, torch.float32, dev, stream)
+            out["lse"] = _empty(R, torch.float32, dev, stream)
     if ws is None and not fused:
-        ws = workspace(lib().hs_draft_entropy_topk_workspace(R, V, K), logits.device)
+        ws = workspace(lib().hs_draft_entropy_topk_workspace(R, V, K), logits.device, stream)
     stride = logits.stride(0) if N > 1 else max(V, logits.stride(0))
     tail = (R, V, K, temperature, out["topk_idx"], out["topk_logp"], out["ent_topk"], out.get("ent_full"), out.get("lse"), ws,
             stream)
@@ -225,14 +236,14 @@ def hs_tree_prune(parent: torch.Tensor, logc: torch.Tensor, node_offsets: torch.
     NN, B = parent.numel(), node_offsets.numel() - 1
     if out is None:
         dev = parent.device
-        out = dict(depth=torch.empty(NN, dtype=torch.int32, device=dev),
-                   cumlogp=torch.empty(NN, dtype=torch.float32, device=dev),
-                   keep=torch.empty(NN, dtype=torch.uint8, device=dev),
-                   out_offsets=torch.empty(B + 1, dtype=torch.int32, device=dev),
-                   out_src=torch.empty(max(NN, 1), dtype=torch.int32, device=dev),
-                   out_parent=torch.empty(max(NN, 1), dtype=torch.int32, device=dev))
+        out = dict(depth=_empty(NN, torch.int32, dev, stream),
+                   cumlogp=_empty(NN, torch.float32, dev, stream),
+                   keep=_empty(NN, torch.uint8, dev, stream),
+                   out_offsets=_empty(B + 1, torch.int32, dev, stream),
+                   out_src=_empty(max(NN, 1), torch.int32, dev, stream),
+                   out_parent=_empty(max(NN, 1), torch.int32, dev, stream))
     if ws is None:
-        ws = workspace(lib().hs_tree_prune_workspace(B, NN), parent.device)
+        ws = workspace(lib().hs_tree_prune_workspace(B, NN), parent.device, stream)
     tail = (B, NN, d_max, theta, max_nodes, out["depth"], out["cumlogp"], out["keep"], out["out_offsets"], out["out_src"],
             out["out_parent"], ws, stream)
     if node_counts is None:
@@ -296,9 +307,9 @@ def hs_adaptive_control(parent, logc, ent, node_offsets, node_counts, bin_edges,
     B, NN = node_offsets.numel() - 1, parent.numel()
     if out is None:
         dev = parent.device
-        out = dict(phi=torch.empty(B, dtype=torch.float32, device=dev))
+        out = dict(phi=_empty(B, torch.float32, dev, stream))
         for k in ("pstar", "bin", "d_prime", "n_prime"):
-            out[k] = torch.empty(B, dtype=torch.int32, device=dev)
+            out[k] = _empty(B, torch.int32, dev, stream)
     st = _calls.hs_adaptive_control(parent, logc, ent, node_offsets, node_counts, B, NN, bin_edges, len(bin_edges) + 1, gamma,
                                     len(gamma), int(alpha), int(d_base), int(n_default), int(mode), out["phi"], out["pstar"],
                                     out["bin"], out["d_prime"], out["n_prime"], stream)
@@ -341,11 +352,11 @@ def hs_tree_attention(q, k_prefix, v_prefix, k_tree, v_tree, parent, node_offset
     Hkv = k_tree.shape[1]
     B = host_node_offsets.numel() - 1
     if out is None:
-        out = torch.empty_like(q)
+        out = _empty(q.shape, q.dtype, q.device, stream)
     if want_lse and lse is None:
-        lse = torch.empty((NN, Hq), dtype=torch.float32, device=q.device)
+        lse = _empty((NN, Hq), torch.float32, q.device, stream)
     if ws is None:
-        ws = workspace(lib().hs_tree_attention_workspace(B, NN, int(host_prefix_offsets[-1]), Hq, Hkv, D, _dtype_code(q)), q.device)
+        ws = workspace(lib().hs_tree_attention_workspace(B, NN, int(host_prefix_offsets[-1]), Hq, Hkv, D, _dtype_code(q)), q.device, stream)
     if shared_tree:
         if prefix_lens is not None:
             raise ValueError("shared_tree and prefix_lens cannot be combined")
@@ -375,11 +386,11 @@ def hs_tree_attention_paged(q, k_pages, v_pages, k_tree, v_tree, parent, node_of
     if block_table.dim() != 2 or block_table.shape[0] != B or k_pages.dim() != 4:
         raise ValueError("block_table must be [B, max_blocks] and the pools [n_pages, page_tokens, Hkv, D]")
     if out is None:
-        out = torch.empty_like(q)
+        out = _empty(q.shape, q.dtype, q.device, stream)
     if want_lse and lse is None:
-        lse = torch.empty((NN, Hq), dtype=torch.float32, device=q.device)
+        lse = _empty((NN, Hq), torch.float32, q.device, stream)
     if ws is None:
-        ws = workspace(lib().hs_tree_attention_workspace(B, NN, int(host_prefix_lens.sum()), Hq, Hkv, D, _dtype_code(q)), q.device)
+        ws = workspace(lib().hs_tree_attention_workspace(B, NN, int(host_prefix_lens.sum()), Hq, Hkv, D, _dtype_code(q)), q.device, stream)
     st = _calls.hs_tree_attention_paged(q, k_pages, v_pages, k_tree, v_tree, parent, node_offsets, host_node_offsets, block_table,
                                         block_table.shape[1], k_pages.shape[1], prefix_lens, host_prefix_lens, B, Hq, Hkv, D,
                                         scale, out, lse, ws, stream)
@@ -427,13 +438,13 @@ def hs_rotary_frequencies(rot_dim: int, base: float = 10000.0, *, scaling: str =
     return table if device is None else table.to(device), float(m.value)
 
 
-def _rotary_args(q, k, inv_freq, q_out, k_out):
+def _rotary_args(q, k, inv_freq, q_out, k_out, stream):
     if q.dim() != 3 or (k is not None and (k.dim() != 3 or k.shape[0] != q.shape[0] or k.shape[2] != q.shape[2])):
         raise ValueError("q and k must be [N, heads, D] with the same N and D")
     if q_out is None:
-        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        q_out = _empty(q.shape, q.dtype, q.device, stream)
     if k_out is None and k is not None:
-        k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
+        k_out = _empty(k.shape, k.dtype, k.device, stream)
     if q_out.shape != q.shape or (k_out is None) != (k is None) or (k is not None and k_out.shape != k.shape):
         raise ValueError("outputs must have their inputs' shapes")
     return q_out, k_out, (0 if k is None else k.shape[1])
@@ -443,7 +454,7 @@ def hs_rotary(q, k, positions, inv_freq, *, interleaved: bool = False, mscale: f
     """q [N,Hq,D], k [N,Hkv,D] or None (float32 or bfloat16, GPU; rows may have a stride of their own, e.g. slices of a fused
     projection), positions int64 [N], inv_freq float64 [rot_dim / 2] on the GPU (hs_rotary_frequencies).  interleaved: pairs
     are neighbours, otherwise halves.  q_out / k_out may be q / k themselves.  Returns (q_out, k_out)."""
-    q_out, k_out, Hkv = _rotary_args(q, k, inv_freq, q_out, k_out)
+    q_out, k_out, Hkv = _rotary_args(q, k, inv_freq, q_out, k_out, stream)
     N, Hq, D = q.shape
     if positions.numel() != N:
         raise ValueError("positions must hold N values")
@@ -456,7 +467,7 @@ def hs_tree_rotary(q, k, parent, node_offsets, prefix_lens, inv_freq, *, interle
                    k_out=None, stream=None):
     """hs_rotary of the rows of draft trees (parent int32 [N], node_offsets int32 [B+1], GPU): a row's position is
     prefix_lens[s] (int64 [B], GPU) plus its depth."""
-    q_out, k_out, Hkv = _rotary_args(q, k, inv_freq, q_out, k_out)
+    q_out, k_out, Hkv = _rotary_args(q, k, inv_freq, q_out, k_out, stream)
     N, Hq, D = q.shape
     B = node_offsets.numel() - 1
     if parent.numel() != N or prefix_lens.numel() != B:
@@ -529,7 +540,7 @@ def hs_kv_read_mx(cache, block_table, out_offsets, total: int, *, first=None, dt
     B = out_offsets.numel() - 1
     pool, n_pages, Hkv, D = _mx_cache(cache, block_table, B)
     if out is None:
-        out = tuple(torch.empty((total, Hkv, D), dtype=dtype, device=block_table.device) for _ in range(2))
+        out = tuple(_empty((total, Hkv, D), dtype, block_table.device, stream) for _ in range(2))
     if any(tuple(t.shape) != (total, Hkv, D) for t in out) or (first is not None and first.numel() != B):
         raise ValueError("out must be two tensors [total, Hkv, D], first must hold B values")
     _check(_calls.hs_kv_read_mx(*pool, block_table, block_table.shape[1], n_pages, first, out_offsets, total, out[0], out[1], B, Hkv, D,
@@ -537,13 +548,13 @@ def hs_kv_read_mx(cache, block_table, out_offsets, total: int, *, first=None, dt
     return out[0], out[1]
 
 
-def hs_tree_attention_mx_workspace(host_node_offsets, host_prefix_lens, Hq: int, Hkv: int, D: int, device) -> Optional[torch.Tensor]:
-    """A workspace for hs_tree_attention_mx calls of these row counts and lengths (CPU tensors); None where none is needed."""
+def hs_tree_attention_mx_workspace(host_node_offsets, host_prefix_lens, Hq: int, Hkv: int, D: int, device, *, stream=None) -> Optional[torch.Tensor]:
+    """A workspace for hs_tree_attention_mx calls of these row counts and lengths (CPU tensors) on `stream`; None where none is needed."""
     if host_node_offsets.numel() != host_prefix_lens.numel() + 1:
         raise ValueError("the offsets must hold B + 1 values, the lengths B")
     no, pl = host_node_offsets.to("cpu", torch.int32).contiguous(), host_prefix_lens.to("cpu", torch.int64).contiguous()
     n = lib().hs_tree_attention_mx_workspace(no.data_ptr(), pl.data_ptr(), no.numel() - 1, int(Hq), int(Hkv), int(D))
-    return workspace(n, device)
+    return workspace(n, device, stream)
 
 
 def hs_tree_attention_mx(q, cache, k_tree, v_tree, parent, node_offsets, host_node_offsets, block_table, prefix_lens,
@@ -562,13 +573,13 @@ def hs_tree_attention_mx(q, cache, k_tree, v_tree, parent, node_offsets, host_no
             (B > 0 and int(host_node_offsets[B]) != NN):
         raise ValueError("parent must hold NN values, the offsets B + 1 (the last one NN), the lengths B")
     if out is None:
-        out = torch.empty((NN, Hq, D), dtype=q.dtype, device=q.device)
+        out = _empty((NN, Hq, D), q.dtype, q.device, stream)
     if want_lse and lse is None:
-        lse = torch.empty((NN, Hq), dtype=torch.float32, device=q.device)
+        lse = _empty((NN, Hq), torch.float32, q.device, stream)
     if out.shape != q.shape or (lse is not None and lse.numel() != NN * Hq):
         raise ValueError("out must be [NN, Hq, D], lse [NN, Hq]")
     if ws is None:
-        ws = hs_tree_attention_mx_workspace(host_node_offsets, host_prefix_lens, Hq, Hkv, D, q.device)
+        ws = hs_tree_attention_mx_workspace(host_node_offsets, host_prefix_lens, Hq, Hkv, D, q.device, stream=stream)
     _check(_calls.hs_tree_attention_mx(q, *pool, k_tree, v_tree, parent, node_offsets, host_node_offsets, block_table,
                                        block_table.shape[1], n_pages, prefix_lens, host_prefix_lens, B, Hq, Hkv, D, scale, out, lse, ws,
                                        stream), "hs_tree_attention_mx")
@@ -596,11 +607,11 @@ def hs_verify_accept(target_logits, draft_logits, token, parent, node_offsets, m
         raise ValueError("uniforms must hold NN + B values")
     if out is None:
         dev = target_logits.device
-        out = dict(accept_len=torch.empty(B, dtype=torch.int32, device=dev),
-                   accept_path=torch.empty((B, max_depth), dtype=torch.int32, device=dev),
-                   bonus_token=torch.empty(B, dtype=torch.int32, device=dev))
+        out = dict(accept_len=_empty(B, torch.int32, dev, stream),
+                   accept_path=_empty((B, max_depth), torch.int32, dev, stream),
+                   bonus_token=_empty(B, torch.int32, dev, stream))
     if ws is None:
-        ws = workspace(lib().hs_verify_accept_workspace_mode(B, NN, V, int(mode)), target_logits.device)
+        ws = workspace(lib().hs_verify_accept_workspace_mode(B, NN, V, int(mode)), target_logits.device, stream)
     st = _calls.hs_verify_accept(target_logits, draft_logits, row_stride, token, parent, node_offsets, B, NN, V, int(mode),
                                  temperature, uniforms, int(max_depth), out["accept_len"], out["accept_path"],
                                  out["bonus_token"], ws, stream)
@@ -655,7 +666,7 @@ def hs_tree_validate(parent, token, node_offsets, *, stream=None) -> torch.Tenso
     _dev(parent, torch.int32, "parent"); _dev(node_offsets, torch.int32, "node_offsets")
     if token is not None:
         _dev(token, torch.int32, "token")
-    report = torch.empty(2, dtype=torch.int32, device=parent.device)
+    report = _empty(2, torch.int32, parent.device, stream)
     st = lib().hs_tree_validate(_ptr(parent), _ptr(token), _ptr(node_offsets), node_offsets.numel() - 1,
                                 parent.numel(), _ptr(report), _stream(stream))
     _check(st, "hs_tree_validate")
