@@ -575,8 +575,9 @@ hs_status hs_kv_read_mx(const void* k_codes, const void* k_scales, const void* v
  *   q [NN,Hq,D], k_tree, v_tree [NN,Hkv,D] bfloat16, row n at base + n * stride (elements); o [NN,Hq,D] bfloat16, dense.
  *   parent, node_offsets, host_node_offsets, prefix_lens, host_prefix_lens, lse as in hs_tree_attention_paged: the host copies are what
  *   the launch is planned from, they must equal the device arrays, and a captured launch keeps them.
- * Float32 sums and softmax; P is rounded to bfloat16 for the second product, the output once.  A token with a NaN block makes
- * the rows that see it NaN.  Block-table entries behind a sequence's last token are not looked at.  The same call gives the same
+ * Float32 sums and softmax; P is rounded to bfloat16 for the second product, the output once.  Values of any size that the cache or
+ * bfloat16 holds: the sums are of weighted means, and a row whose sums leave float32's range all the same is computed again, slower.  A
+ * token with a NaN block among its keys makes the rows that see it NaN, one among its values their 32 columns.  Block-table entries behind a sequence's last token are not looked at.  The same call gives the same
  * bits; how a sequence's keys are cut, and with it the order of its sums, depends on the others of the call.
  * Requires dt = HS_BF16, D in {64, 128}, Hq % Hkv == 0, Hq / Hkv <= 1024, Hkv <= 4096, at most 1024 tree rows and HS_MX_MAX_TOKENS
  * stored tokens per sequence, NN * Hq < 2^26, fewer than 2^23 blocks of 32 rows of a KV head, scale > 0, rows that begin at

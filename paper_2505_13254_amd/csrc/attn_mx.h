@@ -106,7 +106,7 @@ struct MxAttnArgs {
   float c2;              // scale * log2(e)
   void* o;
   float* lse;
-  float* part;           // records of D + 4 floats: o (not normalised), maximum (in octaves), denominator
+  float* part;           // records of D + 4 floats: o of the split's keys, maximum (in octaves), denominator
   int n_entries;         // 0: more sequences than entries
   alignas(16) MxEntry entries[MXA_ENTRIES];
 };
@@ -301,6 +301,18 @@ struct MxState {
     P = make_uint4(w[0], w[1], w[2], w[3]);
   }
   __device__ __forceinline__ static bool over(float s) { return __ballot(s >= MX_LIMIT) != 0ull; }  // (a NaN stays one)
+  // Rows (bits) of `wave`'s 32 whose sums left their range, for attn_mx_follow: [0] those of a denominator beyond MX_LIMIT (`over`: it
+  // was), [1] those of an accumulator that is not finite although no score was a NaN (the denominator would be one).  `sum`: of both halves.
+  __device__ __forceinline__ void note_lost(bool over, float sum, int wave, int lane, unsigned (*lost)[2]) const {
+    float x = 0.f, y = 0.f;
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int v = 0; v < 16; v += 2) x = __builtin_fmaf(acc[t][v], 0.f, x), y = __builtin_fmaf(acc[t][v + 1], 0.f, y);
+    x += y;
+    const unsigned long long beyond = __ballot(over || l >= MX_LIMIT), odd = __ballot(x != x && sum == sum);
+    if (lane == 0) lost[wave][0] = (unsigned)beyond | (unsigned)(beyond >> 32), lost[wave][1] = (unsigned)odd | (unsigned)(odd >> 32);
+  }
   // Scores (masked ones at -inf) to P: bfloat16 pairs of the first 16 and the second 16 keys.
   __device__ __forceinline__ void softmax(const floatx16& S, float c2, uint4& p0, uint4& p1) {
     float s = l;
@@ -399,10 +411,14 @@ __device__ __forceinline__ unsigned mx_path_word(bool small, const int2* hops, M
   return (unsigned)hop.x;
 }
 
+// What a row's accumulators are multiplied by, ahead of any sum over waves or splits: their mean is in range where a sum need not be.
+// (A split without weight, all its scores at -infinity, leaves a record of zeros.)
+__device__ __forceinline__ float mx_inverse(float total, bool whole) { return whole || total > 0.f ? 1.f / total : 0.f; }
+
 // Columns d .. d + 3 of a row: a result (the sequence has one split), or a part of the split's record.
-__device__ __forceinline__ void mx_write4(const MxAttnArgs& a, bool whole, int64_t out, float* rec, int d, float4 sum, float inv) {
+__device__ __forceinline__ void mx_write4(const MxAttnArgs& a, bool whole, int64_t out, float* rec, int d, float4 sum) {
   if (whole) {
-    const floatx2 lo = {sum.x * inv, sum.y * inv}, hi = {sum.z * inv, sum.w * inv};
+    const floatx2 lo = {sum.x, sum.y}, hi = {sum.z, sum.w};
     uint2 w;
     w.x = __builtin_bit_cast(unsigned, __builtin_convertvector(lo, bf16x2));
     w.y = __builtin_bit_cast(unsigned, __builtin_convertvector(hi, bf16x2));
@@ -447,7 +463,8 @@ __device__ __forceinline__ void mx_write_half(const MxAttnArgs& a, const MxItem&
     for (int t = 0; t < NT; ++t)
 #pragma unroll
       for (int b = 0; b < 4; ++b)
-        *reinterpret_cast<float4*>(mine + 128 * t + 32 * b + 16 * half) = make_float4(acc[t][4 * b], acc[t][4 * b + 1], acc[t][4 * b + 2], acc[t][4 * b + 3]);
+        *reinterpret_cast<float4*>(mine + 128 * t + 32 * b + 16 * half) =
+            make_float4(acc[t][4 * b] * inv, acc[t][4 * b + 1] * inv, acc[t][4 * b + 2] * inv, acc[t][4 * b + 3] * inv);
     rows(std::integral_constant<int, D / 8>{}, [&](const MxOwn& o, int c, const uint4& w) {
       *reinterpret_cast<uint4*>(a.part + (it.rec0 + ((int64_t)o.i * a.Hq + o.h) * it.n_sp + it.sp) * (D + ATTN_REC_PAD) + x * (D / 2) + 4 * c) = w;
     });
@@ -470,7 +487,14 @@ struct MxLds {
   float den[MXA_WAVES][2][32];  // maxima and sums of the waves
   int par[MXA_MAX_M];
   int2 hops[MXA_MAX_M];         // of a tree row: its root path inside its own 32 rows as bits, the next row of it outside
-  int odd, redo;
+  int odd;
+  unsigned lost[MXA_WAVES][2];  // see MxState::note_lost
+  unsigned nan_columns;
 };
+// Whether no wave noted a row.  (behind a barrier; the same for all waves)
+template <int D>
+__device__ __forceinline__ bool mx_none_lost(const MxLds<D>& mem) {
+  return __ballot((&mem.lost[0][0])[threadIdx.x & (2 * MXA_WAVES - 1)] != 0u) == 0ull;
+}
 
 }  // namespace hs

@@ -16,8 +16,6 @@ __global__ __launch_bounds__(MXA_THREADS) void k_attn_mx(MxAttnArgs a) {
                "s"(a.entries[0].n0), "s"(a.entries[0].M), "s"(a.entries[0].L), "s"(a.entries[0].pages), "s"(a.entries[0].n_sp_form), "s"(a.entries[0].groups));
   MxItem it;
   if (!mx_item(a, blockIdx.x, it)) return;
-  if (threadIdx.x == 0) mem.redo = 0;  // (set behind a barrier at the earliest)
-  mx_meet();
   bool held;
   switch (it.form) {
     case MX_PRIVATE_1: held = attn_mx_private<FMT, D, 1>(a, it, mem); break;
@@ -25,7 +23,10 @@ __global__ __launch_bounds__(MXA_THREADS) void k_attn_mx(MxAttnArgs a) {
     case MX_SHARED_4: held = attn_mx_shared<FMT, D, 2>(a, it, mem); break;
     default: held = attn_mx_shared<FMT, D, 1>(a, it, mem); break;
   }
-  if (!held) attn_mx_follow<FMT, D>(a, it, mem);
+  if (!held) {  // (its rows are written again: behind everything that was written)
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    attn_mx_follow<FMT, D>(a, it, mem);
+  }
 }
 
 template <int FMT>

@@ -9,7 +9,7 @@
 //
 // A row's maximum stays that of the tree's rows and the wave's first 32 keys: neither a block's maximum nor a rescaling is
 // computed in almost every step.  Weights above one cost no precision (P, sums and accumulators are floating point) until
-// a denominator reaches 2^80 (a score 55 above the first ones): attn_mx_follow then takes the item.
+// a denominator reaches 2^80 (a score 55 above the first ones) or an accumulator overflows: attn_mx_follow then takes the row.
 #pragma once
 #include <type_traits>
 
@@ -17,7 +17,7 @@
 
 namespace hs {
 
-// Returns whether the fixed maximum held; nothing is written where it did not.
+// Returns whether all rows' sums stayed in range (mem.lost: which did not); rows that did not are written, but wrong.
 template <int FMT, int D, int R>
 __device__ __forceinline__ bool attn_mx_private(const MxAttnArgs& a, const MxItem& it, MxLds<D>& mem) {
   constexpr int W = MXA_WAVES / R;       // ways: waves that share a row block's keys
@@ -267,15 +267,15 @@ __device__ __forceinline__ bool attn_mx_private(const MxAttnArgs& a, const MxIte
       if (j > 1) page_of = pages_from(page_j = j);
       for (const int stop = page_j + 63; j < mine && j < stop; ++j) step(j, std::false_type{});  // (the last one requests page_j + 63)
     }
-    if (st.over(st.l)) mem.redo = 1;  // (lanes of a wave agree)
-    st.l = half_sum(st.l);
-    if (half == 0) {
-      den[wave][0][col] = st.m;
-      den[wave][1][col] = st.l;
-    }
+  }
+  const float sum = half_sum(st.l);
+  st.note_lost(false, sum, wave, lane, mem.lost);  // (an inactive wave has zeros)
+  if (half == 0) {
+    den[wave][0][col] = st.m;
+    den[wave][1][col] = sum;
   }
   mx_meet();  // every wave has its sums (and no tile is read any more)
-  if (mem.redo != 0) return false;
+  const bool held = mx_none_lost<D>(mem);
 
   // ---- the ways of a row block meet: each leaves its accumulators, scaled to the common maximum, and adds up its share
   // of the columns
@@ -285,7 +285,7 @@ __device__ __forceinline__ bool attn_mx_private(const MxAttnArgs& a, const MxIte
     for (int x = 0; x < W; ++x) top = fmaxf(top, den[x * R + rb][0][col]);
 #pragma unroll
     for (int x = 0; x < W; ++x) total += den[x * R + rb][1][col] * exp2_fast(den[x * R + rb][0][col] - top);
-    const float mine = exp2_fast(st.m - top);
+    const float mine = exp2_fast(st.m - top) * mx_inverse(total, it.n_sp == 1);
     float4* const to = reinterpret_cast<float4*>(lds) + wave * (NT * 4 * 64) + lane;
     if (row_base + col < Rh)
 #pragma unroll
@@ -295,10 +295,9 @@ __device__ __forceinline__ bool attn_mx_private(const MxAttnArgs& a, const MxIte
         to[(t * 4 + b) * 64] = make_float4(st.acc[t][4 * b] * mine, st.acc[t][4 * b + 1] * mine, st.acc[t][4 * b + 2] * mine, st.acc[t][4 * b + 3] * mine);
   }
   mx_meet();
-  if (!active || row_base + col >= Rh) return true;
+  if (!active || row_base + col >= Rh) return held;
   const int64_t out_row = (int64_t)(it.n0 + own.i) * a.Hq + own.h;
   float* const rec = a.part + (it.rec0 + ((int64_t)own.i * a.Hq + own.h) * it.n_sp + it.sp) * (D + ATTN_REC_PAD);
-  const float inv = 1.f / total;
   for (int x = way; x < NT * 4; x += W) {
     float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
@@ -306,7 +305,7 @@ __device__ __forceinline__ bool attn_mx_private(const MxAttnArgs& a, const MxIte
       const float4 f = reinterpret_cast<const float4*>(lds)[(y * R + rb) * (NT * 4 * 64) + x * 64 + lane];
       sum.x += f.x, sum.y += f.y, sum.z += f.z, sum.w += f.w;
     }
-    mx_write4(a, it.n_sp == 1, out_row, rec, 8 * x + 4 * half, sum, inv);  // (column 32 (x / 4) + 8 (x % 4) + 4 half)
+    mx_write4(a, it.n_sp == 1, out_row, rec, 8 * x + 4 * half, sum);  // (column 32 (x / 4) + 8 (x % 4) + 4 half)
   }
   if (way == 0 && half == 0) {
     if (it.n_sp == 1) {
@@ -316,7 +315,7 @@ __device__ __forceinline__ bool attn_mx_private(const MxAttnArgs& a, const MxIte
       rec[D + 1] = total;
     }
   }
-  return true;
+  return held;
 }
 
 }  // namespace hs

@@ -24,7 +24,7 @@
 
 namespace hs {
 
-// Returns whether the fixed maximum held; nothing is written where it did not.
+// Returns whether all rows' sums stayed in range (mem.lost: which did not); rows that did not are written, but wrong.
 template <int FMT, int D, int W>
 __device__ __forceinline__ bool attn_mx_shared(const MxAttnArgs& a, const MxItem& it, MxLds<D>& mem) {
   constexpr int NK = D / 16, NT = D / 32, STEPS = NK / 2, EPS = 4 / STEPS;
@@ -42,7 +42,7 @@ __device__ __forceinline__ bool attn_mx_shared(const MxAttnArgs& a, const MxItem
   auto& den = mem.den;
   int* const par = mem.par;
   int2* const hops = mem.hops;
-  int &odd_lds = mem.odd, &redo = mem.redo;
+  int& odd_lds = mem.odd;
   char* const lds_k = lds;
   char* const lds_v = lds + MXS_BUF * KT;
 
@@ -389,7 +389,7 @@ __device__ __forceinline__ bool attn_mx_shared(const MxAttnArgs& a, const MxItem
     }
   }
   // (before the partial page, which may move a maximum: scaled down, a sum that has left its range could pass for one within it)
-  if (st.over(st.l)) redo = 1;  // (lanes of a wave agree)
+  const bool over = st.l >= MX_LIMIT;
   if (keys > n_full * MX_PAGE) {
     const int rest = keys - n_full * MX_PAGE;
     load(n_full, rest, ra);
@@ -408,13 +408,13 @@ __device__ __forceinline__ bool attn_mx_shared(const MxAttnArgs& a, const MxItem
       }
     }
   }
-  if (st.over(st.l)) redo = 1;
+  float top = st.m, total = half_sum(st.l);
+  st.note_lost(over, total, wave, lane, mem.lost);
+  st.l = total;
   meet();
-  if (redo != 0) return false;
+  const bool held = mx_none_lost<D>(mem);
 
   // ---- out
-  st.l = half_sum(st.l);
-  float top = st.m, total = st.l;
   if constexpr (W == 2) {  // each way of a row block hands over the columns that the other one writes
     if (half == 0) {
       den[wave][0][col] = st.m;
@@ -424,8 +424,9 @@ __device__ __forceinline__ bool attn_mx_shared(const MxAttnArgs& a, const MxItem
     const int other = wave ^ BLOCKS;
     const float m2 = den[other][0][col];
     top = fmaxf(st.m, m2);
-    const float mine = exp2_fast(st.m - top);
+    float mine = exp2_fast(st.m - top);
     total = st.l * mine + den[other][1][col] * exp2_fast(m2 - top);
+    mine *= mx_inverse(total, it.n_sp == 1);
     floatx16 keep[NT / 2];
     float4* const to = reinterpret_cast<float4*>(lds) + wave * (NT / 2 * 4 * 64) + lane;
     const float4* const from = reinterpret_cast<const float4*>(lds) + other * (NT / 2 * 4 * 64) + lane;
@@ -447,15 +448,15 @@ __device__ __forceinline__ bool attn_mx_shared(const MxAttnArgs& a, const MxItem
         keep[t][4 * b + 2] = keep[t][4 * b + 2] * mine + f.z, keep[t][4 * b + 3] = keep[t][4 * b + 3] * mine + f.w;
       }
     meet();
-    if (!active) return true;
-    mx_write_half<D>(a, it, row_base, way, keep, 1.f / total, q_lds, lane);
+    if (!active) return held;
+    mx_write_half<D>(a, it, row_base, way, keep, 1.f, q_lds, lane);
   } else {
-    if (!active) return true;
-    const float inv = 1.f / total;
+    if (!active) return held;
+    const float inv = mx_inverse(total, it.n_sp == 1);
     mx_write_half<D>(a, it, row_base, 0, st.acc, inv, q_lds, lane);
     mx_write_half<D>(a, it, row_base, 1, st.acc + NT / 2, inv, q_lds, lane);
   }
-  if (row_base + col >= Rh || way != 0 || half != 0) return true;
+  if (row_base + col >= Rh || way != 0 || half != 0) return held;
   const MxOwn o = own();
   if (it.n_sp == 1) {
     if (a.lse != nullptr) a.lse[(int64_t)(it.n0 + o.i) * a.Hq + o.h] = (top + __log2f(total)) * MXA_LN2;
@@ -464,7 +465,7 @@ __device__ __forceinline__ bool attn_mx_shared(const MxAttnArgs& a, const MxItem
     rec[D] = top;
     rec[D + 1] = total;
   }
-  return true;
+  return held;
 }
 
 }  // namespace hs

@@ -85,7 +85,7 @@ __global__ __launch_bounds__(MXM_THREADS) void k_attn_mx_merge(MxAttnArgs a, int
   const float2 ml = *reinterpret_cast<const float2*>(from + sp * (D + ATTN_REC_PAD) + D);
   fetch(0);  // (the first records with their maxima: one trip to memory)
   const float m = lane < n_sp ? ml.x : MXA_FLOOR, l = lane < n_sp ? ml.y : 0.f;
-  const float top = wave_max(m), weight = exp2_fast(m - top), total = wave_sum(weight * l);
+  const float top = wave_max(m), part = exp2_fast(m - top) * l, total = wave_sum(part), weight = part * (1.f / total);
   float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
   for (int k = 0;;) {
 #pragma unroll
@@ -102,9 +102,8 @@ __global__ __launch_bounds__(MXM_THREADS) void k_attn_mx_merge(MxAttnArgs a, int
   for (int o = LANES; o < 64; o *= 2) {
     sum.x += __shfl_xor(sum.x, o), sum.y += __shfl_xor(sum.y, o), sum.z += __shfl_xor(sum.z, o), sum.w += __shfl_xor(sum.w, o);
   }
-  const float inv = 1.f / total;
   if (k0 == 0) {
-    const floatx2 lo = {sum.x * inv, sum.y * inv}, hi = {sum.z * inv, sum.w * inv};
+    const floatx2 lo = {sum.x, sum.y}, hi = {sum.z, sum.w};
     uint2 w;
     w.x = __builtin_bit_cast(unsigned, __builtin_convertvector(lo, bf16x2));
     w.y = __builtin_bit_cast(unsigned, __builtin_convertvector(hi, bf16x2));

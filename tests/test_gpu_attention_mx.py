@@ -264,6 +264,74 @@ def test_scores_that_jump_behind_the_first_keys(hs, kind, rows, L, fmt):
             st.check(*st.run())
 
 
+@pytest.mark.parametrize("fmt", [0, 1])
+@pytest.mark.parametrize("kind,rows", KINDS + [("cut", None)])
+def test_large_values(hs, kind, rows, fmt):
+    """Values that float32 holds, whose sums weighted against the first keys' maximum it does not: far above it in the scores, or so
+    large that a few of them overflow.  The weighted mean is always in range."""
+    rows, lens = CUT if kind == "cut" else (rows, [230] * len(rows))
+    st = Step(hs, rows, lens, 32, 8, 128, fmt, seed=5)
+    N = sum(st.lens)
+    g = torch.Generator(device=DEV).manual_seed(6)
+    q, kt, vt = st.q.clone(), st.kt.clone(), st.vt.clone()
+    token = torch.cat([torch.arange(int(n), device=DEV) for n in lens])
+    for jump, size in ((0, 1e37), (60, 1e25), (70, 1e37), (-40, 1e37)):
+        st.q, st.kt, st.vt = q.clone(), torch.zeros_like(kt) if jump else kt, (vt.float() * size).bfloat16()
+        k = torch.randn((N, 8, 128), generator=g, device=DEV)
+        if jump:                                         # scores of 0, and of `jump` octaves behind the first 40 keys
+            st.q[..., 0] = 1.0
+            k.zero_()
+            k[..., 0] = (torch.where(token < 40, 0, jump) * (math.log(2.0) / st.scale))[:, None]
+        v = torch.randn((N, 8, 128), generator=g, device=DEV)
+        v = v.clamp(-4, 4) + 2.0                         # (mostly of one sign)
+        hs.hs_kv_append_mx(k, v * size, dev(st.po.astype(np.int32)), st.cache, dev(st.table), torch.zeros(len(rows), dtype=torch.int64, device=DEV))
+        st.check(*st.run())
+
+
+@pytest.mark.parametrize("fmt", [0, 1])
+@pytest.mark.parametrize("kind,rows", [KINDS[0], KINDS[1], KINDS[2], KINDS[5], ("cut", None)])
+def test_a_nan_block_takes_its_columns(hs, kind, rows, fmt):
+    """A NaN block among the values takes its 32 columns of its KV head's rows; the other columns keep their bits, also where sums overflow."""
+    rows, lens = CUT if kind == "cut" else (rows, [230] * len(rows))
+    st = Step(hs, rows, lens, 32, 8, 128, fmt, seed=5)
+    N = sum(st.lens)
+    vt, v = st.vt.clone(), torch.randn((N, 8, 128), generator=torch.Generator(device=DEV).manual_seed(6), device=DEV) + 3.0
+    for size in (1.0, 1e37):
+        st.vt = (vt.float() * size).bfloat16()
+        hs.hs_kv_append_mx(v, v * size, dev(st.po.astype(np.int32)), st.cache, dev(st.table), torch.zeros(len(rows), dtype=torch.int64, device=DEV))
+        o, lse = st.run()
+        assert o.isfinite().all()
+        page, slot = st.table[0, 1], 70 - 64
+        kept = int(st.cache["v_scales"][page, 5, slot, 2])
+        st.cache["v_scales"][page, 5, slot, 2] = 255
+        o2, lse2 = st.run()
+        st.cache["v_scales"][page, 5, slot, 2] = kept
+        hit = torch.zeros_like(o, dtype=torch.bool)
+        hit[:rows[0], 20:24, 64:96] = True
+        assert o2[hit].isnan().all() and torch.equal(o2[~hit], o[~hit]) and torch.equal(lse, lse2)
+
+
+@pytest.mark.parametrize("kind,rows", [KINDS[0], KINDS[1], KINDS[2], KINDS[5], ("cut", None)])
+def test_an_infinite_tree_value_takes_its_column(hs, kind, rows):
+    """An infinity in one column of a tree row's value takes that column of the rows below it; all others keep their bits, also where sums overflow."""
+    rows, lens = CUT if kind == "cut" else (rows, [230] * len(rows))
+    st = Step(hs, rows, lens, 32, 8, 128, 0, seed=5)
+    N, n = sum(st.lens), rows[0]
+    st.parent[:n] = [-1, 0, 0] + [1 + (i & 1) for i in range(n - 3)]
+    vt, v = st.vt.clone(), torch.randn((N, 8, 128), generator=torch.Generator(device=DEV).manual_seed(6), device=DEV) + 3.0
+    below = torch.zeros(len(st.parent), dtype=torch.bool, device=DEV)
+    below[[2] + [i for i in range(3, n) if st.parent[i] == 2]] = True
+    for size in (1.0, 1e37):
+        st.vt = (vt.float() * size).bfloat16()
+        hs.hs_kv_append_mx(v, v * size, dev(st.po.astype(np.int32)), st.cache, dev(st.table), torch.zeros(len(rows), dtype=torch.int64, device=DEV))
+        o, lse = st.run()
+        st.vt[2, 3, 77] = float("inf")
+        o2, lse2 = st.run()
+        hit = torch.zeros_like(o, dtype=torch.bool)
+        hit[:, 12:16, 77] = below[:, None]
+        assert o.isfinite().all() and not o2[hit].isfinite().any() and torch.equal(o2[~hit], o[~hit]) and torch.equal(lse, lse2)
+
+
 def test_strided_rows_and_outputs(hs):
     """q, k and v of the tree as slices of one projection; outputs into given tensors, no lse."""
     st = Step(hs, [20, 5], [300, 64], 8, 2, 128, 0, seed=7)
