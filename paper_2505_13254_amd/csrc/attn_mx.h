@@ -78,8 +78,9 @@ __host__ __device__ __forceinline__ MxCut mx_cut(int M, int G, int L, const MxCu
   return c;
 }
 
-// A sequence with rows as the host cut it.  The entries of up to MXA_ENTRIES sequences, in the order of their items, travel in the kernel's arguments: a workgroup then
-// knows its item after one trip to memory instead of two (2000 cycles).  Longer batches cut on the device.
+// What a launch attends to travels in its arguments, taken from the host arrays: a captured launch keeps it, whatever becomes of the device's.
+// A sequence with rows as the host cut it.  The entries of up to MXA_ENTRIES sequences, in the order of their items: a workgroup
+// knows its item after one trip to memory.  Of longer batches the rows and lengths of up to MXA_SEQS sequences to a launch, which the device cuts.
 struct MxEntry {
   int first;       // its first item
   int n0, M, L;
@@ -90,6 +91,10 @@ struct MxEntry {
 };
 static_assert(sizeof(MxEntry) == 32, "two 16-byte loads");
 constexpr int MXA_ENTRIES = 64;
+struct MxSeq {
+  int n0, L;  // first row (behind the last sequence: where its rows end), prefix tokens
+};
+constexpr int MXA_SEQS = MXA_ENTRIES * (int)(sizeof(MxEntry) / sizeof(MxSeq)) - 1;  // (in the entries' place)
 
 struct MxAttnArgs {
   const void* q;
@@ -98,9 +103,7 @@ struct MxAttnArgs {
   int64_t q_stride, k_stride, v_stride;  // elements from row to row
   MxPool pool;
   const int32_t* parent;
-  const int32_t* node_offsets;
-  const int64_t* lens;
-  int B, Hq, G;
+  int Hq, G;
   MxCuts cuts;
   float inv_G;           // 1 / G
   float c2;              // scale * log2(e)
@@ -108,8 +111,13 @@ struct MxAttnArgs {
   float* lse;
   float* part;           // records of D + 4 floats: o of the split's keys, maximum (in octaves), denominator
   int n_entries;         // 0: more sequences than entries
-  alignas(16) MxEntry entries[MXA_ENTRIES];
+  int n_seqs, seq0;      // then: sequences of the launch, and the first one's number
+  union {
+    alignas(16) MxEntry entries[MXA_ENTRIES];
+    alignas(16) MxSeq seqs[MXA_SEQS + 1];
+  };
 };
+static_assert(sizeof(MxAttnArgs) <= 4096 && sizeof(MxSeq) * (MXA_SEQS + 1) == sizeof(MxEntry) * MXA_ENTRIES, "kernel arguments");
 
 // The work item of this workgroup: items are numbered sequence by sequence, in a sequence
 // (split * row groups + row group) * Hkv + KV head.  Every wave finds it by a prefix sum over the sequences.
@@ -155,13 +163,13 @@ __device__ __forceinline__ bool mx_item(const MxAttnArgs& a, int item, MxItem& w
   }
   int done = 0;
   int64_t recs = 0;
-  for (int base = 0; base < a.B; base += 64) {
+  for (int base = 0; base < a.n_seqs; base += 64) {
     const int s = base + lane;
     int n0 = 0, M = 0, L = 0;
-    if (s < a.B) {
-      n0 = a.node_offsets[s];
-      M = a.node_offsets[s + 1] - n0;
-      L = (int)a.lens[s];
+    if (s < a.n_seqs) {
+      n0 = a.seqs[s].n0;
+      M = a.seqs[s + 1].n0 - n0;
+      L = a.seqs[s].L;
     }
     const MxCut c = mx_cut(M, a.G, L, a.cuts);
     const int items = M > 0 ? c.n_sp * c.n_rg * a.pool.Hkv : 0;
@@ -170,7 +178,7 @@ __device__ __forceinline__ bool mx_item(const MxAttnArgs& a, int item, MxItem& w
     const unsigned long long behind = __ballot(upto > item);
     if (behind != 0ull) {
       const int e = __builtin_ctzll(behind);
-      w.s = base + e;
+      w.s = a.seq0 + base + e;
       w.n0 = __builtin_amdgcn_readlane(n0, e);
       w.M = __builtin_amdgcn_readlane(M, e);
       w.L = __builtin_amdgcn_readlane(L, e);

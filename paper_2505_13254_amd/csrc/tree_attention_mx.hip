@@ -30,14 +30,15 @@ void attn_mx_launch_e4m3(const MxAttnArgs& a, unsigned items, hipStream_t stream
 void attn_mx_launch_e2m1(const MxAttnArgs& a, unsigned items, hipStream_t stream);
 
 // The splits of a (row, head) meet: a wave each, whose lanes first find the splits' weights, a split to a lane, and then add up
-// the records, D / 4 lanes and four columns to a lane to each of 64 / (D / 4) records at a time.
+// the records, D / 4 lanes and four columns to a lane to each of 64 / (D / 4) records at a time.  Rows first .. first + rows - 1 of n * Hq + h.
 constexpr int MXM_THREADS = 256;
 template <int D>
-__global__ __launch_bounds__(MXM_THREADS) void k_attn_mx_merge(MxAttnArgs a, int64_t rows) {
+__global__ __launch_bounds__(MXM_THREADS) void k_attn_mx_merge(MxAttnArgs a, int row0, int rows) {
   constexpr int LANES = D / 4, AT_ONCE = 64 / LANES;
   const int lane = (int)(threadIdx.x & 63);
-  const int64_t x = __builtin_amdgcn_readfirstlane((int)((int64_t)blockIdx.x * (MXM_THREADS / 64) + (threadIdx.x >> 6)));  // n * Hq + h
-  if (x >= rows) return;
+  const int at = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * (MXM_THREADS / 64) + (threadIdx.x >> 6)));
+  if (at >= rows) return;
+  const int64_t x = row0 + at;  // n * Hq + h  (less than 2^26 of them)
   const int n = (int)(x / a.Hq);
   // its sequence and the records before
   int64_t recs = 0, first = -1;
@@ -50,13 +51,13 @@ __global__ __launch_bounds__(MXM_THREADS) void k_attn_mx_merge(MxAttnArgs a, int
     n_sp = __builtin_amdgcn_readlane(hi.y, e) & 255;
     first = __builtin_amdgcn_readlane(hi.w, e) + (x - (int64_t)__builtin_amdgcn_readlane(lo.y, e) * a.Hq) * n_sp;
   }
-  for (int base = 0; a.n_entries == 0 && base < a.B; base += 64) {
+  for (int base = 0; a.n_entries == 0 && base < a.n_seqs; base += 64) {
     const int s = base + lane;
     int n0 = 0, M = 0, sp = 0;
-    if (s < a.B) {
-      n0 = a.node_offsets[s];
-      M = a.node_offsets[s + 1] - n0;
-      sp = mx_cut(M, a.G, (int)a.lens[s], a.cuts).n_sp;
+    if (s < a.n_seqs) {
+      n0 = a.seqs[s].n0;
+      M = a.seqs[s + 1].n0 - n0;
+      sp = mx_cut(M, a.G, a.seqs[s].L, a.cuts).n_sp;
     }
     const int rec = M > 0 && sp > 1 ? M * a.Hq * sp : 0;
     const int upto = wave_prefix_sum(rec);
@@ -345,10 +346,10 @@ extern "C" hs_status hs_tree_attention_mx(const void* q, int64_t q_stride, const
                  (q_stride | k_stride | v_stride) % 8 == 0,
              HS_ERR_UNSUPPORTED, "%s: rows must begin at multiples of 16 bytes", what);
   a.q = q, a.k_tree = k_tree, a.v_tree = v_tree, a.q_stride = q_stride, a.k_stride = k_stride, a.v_stride = v_stride;
-  a.parent = parent, a.node_offsets = node_offsets, a.lens = prefix_lens;
-  a.B = B, a.Hq = Hq, a.G = Hq / Hkv, a.inv_G = 1.f / (float)(Hq / Hkv);
+  a.parent = parent;
+  a.Hq = Hq, a.G = Hq / Hkv, a.inv_G = 1.f / (float)(Hq / Hkv);
   a.c2 = scale * MXA_LOG2E;
-  a.o = o, a.lse = lse, a.part = static_cast<float*>(workspace);
+  a.o = o, a.lse = lse;
   MxPlan p;
   mx_plan(host_node_offsets, host_prefix_lens, B, Hq, Hkv, D, (int)fmt, p);
   HS_REQUIRE(p.items < ((int64_t)1 << 23), HS_ERR_UNSUPPORTED, "%s: too many rows for one call", what);  // (2^32 threads)
@@ -358,19 +359,44 @@ extern "C" hs_status hs_tree_attention_mx(const void* q, int64_t q_stride, const
                "%s: workspace of %zu bytes, %zu are needed (256-byte aligned)", what, workspace_bytes, need);
   }
   a.cuts = p.cuts;
-  a.n_entries = B <= MXA_ENTRIES ? p.n_seq : 0;
-  for (int e = 0, first = 0, rec0 = 0; e < a.n_entries; ++e) {
-    const MxCut& c = p.seq[e].cut;
-    const int s = p.seq[e].s, n0 = host_node_offsets[s], M = host_node_offsets[s + 1] - n0;
-    a.entries[e] = MxEntry{first, n0, M, (int)host_prefix_lens[s], c.pages, c.n_sp | c.form << 8 | s << 16, (int)((unsigned)c.n_blk | (unsigned)c.n_rg << 16), rec0};
-    first += c.n_sp * c.n_rg * Hkv, rec0 += c.n_sp > 1 ? M * Hq * c.n_sp : 0;
+  a.part = static_cast<float*>(workspace);
+  // One launch of all items, and one more where splits meet.  (rows: of the launch's sequences)
+  auto launch = [&](int64_t items, int64_t records, int n_first, int n_end) {
+    if (items == 0) return HS_OK;
+    (fmt == HS_MX_E4M3 ? attn_mx_launch_e4m3 : attn_mx_launch_e2m1)(a, (unsigned)items, static_cast<hipStream_t>(stream));
+    const hs_status failed = launch_status(what);
+    if (failed != HS_OK || records == 0) return failed;
+    const int row0 = n_first * Hq, rows = (n_end - n_first) * Hq;
+    const dim3 grid((unsigned)((rows + MXM_THREADS / 64 - 1) / (MXM_THREADS / 64)));
+    if (D == 128) hipLaunchKernelGGL((k_attn_mx_merge<128>), grid, dim3(MXM_THREADS), 0, static_cast<hipStream_t>(stream), a, row0, rows);
+    else hipLaunchKernelGGL((k_attn_mx_merge<64>), grid, dim3(MXM_THREADS), 0, static_cast<hipStream_t>(stream), a, row0, rows);
+    return launch_status(what);
+  };
+  if (B <= MXA_ENTRIES) {
+    a.n_entries = p.n_seq;
+    for (int e = 0, first = 0, rec0 = 0; e < a.n_entries; ++e) {
+      const MxCut& c = p.seq[e].cut;
+      const int s = p.seq[e].s, n0 = host_node_offsets[s], M = host_node_offsets[s + 1] - n0;
+      a.entries[e] = MxEntry{first, n0, M, (int)host_prefix_lens[s], c.pages, c.n_sp | c.form << 8 | s << 16, (int)((unsigned)c.n_blk | (unsigned)c.n_rg << 16), rec0};
+      first += c.n_sp * c.n_rg * Hkv, rec0 += c.n_sp > 1 ? M * Hq * c.n_sp : 0;
+    }
+    return launch(p.items, p.records, 0, NN);
   }
-  (fmt == HS_MX_E4M3 ? attn_mx_launch_e4m3 : attn_mx_launch_e2m1)(a, (unsigned)p.items, static_cast<hipStream_t>(stream));
-  st = launch_status(what);
-  if (st != HS_OK || p.records == 0) return st;
-  const int64_t rows = (int64_t)NN * Hq;
-  const dim3 merge_grid((unsigned)((rows + MXM_THREADS / 64 - 1) / (MXM_THREADS / 64)));
-  if (D == 128) hipLaunchKernelGGL((k_attn_mx_merge<128>), merge_grid, dim3(MXM_THREADS), 0, static_cast<hipStream_t>(stream), a, rows);
-  else hipLaunchKernelGGL((k_attn_mx_merge<64>), merge_grid, dim3(MXM_THREADS), 0, static_cast<hipStream_t>(stream), a, rows);
-  return launch_status(what);
+  // (the launches share a cut, and the workspace one after the other)
+  const int parts = (B + MXA_SEQS - 1) / MXA_SEQS, each = (B + parts - 1) / parts;
+  for (int s0 = 0; s0 < B; s0 += each) {
+    a.seq0 = s0, a.n_seqs = std::min(each, B - s0);
+    int64_t items = 0, records = 0;
+    for (int i = 0; i <= a.n_seqs; ++i) {
+      const int s = s0 + i;
+      a.seqs[i] = MxSeq{host_node_offsets[s], i < a.n_seqs ? (int)host_prefix_lens[s] : 0};
+      const int M = i < a.n_seqs ? host_node_offsets[s + 1] - host_node_offsets[s] : 0;
+      if (M == 0) continue;
+      const MxCut c = mx_cut(M, a.G, (int)host_prefix_lens[s], a.cuts);
+      items += (int64_t)c.n_sp * c.n_rg * Hkv, records += c.n_sp > 1 ? (int64_t)M * Hq * c.n_sp : 0;
+    }
+    st = launch(items, records, host_node_offsets[s0], host_node_offsets[s0 + a.n_seqs]);
+    if (st != HS_OK) return st;
+  }
+  return HS_OK;
 }

@@ -2,6 +2,8 @@
 // planner's source, with AddressSanitizer and UndefinedBehaviorSanitizer on the host side).  Nothing touches a GPU.
 //
 //   plan_mx fuzz N SEED   plans N random batches and checks what the kernels rely on; "ok ITEMS"
+//   plan_mx args N SEED   makes the real call of N random batches on addresses that nothing looks at and checks what its launches are
+//                         given: every sequence of the host arrays, and no address of the device's; "ok LAUNCHES"
 //   plan_mx form          reads "FMT Hq Hkv D B rows... lens..." lines and prints, for every sequence with rows,
 //                         "form blocks groups splits pages" (form: 0, 1 private, 2, 3 shared), a line to a batch
 #include <cstdio>
@@ -11,9 +13,12 @@
 
 #include "tree_attention_mx.hip"
 
+extern "C" hipError_t hipGetLastError() { return hipSuccess; }  // (the launches are stubs)
+
+static std::vector<std::pair<hs::MxAttnArgs, unsigned>> launched;
 namespace hs {
-void attn_mx_launch_e4m3(const MxAttnArgs&, unsigned, hipStream_t) { std::abort(); }
-void attn_mx_launch_e2m1(const MxAttnArgs&, unsigned, hipStream_t) { std::abort(); }
+void attn_mx_launch_e4m3(const MxAttnArgs& a, unsigned items, hipStream_t) { launched.emplace_back(a, items); }
+void attn_mx_launch_e2m1(const MxAttnArgs& a, unsigned items, hipStream_t) { launched.emplace_back(a, items); }
 }  // namespace hs
 
 static unsigned long long state = 88172645463325252ull;
@@ -137,6 +142,58 @@ static Batch random_batch(int it) {
   return b;
 }
 
+// A launch's arguments name sequences of the batch, as the host arrays have them, and as many items as its grid.
+static void check_arguments(const hs::MxAttnArgs& a, unsigned grid, const Batch& b, std::vector<int>& seen) {
+  const int B = (int)b.lens.size();
+  int64_t items = 0;
+  auto one = [&](int s, int n0, int M, int64_t L, const hs::MxCut& c) {
+    CHECK(s >= 0 && s < B && n0 == b.no[s] && M == b.no[s + 1] - n0 && L == b.lens[s]);
+    ++seen[s];
+    items += (int64_t)c.n_sp * c.n_rg * b.Hkv;
+  };
+  CHECK((a.n_entries > 0) == (B <= hs::MXA_ENTRIES) && a.n_entries <= hs::MXA_ENTRIES);
+  for (int i = 0; i < a.n_entries; ++i) {
+    const hs::MxEntry& e = a.entries[i];
+    hs::MxCut c = {};
+    c.n_sp = e.n_sp_form & 255, c.n_rg = (int)((unsigned)e.groups >> 16);
+    CHECK(e.first == items);
+    one(e.n_sp_form >> 16, e.n0, e.M, e.L, c);
+  }
+  if (a.n_entries == 0) {
+    CHECK(a.n_seqs >= 1 && a.n_seqs <= hs::MXA_SEQS && a.seq0 >= 0 && a.seq0 + a.n_seqs <= B);
+    for (int i = 0; i < a.n_seqs; ++i) {
+      const int M = a.seqs[i + 1].n0 - a.seqs[i].n0;
+      if (M > 0) one(a.seq0 + i, a.seqs[i].n0, M, a.seqs[i].L, hs::mx_cut(M, a.G, a.seqs[i].L, a.cuts));
+    }
+  }
+  CHECK(items == (int64_t)grid);
+}
+
+// Addresses of device arrays that a launch must not depend on: a captured one keeps the lengths that it was planned with.
+static int check_launches(const Batch& b) {
+  const int B = (int)b.lens.size();
+  if (mx_attn_host_check(b.no.data(), b.lens.data(), B, b.Hq, b.Hkv, b.D) != HS_OK || b.no.back() == 0) return 0;
+  const int64_t lens_at = 0x5a5a5a5a00ll, offsets_at = 0x6b6b6b6b00ll, other = 0x7c7c7c7c00ll;
+  auto at = [](int64_t x) { return reinterpret_cast<void*>(x); };
+  launched.clear();
+  const hs_status st = hs_tree_attention_mx(at(other), (int64_t)b.Hq * b.D, at(other), at(other), at(other), at(other), HS_MX_E4M3, at(other), (int64_t)b.Hkv * b.D, at(other),
+                                            (int64_t)b.Hkv * b.D, (const int32_t*)at(other), (const int32_t*)at(offsets_at), b.no.data(), (const int32_t*)at(other), 4, 1000,
+                                            (const int64_t*)at(lens_at), b.lens.data(), B, b.Hq, b.Hkv, b.D, HS_BF16, 0.1f, at(other), nullptr, at(other), 1ll << 40, nullptr);
+  CHECK(!launched.empty());
+  std::vector<int> seen(B, 0);
+  for (const auto& l : launched) {
+    for (size_t i = 0; i + 8 <= sizeof(l.first); i += 8) {
+      int64_t word;
+      std::memcpy(&word, reinterpret_cast<const char*>(&l.first) + i, 8);
+      CHECK(word != lens_at && word != offsets_at);
+    }
+    check_arguments(l.first, l.second, b, seen);
+  }
+  for (int s = 0; s < B; ++s) CHECK(seen[s] == (b.no[s + 1] > b.no[s] ? 1 : 0));
+  CHECK(st == HS_OK);
+  return (int)launched.size();
+}
+
 int main(int argc, char** argv) {
   if (argc >= 2 && std::strcmp(argv[1], "fuzz") == 0) {
     const int n = std::atoi(argv[2]);
@@ -164,6 +221,17 @@ int main(int argc, char** argv) {
           for (int ulps = -1; ulps <= 1; ++ulps) CHECK(div_by_product(x, d, d == 1 ? 0 : ulps) == x / d);  // (1 / 1 is exact)
     }
     std::printf("ok %ld\n", rows);
+    return 0;
+  }
+  if (argc >= 2 && std::strcmp(argv[1], "args") == 0) {
+    state ^= (unsigned long long)std::atoll(argv[3]) * 0x9e3779b97f4a7c15ull;
+    long launches = 0;
+    for (int it = 0; it < std::atoi(argv[2]); ++it, ++batch) {
+      Batch b = random_batch(it % 2 ? 40 : it);
+      for (auto& l : b.lens) l %= 200;  // (no splits: the merge's launch is not a stub)
+      launches += check_launches(b);
+    }
+    std::printf("ok %ld\n", launches);
     return 0;
   }
   if (argc >= 2 && std::strcmp(argv[1], "form") == 0) {

@@ -54,6 +54,14 @@ def test_random_batches(planner, seed):
     assert planner("fuzz", 3000, seed).startswith("ok")
 
 
+@pytest.mark.parametrize("seed", [1, 2])
+def test_launches_hold_what_they_attend_to(planner, seed):
+    """The arguments of a call's launches name every sequence of the host arrays once, with its rows and length, and neither of the
+    device arrays of offsets and lengths: a captured launch that read them would, once they have changed, work on other items than it was
+    planned for and write records behind its workspace."""
+    assert planner("args", 400, seed).startswith("ok")
+
+
 def test_the_kinds_of_the_gpu_tests(planner):
     """Batches that are there to reach one kind of work item reach it, uncut, in both formats."""
     batches = [(f, 32, 8, 128, rows, [L] * len(rows)) for f in (0, 1) for L in (100, 230) for _, rows in gpu.KINDS]

@@ -423,6 +423,28 @@ def test_graphs_that_share_a_workspace_and_streams(hs):
     assert torch.equal(got[0], want[0][0])
 
 
+@pytest.mark.parametrize("rows,lens", [([3], [700]), ([2, 1, 0] * 23 + [40], [90, 300, 5] * 23 + [5000]),
+                                       ([1] * 254 + [9, 0, 17] + [2] * 300, [200] * 255 + [9000, 9000] + [70] * 300)])
+def test_captured_calls_keep_their_lengths(hs, rows, lens):
+    """A captured call attends to the lengths and rows of its capture, however many sequences it has, after the device arrays have changed;
+    batches beyond 64 and beyond 255 sequences, cut sequences among them."""
+    st = Step(hs, rows, lens, 8, 2, 128, 0, seed=2)
+    want = st.run()
+    st.check(*want)
+    args, out, lse = st.args(), torch.empty_like(st.q), torch.empty(st.q.shape[:2], device=DEV)
+    ws = hs.hs_tree_attention_mx_workspace(args["host_node_offsets"], args["host_prefix_lens"], 8, 2, 128, DEV)
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        hs.hs_tree_attention_mx(**args, out=out, lse=lse, ws=ws)
+    for change in (lambda: args["prefix_lens"].add_(64), lambda: args["node_offsets"].zero_(), lambda: args["prefix_lens"].zero_()):
+        change()
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
+
+
 def test_refusals(hs):
     st = Step(hs, [3, 2], [100, 70], 8, 2, 128, 0, seed=1)
     good = st.args()
