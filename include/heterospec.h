@@ -497,7 +497,9 @@ hs_status hs_kv_commit_paged(const void* k_tree, const void* v_tree, const int32
  * hs_rotary: positions [N] int64.
  * hs_tree_rotary: the rows of B draft trees (node_offsets [B+1], parent [N] local, as everywhere): the root is at position
  *   prefix_lens[s] (int64 [B]: the tokens in the cache, the root's own not among them), a row at that plus its depth.
- *   Trees of any size; parents of a sequence's rows beyond the 1024th are followed one by one.  B = 0 with N = 0 only.
+ *   Outputs of rows node_offsets[B] .. N - 1 are left as they were.  Trees of any size; every row finds its depth by itself, parents of a
+ *   sequence's rows beyond the 1024th followed one by one, so that a chain takes time with the square of its length (20000 rows 6 ms): meant
+ *   for draft trees.  B = 0 with N = 0 only.
  * A rotation's gradient, and its undoing where mscale is 1, is the rotation by the opposite angles: the same call with
  * inv_freq negated.
  * Requires rot_dim even, 2 <= rot_dim <= D <= 1024, (Hq + Hkv) * D <= 2^24, hs_tree_rotary: N <= 2^23.  No workspace.  Rows that begin at

@@ -127,11 +127,13 @@ __global__ __launch_bounds__(ROT_THREADS) void k_rotary(RotaryArgs a) {
     if (x >= units) x -= units, ++head_t;
     if (head_t >= heads) head_t -= heads, ++t;
   };
-  auto angles = [&]() {
+  auto angles = [&]() {  // false: the row lies behind the last sequence
     int64_t tree_pos = 0;
     if constexpr (TREE) {  // (one row to a workgroup)
+      const int end = a.node_offsets[a.B];
       const int s = seq_of_row(a.node_offsets, a.B, n0);
       const int first = a.node_offsets[s];
+      if (n0 >= end) return false;
       tree_pos = a.prefix_lens[s] + tree_depth(a.parent + first, n0 - first, reinterpret_cast<int2*>(lds_raw + 8 * h));
     }
     for (int u = tid; u < n_here * h; u += ROT_THREADS) {
@@ -145,6 +147,7 @@ __global__ __launch_bounds__(ROT_THREADS) void k_rotary(RotaryArgs a) {
       s_lds[u] = sn * a.mscale;
     }
     __syncthreads();
+    return true;
   };
   if constexpr (VEC) {
     // A thread's first unit is read while the angles are computed, every later one ahead of the write of the one before, which a wait for it
@@ -169,7 +172,7 @@ __global__ __launch_bounds__(ROT_THREADS) void k_rotary(RotaryArgs a) {
       return r;
     };
     Unit ahead = read();
-    angles();
+    if (!angles()) return;
     while (ahead.to != nullptr) {
       const Unit now = ahead;
       ahead = read();
@@ -199,7 +202,7 @@ __global__ __launch_bounds__(ROT_THREADS) void k_rotary(RotaryArgs a) {
       }
     }
   } else {
-    angles();
+    if (!angles()) return;
     while (t < n_here) {
       const int which = head_t < a.heads[0] ? 0 : 1, head = which ? head_t - a.heads[0] : head_t;
       const T* const src = static_cast<const T*>(a.in[which]) + (n0 + t) * a.in_stride[which] + (int64_t)head * a.D;

@@ -102,6 +102,24 @@ def test_tree_rotary(hs, sizes, back, D, rot):
     assert torch.equal(qo, hs.hs_rotary(q, k, dev(pos), f)[0]) and torch.equal(ko, hs.hs_rotary(q, k, dev(pos), f)[1])
 
 
+@pytest.mark.parametrize("D,interleaved", [(128, False), (64, True), (20, False)])
+def test_rows_behind_the_last_sequence(hs, D, interleaved):
+    """A fixed budget of rows of which the trees use fewer (a captured step, say): the rows behind are left as they were."""
+    sizes, N = [5, 0, 9, 0], 40
+    rs, g = np.random.RandomState(3), torch.Generator(device=DEV).manual_seed(1)
+    parent = torch.zeros(N, dtype=torch.int32, device=DEV)
+    parent[:14] = torch.tensor(_parents(rs, 5, 3) + _parents(rs, 9, 3), dtype=torch.int32)
+    no = torch.from_numpy(np.concatenate([[0], np.cumsum(sizes)]).astype(np.int32)).to(DEV)
+    lens = torch.tensor([7, 100, 30, 5], device=DEV)
+    f, _ = hs.hs_rotary_frequencies(min(D, 18), device=DEV)
+    q, k = (torch.randn((N, h, D), generator=g, device=DEV) for h in (3, 1))
+    out = (torch.full_like(q, 5.0), torch.full_like(k, 5.0))
+    hs.hs_tree_rotary(q, k, parent, no, lens, f, interleaved=interleaved, q_out=out[0], k_out=out[1])
+    for x, y in zip((q, k), out):
+        want, _ = hs.hs_tree_rotary(x[:14], None, parent[:14].contiguous(), no, lens, f, interleaved=interleaved)
+        assert torch.equal(y[:14], want) and (y[14:] == 5.0).all()
+
+
 def test_gradient_is_the_opposite_rotation(hs):
     """d/dx <w, rotary(x)> against central differences of the call itself (float32, steps of a power of two: the outputs' rounding
     of 2^-24 of numbers of order one over a step of 2^-6 leaves 2^-17 a term, of which two contribute)."""
