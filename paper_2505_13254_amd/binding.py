@@ -570,7 +570,7 @@ def hs_tree_attention_mx(q, cache, k_tree, v_tree, parent, node_offsets, host_no
     if cache_D != D or tuple(k_tree.shape) != (NN, Hkv, D) or v_tree.shape != k_tree.shape:
         raise ValueError("k_tree and v_tree must be [NN, Hkv, D] of the cache's Hkv, and D that of q")
     if parent.numel() != NN or node_offsets.numel() != B + 1 or prefix_lens.numel() != B or host_prefix_lens.numel() != B or \
-            (B > 0 and int(host_node_offsets[B]) != NN):
+            int(host_node_offsets[B]) != NN:
         raise ValueError("parent must hold NN values, the offsets B + 1 (the last one NN), the lengths B")
     if out is None:
         out = _empty((NN, Hq, D), q.dtype, q.device, stream)

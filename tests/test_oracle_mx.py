@@ -185,6 +185,16 @@ def test_refusals_need_no_gpu(hs):
         assert attend(**long, **bad) == 4, bad
 
 
+def test_rows_of_no_sequence_are_refused(hs):
+    """q with rows, but no sequence that they belong to: nothing would be written to the output."""
+    import torch
+    pool = hs.new_mx_cache(1, 2, 64, 0, "cpu")
+    i32, rows = dict(dtype=torch.int32), torch.zeros((3, 2, 64), dtype=torch.bfloat16)
+    none = torch.zeros(0, dtype=torch.int64)
+    with pytest.raises(ValueError, match="the last one NN"):
+        hs.hs_tree_attention_mx(rows, pool, rows, rows, torch.zeros(3, **i32), torch.zeros(1, **i32), torch.zeros(1, **i32), torch.zeros((0, 1), **i32), none, none, 0.1)
+
+
 def test_workspace_query_is_host_arithmetic(hs):
     import torch
     def need(rows, lens, *a):
