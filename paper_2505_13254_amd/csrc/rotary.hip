@@ -257,7 +257,7 @@ static hs_status rotary_impl(RotaryArgs a, hs_dtype dt, hs_rotary_pairs pairs, b
   HS_REQUIRE((a.N - 1) / a.tokens < 1 << 23, HS_ERR_UNSUPPORTED, "hs_tree_rotary: %d rows are too many for one call", a.N);
   const int h = a.rot / 2;
   const size_t lds = (size_t)a.tokens * h * 8 + (tree ? ROT_STAGE * 8 : 0);
-  const dim3 grid((unsigned)((a.N + a.tokens - 1) / a.tokens)), block(ROT_THREADS);
+  const dim3 grid((unsigned)((a.N - 1) / a.tokens + 1)), block(ROT_THREADS);
 #define ROT_LAUNCH(T, P, TR, V) hipLaunchKernelGGL((k_rotary<T, P, TR, V>), grid, block, lds, static_cast<hipStream_t>(stream), a)
 #define ROT_VEC(T, P, TR) \
   do {                    \

@@ -120,6 +120,17 @@ def test_rows_behind_the_last_sequence(hs, D, interleaved):
         assert torch.equal(y[:14], want) and (y[14:] == 5.0).all()
 
 
+def test_the_most_rows(hs):
+    """As many rows as the count holds, in place, a pair each: 26 GB."""
+    N, ends = (1 << 31) - 1, [0, 1, 255, 1 << 23, (1 << 31) - 258, (1 << 31) - 257, (1 << 31) - 256, (1 << 31) - 3, (1 << 31) - 2]
+    q = torch.ones((N, 1, 2), dtype=torch.bfloat16, device=DEV)
+    pos = torch.arange(N, device=DEV)
+    f = torch.tensor([0.25], dtype=torch.float64, device=DEV)
+    hs.hs_rotary(q, None, pos, f, q_out=q)
+    rows = torch.tensor(ends, device=DEV)
+    _check(q[rows], torch.ones((len(ends), 1, 2), dtype=torch.bfloat16), np.asarray(ends), f.cpu().numpy(), False, 1.0)
+
+
 def test_gradient_is_the_opposite_rotation(hs):
     """d/dx <w, rotary(x)> against central differences of the call itself (float32, steps of a power of two: the outputs' rounding
     of 2^-24 of numbers of order one over a step of 2^-6 leaves 2^-17 a term, of which two contribute)."""
