@@ -25,7 +25,7 @@
  *   hs_tree_attention_paged, hs_kv_commit_paged   the same two on caches made of pages
  *   hs_tree_attention_shared_tree   hs_tree_attention on batch entries that all verify one tree
  *
- * and a step on a quantised cache, which holds a third to a half of what the bfloat16 cache holds in the same bytes:
+ * and a step on a quantised cache, which holds 1.9 (e4m3) to 3.8 (e2m1) times the tokens of a bfloat16 cache in the same bytes:
  *
  *   hs_rotary, hs_tree_rotary   rotary positions of query and key rows; tree rows find theirs from the tree
  *   hs_kv_append_mx, hs_kv_commit_mx, hs_kv_read_mx   prompt rows and accepted paths join the cache, and are read back
@@ -485,7 +485,8 @@ hs_status hs_kv_commit_paged(const void* k_tree, const void* v_tree, const int32
  * hs_rotary, hs_tree_rotary  (what the attention calls leave to their caller: "no positional encoding is applied")
  *
  * The first rot_dim elements of every head's row are turned, pair by pair: row n at position p, pair j, angle
- *   t = p * inv_freq[j]          (double precision: exact to 2^-50 of a turn for every position below 2^24 or so)
+ *   t = p * inv_freq[j]          (in turns, in double precision: off by up to 2^-51 of their number, 2^-29 of a turn at position 2^24; the rest
+ *                                 of a turn is then rounded to float32, 2^-26 of a turn at most)
  *   (a, b) -> mscale * (a cos t - b sin t, b cos t + a sin t)
  * with (a, b) = elements (j, j + rot_dim / 2) (HS_ROTARY_HALF) or (2 j, 2 j + 1) (HS_ROTARY_NEIGHBOURS) of the head.  The
  * elements behind rot_dim are copied as they are.
@@ -546,7 +547,7 @@ hs_status hs_rotary_frequencies(int32_t rot_dim, double base, hs_rotary_scaling 
  * hs_kv_commit_mx: the rows of the tree's root and of the accepted path, as in hs_kv_commit.
  * Both leave cache_lens (int64 [B]) alone, so that the layers of a model share it; new_lens (int64 [B], may be NULL, must not overlap
  *   cache_lens) receives cache_lens[s] plus the rows that sequence s took.  A sequence takes at most max_blocks * 64 tokens: the
- *   leading rows that fit.  Rows whose block-table entry is not a page (0 .. n_pages - 1) are dropped.
+ *   leading rows that fit.  Rows whose block-table entry is not a page (0 .. n_pages - 1) are dropped, but counted.
  * hs_kv_read_mx: tokens first[s] .. (int64 [B], device; NULL: from 0) of sequence s as rows out_offsets[s] .. out_offsets[s+1] - 1
  *   (int64 [B+1], device; total = out_offsets[B]) of k_out / v_out [total, Hkv, D] of element type dt.  The tokens must have been stored.
  *   Rows beyond the table, or of entries that are no page, are left as they were.

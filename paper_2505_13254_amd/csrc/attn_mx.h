@@ -20,7 +20,7 @@ typedef __attribute__((address_space(3))) shortx4* lds_s4_ptr;
 constexpr int MXA_THREADS = 512;
 constexpr int MXA_WAVES = 8;
 constexpr int MXA_MAX_M = 1024;       // tree rows of a sequence
-constexpr float MX_LIMIT = 0x1p80f;   // a denominator (of a half-wave's keys) that reaches it moves the maximum
+constexpr float MX_LIMIT = 0x1p80f;   // a denominator (of a half-wave's keys) that reaches it moves the maximum, or sends its row to attn_mx_follow
 constexpr float MXA_FLOOR = -3.402823466e38f;
 constexpr float MXA_LOG2E = 1.4426950408889634f, MXA_LN2 = 0.6931471805599453f;
 
@@ -339,7 +339,7 @@ struct MxState {
 // Barrier of the workgroup for LDS; loads in flight stay in flight.
 __device__ __forceinline__ void mx_meet() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
-// Tree row i and query head h of row r of a KV head (r < 2^16, G <= 1024: r / G by a float product is exact).
+// Tree row i and query head h of row r of a KV head (r / G < 1024 and G <= 1024: by a float product it is exact).
 struct MxOwn {
   int i, h;
 };
