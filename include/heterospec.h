@@ -31,6 +31,13 @@
  *   hs_kv_append_mx, hs_kv_commit_mx, hs_kv_read_mx   prompt rows and accepted paths join the cache, and are read back
  *   hs_tree_attention_mx        tree-masked attention over it
  *
+ * and on a cache of latents, where all heads of a layer share one vector a token:
+ *
+ *   hs_latent_store, hs_latent_read   rows of latents into the paged cache and out of it, by slots
+ *   hs_tree_attention_latent    tree-masked attention over it (absorbed form; decoding: trees of one row)
+ *   hs_prompt_attention_latent  causal attention of prompt rows on expanded keys and values
+ *   hs_block_tables, hs_slot_map   pages for sequences, and the slots of their rows, on the GPU (for every paged call)
+ *
  * Conventions that hold for every call
  *   - Pointers are DEVICE pointers unless the parameter name starts with host_.  The caller owns
  *     every buffer; the library allocates and frees nothing, and keeps nothing after a call.
@@ -599,6 +606,96 @@ hs_status hs_tree_attention_mx(const void* q, int64_t q_stride,
                                const int64_t* prefix_lens, const int64_t* host_prefix_lens,
                                int32_t B, int32_t Hq, int32_t Hkv, int32_t D, hs_dtype dt, float scale,
                                void* o, float* lse, void* workspace, size_t workspace_bytes, hs_stream stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * hs_block_tables, hs_slot_map  (what every paged call takes as given: which pages a sequence has, and where its rows go)
+ *
+ * hs_block_tables: sequence s is to have pages for want[s] tokens (int64 [B], device; <= 0: none), need = ceil(want[s] / page_tokens) of them, and has
+ *   held[s] (int32 [B]), entries 0 .. held[s] - 1 of its row of block_table [B, max_blocks].
+ *   need < held[s]: the entries behind need go back to the free pages.  need > held[s]: entries held[s] .. need - 1 are filled with free
+ *   pages; sequences are served in ascending order, and from the first whose request is more than what is left on, none is.  need > max_blocks:
+ *   the sequence keeps what it has.
+ *   free_pages [n_pages] int32 is a stack of free_count[0] pages (device, int32 [1]).  The pages that go back are put on it in ascending order of
+ *   (sequence, entry), then the requested ones are taken off its top, in ascending order.  Entries of the stack at and behind the new count, and
+ *   entries of the table behind a sequence's new count, are left as they were.
+ *   new_held [B], new_free_count [1]: the counts afterwards; they must not overlap held and free_count, so that two calls can
+ *   go back and forth between two pairs.  refused [B] int32 (may be NULL): 0, 1 (not served: too few free pages) or 2 (more than max_blocks).
+ *   The pages of the stack and the table must be distinct and fewer than n_pages + 1 in all.  B * max_blocks and n_pages below 2^30.
+ *
+ * hs_slot_map: rows node_offsets[s] .. node_offsets[s+1] - 1 (int32 [B+1]) are to become tokens cache_lens[s], cache_lens[s] + 1, ... (int64 [B], left alone) of
+ *   sequence s: slots[n] (int64 [NN]) is page * page_tokens + (token mod page_tokens), the place of row n in a pool [n_pages, page_tokens, ...].
+ *   With accept_path [B, max_depth] and accept_len [B] (int32, device, as hs_verify_accept writes them; both NULL otherwise): the tree's
+ *   root and the accepted rows, in path order, as in hs_kv_commit; rows that are not accepted have no slot.
+ *   slots[n] = -1 for a row without a slot: not accepted, behind the sequence's pages (held [B] int32 of them; NULL: max_blocks), an entry that is not a page (0 ..
+ *   n_pages - 1), or a row at or behind node_offsets[B].
+ *   new_lens (int64 [B], may be NULL, must not overlap cache_lens): cache_lens[s] plus the rows that sequence s has tokens for: all, or the leading ones that its
+ *   pages hold.
+ * Both: no workspace.
+ */
+hs_status hs_block_tables(const int64_t* want, int32_t page_tokens, int32_t* block_table, int32_t max_blocks, const int32_t* held,
+                          int32_t* new_held, int32_t* free_pages, int32_t n_pages, const int32_t* free_count, int32_t* new_free_count,
+                          int32_t* refused, int32_t B, hs_stream stream);
+hs_status hs_slot_map(const int32_t* node_offsets, int32_t NN, const int32_t* accept_path, const int32_t* accept_len, int32_t max_depth,
+                      const int32_t* block_table, int32_t max_blocks, int32_t page_tokens, int32_t n_pages, const int32_t* held,
+                      const int64_t* cache_lens, int64_t* slots, int64_t* new_lens, int32_t B, hs_stream stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * hs_latent_store, hs_latent_read  (a cache of latents: one vector a token that all heads share)
+ *
+ * A pool is [n_slots, R + Dr] elements of type dt: a token's latent (R) and behind it the rotary part of its key (Dr), already turned.
+ * hs_latent_store: rows c [N, R] and r [N, Dr] (row n at base + n * stride, elements) go to slots[n] (int64 [N], device; hs_slot_map).  A row whose
+ *   slot is not one (0 .. n_slots - 1) goes nowhere.  Two rows must not have the same slot.
+ * hs_latent_read: the rows at slots[n] (not necessarily distinct) to c and r; a row whose slot is not one is left as it was.
+ * Requires R and Dr to be multiples of 16 bytes (Dr = 0: no r), rows that begin at multiples of 16 bytes.  No workspace.
+ */
+hs_status hs_latent_store(const void* c, int64_t c_stride, const void* r, int64_t r_stride, const int64_t* slots, int32_t N, void* pool,
+                          int64_t n_slots, int32_t R, int32_t Dr, hs_dtype dt, hs_stream stream);
+hs_status hs_latent_read(const void* pool, int64_t n_slots, const int64_t* slots, int32_t N, void* c, int64_t c_stride, void* r, int64_t r_stride,
+                         int32_t R, int32_t Dr, hs_dtype dt, hs_stream stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * hs_tree_attention_latent  (hs_tree_attention_paged on a cache of latents, absorbed form; decoding of single tokens: trees of one row)
+ *
+ * With c_j, r_j the latent and the rotary part of token j, for tree row i of sequence s and query head h:
+ *   o[i,h,:] = softmax_j( scale * (<q[i,h,:], c_j> + <q_rope[i,h,:], r_j>) ) . c_j
+ * over j = the prefix_lens[s] stored tokens of sequence s and the tree rows on the root path of i.  (q is the head's query times its key
+ * matrix, o times its value matrix is the head's output: both products are the caller's.)
+ *   q [NN,Hq,R], q_rope [NN,Hq,Dr], o [NN,Hq,R]: row n, head h at base + n * stride + h * head_stride (elements).  c_tree [NN,R], r_tree [NN,Dr]: rows
+ *   with a stride.  pool [n_pages, 64, R + Dr] dense.  All of type dt; float32 sums and softmax, with HS_BF16 P is rounded to bfloat16 for the
+ *   second product and the output once.
+ *   parent, node_offsets, host_node_offsets, block_table, prefix_lens, host_prefix_lens as in hs_tree_attention_paged; lse [NN,Hq] dense, may be NULL.
+ *   The launch is planned from the host copies: they must equal the device arrays, and a captured launch keeps them.
+ * A NaN or an infinity in a token reaches the rows that see it and no others: they are NaN, as a whole or in some columns.  Weights are relative to a
+ * running maximum, values may have any magnitude below 2^90.  Block-table entries behind a sequence's last token are not looked at.  The same call gives the
+ * same bits.
+ * Requires R <= 1024, Dr <= 1024, at most 1024 tree rows and HS_MX_MAX_TOKENS stored tokens per sequence, NN * Hq < 2^24, scale > 0, output rows that do not overlap.
+ */
+size_t hs_tree_attention_latent_workspace(const int32_t* host_node_offsets, const int64_t* host_prefix_lens, int32_t B, int32_t Hq, int32_t R,
+                                          int32_t Dr);
+hs_status hs_tree_attention_latent(const void* q, int64_t q_stride, int64_t q_head_stride, const void* q_rope, int64_t q_rope_stride,
+                                   int64_t q_rope_head_stride, const void* pool, const void* c_tree, int64_t c_stride, const void* r_tree,
+                                   int64_t r_stride, const int32_t* parent, const int32_t* node_offsets, const int32_t* host_node_offsets,
+                                   const int32_t* block_table, int32_t max_blocks, int32_t n_pages, const int64_t* prefix_lens,
+                                   const int64_t* host_prefix_lens, int32_t B, int32_t Hq, int32_t R, int32_t Dr, hs_dtype dt, float scale, void* o,
+                                   int64_t o_stride, int64_t o_head_stride, float* lse, void* workspace, size_t workspace_bytes, hs_stream stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * hs_prompt_attention_latent  (the rows of prompts, expanded form: every head has keys and values of its own, made from the latents)
+ *
+ * Sequence s has rows q_offsets[s] .. q_offsets[s+1] - 1 (int32 [B+1]) and keys kv_offsets[s] .. kv_offsets[s+1] - 1 (int64 [B+1]): what is cached already and, last, its
+ * own.  Row i of n sees the keys 0 .. T - n + i of its T (none where that is negative: o = 0, lse = -infinity):
+ *   o[i,h,:] = softmax_j( scale * (<q[i,h,:], k[j,h,:]> + <q_rope[i,h,:], k_rope[j,:]>) ) . v[j,h,:]
+ *   q [N,H,Dn], q_rope [N,H,Dr], k [T,H,Dn], v [T,H,Dv], o [N,H,Dv]: row n, head h at base + n * stride + h * head_stride (elements; k and v may be
+ *   slices of one product's result).  k_rope [T,Dr]: rows with a stride.  Types, sums, NaN, magnitudes and the host copies as in hs_tree_attention_latent.
+ * Requires Dn, Dr, Dv <= 1024, at most HS_MX_MAX_TOKENS keys per sequence, N * H < 2^24, scale > 0, output rows that do not overlap.
+ */
+size_t hs_prompt_attention_latent_workspace(const int32_t* host_q_offsets, const int64_t* host_kv_offsets, int32_t B, int32_t H, int32_t Dv);
+hs_status hs_prompt_attention_latent(const void* q, int64_t q_stride, int64_t q_head_stride, const void* q_rope, int64_t q_rope_stride,
+                                     int64_t q_rope_head_stride, const void* k, int64_t k_stride, int64_t k_head_stride, const void* k_rope,
+                                     int64_t k_rope_stride, const void* v, int64_t v_stride, int64_t v_head_stride, const int32_t* q_offsets,
+                                     const int64_t* kv_offsets, const int32_t* host_q_offsets, const int64_t* host_kv_offsets, int32_t B, int32_t H,
+                                     int32_t Dn, int32_t Dr, int32_t Dv, hs_dtype dt, float scale, void* o, int64_t o_stride, int64_t o_head_stride,
+                                     float* lse, void* workspace, size_t workspace_bytes, hs_stream stream);
 
 /* ------------------------------------------------------------------------------------------------
  * hs_time_next_attention  (measurement aid, not a step of the method)

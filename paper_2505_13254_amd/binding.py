@@ -78,6 +78,16 @@ _SIGNATURES = {
     "hs_tree_attention_mx_workspace": (_sz, [_vp, _vp, _i32, _i32, _i32, _i32]),
     "hs_tree_attention_mx": (_c.c_int, [_vp, _i64, _vp, _vp, _vp, _vp, _c.c_int, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _vp, _i32, _i32,
                                         _vp, _vp, _i32, _i32, _i32, _i32, _c.c_int, _f32, _vp, _vp, _vp, _sz, _vp]),
+    "hs_block_tables": (_c.c_int, [_vp, _i32, _vp, _i32, _vp, _vp, _vp, _i32, _vp, _vp, _vp, _i32, _vp]),
+    "hs_slot_map": (_c.c_int, [_vp, _i32, _vp, _vp, _i32, _vp, _i32, _i32, _i32, _vp, _vp, _vp, _vp, _i32, _vp]),
+    "hs_latent_store": (_c.c_int, [_vp, _i64, _vp, _i64, _vp, _i32, _vp, _i64, _i32, _i32, _c.c_int, _vp]),
+    "hs_latent_read": (_c.c_int, [_vp, _i64, _vp, _i32, _vp, _i64, _vp, _i64, _i32, _i32, _c.c_int, _vp]),
+    "hs_tree_attention_latent_workspace": (_sz, [_vp, _vp, _i32, _i32, _i32, _i32]),
+    "hs_tree_attention_latent": (_c.c_int, [_vp, _i64, _i64, _vp, _i64, _i64, _vp, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _vp, _i32, _i32, _vp, _vp,
+                                            _i32, _i32, _i32, _i32, _c.c_int, _f32, _vp, _i64, _i64, _vp, _vp, _sz, _vp]),
+    "hs_prompt_attention_latent_workspace": (_sz, [_vp, _vp, _i32, _i32, _i32]),
+    "hs_prompt_attention_latent": (_c.c_int, [_vp, _i64, _i64, _vp, _i64, _i64, _vp, _i64, _i64, _vp, _i64, _vp, _i64, _i64, _vp, _vp, _vp, _vp, _i32,
+                                              _i32, _i32, _i32, _i32, _c.c_int, _f32, _vp, _i64, _i64, _vp, _vp, _sz, _vp]),
     "hs_tree_validate": (_c.c_int, [_vp, _vp, _vp, _i32, _i32, _vp, _vp]),
     "hs_time_next_attention": (_c.c_int, [_vp, _vp]),
     "hs_tree_attention_last_kernel": (_c.c_int32, []),
@@ -583,6 +593,166 @@ def hs_tree_attention_mx(q, cache, k_tree, v_tree, parent, node_offsets, host_no
     _check(_calls.hs_tree_attention_mx(q, *pool, k_tree, v_tree, parent, node_offsets, host_node_offsets, block_table,
                                        block_table.shape[1], n_pages, prefix_lens, host_prefix_lens, B, Hq, Hkv, D, scale, out, lse, ws,
                                        stream), "hs_tree_attention_mx")
+    return out, lse
+
+
+def new_page_tables(B: int, max_blocks: int, n_pages: int, device="cuda:0") -> Dict[str, torch.Tensor]:
+    """The tables of B sequences over a pool of n_pages free pages, as hs_block_tables takes them: block_table int32 [B, max_blocks], held
+    int32 [B], free_pages int32 [n_pages] (page 0 comes first), free_count int32 [1]."""
+    i32 = dict(dtype=torch.int32, device=device)
+    return dict(block_table=torch.full((B, max_blocks), -1, **i32), held=torch.zeros(B, **i32), free_pages=torch.arange(n_pages - 1, -1, -1, **i32),
+                free_count=torch.full((1,), n_pages, **i32))
+
+
+def hs_block_tables(want, block_table, held, free_pages, free_count, *, page_tokens: int = HS_MX_PAGE, new_held=None, new_free_count=None, refused=None,
+                    stream=None):
+    """Pages for want[s] tokens (int64 [B], GPU) of every sequence: block_table int32 [B, max_blocks] and free_pages int32 [n_pages] are updated in
+    place, held int32 [B] and free_count int32 [1] are left alone.  refused: int32 [B] or None.  Returns (new_held, new_free_count)."""
+    B = want.numel()
+    if block_table.dim() != 2 or block_table.shape[0] != B or held.numel() != B:
+        raise ValueError("block_table must be [B, max_blocks], held [B]")
+    if new_held is None:
+        new_held = _empty(B, torch.int32, want.device, stream)
+    if new_free_count is None:
+        new_free_count = _empty(1, torch.int32, want.device, stream)
+    if new_held.numel() != B or free_count.numel() != 1 or new_free_count.numel() != 1 or (refused is not None and refused.numel() != B):
+        raise ValueError("new_held and refused must hold B values, the counts one")
+    _check(_calls.hs_block_tables(want, page_tokens, block_table, block_table.shape[1], held, new_held, free_pages, free_pages.numel(), free_count,
+                                  new_free_count, refused, B, stream), "hs_block_tables")
+    return new_held, new_free_count
+
+
+def hs_slot_map(node_offsets, NN: int, cache_lens, block_table, n_pages: int, *, page_tokens: int = HS_MX_PAGE, held=None, accept_path=None,
+                accept_len=None, slots=None, new_lens=None, stream=None):
+    """Slots (int64 [NN]) of the rows node_offsets[s] .. of sequence s (int32 [B+1]) behind its cache_lens[s] tokens (int64 [B]) in a pool of n_pages
+    pages, -1 for a row without one.  With accept_path int32 [B, max_depth] and accept_len int32 [B]: of a tree's root and accepted rows.  held int32 [B]
+    or None: pages of block_table int32 [B, max_blocks] that a sequence has.  new_lens (int64 [B] or None) receives the lengths afterwards."""
+    B = node_offsets.numel() - 1
+    if block_table.dim() != 2 or block_table.shape[0] != B or cache_lens.numel() != B:
+        raise ValueError("block_table must be [B, max_blocks], cache_lens [B]")
+    if (held is not None and held.numel() != B) or (new_lens is not None and new_lens.numel() != B):
+        raise ValueError("held and new_lens must hold B values")
+    if (accept_path is None) != (accept_len is None) or (accept_path is not None and
+                                                         (accept_path.dim() != 2 or accept_path.shape[0] != B or accept_len.numel() != B)):
+        raise ValueError("accept_path must be [B, max_depth], accept_len [B], both or neither")
+    if slots is None:
+        slots = _empty(NN, torch.int64, node_offsets.device, stream)
+    if slots.numel() != NN:
+        raise ValueError("slots must hold NN values")
+    _check(_calls.hs_slot_map(node_offsets, NN, accept_path, accept_len, 0 if accept_path is None else accept_path.shape[1], block_table,
+                              block_table.shape[1], page_tokens, n_pages, held, cache_lens, slots, new_lens, B, stream), "hs_slot_map")
+    return slots
+
+
+def new_latent_cache(n_pages: int, R: int, Dr: int, dtype=torch.bfloat16, device="cuda:0") -> torch.Tensor:
+    """The pool of a paged cache of latents (uninitialised): [n_pages, 64, R + Dr], a token's latent and behind it its rotary part."""
+    return torch.empty((n_pages, HS_MX_PAGE, R + Dr), dtype=dtype, device=device)
+
+
+def _latent_pool(pool, R: int, Dr: int):
+    if pool.dim() != 3 or pool.shape[2] != R + Dr:
+        raise ValueError("the pool must be [n_pages, page_tokens, R + Dr]")
+    return pool.shape[0] * pool.shape[1]
+
+
+def hs_latent_store(c, r, slots, pool, *, stream=None) -> None:
+    """Rows c [N, R] and r [N, Dr] (float32 or bfloat16, GPU; rows may have a stride of their own) go to slots (int64 [N]; one that the pool does not
+    have: the row goes nowhere) of `pool` (new_latent_cache)."""
+    if c.dim() != 2 or r.dim() != 2 or r.shape[0] != c.shape[0] or slots.numel() != c.shape[0]:
+        raise ValueError("c must be [N, R], r [N, Dr], slots [N]")
+    n = _latent_pool(pool, c.shape[1], r.shape[1])
+    _check(_calls.hs_latent_store(c, r, slots, c.shape[0], pool, n, c.shape[1], r.shape[1], stream), "hs_latent_store")
+
+
+def hs_latent_read(pool, slots, R: int, *, out=None, stream=None):
+    """Rows (c [N, R], r [N, Dr]) at slots (int64 [N]) of a pool, `out` or new ones.  Rows without a slot are left as they were."""
+    N = slots.numel()
+    if out is None:
+        out = tuple(_empty((N, n), pool.dtype, pool.device, stream) for n in (R, pool.shape[-1] - R))
+    c, r = out
+    if c.dim() != 2 or r.dim() != 2 or c.shape[0] != N or r.shape[0] != N or c.shape[1] != R:
+        raise ValueError("out must be two tensors [N, R] and [N, Dr]")
+    n = _latent_pool(pool, R, r.shape[1])
+    _check(_calls.hs_latent_read(pool, n, slots, N, c, r, R, r.shape[1], stream), "hs_latent_read")
+    return c, r
+
+
+def hs_tree_attention_latent_workspace(host_node_offsets, host_prefix_lens, Hq: int, R: int, Dr: int, device, *, stream=None) -> Optional[torch.Tensor]:
+    """A workspace for hs_tree_attention_latent calls of these row counts and lengths (CPU tensors) on `stream`; None where none is needed."""
+    if host_node_offsets.numel() != host_prefix_lens.numel() + 1:
+        raise ValueError("the offsets must hold B + 1 values, the lengths B")
+    no, pl = host_node_offsets.to("cpu", torch.int32).contiguous(), host_prefix_lens.to("cpu", torch.int64).contiguous()
+    n = lib().hs_tree_attention_latent_workspace(no.data_ptr(), pl.data_ptr(), no.numel() - 1, int(Hq), int(R), int(Dr))
+    return workspace(n, device, stream)
+
+
+def hs_tree_attention_latent(q, q_rope, pool, c_tree, r_tree, parent, node_offsets, host_node_offsets, block_table, prefix_lens, host_prefix_lens,
+                             scale: float, *, want_lse: bool = False, out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                             ws: Optional[torch.Tensor] = None, stream=None):
+    """Absorbed latent attention of tree rows: q [NN,Hq,R], q_rope [NN,Hq,Dr], c_tree [NN,R], r_tree [NN,Dr], `pool` [n_pages,64,R+Dr] (float32 or
+    bfloat16, GPU; all but the pool may have strides of their own, heads included), the rest as in hs_tree_attention_paged.  Returns (o [NN,Hq,R], lse
+    [NN,Hq] or None)."""
+    if q.dim() != 3 or q_rope.dim() != 3 or pool.dim() != 3:
+        raise ValueError("q must be [NN, Hq, R], q_rope [NN, Hq, Dr], the pool [n_pages, 64, R + Dr]")
+    NN, Hq, R = q.shape
+    Dr = q_rope.shape[2]
+    B = host_node_offsets.numel() - 1
+    if pool.shape[1] != HS_MX_PAGE or pool.shape[2] != R + Dr or tuple(q_rope.shape[:2]) != (NN, Hq) or tuple(c_tree.shape) != (NN, R) or \
+            tuple(r_tree.shape) != (NN, Dr):
+        raise ValueError("q_rope must be [NN, Hq, Dr], c_tree [NN, R], r_tree [NN, Dr], the pool [n_pages, %d, R + Dr]" % HS_MX_PAGE)
+    if block_table.dim() != 2 or block_table.shape[0] != B:
+        raise ValueError("block_table must be [B, max_blocks]")
+    if parent.numel() != NN or node_offsets.numel() != B + 1 or prefix_lens.numel() != B or host_prefix_lens.numel() != B or \
+            int(host_node_offsets[B]) != NN:
+        raise ValueError("parent must hold NN values, the offsets B + 1 (the last one NN), the lengths B")
+    if out is None:
+        out = _empty((NN, Hq, R), q.dtype, q.device, stream)
+    if want_lse and lse is None:
+        lse = _empty((NN, Hq), torch.float32, q.device, stream)
+    if out.shape != q.shape or (lse is not None and lse.numel() != NN * Hq):
+        raise ValueError("out must be [NN, Hq, R], lse [NN, Hq]")
+    if ws is None:
+        ws = hs_tree_attention_latent_workspace(host_node_offsets, host_prefix_lens, Hq, R, Dr, q.device, stream=stream)
+    _check(_calls.hs_tree_attention_latent(q, q_rope, pool, c_tree, r_tree, parent, node_offsets, host_node_offsets, block_table, block_table.shape[1],
+                                           pool.shape[0], prefix_lens, host_prefix_lens, B, Hq, R, Dr, scale, out, lse, ws, stream),
+           "hs_tree_attention_latent")
+    return out, lse
+
+
+def hs_prompt_attention_latent_workspace(host_q_offsets, host_kv_offsets, H: int, Dv: int, device, *, stream=None) -> Optional[torch.Tensor]:
+    """A workspace for hs_prompt_attention_latent calls of these offsets (CPU tensors) on `stream`; None where none is needed."""
+    if host_q_offsets.numel() != host_kv_offsets.numel():
+        raise ValueError("both offsets must hold B + 1 values")
+    qo, ko = host_q_offsets.to("cpu", torch.int32).contiguous(), host_kv_offsets.to("cpu", torch.int64).contiguous()
+    n = lib().hs_prompt_attention_latent_workspace(qo.data_ptr(), ko.data_ptr(), qo.numel() - 1, int(H), int(Dv))
+    return workspace(n, device, stream)
+
+
+def hs_prompt_attention_latent(q, q_rope, k, k_rope, v, q_offsets, kv_offsets, host_q_offsets, host_kv_offsets, scale: float, *, want_lse: bool = False,
+                               out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None, stream=None):
+    """Expanded latent attention of prompt rows, causal: q [N,H,Dn], q_rope [N,H,Dr], k [T,H,Dn], k_rope [T,Dr], v [T,H,Dv] (float32 or bfloat16, GPU;
+    strides of their own, e.g. k and v slices of one product's result), q_offsets int32 [B+1] and kv_offsets int64 [B+1] on the GPU and the same on the
+    CPU.  Returns (o [N,H,Dv], lse [N,H] or None)."""
+    if q.dim() != 3 or q_rope.dim() != 3 or k.dim() != 3 or k_rope.dim() != 2 or v.dim() != 3:
+        raise ValueError("q must be [N, H, Dn], q_rope [N, H, Dr], k [T, H, Dn], k_rope [T, Dr], v [T, H, Dv]")
+    N, H, Dn = q.shape
+    T, Dr, Dv = k.shape[0], q_rope.shape[2], v.shape[2]
+    B = host_q_offsets.numel() - 1
+    if tuple(q_rope.shape[:2]) != (N, H) or tuple(k.shape[1:]) != (H, Dn) or tuple(k_rope.shape) != (T, Dr) or tuple(v.shape[:2]) != (T, H):
+        raise ValueError("q must be [N, H, Dn], q_rope [N, H, Dr], k [T, H, Dn], k_rope [T, Dr], v [T, H, Dv]")
+    if q_offsets.numel() != B + 1 or kv_offsets.numel() != B + 1 or host_kv_offsets.numel() != B + 1 or int(host_q_offsets[B]) != N or \
+            int(host_kv_offsets[B]) != T:
+        raise ValueError("the offsets must hold B + 1 values, the last ones N and T")
+    if out is None:
+        out = _empty((N, H, Dv), q.dtype, q.device, stream)
+    if want_lse and lse is None:
+        lse = _empty((N, H), torch.float32, q.device, stream)
+    if tuple(out.shape) != (N, H, Dv) or (lse is not None and lse.numel() != N * H):
+        raise ValueError("out must be [N, H, Dv], lse [N, H]")
+    if ws is None:
+        ws = hs_prompt_attention_latent_workspace(host_q_offsets, host_kv_offsets, H, Dv, q.device, stream=stream)
+    _check(_calls.hs_prompt_attention_latent(q, q_rope, k, k_rope, v, q_offsets, kv_offsets, host_q_offsets, host_kv_offsets, B, H, Dn, Dr, Dv, scale, out,
+                                             lse, ws, stream), "hs_prompt_attention_latent")
     return out, lse
 
 

@@ -1,0 +1,50 @@
+// Attention over latents (internal): what the two calls hand to their kernels.
+//
+// Absorbed form: every query head of a tree row scores the same keys, a token's latent c [R] and rotary part r [Dr], and the values
+// are the latents themselves.  Expanded form: every head has keys [Dn] and values [Dv] of its own, the rotary part is shared.
+#pragma once
+#include "attn_common.h"
+
+namespace hs {
+
+struct LatRows {  // [rows, heads, n] with strides of its own, in elements
+  const void* p;
+  int64_t row, head;
+};
+
+struct LatTreeArgs {
+  LatRows q, q_rope;
+  const void* pool;  // [n_pages, 64, R + Dr]
+  const void* c_tree;
+  const void* r_tree;
+  int64_t c_stride, r_stride;
+  const int32_t* parent;
+  const int32_t* node_offsets;
+  const int32_t* table;
+  int max_blocks, n_pages;
+  const int64_t* prefix_lens;
+  int B, NN, Hq, R, Dr;
+  float scale;
+  void* o;
+  int64_t o_row, o_head;
+  float* lse;
+};
+
+struct LatPromptArgs {
+  LatRows q, q_rope, k, v;
+  const void* k_rope;
+  int64_t k_rope_row;
+  const int32_t* q_offsets;
+  const int64_t* kv_offsets;
+  int B, N, H, Dn, Dr, Dv;
+  float scale;
+  void* o;
+  int64_t o_row, o_head;
+  float* lse;
+};
+
+// latent_attn_any.hip: any shape and type, float32 arithmetic throughout.
+hs_status lat_tree_any(const LatTreeArgs& a, hs_dtype dt, hipStream_t stream);
+hs_status lat_prompt_any(const LatPromptArgs& a, hs_dtype dt, hipStream_t stream);
+
+}  // namespace hs

@@ -30,6 +30,8 @@ namespace {
 //   t         float32 or bfloat16, all of a call of one type; D: that type's code (takes no argument)
 //   r         like t, but [rows, heads, D] with a row stride of its own, which follows as the next parameter (code R, takes no argument);
 //             O: may be None
+//   q         like t, but [rows, heads, n] with strides of its own, which follow as the next two parameters (codes R and G, take no argument)
+//   p         like t, but [rows, n] with a row stride of its own, which follows as the next parameter (code R)
 //   x         float64; c: the elements of a quantised cache (float8_e4m3fn or uint8), L: int64 that may be None
 //   o         an address only, not looked at any further (may be None)
 //   h H       on the host, int32 or int64, whatever its layout (converted where needed)
@@ -38,7 +40,7 @@ namespace {
 struct Entry {
   const char* name;
   const char* codes;
-  const char* names;  // of the arguments that are checked (codes i l f u I F t r O x c L), in order
+  const char* names;  // of the arguments that are checked (codes i l f u I F t r O q p x c L), in order
   PyObject* (*call)(const Entry&, void*, PyObject* const*, Py_ssize_t);
   bool one_device;    // every checked tensor has to be on the current device (whose stream the call takes by default)
 };
@@ -67,7 +69,7 @@ struct Call {
   bool typed = false;
   at::ScalarType type = at::kFloat;
   size_t ws_bytes = 0;
-  int64_t row_stride = 0;
+  int64_t row_stride = 0, head_stride = 0;
   int device = -1;
   std::vector<at::Tensor> keep;             // converted host arrays, until the call has returned
   std::vector<std::vector<float>> floats;
@@ -102,7 +104,7 @@ struct Call {
     PyErr_Format(PyExc_ValueError, "%s is on another device than the current one (%d)", next_name().c_str(), device);
     throw Failed{};
   }
-  // one type for all tensors of codes t, r, O
+  // one type for all tensors of codes t, r, O, q, p
   void of_type(PyObject* o) {
     if (!typed) {
       type = tensor(o).scalar_type();
@@ -130,6 +132,22 @@ struct Call {
     on_device(t);
     next_name();
     row_stride = t.size(0) > 1 ? t.stride(0) : t.size(1) * t.size(2);
+    return t.data_ptr();
+  }
+  void* loose(int dims) {
+    PyObject* o = next();
+    of_type(o);
+    const at::Tensor& t = tensor(o);
+    if (!t.is_cuda() || t.scalar_type() != type || t.dim() != dims || (t.size(dims - 1) > 1 && t.stride(dims - 1) != 1)) {
+      PyErr_Format(PyExc_ValueError, "%s must be a %s tensor %s on the GPU with unit stride along the last dimension", next_name().c_str(), type_name(type),
+                   dims == 3 ? "[rows, heads, n]" : "[rows, n]");
+      throw Failed{};
+    }
+    on_device(t);
+    next_name();
+    const int64_t n = t.size(dims - 1), heads = dims == 3 ? t.size(1) : 1;
+    head_stride = dims == 3 && heads > 1 ? t.stride(1) : n;
+    row_stride = t.size(0) > 1 ? t.stride(0) : heads * n;
     return t.data_ptr();
   }
   void* elements() {
@@ -194,6 +212,8 @@ struct Call {
       }
       case 'r': return strided(false);
       case 'O': return strided(true);
+      case 'q': return loose(3);
+      case 'p': return loose(2);
       case 'x': return checked(at::kDouble, false);
       case 'c': return elements();
       case 'L': return checked(at::kLong, true);
@@ -239,6 +259,7 @@ struct Call {
     } else {
       if (code == 'W') return static_cast<P>(ws_bytes);
       if (code == 'R') return static_cast<P>(row_stride);
+      if (code == 'G') return static_cast<P>(head_stride);
       if (code == 'D') return static_cast<P>(type == at::kBFloat16 ? HS_BF16 : HS_F32);
       const long long v = PyLong_AsLongLong(next());
       if (v == -1 && PyErr_Occurred()) throw Failed{};
@@ -327,6 +348,13 @@ const Entry TABLE[] = {
     HS_ENTRY_ON(hs_kv_read_mx, "cucun" "innLlnttnnnDs", HS_MX_CACHE " block_table first out_offsets k_out v_out", true),
     HS_ENTRY_ON(hs_tree_attention_mx, "rRcucunrRrR" "iihinnlH" "nnnnDd" "tFwWs",
                 "q " HS_MX_CACHE " k_tree v_tree parent node_offsets block_table prefix_lens out lse", true),
+    HS_ENTRY_ON(hs_block_tables, "lniniiiniiIns", "want block_table held new_held free_pages free_count new_free_count refused", true),
+    HS_ENTRY_ON(hs_slot_map, "inIIninnnIllLns", "node_offsets accept_path accept_len block_table held cache_lens slots new_lens", true),
+    HS_ENTRY_ON(hs_latent_store, "pRpRlntnnnDs", "c r slots pool", true),
+    HS_ENTRY_ON(hs_latent_read, "tnlnpRpRnnDs", "pool slots c r", true),
+    HS_ENTRY_ON(hs_tree_attention_latent, "qRGqRG" "tpRpR" "iihinnlH" "nnnnDd" "qRGFwWs",
+                "q q_rope pool c_tree r_tree parent node_offsets block_table prefix_lens out lse", true),
+    HS_ENTRY_ON(hs_prompt_attention_latent, "qRGqRG" "qRGpRqRG" "ilhH" "nnnnnDd" "qRGFwWs", "q q_rope k k_rope v q_offsets kv_offsets out lse", true),
 };
 
 // A bound function: self is a tuple (capsule of the entry, capsule of the address).

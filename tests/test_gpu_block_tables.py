@@ -1,0 +1,189 @@
+"""GPU parity of block tables and slots with the checker, number by number, and what a call leaves as it was."""
+import numpy as np
+import pytest
+
+from oracle import page_tables as pt
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+DEV = "cuda:0"
+
+
+@pytest.fixture(scope="module")
+def hs():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    import paper_2505_13254_amd as h
+    return h
+
+
+def dev(a, kind=None):
+    t = torch.from_numpy(np.ascontiguousarray(a))
+    return (t if kind is None else t.to(kind)).to(DEV)
+
+
+class Tables:
+    """Tables on the GPU and the checker's copy of them."""
+
+    def __init__(self, rs, B, max_blocks, spare, page_tokens=64, full=0.5):
+        self.page_tokens, self.B = page_tokens, B
+        self.held = rs.randint(0, int(max_blocks * full) + 1, B).astype(np.int32) if B else np.zeros(0, np.int32)
+        self.n_pages = int(self.held.sum()) + spare
+        ids = rs.permutation(self.n_pages).astype(np.int32)
+        self.table = np.full((B, max_blocks), -7, np.int32)
+        at = 0
+        for s in range(B):
+            self.table[s, :self.held[s]] = ids[at:at + self.held[s]]
+            at += self.held[s]
+        self.stack = ids[at:].tolist()
+        free = np.full(self.n_pages, -9, np.int32)
+        free[:len(self.stack)] = self.stack
+        i32 = torch.int32
+        self.gpu = dict(table=dev(self.table), held=dev(self.held), free=dev(free), count=torch.tensor([len(self.stack)], dtype=i32, device=DEV))
+        self.free_host = free
+
+    def step(self, hs, want, new_held=None, new_count=None):
+        g = self.gpu
+        refused = torch.full((self.B,), -5, dtype=torch.int32, device=DEV)
+        held, count = hs.hs_block_tables(dev(want, torch.int64), g["table"], g["held"], g["free"], g["count"], page_tokens=self.page_tokens, new_held=new_held,
+                                         new_free_count=new_count, refused=refused)
+        before, stack_before = self.held.copy(), len(self.stack)
+        self.table, held_ref, self.stack, refused_ref = pt.block_tables(want, self.page_tokens, self.table, self.held, self.stack)
+        self.free_host[stack_before:len(self.stack)] = self.stack[stack_before:]
+        torch.cuda.synchronize()
+        assert np.array_equal(held.cpu().numpy(), held_ref)
+        assert int(count) == len(self.stack)
+        assert np.array_equal(refused.cpu().numpy(), refused_ref)
+        assert np.array_equal(g["table"].cpu().numpy(), self.table)
+        assert np.array_equal(g["free"].cpu().numpy(), self.free_host)    # behind the count it is left as it was
+        assert np.array_equal(g["held"].cpu().numpy(), before)
+        self.held = np.array(held_ref, np.int32)
+        g["held"], g["count"] = held, count
+        every = self.stack + [int(p) for s in range(self.B) for p in self.table[s, :self.held[s]]]
+        assert sorted(every) == list(range(self.n_pages))
+
+
+@pytest.mark.parametrize("B,max_blocks,spare,page_tokens", [(1, 4, 3, 64), (1, 9000, 4000, 64), (3, 1, 1, 1), (16, 26, 60, 64), (64, 40, 5, 16), (1023, 5, 100, 64),
+                                                            (1024, 3, 900, 64), (1025, 3, 2000, 64), (5000, 4, 300, 3), (2048, 130, 9000, 64)])
+def test_block_tables(hs, B, max_blocks, spare, page_tokens):
+    """Steps in which sequences grow, shrink, end and ask for too much, with the pages short now and then."""
+    rs = np.random.RandomState(B + max_blocks)
+    t = Tables(rs, B, max_blocks, spare, page_tokens)
+    most = max_blocks * page_tokens
+    for x in range(6):
+        now = t.held.astype(np.int64) * page_tokens
+        kind = rs.randint(0, 5, B) if x < 4 else np.full(B, 3 if x == 4 else 1)
+        want = np.where(kind == 0, now, np.where(kind == 1, now + rs.randint(1, 2 * page_tokens + 1, B), np.where(kind == 2, now - rs.randint(0, now + 1), 0)))
+        want = np.where(kind == 4, rs.randint(0, most + page_tokens, B), want)
+        if x == 2:
+            want[rs.randint(B)] = most + 1
+            want[rs.randint(B)] = -5
+            want[rs.randint(B)] = 2 ** 62
+        t.step(hs, want)
+
+
+def test_pages_that_come_back_are_taken_in_the_same_call(hs):
+    rs = np.random.RandomState(5)
+    t = Tables(rs, 40, 30, 0, full=1.0)
+    want = np.where(np.arange(40) % 3 == 0, 0, 30 * 64)
+    t.step(hs, want)
+    t.step(hs, want[::-1].copy())
+
+
+def test_counts_go_back_and_forth_and_a_captured_step_replays(hs):
+    """Two calls in a graph (rows are reserved, and given back), replayed with lengths that change in between."""
+    rs = np.random.RandomState(7)
+    t = Tables(rs, 12, 20, 50)
+    g = t.gpu
+    lens = dev(t.held.astype(np.int64) * 64)
+    grow = torch.empty_like(lens)
+    held2, count2 = torch.empty_like(g["held"]), torch.empty_like(g["count"])
+    refused = torch.empty(12, dtype=torch.int32, device=DEV)
+
+    def step():
+        hs.hs_block_tables(grow, g["table"], g["held"], g["free"], g["count"], new_held=held2, new_free_count=count2, refused=refused)
+        hs.hs_block_tables(lens, g["table"], held2, g["free"], count2, new_held=g["held"], new_free_count=g["count"])
+
+    grow.copy_(lens)
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for x in range(4):
+        more = rs.randint(0, 400, 12)
+        new = np.maximum(0, t.held.astype(np.int64) * 64 + rs.randint(-100, 100, 12))
+        grow.copy_(dev(t.held.astype(np.int64) * 64 + more))
+        lens.copy_(dev(new))
+        torch.cuda.synchronize()
+        before = len(t.stack)
+        t.table, t.held, t.stack, want_refused = pt.block_tables((t.held.astype(np.int64) * 64 + more), 64, t.table, t.held, t.stack)
+        t.table, t.held, t.stack, _ = pt.block_tables(new, 64, t.table, t.held, t.stack)
+        t.held = np.array(t.held, np.int32)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert np.array_equal(g["table"].cpu().numpy(), t.table) and np.array_equal(g["held"].cpu().numpy(), t.held)
+        assert int(g["count"]) == len(t.stack) and g["free"].cpu().numpy()[:len(t.stack)].tolist() == t.stack
+        assert np.array_equal(refused.cpu().numpy(), want_refused), before
+
+
+def test_refused_calls(hs):
+    t = hs.new_page_tables(3, 4, 9)
+    want = torch.zeros(3, dtype=torch.int64, device=DEV)
+    args = (t["block_table"], t["held"], t["free_pages"], t["free_count"])
+    with pytest.raises(hs.HsError):
+        hs.hs_block_tables(want, *args, new_held=t["held"])
+    with pytest.raises(ValueError):
+        hs.hs_block_tables(want.int(), *args)
+    with pytest.raises(ValueError):
+        hs.hs_block_tables(want.cpu(), *args)
+    with pytest.raises(ValueError):
+        hs.hs_block_tables(want[:2], *args)
+    with pytest.raises(ValueError):
+        hs.hs_block_tables(want, t["block_table"].t(), *args[1:])
+    with pytest.raises(ValueError):
+        hs.hs_slot_map(torch.zeros(4, dtype=torch.int32, device=DEV), 0, want, t["block_table"], 9, accept_len=t["held"])
+    with pytest.raises(HsOr(hs)):
+        hs.hs_slot_map(torch.zeros(4, dtype=torch.int32, device=DEV), 0, want, t["block_table"], 9, new_lens=want)
+    new_held, count = hs.hs_block_tables(want + 65, *args)
+    assert new_held.tolist() == [2, 2, 2] and int(count) == 3 and t["block_table"][:, :2].tolist() == [[0, 1], [2, 3], [4, 5]]
+
+
+def HsOr(hs):
+    return (ValueError, hs.HsError)
+
+
+@pytest.mark.parametrize("sizes,lens,page_tokens", [([1], [0], 64), ([5, 0, 70, 1], [60, 5, 0, 127], 64), ([9000], [13], 64), ([1] * 5000, list(range(5000)), 16),
+                                                    ([0, 0], [7, 9], 64), ([200, 3], [2 ** 33, 5], 2 ** 30), ([17] * 300, [3] * 300, 1)])
+@pytest.mark.parametrize("with_held", [False, True])
+def test_slots(hs, sizes, lens, page_tokens, with_held):
+    rs = np.random.RandomState(len(sizes))
+    B, NN = len(sizes), sum(sizes) + 3
+    off = np.concatenate([[0], np.cumsum(sizes)]).astype(np.int32)
+    blocks = max(1, max(-(-(l + n) // page_tokens) for l, n in zip(lens, sizes)))
+    pages = B * blocks + 4
+    table = rs.randint(-1, pages + 1, (B, blocks)).astype(np.int32)      # some entries are no pages
+    held = rs.randint(-1, blocks + 2, B).astype(np.int32) if with_held else None
+    new = torch.full((B,), -5, dtype=torch.int64, device=DEV)
+    got = hs.hs_slot_map(dev(off), NN, dev(np.array(lens, np.int64)), dev(table), pages, page_tokens=page_tokens, held=None if held is None else dev(held), new_lens=new)
+    slots, want = pt.slot_map(off, NN, lens, table, page_tokens, pages, held)
+    assert np.array_equal(got.cpu().numpy(), slots) and np.array_equal(new.cpu().numpy(), want)
+
+
+@pytest.mark.parametrize("B,n,depth", [(1, 61, 10), (16, 129, 12), (3, 1, 1), (100, 30, 7), (2, 1024, 400)])
+def test_slots_of_accepted_paths(hs, B, n, depth):
+    rs = np.random.RandomState(B + n)
+    sizes = rs.randint(0, n + 1, B)
+    sizes[-1] = n
+    off = np.concatenate([[0], np.cumsum(sizes)]).astype(np.int32)
+    path, length = np.full((B, depth), -1, np.int32), np.zeros(B, np.int32)
+    for s in range(B):
+        rows = np.sort(rs.permutation(np.arange(1, max(2, sizes[s])))[:rs.randint(0, depth + 1)]) if sizes[s] > 1 else np.zeros(0, int)
+        path[s, :len(rows)], length[s] = rows, len(rows)
+    lens = rs.randint(0, 200, B).astype(np.int64)
+    table = rs.permutation(B * 8).reshape(B, 8).astype(np.int32)
+    held = rs.randint(2, 6, B).astype(np.int32)
+    new = torch.empty(B, dtype=torch.int64, device=DEV)
+    got = hs.hs_slot_map(dev(off), int(off[-1]), dev(lens), dev(table), B * 8, held=dev(held), accept_path=dev(path), accept_len=dev(length), new_lens=new)
+    slots, want = pt.slot_map(off, int(off[-1]), lens, table, 64, B * 8, held, path, length)
+    assert np.array_equal(got.cpu().numpy(), slots) and np.array_equal(new.cpu().numpy(), want)
