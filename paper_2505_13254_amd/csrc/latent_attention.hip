@@ -38,7 +38,10 @@ using namespace hs;
 
 extern "C" size_t hs_tree_attention_latent_workspace(const int32_t* host_node_offsets, const int64_t* host_prefix_lens, int32_t B, int32_t Hq, int32_t R,
                                                      int32_t Dr) {
-  return 0;
+  clear_error();
+  if (B < 1 || Hq < 1 || host_node_offsets == nullptr || host_prefix_lens == nullptr || R != 512 || Dr != 64) return 0;
+  if (lat_tree_hosts(host_node_offsets, host_prefix_lens, B, 0x7fffffff) != HS_OK || (int64_t)host_node_offsets[B] * Hq >= LAT_MAX_ROWS) return 0;
+  return lat_tree_bytes(lat_tree_plan(host_node_offsets, host_prefix_lens, B, Hq), (int64_t)host_node_offsets[B] * Hq);
 }
 
 extern "C" hs_status hs_tree_attention_latent(const void* q, int64_t q_stride, int64_t q_head_stride, const void* q_rope, int64_t q_rope_stride,
@@ -71,7 +74,12 @@ extern "C" hs_status hs_tree_attention_latent(const void* q, int64_t q_stride, i
              (long long)o_stride, (long long)o_head_stride);
   LatTreeArgs a = {{q, q_stride, q_head_stride}, {q_rope, q_rope_stride, q_rope_head_stride}, pool, c_tree, r_tree, c_stride, r_stride, parent, node_offsets,
                    block_table, max_blocks, n_pages, prefix_lens, B, NN, Hq, R, Dr, scale, o, o_stride, o_head_stride, lse};
-  return lat_tree_any(a, dt, static_cast<hipStream_t>(stream));
+  if (!lat_tree_matrix(a, dt)) return lat_tree_any(a, dt, static_cast<hipStream_t>(stream));
+  const LatPlan p = lat_tree_plan(host_node_offsets, host_prefix_lens, B, Hq);
+  const size_t need = lat_tree_bytes(p, (int64_t)NN * Hq);
+  HS_REQUIRE(need == 0 || (workspace != nullptr && workspace_bytes >= need && reinterpret_cast<uintptr_t>(workspace) % 256 == 0), HS_ERR_WORKSPACE,
+             "hs_tree_attention_latent: needs %zu bytes of workspace, got %zu", need, workspace_bytes);
+  return lat_tree_launch(a, p, workspace, static_cast<hipStream_t>(stream));
 }
 
 extern "C" size_t hs_prompt_attention_latent_workspace(const int32_t* host_q_offsets, const int64_t* host_kv_offsets, int32_t B, int32_t H, int32_t Dv) { return 0; }

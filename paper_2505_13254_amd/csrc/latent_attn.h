@@ -43,6 +43,17 @@ struct LatPromptArgs {
   float* lse;
 };
 
+// latent_attn_tree.hip: bfloat16, R = 512, Dr = 64, everything aligned to 16 bytes, on the matrix cores.
+struct LatPlan {
+  int per;       // pages of a split at most
+  int sp_max;    // splits of a sequence at most
+  int64_t grid;  // workgroups
+};
+bool lat_tree_matrix(const LatTreeArgs& a, hs_dtype dt);
+LatPlan lat_tree_plan(const int32_t* host_node_offsets, const int64_t* host_prefix_lens, int32_t B, int32_t Hq);
+size_t lat_tree_bytes(const LatPlan& p, int64_t rows);
+hs_status lat_tree_launch(const LatTreeArgs& a, const LatPlan& p, void* workspace, hipStream_t stream);
+
 // latent_attn_any.hip: any shape and type, float32 arithmetic throughout.
 hs_status lat_tree_any(const LatTreeArgs& a, hs_dtype dt, hipStream_t stream);
 hs_status lat_prompt_any(const LatPromptArgs& a, hs_dtype dt, hipStream_t stream);

@@ -1,0 +1,504 @@
+// Absorbed attention over latents on the matrix cores (see latent_attn_tree.h).
+//
+// A work item is a group of up to 128 rows of one sequence and one split of its pages; the last split also takes the tree's own rows. The
+// host chooses how many pages a split has at most (lt_plan); everything else of an item is found on the device, from the offsets and
+// lengths.  The groups of a (sequence, split) go to one XCD, side by side, so that they find its pages in that XCD's L2.
+// Splits hand over sums (records of R + 4 floats: O, reference, denominator), which a second launch merges.
+#include <algorithm>
+
+#include "latent_attn_tree.h"
+
+namespace hs {
+
+constexpr int LT_XCD = 8;
+constexpr int LT_REC = LT_R + ATTN_REC_PAD;
+constexpr int LT_OUT_PITCH = 1024 + 16;  // bytes of a row on its way out
+
+struct LtArgs {
+  LatTreeArgs a;
+  float c2;    // scale in octaves
+  int per;     // pages of a split at most
+  int sp_max;  // splits of a sequence at most; 1: results are written directly
+  float* part;
+};
+
+__host__ __device__ __forceinline__ int lt_splits(int64_t pages, int per) { return pages <= per ? 1 : (int)((pages + per - 1) / per); }
+
+struct LtItem {
+  int s, n0, M, sp, n_sp, rg;
+  int64_t L;
+};
+
+struct LtLds {
+  char ring[4 * LT_TILE];
+  int parent[LT_MAX_TREE];
+  float stat[4][2][32];
+  unsigned odd[2];
+  int again;  // some row's reference was too low
+  int found[8];
+  int sums[4][2];
+};
+static_assert(sizeof(LtLds) <= 160 * 1024, "LDS of a compute unit");
+
+// Two prefix sums over the workgroup (inclusive), and the totals.
+__device__ __forceinline__ int lt_scan(int& x, int which, LtLds& mem) {
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  x = wave_prefix_sum(x);
+  if (lane == 63) mem.sums[wave][which] = x;
+  __syncthreads();
+  int before = 0, all = 0;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    const int v = mem.sums[w][which];
+    before += w < wave ? v : 0;
+    all += v;
+  }
+  x += before;
+  return all;
+}
+
+// The item of a workgroup: number j of XCD x.  Bundles, a (sequence, split) each, are numbered through and dealt to the XCDs in turn.
+__device__ __forceinline__ bool lt_find(const LtArgs& g, LtItem& it, LtLds& mem) {
+  const LatTreeArgs& a = g.a;
+  const int x = (int)(blockIdx.x & (LT_XCD - 1)), j = (int)(blockIdx.x / LT_XCD), tid = threadIdx.x;
+  if (tid == 0) mem.found[0] = -1;
+  int bundles = 0, items = 0;
+  for (int base = 0; base < a.B; base += LT_THREADS) {
+    const int s = base + tid;
+    int n0 = 0, M = 0, n_sp = 0, groups = 0;
+    int64_t L = 0;
+    if (s < a.B) {
+      n0 = a.node_offsets[s];
+      M = a.node_offsets[s + 1] - n0;
+      L = a.prefix_lens[s];
+      const int64_t most = (int64_t)a.max_blocks * 64;
+      L = L < 0 ? 0 : (L > most ? most : L);
+      M = M < 0 || n0 < 0 ? 0 : std::min(std::min(M, LT_MAX_TREE), a.NN - n0);  // (the host's copies say so)
+      M = M < 0 ? 0 : M;
+      n_sp = M > 0 ? std::min(lt_splits((L + 63) >> 6, g.per), g.sp_max) : 0;
+      groups = (M * a.Hq + LT_GROUP - 1) / LT_GROUP;
+    }
+    int upto = n_sp;
+    const int more = lt_scan(upto, 0, mem);
+    const int first = bundles + upto - n_sp;
+    bundles += more;
+    const int mine = ((first + n_sp - x + LT_XCD - 1) / LT_XCD - (first - x + LT_XCD - 1) / LT_XCD) * groups;
+    int to = mine;
+    const int all = lt_scan(to, 1, mem);
+    const int at = j - (items + to - mine);
+    items += all;
+    if (at >= 0 && at < mine) {
+      const int q = at / groups;
+      mem.found[0] = s;
+      mem.found[1] = n0;
+      mem.found[2] = M;
+      mem.found[3] = (x - first & (LT_XCD - 1)) + LT_XCD * q;
+      mem.found[4] = n_sp;
+      mem.found[5] = at - q * groups;
+      mem.found[6] = (int)L;
+    }
+    if (j < items) break;
+    __syncthreads();
+  }
+  __syncthreads();
+  auto get = [&](int k) { return __builtin_amdgcn_readfirstlane(mem.found[k]); };
+  it.s = get(0);
+  if (it.s < 0) return false;
+  it.n0 = get(1);
+  it.M = get(2);
+  it.sp = get(3);
+  it.n_sp = get(4);
+  it.rg = get(5);
+  it.L = get(6);
+  return true;
+}
+
+template <int RB>
+__device__ __forceinline__ void lt_run(const LtArgs& g, const LtItem& it, LtLds& mem) {
+  constexpr int NB = RB == 1 ? 8 : 16;
+  const LatTreeArgs& a = g.a;
+  char* const lds = mem.ring;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int col = lane & 31, half = lane >> 5;
+  const int rb = RB == 4 ? wave : RB == 2 ? wave & 1 : 0, kh = RB == 4 ? 0 : wave >> 1, first_block = RB == 1 ? 8 * (wave & 1) : 0;
+  const int rows = it.M * a.Hq, row_base = it.rg * LT_GROUP + 32 * rb;
+  const int row = row_base + col < rows ? row_base + col : rows - 1;  // (rows behind the last repeat it)
+  const int i = row / a.Hq, h = row - i * a.Hq;
+  const bool last = it.sp == it.n_sp - 1;
+  const int pages = (int)((it.L + 63) >> 6), full = (int)(it.L >> 6);
+  const int p_lo = (int)((int64_t)it.sp * pages / it.n_sp), p_hi = (int)((int64_t)(it.sp + 1) * pages / it.n_sp);
+  const int n_pages = std::min(p_hi, full) - p_lo;  // full pages of the split
+  const int rest = p_hi > full ? (int)(it.L & 63) : 0;
+  const int32_t* const table = a.table + (int64_t)it.s * a.max_blocks;
+  const char* const pool = static_cast<const char*>(a.pool);
+
+  // pages, 64 of them at a time in the lanes
+  int page_base = 0, page_of = 0;
+  auto look_up = [&](int t) {  // from the split's page t on
+    const int at = p_lo + t + lane;
+    const int p = at < p_hi ? table[at] : 0;
+    page_of = p < 0 || p >= a.n_pages ? 0 : p;  // (an entry that is no page would be a caller's error)
+    page_base = t;
+  };
+  auto page_at = [&](int t) { return pool + (int64_t)__builtin_amdgcn_readlane(page_of, t - page_base) * LT_PAGE; };
+  const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
+  const unsigned off = 16 * ((lane & ~7) + ((lane & 7) ^ lt_key((lane >> 3) + 8 * (wave & 1))));
+  auto fetch = [&](int t, int b, int slot) { lt_fetch(page_at(t) + b * LT_TILE + wave * 1024, off, lds0 + slot * LT_TILE + wave * 1024); };
+
+  if (p_hi > p_lo) look_up(0);
+  auto first_page = [&]() {  // into the ring's second half
+    if (n_pages > 0) {
+      fetch(0, 0, 2);
+      fetch(0, 1, 3);
+    }
+  };
+  first_page();
+  LtState<NB> st;
+  st.start(lane, first_block);
+  {
+    const bf16_t* const q = static_cast<const bf16_t*>(a.q.p) + (it.n0 + i) * a.q.row + h * a.q.head + 8 * half;
+    const bf16_t* const r = static_cast<const bf16_t*>(a.q_rope.p) + (it.n0 + i) * a.q_rope.row + h * a.q_rope.head + 8 * half;
+#pragma unroll
+    for (int x = 0; x < LT_NK; ++x) st.q[x] = *reinterpret_cast<const lt_bf16x8*>(x < LT_R / 16 ? q + 16 * x : r + 16 * (x - LT_R / 16));
+  }
+  const float c2 = g.c2;
+  float reference = LT_FLOOR;
+#pragma unroll 1
+  for (;;) {
+  st.clear(reference);
+
+  // ---- the tree's own rows, from the last 64 that a row of the group sees down to the first
+  if (last) {
+    for (int x = tid; x < it.M; x += LT_THREADS) mem.parent[x] = a.parent[it.n0 + x];
+    const int row_end = std::min(rows, (it.rg + 1) * LT_GROUP) - 1;
+    int cursor = i;  // the next row of the lane's root path
+    for (int t = row_end / a.Hq / 64; t >= 0; --t) {
+      lt_meet();  // (the buffer's last readers are done)
+      if (tid < 2) mem.odd[tid] = 0u;
+      lt_meet();
+      // rows with a NaN or an infinity are noted, and those elements left out: 0 x NaN must not reach rows that do not see them
+      const int left = std::min(64, it.M - 64 * t);
+#pragma unroll 6
+      for (int x = 0; x < LT_PAGE / 16 / LT_THREADS; ++x) {
+        const int id = x * LT_THREADS + tid, r = id / 72, c = id - 72 * r;
+        const int64_t from = it.n0 + 64 * t + (r < left ? r : left - 1);
+        uint4 w = *reinterpret_cast<const uint4*>(c < 64 ? static_cast<const bf16_t*>(a.c_tree) + from * a.c_stride + 8 * c
+                                                         : static_cast<const bf16_t*>(a.r_tree) + from * a.r_stride + 8 * (c - 64));
+        unsigned* const e = &w.x;
+        bool odd = false;
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+          if ((e[y] & 0x7f80u) == 0x7f80u) e[y] &= 0xffff0000u, odd = true;
+          if ((e[y] & 0x7f800000u) == 0x7f800000u) e[y] &= 0xffffu, odd = true;
+        }
+        if (odd) atomicOr(&mem.odd[r >> 5], 1u << (r & 31));
+        *reinterpret_cast<uint4*>(lds + lt_at(r, c)) = w;
+      }
+      lt_meet();
+#pragma unroll 1
+      for (int b = 1; b >= 0; --b) {
+        unsigned word = 0u;  // the rows of these 32 that the lane's row sees
+        const int base = 64 * t + 32 * b;
+        while (cursor >= base) {
+          word |= 1u << (cursor & 31);
+          const int up = mem.parent[cursor];
+          cursor = up < cursor ? up : -1;  // (a malformed tree cannot keep the walk from ending)
+        }
+        if (RB != 4 && b != kh) continue;
+        if (__ballot(word != 0u) == 0ull) continue;
+        const unsigned odd = mem.odd[b];
+        lt_floatx16 S = st.scores(lds, b * LT_TILE);
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+          const int k = 8 * (v >> 2) + 4 * half + (v & 3);
+          S[v] = (word >> k) & 1u ? ((odd >> k) & 1u ? __builtin_nanf("") : S[v]) : -HS_INF;
+        }
+        st.take(lds, b * LT_TILE, S, c2);
+      }
+    }
+  }
+  // ---- the page that ends inside
+  if (rest > 0) {
+    lt_meet();
+    const int p = __builtin_amdgcn_readfirstlane(table[p_hi - 1]);
+    const char* const from = pool + (int64_t)(p < 0 || p >= a.n_pages ? 0 : p) * LT_PAGE;
+#pragma unroll 6
+    for (int x = 0; x < LT_PAGE / 16 / LT_THREADS; ++x) {
+      const int id = x * LT_THREADS + tid, r = id / 72, c = id - 72 * r;
+      *reinterpret_cast<uint4*>(lds + lt_at(r, c)) = *reinterpret_cast<const uint4*>(from + (r < rest ? r : rest - 1) * LT_ROW + 16 * c);
+    }
+    lt_meet();
+#pragma unroll 1
+    for (int b = 0; b < 2; ++b) {
+      if (RB != 4 && b != kh) continue;
+      if (32 * b >= rest) continue;
+      lt_floatx16 S = st.scores(lds, b * LT_TILE);
+#pragma unroll
+      for (int v = 0; v < 16; ++v) S[v] = 32 * b + 8 * (v >> 2) + 4 * half + (v & 3) < rest ? S[v] : -HS_INF;
+      st.take(lds, b * LT_TILE, S, c2);
+    }
+  }
+  // ---- full pages
+  if (n_pages > 0) {
+    if (last || rest > 0) lt_meet();  // (the ring's first half is free)
+    if constexpr (RB == 4) {
+      // tile n: page n / 2, in slot (n + 2) % 4.  Three tiles are in the ring or on their way besides the one whose values are multiplied.
+      const int tiles = 2 * n_pages;
+      auto request = [&](int n) {
+        if (n < tiles) fetch(n >> 1, n & 1, (n + 2) & 3);
+      };
+      request(2);
+      if (tiles > 2) asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(2 * LT_LOADS) : "memory");
+      else asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(LT_LOADS) : "memory");
+      lt_floatx16 S = st.scores(lds, 2 * LT_TILE);
+      uint4 P0, P1;
+      for (int n = 0; n + 1 < tiles; ++n) {
+        if (n + 2 < tiles) asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(LT_LOADS) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+        if (((n + 3) >> 1) - page_base >= 64) look_up((n + 3) >> 1);
+        request(n + 3);
+        const lt_floatx16 N = st.ahead(lds, ((n + 3) & 3) * LT_TILE, S, c2, P0, P1);
+        st.product(lds, ((n + 2) & 3) * LT_TILE, P0, P1);
+        S = N;
+      }
+      st.take(lds, ((tiles + 1) & 3) * LT_TILE, S, c2);
+    } else {
+      // page n in ring half (n + 1) % 2; each wave has one 32-key half of it
+      auto request = [&](int n) {
+        if (n < n_pages) {
+          fetch(n, 0, 2 * ((n + 1) & 1));
+          fetch(n, 1, 2 * ((n + 1) & 1) + 1);
+        }
+      };
+      request(1);
+      for (int n = 0; n < n_pages; ++n) {
+        if (n + 1 < n_pages) asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(2 * LT_LOADS) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+        const unsigned tile = (2 * ((n + 1) & 1) + kh) * LT_TILE;
+        const lt_floatx16 S = st.scores(lds, tile);
+        st.take(lds, tile, S, c2);
+        if (n + 2 - page_base >= 64) look_up(n + 2);
+        lt_meet();  // every wave is done with the page
+        request(n + 2);
+      }
+    }
+  }
+
+  // ---- a row whose scores rose too far above its reference?
+  if (tid == 0) mem.again = 0;
+  lt_meet();
+  if (__ballot(st.seen > st.m + LT_RISE) != 0ull && lane == 0) mem.again = 1;
+  lt_meet();
+  if (mem.again == 0) break;
+  reference = st.seen;
+  if (p_hi > p_lo) look_up(0);
+  first_page();
+  }
+
+  // ---- out: the halves of the keys meet, then rows leave by way of LDS
+  lt_meet();
+  float total = lt_half_sum(st.l), top = st.m;
+  constexpr int KEEP = RB == 4 ? NB : NB / 2;  // blocks that the wave writes
+  int out_block = first_block;
+  if constexpr (RB != 4) {
+    const int other = wave ^ 2;
+    if (half == 0) {
+      mem.stat[wave][0][col] = top;
+      mem.stat[wave][1][col] = total;
+    }
+    lt_meet();
+    const float m2 = mem.stat[other][0][col], l2 = mem.stat[other][1][col];
+    top = fmaxf(st.m, m2);
+    const float mine = exp2_fast(st.m - top), theirs = exp2_fast(m2 - top);
+    total = total * mine + l2 * theirs;
+    float4* const to = reinterpret_cast<float4*>(lds) + wave * (KEEP * 4 * 64) + lane;
+    const float4* const from = reinterpret_cast<const float4*>(lds) + other * (KEEP * 4 * 64) + lane;
+#pragma unroll
+    for (int t = 0; t < KEEP; ++t)
+#pragma unroll
+      for (int b = 0; b < 4; ++b) {
+        const lt_floatx16 &lo = st.acc[t], &hi = st.acc[KEEP + t];
+        to[(t * 4 + b) * 64] = kh == 0 ? make_float4(hi[4 * b] * mine, hi[4 * b + 1] * mine, hi[4 * b + 2] * mine, hi[4 * b + 3] * mine)
+                                       : make_float4(lo[4 * b] * mine, lo[4 * b + 1] * mine, lo[4 * b + 2] * mine, lo[4 * b + 3] * mine);
+      }
+    lt_meet();
+#pragma unroll
+    for (int t = 0; t < KEEP; ++t)
+#pragma unroll
+      for (int b = 0; b < 4; ++b) {
+        const float4 f = from[(t * 4 + b) * 64];
+        const float add[4] = {f.x, f.y, f.z, f.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) st.acc[t][4 * b + e] = (kh == 0 ? st.acc[t][4 * b + e] : st.acc[KEEP + t][4 * b + e]) * mine + add[e];
+      }
+    out_block += kh * KEEP;
+    lt_meet();
+  }
+  const int mine_rows = std::min(32, rows - row_base);
+  if (mine_rows <= 0) return;
+  const bool writes_stat = half == 0 && col < mine_rows && out_block == 0;
+  char* const stage = lds + wave * 32 * LT_OUT_PITCH;
+  const int64_t row0 = (int64_t)it.n0 * a.Hq + row_base;  // (records: row, then split)
+  if (it.n_sp == 1) {
+    const float inv = 1.f / total;
+    if (writes_stat && a.lse != nullptr) a.lse[row0 + col] = (top + __log2f(total)) * LT_LN2;
+#pragma unroll
+    for (int t = 0; t < KEEP; ++t)
+#pragma unroll
+      for (int b = 0; b < 4; ++b) {
+        const lt_floatx2 x = {st.acc[t][4 * b] * inv, st.acc[t][4 * b + 1] * inv}, y = {st.acc[t][4 * b + 2] * inv, st.acc[t][4 * b + 3] * inv};
+        *reinterpret_cast<uint2*>(stage + col * LT_OUT_PITCH + 64 * t + 16 * b + 8 * half) =
+            make_uint2(__builtin_bit_cast(unsigned, __builtin_convertvector(x, lt_bf16x2)), __builtin_bit_cast(unsigned, __builtin_convertvector(y, lt_bf16x2)));
+      }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    constexpr int PER_ROW = KEEP * 4;  // 16-byte pieces
+#pragma unroll 4
+    for (int x = lane; x < mine_rows * PER_ROW; x += 64) {
+      const int r = x / PER_ROW, c = x % PER_ROW, ri = (row_base + r) / a.Hq, rh = row_base + r - ri * a.Hq;
+      *reinterpret_cast<uint4*>(static_cast<bf16_t*>(a.o) + (it.n0 + ri) * a.o_row + rh * a.o_head + 32 * out_block + 8 * c) =
+          *reinterpret_cast<const uint4*>(stage + r * LT_OUT_PITCH + 16 * c);
+    }
+  } else {
+    if (writes_stat) {
+      float* const rec = g.part + ((row0 + col) * g.sp_max + it.sp) * LT_REC;
+      rec[LT_R] = top;
+      rec[LT_R + 1] = total;
+    }
+    constexpr int PASS = KEEP < 8 ? KEEP : 8;  // blocks that a row on its way out has room for
+#pragma unroll
+    for (int x0 = 0; x0 < KEEP; x0 += PASS) {
+#pragma unroll
+      for (int t = 0; t < PASS; ++t)
+#pragma unroll
+        for (int b = 0; b < 4; ++b)
+          *reinterpret_cast<float4*>(stage + col * LT_OUT_PITCH + 128 * t + 32 * b + 16 * half) =
+              make_float4(st.acc[x0 + t][4 * b], st.acc[x0 + t][4 * b + 1], st.acc[x0 + t][4 * b + 2], st.acc[x0 + t][4 * b + 3]);
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      constexpr int PER_ROW = PASS * 8;
+#pragma unroll 4
+      for (int x = lane; x < mine_rows * PER_ROW; x += 64) {
+        const int r = x / PER_ROW, c = x % PER_ROW;
+        *reinterpret_cast<float4*>(g.part + ((row0 + r) * g.sp_max + it.sp) * LT_REC + 32 * (out_block + x0) + 4 * c) =
+            *reinterpret_cast<const float4*>(stage + r * LT_OUT_PITCH + 16 * c);
+      }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    }
+  }
+}
+
+__global__ __launch_bounds__(LT_THREADS, 1) void k_lat_tree(LtArgs g) {
+  __shared__ LtLds mem;
+  LtItem it;
+  if (!lt_find(g, it, mem)) return;
+  const int left = it.M * g.a.Hq - it.rg * LT_GROUP;
+  if (left > 64) lt_run<4>(g, it, mem);
+  else if (left > 32) lt_run<2>(g, it, mem);
+  else lt_run<1>(g, it, mem);
+}
+
+// The merge of the splits: a wave to a row.
+constexpr int LTM_THREADS = 256;
+__global__ __launch_bounds__(LTM_THREADS) void k_lat_tree_merge(LtArgs g) {
+  const LatTreeArgs& a = g.a;
+  const int lane = threadIdx.x & 63;
+  const int64_t row = (int64_t)blockIdx.x * (LTM_THREADS / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (row >= (int64_t)a.NN * a.Hq) return;
+  const int n = (int)(row / a.Hq), h = (int)(row - (int64_t)n * a.Hq);
+  int s = 0;
+  for (int base = 0; base < a.B; base += 64) {
+    const bool below = base + lane < a.B && a.node_offsets[base + lane] <= n;
+    const int c = __builtin_popcountll(__ballot(below));
+    s = base + c - 1;
+    if (c < 64) break;
+  }
+  s = s < 0 ? 0 : s;
+  int64_t L = a.prefix_lens[s];
+  const int64_t most = (int64_t)a.max_blocks * 64;
+  L = L < 0 ? 0 : (L > most ? most : L);
+  const int n_sp = std::min(lt_splits((L + 63) >> 6, g.per), g.sp_max);
+  if (n_sp == 1) return;
+  const float* const rec = g.part + row * g.sp_max * LT_REC;
+  float m = LT_FLOOR;
+  for (int x = lane; x < n_sp; x += 64) m = fmaxf(m, rec[(int64_t)x * LT_REC + LT_R]);
+  m = wave_max(m);
+  float total = 0.f;
+  float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int x = 0; x < n_sp; ++x) {
+    const float* const r = rec + (int64_t)x * LT_REC;
+    const float w = exp2_fast(r[LT_R] - m);
+    const float4 lo = *reinterpret_cast<const float4*>(r + 8 * lane), hi = *reinterpret_cast<const float4*>(r + 8 * lane + 4);
+    total = __builtin_fmaf(w, r[LT_R + 1], total);
+    acc[0] = __builtin_fmaf(w, lo.x, acc[0]), acc[1] = __builtin_fmaf(w, lo.y, acc[1]), acc[2] = __builtin_fmaf(w, lo.z, acc[2]), acc[3] = __builtin_fmaf(w, lo.w, acc[3]);
+    acc[4] = __builtin_fmaf(w, hi.x, acc[4]), acc[5] = __builtin_fmaf(w, hi.y, acc[5]), acc[6] = __builtin_fmaf(w, hi.z, acc[6]), acc[7] = __builtin_fmaf(w, hi.w, acc[7]);
+  }
+  const float inv = 1.f / total;
+  unsigned w[4];
+#pragma unroll
+  for (int x = 0; x < 4; ++x) w[x] = __builtin_bit_cast(unsigned, __builtin_convertvector((lt_floatx2{acc[2 * x] * inv, acc[2 * x + 1] * inv}), lt_bf16x2));
+  *reinterpret_cast<uint4*>(static_cast<bf16_t*>(a.o) + n * a.o_row + h * a.o_head + 8 * lane) = make_uint4(w[0], w[1], w[2], w[3]);
+  if (lane == 0 && a.lse != nullptr) a.lse[row] = (m + __log2f(total)) * LT_LN2;
+}
+
+// ------------------------------------------------------------------------------------------------ the host's part
+bool lat_tree_matrix(const LatTreeArgs& a, hs_dtype dt) {
+  auto fits = [](const void* p, int64_t s, int64_t t) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && s % 8 == 0 && t % 8 == 0; };
+  return dt == HS_BF16 && a.R == LT_R && a.Dr == LT_DR && fits(a.q.p, a.q.row, a.q.head) && fits(a.q_rope.p, a.q_rope.row, a.q_rope.head) &&
+         fits(a.pool, 0, 0) && fits(a.c_tree, a.c_stride, 0) && fits(a.r_tree, a.r_stride, 0) && fits(a.o, a.o_row, a.o_head);
+}
+
+// Pages of a split, by estimated times.
+LatPlan lat_tree_plan(const int32_t* no, const int64_t* pl, int32_t B, int32_t Hq) {
+  int64_t longest = 1;
+  for (int s = 0; s < B; ++s)
+    if (no[s + 1] > no[s]) longest = std::max(longest, (pl[s] + 63) >> 6);
+  constexpr double FIXED = 6.0, CU = 256.0, REC = 0.0012;  // us of an item without pages, compute units, us a row's record (all together)
+  LatPlan best = {0, 1, 0};
+  double best_us = 0.0;
+  for (int64_t k = 1; k <= longest; k = k < 4 ? k + 1 : k < 8 ? k + 2 : k + k / 4) {  // splits of the longest sequence
+    const int64_t per = (longest + k - 1) / k;
+    double sum = 0.0, most = 0.0, records = 0.0;
+    int64_t items = 0, sp_max = 1;
+    for (int s = 0; s < B; ++s) {
+      const int64_t rows = (int64_t)(no[s + 1] - no[s]) * Hq;
+      if (rows == 0) continue;
+      const int64_t pages = (pl[s] + 63) >> 6, n_sp = lt_splits(pages, (int)per), groups = (rows + LT_GROUP - 1) / LT_GROUP;
+      const double page = rows > 64 ? 3.0 : rows > 32 ? 1.6 : 1.3;
+      const double item = FIXED + page * (double)((pages + n_sp - 1) / n_sp);
+      sum += item * (double)(n_sp * groups);
+      most = std::max(most, item);
+      items += n_sp * groups;
+      sp_max = std::max(sp_max, n_sp);
+      if (n_sp > 1) records += (double)(rows * n_sp);
+    }
+    const double rounds = std::max(1.0, (double)items / CU);
+    double us = std::max(most, sum / CU + (rounds > 1.0 ? 0.5 * most : 0.0));
+    if (sp_max > 1) us += 4.0 + REC * records;
+    if (best.per == 0 || us < best_us) best_us = us, best.per = (int)per, best.sp_max = (int)sp_max;
+    if (items > 8 * CU) break;
+  }
+  int64_t bundles = 0, items[LT_XCD] = {0};
+  for (int s = 0; s < B; ++s) {
+    const int64_t rows = (int64_t)(no[s + 1] - no[s]) * Hq;
+    if (rows == 0) continue;
+    const int64_t n_sp = lt_splits((pl[s] + 63) >> 6, best.per), groups = (rows + LT_GROUP - 1) / LT_GROUP;
+    for (int x = 0; x < LT_XCD; ++x) items[x] += ((bundles + n_sp - x + LT_XCD - 1) / LT_XCD - (bundles - x + LT_XCD - 1) / LT_XCD) * groups;
+    bundles += n_sp;
+  }
+  best.grid = LT_XCD * *std::max_element(items, items + LT_XCD);
+  return best;
+}
+
+size_t lat_tree_bytes(const LatPlan& p, int64_t rows) { return p.sp_max > 1 ? align_up((size_t)rows * p.sp_max * LT_REC * 4, 256) : 0; }
+
+hs_status lat_tree_launch(const LatTreeArgs& a, const LatPlan& p, void* workspace, hipStream_t stream) {
+  LtArgs g = {a, a.scale * LT_LOG2E, p.per, p.sp_max, static_cast<float*>(workspace)};
+  hipLaunchKernelGGL(k_lat_tree, dim3((unsigned)p.grid), dim3(LT_THREADS), 0, stream, g);
+  const hs_status st = launch_status("latent attention");
+  if (st != HS_OK || p.sp_max == 1) return st;
+  const int64_t rows = (int64_t)a.NN * a.Hq;
+  hipLaunchKernelGGL(k_lat_tree_merge, dim3((unsigned)((rows + LTM_THREADS / 64 - 1) / (LTM_THREADS / 64))), dim3(LTM_THREADS), 0, stream, g);
+  return launch_status("latent attention, merge");
+}
+
+}  // namespace hs
