@@ -47,7 +47,8 @@ struct LatPromptArgs {
 struct LatPlan {
   int per;       // pages of a split at most
   int sp_max;    // splits of a sequence at most
-  int64_t grid;  // workgroups
+  int64_t first[9];  // the first item of each XCD, and the number of items
+  int64_t grid;      // workgroups
 };
 bool lat_tree_matrix(const LatTreeArgs& a, hs_dtype dt);
 LatPlan lat_tree_plan(const int32_t* host_node_offsets, const int64_t* host_prefix_lens, int32_t B, int32_t Hq);

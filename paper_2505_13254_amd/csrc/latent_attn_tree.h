@@ -79,14 +79,25 @@ __device__ __forceinline__ void lt_fetch(const char* from, unsigned off, unsigne
 }
 static_assert(LT_LOADS == 9, "lt_fetch");
 
+// Step i of a score chain, in ordinary registers.  (As builtins the chain's results go to the accumulation registers, of which O takes all 256: sixteen of O's
+// then live in memory, and a load from there waits for every tile on its way.)  Steps of one chain may follow each other at once; the last one waits until
+// anything may read the result (twelve wait states behind a matrix instruction of eight passes), in the same statement.  (The two wait states ahead: k or q may come straight from a
+// vector instruction.)
+__device__ __forceinline__ void lt_step(lt_floatx16& S, const lt_bf16x8& k, const lt_bf16x8& q, int i) {
+  if (i == 0) asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=&v"(S) : "v"(k), "v"(q));
+  else asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(S) : "v"(k), "v"(q));
+}
+__device__ __forceinline__ void lt_last(lt_floatx16& S, const lt_bf16x8& k, const lt_bf16x8& q) {
+  asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, %0\n\ts_nop 11" : "+v"(S) : "v"(k), "v"(q));
+}
 // 32 queries of a wave (col: the lane's), over NB blocks of 32 columns of the values from the wave's first one on.
 template <int NB>
 struct LtState {
   lt_bf16x8 q[LT_NK];  // element 16 i + 8 half + j of step i
   lt_floatx16 acc[NB]; // O^T: column 32 t + 8 (v / 4) + 4 half + v % 4
   float m, l, seen;    // reference of the scores (octaves), sum of the weights relative to it (of this half-wave's keys), largest score
-  unsigned k_at[9];    // the lane's place in group k of its K row of a tile
-  unsigned v_row, v_in;  // its V row's first group (the wave's first column on), and chunk and byte within a group
+  unsigned k_row, k_in;  // the first group of the lane's K row of a tile, and the byte of its chunk within a group
+  unsigned v_row, v_in;  // of its V rows (the wave's first column on)
 
   __device__ __forceinline__ void clear(float reference) {
     m = seen = reference;
@@ -98,19 +109,17 @@ struct LtState {
   }
   __device__ __forceinline__ void start(int lane, int first_block) {
     const unsigned half = lane >> 5, col = lane & 31;
-#pragma unroll
-    for (int k = 0; k < 9; ++k) k_at[k] = (9 * col + k) * 128 + 16 * (half ^ lt_key(9 * col + k));
+    k_row = 9 * col;
+    k_in = 16 * half;
     const unsigned a = lane & 3, j = (lane >> 2) & 3, dh = (lane >> 4) & 1, r0 = 4 * half + j;
     v_row = 9 * r0 + first_block / 2;
     v_in = 16 * (2 * dh + (a >> 1)) + 8 * (a & 1);
   }
-  // The lane's place in group u of its V rows (found again for every tile: there are no registers to keep them in).
-  __device__ __forceinline__ unsigned value_at(unsigned row, int u) const {
-    const unsigned G = row + u;
-    return (G << 7) + (v_in ^ (((__builtin_bitreverse32(G) >> 28) & 7u) << 4));
-  }
-  __device__ __forceinline__ lt_bf16x8 key(const char* lds, unsigned tile, int i) const {  // chunk 2 i + half of the lane's K row
-    return *reinterpret_cast<const lt_bf16x8*>(lds + ((k_at[i >> 2] ^ (32u * (i & 3))) + tile));
+  // The place of the lane's chunk in a group (found again for every tile: there are no registers to keep them in).
+  __device__ __forceinline__ static unsigned place(unsigned G, unsigned in) { return (G << 7) + (in ^ (((__builtin_bitreverse32(G) >> 28) & 7u) << 4)); }
+  // Chunk 2 i + half of the lane's K row; at: its place in group i / 4.
+  __device__ __forceinline__ static lt_bf16x8 key(const char* lds, unsigned tile, unsigned at, int i) {
+    return *reinterpret_cast<const lt_bf16x8*>(lds + ((at ^ (32u * (i & 3))) + tile));
   }
   // V^T of block t, keys 16 k2 .. of a tile.
   __device__ __forceinline__ lt_bf16x8 value(char* lds, unsigned tile, unsigned at, int t, int k2) const {
@@ -125,9 +134,25 @@ struct LtState {
     return f;
   }
   __device__ __forceinline__ lt_floatx16 scores(const char* lds, unsigned tile) const {
-    lt_floatx16 S = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    lt_floatx16 S;
+    unsigned row = k_row, at;
+    asm volatile("" : "+v"(row));
+    constexpr int AHEAD = 4;
+    lt_bf16x8 f[AHEAD];
+    at = place(row, k_in);
 #pragma unroll
-    for (int i = 0; i < LT_NK; ++i) S = __builtin_amdgcn_mfma_f32_32x32x16_bf16(key(lds, tile, i), q[i], S, 0, 0, 0);
+    for (int i = 0; i < AHEAD; ++i) f[i] = key(lds, tile, at, i);
+#pragma unroll
+    for (int i = 0; i < LT_NK; ++i) {
+      if (i + 1 < LT_NK) lt_step(S, f[i % AHEAD], q[i], i);
+      else lt_last(S, f[i % AHEAD], q[i]);
+      const int n = i + AHEAD;
+      if (n < LT_NK) {
+        if ((n & 3) == 0) at = place(row + (n >> 2), k_in);
+        f[i % AHEAD] = key(lds, tile, at, n);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
     return S;
   }
   // A row's reference is the largest score of the first tile in which it sees a key, and stays: a weight may be as large as 2^LT_RISE.  `seen` is the
@@ -162,7 +187,7 @@ struct LtState {
     unsigned row = v_row;
     asm volatile("" : "+v"(row));
     lt_bf16x8 f[4];
-    unsigned at = value_at(row, 0);
+    unsigned at = place(row, v_in);
 #pragma unroll
     for (int x = 0; x < 4; ++x) f[x] = value(lds, tile, at, x & 1, x >> 1);
 #pragma unroll
@@ -171,25 +196,32 @@ struct LtState {
       acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[x & 3], k2 == 0 ? b0 : b1, acc[t], 0, 0, 0);
       const int n = x + 4;
       if (n < 2 * NB) {
-        if ((n & 3) == 0) at = value_at(row, n >> 2);
+        if ((n & 3) == 0) at = place(row + (n >> 2), v_in);
         f[x & 3] = value(lds, tile, at, 2 * (n >> 2) + (n & 1), (n >> 1) & 1);
       }
       __builtin_amdgcn_sched_barrier(0);
     }
   }
   // The scores of tile `next` beside the softmax of S (tile by tile, RB = 4), whose weights become P0, P1.
-  __device__ __forceinline__ lt_floatx16 ahead(const char* lds, unsigned next, const lt_floatx16& S, float c2, uint4& P0, uint4& P1) {
-    constexpr int AHEAD = 5;
-    lt_floatx16 N = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  __device__ __forceinline__ void ahead(const char* lds, unsigned next, const lt_floatx16& S, lt_floatx16& N, float c2, uint4& P0, uint4& P1) {
+    constexpr int AHEAD = 4;
+    unsigned row = k_row, at;
+    asm volatile("" : "+v"(row));
+    at = place(row, k_in);
     lt_bf16x8 f[AHEAD];
 #pragma unroll
-    for (int i = 0; i < AHEAD; ++i) f[i] = key(lds, next, i);
+    for (int i = 0; i < AHEAD; ++i) f[i] = key(lds, next, at, i);
     float top = S[0];
     unsigned w[8];
 #pragma unroll
     for (int i = 0; i < LT_NK; ++i) {
-      N = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[i % AHEAD], q[i], N, 0, 0, 0);
-      if (i + AHEAD < LT_NK) f[i % AHEAD] = key(lds, next, i + AHEAD);
+      if (i + 1 < LT_NK) lt_step(N, f[i % AHEAD], q[i], i);
+      else lt_last(N, f[i % AHEAD], q[i]);
+      const int n = i + AHEAD;
+      if (n < LT_NK) {
+        if ((n & 3) == 0) at = place(row + (n >> 2), k_in);
+        f[i % AHEAD] = key(lds, next, at, n);
+      }
       if (i < 5) {
 #pragma unroll
         for (int v = 3 * i + 1; v < 3 * i + 4; ++v) top = fmaxf(top, S[v]);
@@ -200,7 +232,6 @@ struct LtState {
     }
     P0 = make_uint4(w[0], w[1], w[2], w[3]);
     P1 = make_uint4(w[4], w[5], w[6], w[7]);
-    return N;
   }
 };
 

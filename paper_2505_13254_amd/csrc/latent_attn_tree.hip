@@ -2,7 +2,7 @@
 //
 // A work item is a group of up to 128 rows of one sequence and one split of its pages; the last split also takes the tree's own rows. The
 // host chooses how many pages a split has at most (lt_plan); everything else of an item is found on the device, from the offsets and
-// lengths.  The groups of a (sequence, split) go to one XCD, side by side, so that they find its pages in that XCD's L2.
+// lengths.  Items are numbered by sequence, split and group, and each XCD has a run of neighbouring ones: the groups of a (sequence, split) find its pages in one L2.
 // Splits hand over sums (records of R + 4 floats: O, reference, denominator), which a second launch merges.
 #include <algorithm>
 
@@ -20,6 +20,7 @@ struct LtArgs {
   int per;     // pages of a split at most
   int sp_max;  // splits of a sequence at most; 1: results are written directly
   float* part;
+  int first[LT_XCD + 1];  // the first item of each XCD
 };
 
 __host__ __device__ __forceinline__ int lt_splits(int64_t pages, int per) { return pages <= per ? 1 : (int)((pages + per - 1) / per); }
@@ -36,20 +37,20 @@ struct LtLds {
   unsigned odd[2];
   int again;  // some row's reference was too low
   int found[8];
-  int sums[4][2];
+  int sums[4];
 };
 static_assert(sizeof(LtLds) <= 160 * 1024, "LDS of a compute unit");
 
-// Two prefix sums over the workgroup (inclusive), and the totals.
-__device__ __forceinline__ int lt_scan(int& x, int which, LtLds& mem) {
+// Inclusive prefix sums over the workgroup, and the total.
+__device__ __forceinline__ int lt_scan(int& x, LtLds& mem) {
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   x = wave_prefix_sum(x);
-  if (lane == 63) mem.sums[wave][which] = x;
+  if (lane == 63) mem.sums[wave] = x;
   __syncthreads();
   int before = 0, all = 0;
 #pragma unroll
   for (int w = 0; w < 4; ++w) {
-    const int v = mem.sums[w][which];
+    const int v = mem.sums[w];
     before += w < wave ? v : 0;
     all += v;
   }
@@ -57,13 +58,15 @@ __device__ __forceinline__ int lt_scan(int& x, int which, LtLds& mem) {
   return all;
 }
 
-// The item of a workgroup: number j of XCD x.  Bundles, a (sequence, split) each, are numbered through and dealt to the XCDs in turn.
+// The item of a workgroup: the j-th of XCD x's.
 __device__ __forceinline__ bool lt_find(const LtArgs& g, LtItem& it, LtLds& mem) {
   const LatTreeArgs& a = g.a;
   const int x = (int)(blockIdx.x & (LT_XCD - 1)), j = (int)(blockIdx.x / LT_XCD), tid = threadIdx.x;
+  const int item = g.first[x] + j;
+  if (item >= g.first[x + 1]) return false;
   if (tid == 0) mem.found[0] = -1;
-  int bundles = 0, items = 0;
-  for (int base = 0; base < a.B; base += LT_THREADS) {
+  int items = 0;
+  for (int base = 0; base < a.B && items <= item; base += LT_THREADS) {
     const int s = base + tid;
     int n0 = 0, M = 0, n_sp = 0, groups = 0;
     int64_t L = 0;
@@ -78,29 +81,23 @@ __device__ __forceinline__ bool lt_find(const LtArgs& g, LtItem& it, LtLds& mem)
       n_sp = M > 0 ? std::min(lt_splits((L + 63) >> 6, g.per), g.sp_max) : 0;
       groups = (M * a.Hq + LT_GROUP - 1) / LT_GROUP;
     }
-    int upto = n_sp;
-    const int more = lt_scan(upto, 0, mem);
-    const int first = bundles + upto - n_sp;
-    bundles += more;
-    const int mine = ((first + n_sp - x + LT_XCD - 1) / LT_XCD - (first - x + LT_XCD - 1) / LT_XCD) * groups;
+    const int mine = n_sp * groups;
     int to = mine;
-    const int all = lt_scan(to, 1, mem);
-    const int at = j - (items + to - mine);
+    const int all = lt_scan(to, mem);
+    const int at = item - (items + to - mine);
     items += all;
     if (at >= 0 && at < mine) {
-      const int q = at / groups;
+      const int sp = at / groups;
       mem.found[0] = s;
       mem.found[1] = n0;
       mem.found[2] = M;
-      mem.found[3] = (x - first & (LT_XCD - 1)) + LT_XCD * q;
+      mem.found[3] = sp;
       mem.found[4] = n_sp;
-      mem.found[5] = at - q * groups;
+      mem.found[5] = at - sp * groups;
       mem.found[6] = (int)L;
     }
-    if (j < items) break;
     __syncthreads();
   }
-  __syncthreads();
   auto get = [&](int k) { return __builtin_amdgcn_readfirstlane(mem.found[k]); };
   it.s = get(0);
   if (it.s < 0) return false;
@@ -250,18 +247,26 @@ __device__ __forceinline__ void lt_run(const LtArgs& g, const LtItem& it, LtLds&
       request(2);
       if (tiles > 2) asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(2 * LT_LOADS) : "memory");
       else asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(LT_LOADS) : "memory");
-      lt_floatx16 S = st.scores(lds, 2 * LT_TILE);
+      lt_floatx16 S = st.scores(lds, 2 * LT_TILE), N;
       uint4 P0, P1;
-      for (int n = 0; n + 1 < tiles; ++n) {
-        if (n + 2 < tiles) asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(LT_LOADS) : "memory");
-        else asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
-        if (((n + 3) >> 1) - page_base >= 64) look_up((n + 3) >> 1);
-        request(n + 3);
-        const lt_floatx16 N = st.ahead(lds, ((n + 3) & 3) * LT_TILE, S, c2, P0, P1);
-        st.product(lds, ((n + 2) & 3) * LT_TILE, P0, P1);
-        S = N;
+      unsigned here = 2 * LT_TILE;  // of the page's first tile
+      // (two tiles a trip: the scores of one and of the next change places without a copy)
+      for (int p = 0; p + 1 < n_pages; ++p) {
+        asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(LT_LOADS) : "memory");  // tile 2 p + 1 is there, 2 p + 2 on its way
+        request(2 * p + 3);
+        st.ahead(lds, here + LT_TILE, S, N, c2, P0, P1);
+        st.product(lds, here, P0, P1);
+        if (p + 2 - page_base >= 64) look_up(p + 2);
+        asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(LT_LOADS) : "memory");
+        request(2 * p + 4);
+        st.ahead(lds, 2 * LT_TILE - here, N, S, c2, P0, P1);
+        st.product(lds, here + LT_TILE, P0, P1);
+        here = 2 * LT_TILE - here;
       }
-      st.take(lds, ((tiles + 1) & 3) * LT_TILE, S, c2);
+      asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+      st.ahead(lds, here + LT_TILE, S, N, c2, P0, P1);
+      st.product(lds, here, P0, P1);
+      st.take(lds, here + LT_TILE, N, c2);
     } else {
       // page n in ring half (n + 1) % 2; each wave has one 32-key half of it
       auto request = [&](int n) {
@@ -453,7 +458,9 @@ LatPlan lat_tree_plan(const int32_t* no, const int64_t* pl, int32_t B, int32_t H
   for (int s = 0; s < B; ++s)
     if (no[s + 1] > no[s]) longest = std::max(longest, (pl[s] + 63) >> 6);
   constexpr double FIXED = 6.0, CU = 256.0, REC = 0.0012;  // us of an item without pages, compute units, us a row's record (all together)
-  LatPlan best = {0, 1, 0};
+  auto page_us = [](int64_t rows) { return rows > 64 ? 3.0 : rows > 32 ? 1.6 : 1.3; };
+  LatPlan best = {};
+  best.sp_max = 1;
   double best_us = 0.0;
   for (int64_t k = 1; k <= longest; k = k < 4 ? k + 1 : k < 8 ? k + 2 : k + k / 4) {  // splits of the longest sequence
     const int64_t per = (longest + k - 1) / k;
@@ -463,8 +470,7 @@ LatPlan lat_tree_plan(const int32_t* no, const int64_t* pl, int32_t B, int32_t H
       const int64_t rows = (int64_t)(no[s + 1] - no[s]) * Hq;
       if (rows == 0) continue;
       const int64_t pages = (pl[s] + 63) >> 6, n_sp = lt_splits(pages, (int)per), groups = (rows + LT_GROUP - 1) / LT_GROUP;
-      const double page = rows > 64 ? 3.0 : rows > 32 ? 1.6 : 1.3;
-      const double item = FIXED + page * (double)((pages + n_sp - 1) / n_sp);
+      const double item = FIXED + page_us(rows) * (double)((pages + n_sp - 1) / n_sp);
       sum += item * (double)(n_sp * groups);
       most = std::max(most, item);
       items += n_sp * groups;
@@ -477,22 +483,46 @@ LatPlan lat_tree_plan(const int32_t* no, const int64_t* pl, int32_t B, int32_t H
     if (best.per == 0 || us < best_us) best_us = us, best.per = (int)per, best.sp_max = (int)sp_max;
     if (items > 8 * CU) break;
   }
-  int64_t bundles = 0, items[LT_XCD] = {0};
-  for (int s = 0; s < B; ++s) {
+  // runs of items for the XCDs: equal numbers while each has a compute unit, equal times otherwise
+  auto items_of = [&](int s, double* cost) {
     const int64_t rows = (int64_t)(no[s + 1] - no[s]) * Hq;
-    if (rows == 0) continue;
-    const int64_t n_sp = lt_splits((pl[s] + 63) >> 6, best.per), groups = (rows + LT_GROUP - 1) / LT_GROUP;
-    for (int x = 0; x < LT_XCD; ++x) items[x] += ((bundles + n_sp - x + LT_XCD - 1) / LT_XCD - (bundles - x + LT_XCD - 1) / LT_XCD) * groups;
-    bundles += n_sp;
+    if (rows == 0) return (int64_t)0;
+    const int64_t pages = (pl[s] + 63) >> 6, n_sp = lt_splits(pages, best.per);
+    *cost = FIXED + page_us(rows) * (double)((pages + n_sp - 1) / n_sp);
+    return n_sp * ((rows + LT_GROUP - 1) / LT_GROUP);
+  };
+  int64_t items = 0;
+  double sum = 0.0, cost = 0.0;
+  for (int s = 0; s < B; ++s) {
+    const int64_t n = items_of(s, &cost);
+    items += n;
+    sum += cost * (double)n;
   }
-  best.grid = LT_XCD * *std::max_element(items, items + LT_XCD);
+  for (int x = 0; x <= LT_XCD; ++x) best.first[x] = items * x / LT_XCD;
+  if (items > (int64_t)CU) {
+    int64_t before = 0;
+    double spent = 0.0;
+    int x = 1;
+    for (int s = 0; s < B; ++s) {
+      const int64_t n = items_of(s, &cost);
+      for (; x < LT_XCD && n > 0 && spent + cost * (double)n >= sum * x / LT_XCD; ++x)
+        best.first[x] = before + std::min(n, (int64_t)((sum * x / LT_XCD - spent) / cost + 0.5));
+      before += n;
+      spent += cost * (double)n;
+    }
+    for (; x < LT_XCD; ++x) best.first[x] = items;
+  }
+  int64_t most = 0;
+  for (int x = 0; x < LT_XCD; ++x) most = std::max(most, best.first[x + 1] - best.first[x]);
+  best.grid = LT_XCD * most;
   return best;
 }
 
 size_t lat_tree_bytes(const LatPlan& p, int64_t rows) { return p.sp_max > 1 ? align_up((size_t)rows * p.sp_max * LT_REC * 4, 256) : 0; }
 
 hs_status lat_tree_launch(const LatTreeArgs& a, const LatPlan& p, void* workspace, hipStream_t stream) {
-  LtArgs g = {a, a.scale * LT_LOG2E, p.per, p.sp_max, static_cast<float*>(workspace)};
+  LtArgs g = {a, a.scale * LT_LOG2E, p.per, p.sp_max, static_cast<float*>(workspace), {}};
+  for (int x = 0; x <= LT_XCD; ++x) g.first[x] = (int)p.first[x];
   hipLaunchKernelGGL(k_lat_tree, dim3((unsigned)p.grid), dim3(LT_THREADS), 0, stream, g);
   const hs_status st = launch_status("latent attention");
   if (st != HS_OK || p.sp_max == 1) return st;
