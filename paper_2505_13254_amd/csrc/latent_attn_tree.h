@@ -67,17 +67,29 @@ __device__ __forceinline__ void lt_meet() { asm volatile("s_waitcnt lgkmcnt(0)\n
 
 // A wave's nine loads of a tile (1 KB each, every fourth of its 36): from `from` (the tile, uniform) + `off` (the lane's place, see the head of
 // this file) to `to`, both moved to the wave's first load.  The caller waits for them with vmcnt.
-__device__ __forceinline__ void lt_fetch(const char* from, unsigned off, unsigned to) {
+// once: nobody else reads the pages.  The loads then carry the non-temporal hint.
+__device__ __forceinline__ void lt_fetch(const char* from, unsigned off, unsigned to, bool once) {
   unsigned saved;
-#define LT_NEXT "s_add_u32 m0, m0, 0x1000\n\tv_add_u32 %1, 0x1000, %1\n\tglobal_load_lds_dwordx4 %1, %3\n\t"
-  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %3\n\t" LT_NEXT LT_NEXT LT_NEXT LT_NEXT LT_NEXT LT_NEXT LT_NEXT LT_NEXT
-               "s_mov_b32 m0, %0"
-               : "=&s"(saved), "+v"(off)
-               : "s"(to), "s"(from)
-               : "memory", "scc");
+#define LT_LOAD(HINT) "global_load_lds_dwordx4 %1, %3" HINT "\n\t"
+#define LT_NEXT(HINT) "s_add_u32 m0, m0, 0x1000\n\tv_add_u32 %1, 0x1000, %1\n\t" LT_LOAD(HINT)
+#define LT_FETCH(HINT)                                                                                                                            \
+  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %2\n\ts_nop 0\n\t" LT_LOAD(HINT) LT_NEXT(HINT) LT_NEXT(HINT) LT_NEXT(HINT) LT_NEXT(HINT) LT_NEXT(HINT) \
+                   LT_NEXT(HINT) LT_NEXT(HINT) LT_NEXT(HINT) "s_mov_b32 m0, %0"                                                                     \
+               : "=&s"(saved), "+v"(off)                                                                                                          \
+               : "s"(to), "s"(from)                                                                                                               \
+               : "memory", "scc")
+  if (once) LT_FETCH(" nt");
+  else LT_FETCH("");
+#undef LT_FETCH
 #undef LT_NEXT
+#undef LT_LOAD
 }
 static_assert(LT_LOADS == 9, "lt_fetch");
+// 16 bytes of each lane's own address, lane l's to the wave's `to` + 16 l.
+__device__ __forceinline__ void lt_fetch_one(const void* from, unsigned to) {
+  unsigned saved;
+  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, off\n\ts_mov_b32 m0, %0" : "=&s"(saved) : "s"(to), "v"(from) : "memory");
+}
 
 // Step i of a score chain, in ordinary registers.  (As builtins the chain's results go to the accumulation registers, of which O takes all 256: sixteen of O's
 // then live in memory, and a load from there waits for every tile on its way.)  Steps of one chain may follow each other at once; the last one waits until

@@ -23,7 +23,13 @@ struct LtArgs {
   int first[LT_XCD + 1];  // the first item of each XCD
 };
 
-__host__ __device__ __forceinline__ int lt_splits(int64_t pages, int per) { return pages <= per ? 1 : (int)((pages + per - 1) / per); }
+// Splits of a sequence, and the first page of one.  The last split has the tree's own rows besides, and the page that ends inside: they count as LT_EXTRA pages.
+constexpr int LT_EXTRA = 2;
+__host__ __device__ __forceinline__ int lt_splits(int64_t pages, int per) { return pages <= per ? 1 : (int)((pages + LT_EXTRA + per - 1) / per); }
+__host__ __device__ __forceinline__ int lt_first_page(int sp, int n_sp, int pages) {
+  const int p = (int)((int64_t)sp * (pages + LT_EXTRA) / n_sp);
+  return sp == n_sp || p > pages ? pages : p;
+}
 
 struct LtItem {
   int s, n0, M, sp, n_sp, rg;
@@ -34,6 +40,7 @@ struct LtLds {
   char ring[4 * LT_TILE];
   int parent[LT_MAX_TREE];
   float stat[4][2][32];
+  int64_t out_at[4][32];  // where a wave's rows go
   unsigned odd[2];
   int again;  // some row's reference was too low
   int found[8];
@@ -110,6 +117,11 @@ __device__ __forceinline__ bool lt_find(const LtArgs& g, LtItem& it, LtLds& mem)
   return true;
 }
 
+// Rows r >= first of a page in the ring become zero (what lies behind a sequence's last token may be anything, and 0 x NaN is NaN).
+__device__ __forceinline__ void lt_blank(char* page, int first) {
+  for (int x = first * (LT_ROW / 16) + (int)threadIdx.x; x < LT_PAGE / 16; x += LT_THREADS) *reinterpret_cast<uint4*>(page + 16 * x) = make_uint4(0u, 0u, 0u, 0u);
+}
+
 template <int RB>
 __device__ __forceinline__ void lt_run(const LtArgs& g, const LtItem& it, LtLds& mem) {
   constexpr int NB = RB == 1 ? 8 : 16;
@@ -122,74 +134,112 @@ __device__ __forceinline__ void lt_run(const LtArgs& g, const LtItem& it, LtLds&
   const int row = row_base + col < rows ? row_base + col : rows - 1;  // (rows behind the last repeat it)
   const int i = row / a.Hq, h = row - i * a.Hq;
   const bool last = it.sp == it.n_sp - 1;
-  const int pages = (int)((it.L + 63) >> 6), full = (int)(it.L >> 6);
-  const int p_lo = (int)((int64_t)it.sp * pages / it.n_sp), p_hi = (int)((int64_t)(it.sp + 1) * pages / it.n_sp);
-  const int n_pages = std::min(p_hi, full) - p_lo;  // full pages of the split
-  const int rest = p_hi > full ? (int)(it.L & 63) : 0;
-  const int32_t* const table = a.table + (int64_t)it.s * a.max_blocks;
+  const int all_pages = (int)((it.L + 63) >> 6);
+  const int p_lo = lt_first_page(it.sp, it.n_sp, all_pages), n_pages = lt_first_page(it.sp + 1, it.n_sp, all_pages) - p_lo;
+  const int rest = n_pages > 0 && p_lo + n_pages == all_pages ? (int)(it.L & 63) : 0;  // tokens of the last page, where it ends inside
+  const int n_full = n_pages - (rest > 0 ? 1 : 0);
+  const int32_t* const table = a.table + (int64_t)it.s * a.max_blocks + p_lo;
   const char* const pool = static_cast<const char*>(a.pool);
+  const bool once = rows <= LT_GROUP;  // nobody else reads the pages
+  const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
 
-  // pages, 64 of them at a time in the lanes
-  int page_base = 0, page_of = 0;
-  auto look_up = [&](int t) {  // from the split's page t on
-    const int at = p_lo + t + lane;
-    const int p = at < p_hi ? table[at] : 0;
+  // ---- requests, in the order in which they are needed: pages' numbers, the tree's last 64 rows that the group sees and the parents, Q, the first page
+  int page_base = 0, page_of = 0;  // pages, 64 of them at a time in the lanes
+  auto look_up = [&](int t) {      // from the split's page t on
+    const int p = t + lane < n_pages ? table[t + lane] : 0;
     page_of = p < 0 || p >= a.n_pages ? 0 : p;  // (an entry that is no page would be a caller's error)
     page_base = t;
   };
-  auto page_at = [&](int t) { return pool + (int64_t)__builtin_amdgcn_readlane(page_of, t - page_base) * LT_PAGE; };
-  const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
-  const unsigned off = 16 * ((lane & ~7) + ((lane & 7) ^ lt_key((lane >> 3) + 8 * (wave & 1))));
-  auto fetch = [&](int t, int b, int slot) { lt_fetch(page_at(t) + b * LT_TILE + wave * 1024, off, lds0 + slot * LT_TILE + wave * 1024); };
-
-  if (p_hi > p_lo) look_up(0);
-  auto first_page = [&]() {  // into the ring's second half
-    if (n_pages > 0) {
-      fetch(0, 0, 2);
-      fetch(0, 1, 3);
+  look_up(0);
+  // 64 tree rows (from 64 t on; rows behind the last repeat it) straight into the ring's first half, each piece to the place that it has in a page.
+  constexpr int PIECES = LT_PAGE / 16 / LT_THREADS;  // 16-byte pieces to a thread
+  auto tree_rows = [&](int t) {
+    const int left = std::min(64, it.M - 64 * t);
+    int id0 = tid;
+    asm volatile("" : "+v"(id0));  // (no address of these is kept in registers through the pages)
+#pragma unroll 1
+    for (int x = 0; x < PIECES; ++x) {
+      const unsigned id = x * LT_THREADS + id0, G = id >> 3, r = G / 9, c = 8 * (G - 9 * r) + ((id & 7) ^ lt_key(G));
+      const int64_t from = it.n0 + 64 * t + ((int)r < left ? (int)r : left - 1);
+      lt_fetch_one(c < 64 ? static_cast<const bf16_t*>(a.c_tree) + from * a.c_stride + 8 * c : static_cast<const bf16_t*>(a.r_tree) + from * a.r_stride + 8 * (c - 64),
+                   lds0 + (x * LT_THREADS + wave * 64) * 16);
     }
   };
-  first_page();
+  // What a thread fetched, once it is there: rows with a NaN or an infinity are noted, and those elements made zero: 0 x NaN must not reach rows that do not
+  // see them.
+  auto mend_tree = [&]() {
+    int id0 = tid;
+    asm volatile("" : "+v"(id0));
+#pragma unroll 6
+    for (int x = 0; x < PIECES; ++x) {
+      const unsigned id = x * LT_THREADS + id0;
+      uint4 w = *reinterpret_cast<const uint4*>(lds + 16 * id);
+      lt_ushort2 most = {0, 0};
+      unsigned* const e = &w.x;
+#pragma unroll
+      for (int y = 0; y < 4; ++y) most = __builtin_elementwise_max(most, __builtin_bit_cast(lt_ushort2, e[y] & 0x7fff7fffu));
+      if (most[0] >= 0x7f80 || most[1] >= 0x7f80) {
+        const unsigned r = (id >> 3) / 9;
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+          if ((e[y] & 0x7f80u) == 0x7f80u) e[y] &= 0xffff0000u;
+          if ((e[y] & 0x7f800000u) == 0x7f800000u) e[y] &= 0xffffu;
+        }
+        *reinterpret_cast<uint4*>(lds + 16 * id) = w;
+        atomicOr(&mem.odd[r >> 5], 1u << (r & 31));
+      }
+    }
+  };
+  const int top_tree = (std::min(rows, (it.rg + 1) * LT_GROUP) - 1) / a.Hq / 64;
+  int up[LT_MAX_TREE / LT_THREADS];
+  if (last) {
+    tree_rows(top_tree);
+#pragma unroll
+    for (int x = 0; x < LT_MAX_TREE / LT_THREADS; ++x) up[x] = a.parent[it.n0 + std::min(x * LT_THREADS + tid, it.M - 1)];
+  }
   LtState<NB> st;
-  st.start(lane, first_block);
   {
     const bf16_t* const q = static_cast<const bf16_t*>(a.q.p) + (it.n0 + i) * a.q.row + h * a.q.head + 8 * half;
     const bf16_t* const r = static_cast<const bf16_t*>(a.q_rope.p) + (it.n0 + i) * a.q_rope.row + h * a.q_rope.head + 8 * half;
 #pragma unroll
     for (int x = 0; x < LT_NK; ++x) st.q[x] = *reinterpret_cast<const lt_bf16x8*>(x < LT_R / 16 ? q + 16 * x : r + 16 * (x - LT_R / 16));
   }
+  st.start(lane, first_block);
+  const unsigned off = 16 * ((lane & ~7) + ((lane & 7) ^ lt_key((lane >> 3) + 8 * (wave & 1))));
+  // 32-key tile n of the split: page n / 2, in slot (n + 2) % 4 of the ring
+  auto request = [&](int n) {
+    if (n < 2 * n_pages) {
+      const char* const from = pool + (int64_t)__builtin_amdgcn_readlane(page_of, (n >> 1) - page_base) * LT_PAGE + (n & 1) * LT_TILE + wave * 1024;
+      lt_fetch(from, off, lds0 + ((n + 2) & 3) * LT_TILE + wave * 1024, once);
+    }
+  };
+  request(0);
+  request(1);
   const float c2 = g.c2;
+  if (last) {
+    if (tid < 2) mem.odd[tid] = 0u;
+#pragma unroll
+    for (int x = 0; x < LT_MAX_TREE / LT_THREADS; ++x) mem.parent[x * LT_THREADS + tid] = up[x];
+    lt_meet();
+    mend_tree();  // (the parents were requested behind the tree's rows, and are there)
+  }
   float reference = LT_FLOOR;
 #pragma unroll 1
-  for (;;) {
+  for (bool first = true;; first = false) {
   st.clear(reference);
 
-  // ---- the tree's own rows, from the last 64 that a row of the group sees down to the first
+  // ---- the tree's own rows, from the last 64 that a row of the group sees down to the first, in the ring's first half
   if (last) {
-    for (int x = tid; x < it.M; x += LT_THREADS) mem.parent[x] = a.parent[it.n0 + x];
-    const int row_end = std::min(rows, (it.rg + 1) * LT_GROUP) - 1;
     int cursor = i;  // the next row of the lane's root path
-    for (int t = row_end / a.Hq / 64; t >= 0; --t) {
-      lt_meet();  // (the buffer's last readers are done)
-      if (tid < 2) mem.odd[tid] = 0u;
-      lt_meet();
-      // rows with a NaN or an infinity are noted, and those elements left out: 0 x NaN must not reach rows that do not see them
-      const int left = std::min(64, it.M - 64 * t);
-#pragma unroll 6
-      for (int x = 0; x < LT_PAGE / 16 / LT_THREADS; ++x) {
-        const int id = x * LT_THREADS + tid, r = id / 72, c = id - 72 * r;
-        const int64_t from = it.n0 + 64 * t + (r < left ? r : left - 1);
-        uint4 w = *reinterpret_cast<const uint4*>(c < 64 ? static_cast<const bf16_t*>(a.c_tree) + from * a.c_stride + 8 * c
-                                                         : static_cast<const bf16_t*>(a.r_tree) + from * a.r_stride + 8 * (c - 64));
-        unsigned* const e = &w.x;
-        bool odd = false;
-#pragma unroll
-        for (int y = 0; y < 4; ++y) {
-          if ((e[y] & 0x7f80u) == 0x7f80u) e[y] &= 0xffff0000u, odd = true;
-          if ((e[y] & 0x7f800000u) == 0x7f800000u) e[y] &= 0xffffu, odd = true;
-        }
-        if (odd) atomicOr(&mem.odd[r >> 5], 1u << (r & 31));
-        *reinterpret_cast<uint4*>(lds + lt_at(r, c)) = w;
+#pragma unroll 1
+    for (int t = top_tree; t >= 0; --t) {
+      if (!first || t < top_tree) {
+        lt_meet();  // (the buffer's last readers are done)
+        if (tid < 2) mem.odd[tid] = 0u;
+        lt_meet();
+        tree_rows(t);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        mend_tree();
       }
       lt_meet();
 #pragma unroll 1
@@ -198,8 +248,8 @@ __device__ __forceinline__ void lt_run(const LtArgs& g, const LtItem& it, LtLds&
         const int base = 64 * t + 32 * b;
         while (cursor >= base) {
           word |= 1u << (cursor & 31);
-          const int up = mem.parent[cursor];
-          cursor = up < cursor ? up : -1;  // (a malformed tree cannot keep the walk from ending)
+          const int to = mem.parent[cursor];
+          cursor = to < cursor ? to : -1;  // (a malformed tree cannot keep the walk from ending)
         }
         if (RB != 4 && b != kh) continue;
         if (__ballot(word != 0u) == 0ull) continue;
@@ -213,45 +263,20 @@ __device__ __forceinline__ void lt_run(const LtArgs& g, const LtItem& it, LtLds&
         st.take(lds, b * LT_TILE, S, c2);
       }
     }
-  }
-  // ---- the page that ends inside
-  if (rest > 0) {
-    lt_meet();
-    const int p = __builtin_amdgcn_readfirstlane(table[p_hi - 1]);
-    const char* const from = pool + (int64_t)(p < 0 || p >= a.n_pages ? 0 : p) * LT_PAGE;
-#pragma unroll 6
-    for (int x = 0; x < LT_PAGE / 16 / LT_THREADS; ++x) {
-      const int id = x * LT_THREADS + tid, r = id / 72, c = id - 72 * r;
-      *reinterpret_cast<uint4*>(lds + lt_at(r, c)) = *reinterpret_cast<const uint4*>(from + (r < rest ? r : rest - 1) * LT_ROW + 16 * c);
-    }
-    lt_meet();
-#pragma unroll 1
-    for (int b = 0; b < 2; ++b) {
-      if (RB != 4 && b != kh) continue;
-      if (32 * b >= rest) continue;
-      lt_floatx16 S = st.scores(lds, b * LT_TILE);
-#pragma unroll
-      for (int v = 0; v < 16; ++v) S[v] = 32 * b + 8 * (v >> 2) + 4 * half + (v & 3) < rest ? S[v] : -HS_INF;
-      st.take(lds, b * LT_TILE, S, c2);
-    }
+    lt_meet();  // (the ring's first half is free)
   }
   // ---- full pages
-  if (n_pages > 0) {
-    if (last || rest > 0) lt_meet();  // (the ring's first half is free)
-    if constexpr (RB == 4) {
-      // tile n: page n / 2, in slot (n + 2) % 4.  Three tiles are in the ring or on their way besides the one whose values are multiplied.
-      const int tiles = 2 * n_pages;
-      auto request = [&](int n) {
-        if (n < tiles) fetch(n >> 1, n & 1, (n + 2) & 3);
-      };
-      request(2);
-      if (tiles > 2) asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(2 * LT_LOADS) : "memory");
+  unsigned here = 2 * LT_TILE;  // where the page is in the ring
+  if constexpr (RB == 4) {
+    // three tiles are in the ring or on their way besides the one whose values are multiplied
+    request(2);
+    if (n_full > 0) {
+      if (n_pages > 1) asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(2 * LT_LOADS) : "memory");
       else asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(LT_LOADS) : "memory");
-      lt_floatx16 S = st.scores(lds, 2 * LT_TILE), N;
+      lt_floatx16 S = st.scores(lds, here), N;
       uint4 P0, P1;
-      unsigned here = 2 * LT_TILE;  // of the page's first tile
       // (two tiles a trip: the scores of one and of the next change places without a copy)
-      for (int p = 0; p + 1 < n_pages; ++p) {
+      for (int p = 0; p + 1 < n_full; ++p) {
         asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(LT_LOADS) : "memory");  // tile 2 p + 1 is there, 2 p + 2 on its way
         request(2 * p + 3);
         st.ahead(lds, here + LT_TILE, S, N, c2, P0, P1);
@@ -263,32 +288,46 @@ __device__ __forceinline__ void lt_run(const LtArgs& g, const LtItem& it, LtLds&
         st.product(lds, here + LT_TILE, P0, P1);
         here = 2 * LT_TILE - here;
       }
-      asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+      if (rest > 0) asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(LT_LOADS) : "memory");
+      else asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+      request(2 * n_full + 1);
       st.ahead(lds, here + LT_TILE, S, N, c2, P0, P1);
       st.product(lds, here, P0, P1);
       st.take(lds, here + LT_TILE, N, c2);
-    } else {
-      // page n in ring half (n + 1) % 2; each wave has one 32-key half of it
-      auto request = [&](int n) {
-        if (n < n_pages) {
-          fetch(n, 0, 2 * ((n + 1) & 1));
-          fetch(n, 1, 2 * ((n + 1) & 1) + 1);
-        }
-      };
-      request(1);
-      for (int n = 0; n < n_pages; ++n) {
-        if (n + 1 < n_pages) asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(2 * LT_LOADS) : "memory");
-        else asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
-        const unsigned tile = (2 * ((n + 1) & 1) + kh) * LT_TILE;
-        const lt_floatx16 S = st.scores(lds, tile);
-        st.take(lds, tile, S, c2);
-        if (n + 2 - page_base >= 64) look_up(n + 2);
-        lt_meet();  // every wave is done with the page
-        request(n + 2);
-      }
+      here = 2 * LT_TILE - here;
+    }
+  } else {
+    // each wave has one 32-key half of a page
+    request(2);
+    request(3);
+    for (int n = 0; n < n_full; ++n) {
+      if (n + 1 < n_pages) asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(2 * LT_LOADS) : "memory");
+      else asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+      const unsigned tile = here + kh * LT_TILE;
+      const lt_floatx16 S = st.scores(lds, tile);
+      st.take(lds, tile, S, c2);
+      if (n + 2 - page_base >= 64) look_up(n + 2);
+      lt_meet();  // every wave is done with the page
+      request(2 * n + 4);
+      request(2 * n + 5);
+      here = 2 * LT_TILE - here;
     }
   }
-
+  // ---- the page that ends inside
+  if (rest > 0) {
+    asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+    lt_blank(lds + here, rest);
+    lt_meet();
+#pragma unroll 1
+    for (int b = 0; b < 2; ++b) {
+      if (RB != 4 && b != kh) continue;
+      if (32 * b >= rest) continue;
+      lt_floatx16 S = st.scores(lds, here + b * LT_TILE);
+#pragma unroll
+      for (int v = 0; v < 16; ++v) S[v] = 32 * b + 8 * (v >> 2) + 4 * half + (v & 3) < rest ? S[v] : -HS_INF;
+      st.take(lds, here + b * LT_TILE, S, c2);
+    }
+  }
   // ---- a row whose scores rose too far above its reference?
   if (tid == 0) mem.again = 0;
   lt_meet();
@@ -296,8 +335,9 @@ __device__ __forceinline__ void lt_run(const LtArgs& g, const LtItem& it, LtLds&
   lt_meet();
   if (mem.again == 0) break;
   reference = st.seen;
-  if (p_hi > p_lo) look_up(0);
-  first_page();
+  look_up(0);
+  request(0);
+  request(1);
   }
 
   // ---- out: the halves of the keys meet, then rows leave by way of LDS
@@ -355,12 +395,13 @@ __device__ __forceinline__ void lt_run(const LtArgs& g, const LtItem& it, LtLds&
         *reinterpret_cast<uint2*>(stage + col * LT_OUT_PITCH + 64 * t + 16 * b + 8 * half) =
             make_uint2(__builtin_bit_cast(unsigned, __builtin_convertvector(x, lt_bf16x2)), __builtin_bit_cast(unsigned, __builtin_convertvector(y, lt_bf16x2)));
       }
+    if (half == 0) mem.out_at[wave][col] = (it.n0 + i) * a.o_row + h * a.o_head;
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     constexpr int PER_ROW = KEEP * 4;  // 16-byte pieces
 #pragma unroll 4
     for (int x = lane; x < mine_rows * PER_ROW; x += 64) {
-      const int r = x / PER_ROW, c = x % PER_ROW, ri = (row_base + r) / a.Hq, rh = row_base + r - ri * a.Hq;
-      *reinterpret_cast<uint4*>(static_cast<bf16_t*>(a.o) + (it.n0 + ri) * a.o_row + rh * a.o_head + 32 * out_block + 8 * c) =
+      const int r = x / PER_ROW, c = x % PER_ROW;
+      *reinterpret_cast<uint4*>(static_cast<bf16_t*>(a.o) + mem.out_at[wave][r] + 32 * out_block + 8 * c) =
           *reinterpret_cast<const uint4*>(stage + r * LT_OUT_PITCH + 16 * c);
     }
   } else {
