@@ -11,10 +11,10 @@
 //   RB = 1 (up to 32)        four waves a block: a half of the page and a half of the columns (scores computed twice)
 // The latter two are bound by the stream of pages, not by what the waves do.
 //
-// LDS: a ring of four 32-key tiles, which global_load_lds fills.  A tile lies as in memory, but for the order of the eight 16-byte chunks of every
-// 128 bytes: with G the number of a 128-byte group from the page's start (row r, group k of it: 9 r + k), chunk c stands at c ^ f(G), f(G) = bits 1, 2, 3 of G
-// as bits 2, 1, 0.  16 rows of one chunk (a K fragment's read) and four rows of 64 bytes (a transposing V read) then lie in
-// different banks, and the source address of a lane is the same for every load of a wave.
+// LDS: a ring of four 32-key tiles, which global_load_lds fills.  A tile is its rows' latents, 1024 bytes each, and behind them their rotary parts, 128 bytes
+// each.  16-byte chunk c of row r stands at c ^ lt_key(r) among a latent's, at c ^ (r / 2 mod 8) among a rotary part's: 16 rows of one chunk (a K fragment's
+// read) and four rows of 64 bytes (a transposing V read) lie in different banks.  The key takes four bits, so that the place of every fragment is one of eight
+// patterns, an exclusive or each, plus an immediate; fragments are taken pattern by pattern (the order of a product's steps is free).
 #pragma once
 #include "latent_attn.h"
 
@@ -41,11 +41,14 @@ constexpr float LT_FLOOR = -3e38f;
 constexpr float LT_RISE = 24.f;               // octaves that a score may rise above the reference
 constexpr float LT_LN2 = 0.6931471805599453f, LT_LOG2E = 1.4426950408889634f;
 
-__host__ __device__ __forceinline__ unsigned lt_key(unsigned G) { return ((G >> 1) & 1) << 2 | ((G >> 2) & 1) << 1 | ((G >> 3) & 1); }
-// Byte of 16-byte chunk c (0 .. 71) of row r of a page.
-__device__ __forceinline__ unsigned lt_at(unsigned r, unsigned c) {
-  const unsigned G = 9 * r + (c >> 3);
-  return G * 128 + 16 * ((c & 7) ^ lt_key(G));
+constexpr int LT_ROT = 32 * 2 * LT_R;  // where a tile's rotary parts begin
+__host__ __device__ __forceinline__ unsigned lt_key(unsigned r) { return (r & 3) << 2 | ((r >> 2) & 3); }
+// Row and chunk (0 .. 71) of the 16 bytes at 16 * id of a page in the ring (two tiles).
+__device__ __forceinline__ void lt_what(unsigned id, unsigned* row, unsigned* chunk) {
+  const unsigned tile = id >= LT_TILE / 16 ? 1 : 0, x = id - tile * (LT_TILE / 16), y = x - LT_ROT / 16;
+  const unsigned r = x < LT_ROT / 16 ? x >> 6 : y >> 3;
+  *row = 32 * tile + r;
+  *chunk = x < LT_ROT / 16 ? (x & 63) ^ lt_key(r) : 64 + ((y & 7) ^ ((r >> 1) & 7));
 }
 
 __device__ __forceinline__ float2 lt_halves(float x) {  // this lane's value in the lower and in the upper half-wave
@@ -65,18 +68,23 @@ __device__ __forceinline__ float lt_half_sum(float x) {
 
 __device__ __forceinline__ void lt_meet() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
-// A wave's nine loads of a tile (1 KB each, every fourth of its 36): from `from` (the tile, uniform) + `off` (the lane's place, see the head of
-// this file) to `to`, both moved to the wave's first load.  The caller waits for them with vmcnt.
-// once: nobody else reads the pages.  The loads then carry the non-temporal hint.
-__device__ __forceinline__ void lt_fetch(const char* from, unsigned off, unsigned to, bool once) {
+// A wave's nine loads of a tile, 1 KB each: the latents of rows w, w + 4, .. and the rotary parts of rows 8 w .. 8 w + 7 (w: the wave).  from: the tile's first
+// row; off: the lane's place in row w (16 (lane ^ lt_key(w)) + 1152 w); rot: in the rotary parts of its row (lt_rot_off).  to, to_rot: the wave's first places
+// in LDS.  The caller waits for them with vmcnt.  once: nobody else reads the pages.  The loads then carry the non-temporal hint.
+__device__ __forceinline__ unsigned lt_rot_off(int lane, int wave) {
+  const unsigned r = 8 * wave + (lane >> 3);
+  return LT_ROW * r + 2 * LT_R + 16 * ((lane & 7) ^ ((r >> 1) & 7));
+}
+__device__ __forceinline__ void lt_fetch(const char* from, unsigned off, unsigned rot, unsigned to, unsigned to_rot, bool once) {
   unsigned saved;
 #define LT_LOAD(HINT) "global_load_lds_dwordx4 %1, %3" HINT "\n\t"
-#define LT_NEXT(HINT) "s_add_u32 m0, m0, 0x1000\n\tv_add_u32 %1, 0x1000, %1\n\t" LT_LOAD(HINT)
-#define LT_FETCH(HINT)                                                                                                                            \
-  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %2\n\ts_nop 0\n\t" LT_LOAD(HINT) LT_NEXT(HINT) LT_NEXT(HINT) LT_NEXT(HINT) LT_NEXT(HINT) LT_NEXT(HINT) \
-                   LT_NEXT(HINT) LT_NEXT(HINT) LT_NEXT(HINT) "s_mov_b32 m0, %0"                                                                     \
-               : "=&s"(saved), "+v"(off)                                                                                                          \
-               : "s"(to), "s"(from)                                                                                                               \
+#define LT_NEXT(KEY, HINT) "s_add_u32 m0, m0, 0x1000\n\tv_add_u32 %1, 0x1200, %1\n\tv_xor_b32 %1, " KEY ", %1\n\t" LT_LOAD(HINT)
+#define LT_FETCH(HINT)                                                                                                                                       \
+  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %5\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %4, %3" HINT "\n\ts_mov_b32 m0, %2\n\ts_nop 0\n\t" LT_LOAD(HINT)        \
+                   LT_NEXT("16", HINT) LT_NEXT("48", HINT) LT_NEXT("16", HINT) LT_NEXT("48", HINT) LT_NEXT("16", HINT) LT_NEXT("48", HINT) LT_NEXT("16", HINT) \
+                       "s_mov_b32 m0, %0"                                                                                                                    \
+               : "=&s"(saved), "+v"(off)                                                                                                                     \
+               : "s"(to), "s"(from), "v"(rot), "s"(to_rot)                                                                                                   \
                : "memory", "scc")
   if (once) LT_FETCH(" nt");
   else LT_FETCH("");
@@ -108,8 +116,7 @@ struct LtState {
   lt_bf16x8 q[LT_NK];  // element 16 i + 8 half + j of step i
   lt_floatx16 acc[NB]; // O^T: column 32 t + 8 (v / 4) + 4 half + v % 4
   float m, l, seen;    // reference of the scores (octaves), sum of the weights relative to it (of this half-wave's keys), largest score
-  unsigned k_row, k_in;  // the first group of the lane's K row of a tile, and the byte of its chunk within a group
-  unsigned v_row, v_in;  // of its V rows (the wave's first column on)
+  unsigned k_at, r_at, v_at;  // the lane's places in a tile: of its K row's first chunk, of its rotary part's, of its V rows' (the wave's first column on)
 
   __device__ __forceinline__ void clear(float reference) {
     m = seen = reference;
@@ -121,48 +128,58 @@ struct LtState {
   }
   __device__ __forceinline__ void start(int lane, int first_block) {
     const unsigned half = lane >> 5, col = lane & 31;
-    k_row = 9 * col;
-    k_in = 16 * half;
+    k_at = 1024 * col + 16 * (half ^ lt_key(col));
+    r_at = LT_ROT + 128 * col + 16 * (half ^ ((col >> 1) & 7));
     const unsigned a = lane & 3, j = (lane >> 2) & 3, dh = (lane >> 4) & 1, r0 = 4 * half + j;
-    v_row = 9 * r0 + first_block / 2;
-    v_in = 16 * (2 * dh + (a >> 1)) + 8 * (a & 1);
+    v_at = 1024 * r0 + 16 * ((2 * dh + (a >> 1)) ^ lt_key(r0)) + 8 * (a & 1) + 64 * first_block;
   }
-  // The place of the lane's chunk in a group (found again for every tile: there are no registers to keep them in).
-  __device__ __forceinline__ static unsigned place(unsigned G, unsigned in) { return (G << 7) + (in ^ (((__builtin_bitreverse32(G) >> 28) & 7u) << 4)); }
-  // Chunk 2 i + half of the lane's K row; at: its place in group i / 4.
-  __device__ __forceinline__ static lt_bf16x8 key(const char* lds, unsigned tile, unsigned at, int i) {
-    return *reinterpret_cast<const lt_bf16x8*>(lds + ((at ^ (32u * (i & 3))) + tile));
-  }
-  // V^T of block t, keys 16 k2 .. of a tile.
-  __device__ __forceinline__ lt_bf16x8 value(char* lds, unsigned tile, unsigned at, int t, int k2) const {
-    lt_bf16x8 f;
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      const lt_shortx4 got = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lt_lds_s4)(lds + ((at ^ (64u * (t & 1) | 16u * x)) + tile) + 9216 * x + 18432 * k2));
-      const lt_bf16x4 four = __builtin_bit_cast(lt_bf16x4, got);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) f[4 * x + e] = four[e];
+  // Step n of the first product: chunks 2 i + half, i = step(n), of the lane's K row (the same i for n = 4 m .. 4 m + 3 but for multiples of eight).
+  __device__ __forceinline__ static constexpr int step(int n) { return n < 32 ? 8 * (n & 3) + (n >> 2) : n; }
+  struct Keys {
+    const char* lds;
+    unsigned k, r, at;
+    __device__ __forceinline__ lt_bf16x8 operator()(int n) {
+      if (n >= 32) at = r ^ (32u * (n - 32));
+      else if ((n & 3) == 0) at = k ^ (32u * (n >> 2));
+      return *reinterpret_cast<const lt_bf16x8*>(lds + at + (n < 32 ? 256 * (n & 3) : 0));
     }
-    return f;
+  };
+  __device__ __forceinline__ Keys keys(const char* lds, unsigned tile) const {
+    Keys k = {lds, k_at + tile, r_at + tile, 0u};
+    asm volatile("" : "+v"(k.k), "+v"(k.r));  // (found again for every tile: there are no registers to keep all patterns in)
+    return k;
   }
+  // Fragment x of the second product: block t = block(x) of the wave's columns, keys 16 k2 .. of a tile, k2 = (x / 2) % 2.
+  __device__ __forceinline__ static constexpr int block(int x) { return 4 * (2 * ((x >> 2) % (NB / 8)) + (x & 1)) + (x >> 2) / (NB / 8); }
+  struct Values {
+    char* lds;
+    unsigned v, at0, at1;
+    __device__ __forceinline__ lt_bf16x8 operator()(int x) {
+      const int t = block(x), k2 = (x >> 1) & 1;
+      if (x % (NB / 2) == 0) at0 = v ^ (64u * (t & 3)), at1 = v ^ (64u * (t & 3) | 32u);
+      lt_bf16x8 f;
+#pragma unroll
+      for (int y = 0; y < 2; ++y) {
+        const lt_shortx4 got = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lt_lds_s4)(lds + (y ? at1 : at0) + 256 * (t >> 2) + 8192 * y + 16384 * k2));
+        const lt_bf16x4 four = __builtin_bit_cast(lt_bf16x4, got);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) f[4 * y + e] = four[e];
+      }
+      return f;
+    }
+  };
   __device__ __forceinline__ lt_floatx16 scores(const char* lds, unsigned tile) const {
     lt_floatx16 S;
-    unsigned row = k_row, at;
-    asm volatile("" : "+v"(row));
     constexpr int AHEAD = 4;
+    Keys key = keys(lds, tile);
     lt_bf16x8 f[AHEAD];
-    at = place(row, k_in);
 #pragma unroll
-    for (int i = 0; i < AHEAD; ++i) f[i] = key(lds, tile, at, i);
+    for (int n = 0; n < AHEAD; ++n) f[n] = key(n);
 #pragma unroll
-    for (int i = 0; i < LT_NK; ++i) {
-      if (i + 1 < LT_NK) lt_step(S, f[i % AHEAD], q[i], i);
-      else lt_last(S, f[i % AHEAD], q[i]);
-      const int n = i + AHEAD;
-      if (n < LT_NK) {
-        if ((n & 3) == 0) at = place(row + (n >> 2), k_in);
-        f[i % AHEAD] = key(lds, tile, at, n);
-      }
+    for (int n = 0; n < LT_NK; ++n) {
+      if (n + 1 < LT_NK) lt_step(S, f[n % AHEAD], q[step(n)], n);
+      else lt_last(S, f[n % AHEAD], q[step(n)]);
+      if (n + AHEAD < LT_NK) f[n % AHEAD] = key(n + AHEAD);
       __builtin_amdgcn_sched_barrier(0);
     }
     return S;
@@ -195,51 +212,38 @@ struct LtState {
   }
   __device__ __forceinline__ void product(char* lds, unsigned tile, const uint4& P0, const uint4& P1) {
     const lt_bf16x8 b0 = __builtin_bit_cast(lt_bf16x8, P0), b1 = __builtin_bit_cast(lt_bf16x8, P1);
-    // steps: pairs of blocks in one 128-byte group, the lower 16 keys of both, then the upper ones
-    unsigned row = v_row;
-    asm volatile("" : "+v"(row));
+    Values value = {lds, v_at + tile, 0u, 0u};
+    asm volatile("" : "+v"(value.v));
     lt_bf16x8 f[4];
-    unsigned at = place(row, v_in);
 #pragma unroll
-    for (int x = 0; x < 4; ++x) f[x] = value(lds, tile, at, x & 1, x >> 1);
+    for (int x = 0; x < 4; ++x) f[x] = value(x);
 #pragma unroll
     for (int x = 0; x < 2 * NB; ++x) {
-      const int t = 2 * (x >> 2) + (x & 1), k2 = (x >> 1) & 1;
-      acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[x & 3], k2 == 0 ? b0 : b1, acc[t], 0, 0, 0);
-      const int n = x + 4;
-      if (n < 2 * NB) {
-        if ((n & 3) == 0) at = place(row + (n >> 2), v_in);
-        f[x & 3] = value(lds, tile, at, 2 * (n >> 2) + (n & 1), (n >> 1) & 1);
-      }
+      acc[block(x)] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[x & 3], (x >> 1) & 1 ? b1 : b0, acc[block(x)], 0, 0, 0);
+      if (x + 4 < 2 * NB) f[x & 3] = value(x + 4);
       __builtin_amdgcn_sched_barrier(0);
     }
   }
   // The scores of tile `next` beside the softmax of S (tile by tile, RB = 4), whose weights become P0, P1.
   __device__ __forceinline__ void ahead(const char* lds, unsigned next, const lt_floatx16& S, lt_floatx16& N, float c2, uint4& P0, uint4& P1) {
     constexpr int AHEAD = 4;
-    unsigned row = k_row, at;
-    asm volatile("" : "+v"(row));
-    at = place(row, k_in);
+    Keys key = keys(lds, next);
     lt_bf16x8 f[AHEAD];
 #pragma unroll
-    for (int i = 0; i < AHEAD; ++i) f[i] = key(lds, next, at, i);
+    for (int n = 0; n < AHEAD; ++n) f[n] = key(n);
     float top = S[0];
     unsigned w[8];
 #pragma unroll
-    for (int i = 0; i < LT_NK; ++i) {
-      if (i + 1 < LT_NK) lt_step(N, f[i % AHEAD], q[i], i);
-      else lt_last(N, f[i % AHEAD], q[i]);
-      const int n = i + AHEAD;
-      if (n < LT_NK) {
-        if ((n & 3) == 0) at = place(row + (n >> 2), k_in);
-        f[i % AHEAD] = key(lds, next, at, n);
-      }
-      if (i < 5) {
+    for (int n = 0; n < LT_NK; ++n) {
+      if (n + 1 < LT_NK) lt_step(N, f[n % AHEAD], q[step(n)], n);
+      else lt_last(N, f[n % AHEAD], q[step(n)]);
+      if (n + AHEAD < LT_NK) f[n % AHEAD] = key(n + AHEAD);
+      if (n < 5) {
 #pragma unroll
-        for (int v = 3 * i + 1; v < 3 * i + 4; ++v) top = fmaxf(top, S[v]);
+        for (int v = 3 * n + 1; v < 3 * n + 4; ++v) top = fmaxf(top, S[v]);
       }
-      if (i == 5) refer(top, c2);
-      if (i >= 8 && i < 32 && (i - 8) % 3 == 0) w[(i - 8) / 3] = pair(S, c2, (i - 8) / 3);
+      if (n == 5) refer(top, c2);
+      if (n >= 8 && n < 32 && (n - 8) % 3 == 0) w[(n - 8) / 3] = pair(S, c2, (n - 8) / 3);
       __builtin_amdgcn_sched_barrier(0);
     }
     P0 = make_uint4(w[0], w[1], w[2], w[3]);

@@ -117,9 +117,13 @@ __device__ __forceinline__ bool lt_find(const LtArgs& g, LtItem& it, LtLds& mem)
   return true;
 }
 
-// Rows r >= first of a page in the ring become zero (what lies behind a sequence's last token may be anything, and 0 x NaN is NaN).
+// Rows from `first` on of a page in the ring become zero (what lies behind a sequence's last token may be anything, and 0 x NaN is NaN).
 __device__ __forceinline__ void lt_blank(char* page, int first) {
-  for (int x = first * (LT_ROW / 16) + (int)threadIdx.x; x < LT_PAGE / 16; x += LT_THREADS) *reinterpret_cast<uint4*>(page + 16 * x) = make_uint4(0u, 0u, 0u, 0u);
+  for (int x = (int)threadIdx.x; x < LT_PAGE / 16; x += LT_THREADS) {
+    unsigned row, chunk;
+    lt_what(x, &row, &chunk);
+    if ((int)row >= first) *reinterpret_cast<uint4*>(page + 16 * x) = make_uint4(0u, 0u, 0u, 0u);
+  }
 }
 
 template <int RB>
@@ -159,7 +163,8 @@ __device__ __forceinline__ void lt_run(const LtArgs& g, const LtItem& it, LtLds&
     asm volatile("" : "+v"(id0));  // (no address of these is kept in registers through the pages)
 #pragma unroll 1
     for (int x = 0; x < PIECES; ++x) {
-      const unsigned id = x * LT_THREADS + id0, G = id >> 3, r = G / 9, c = 8 * (G - 9 * r) + ((id & 7) ^ lt_key(G));
+      unsigned r, c;
+      lt_what(x * LT_THREADS + id0, &r, &c);
       const int64_t from = it.n0 + 64 * t + ((int)r < left ? (int)r : left - 1);
       lt_fetch_one(c < 64 ? static_cast<const bf16_t*>(a.c_tree) + from * a.c_stride + 8 * c : static_cast<const bf16_t*>(a.r_tree) + from * a.r_stride + 8 * (c - 64),
                    lds0 + (x * LT_THREADS + wave * 64) * 16);
@@ -179,7 +184,8 @@ __device__ __forceinline__ void lt_run(const LtArgs& g, const LtItem& it, LtLds&
 #pragma unroll
       for (int y = 0; y < 4; ++y) most = __builtin_elementwise_max(most, __builtin_bit_cast(lt_ushort2, e[y] & 0x7fff7fffu));
       if (most[0] >= 0x7f80 || most[1] >= 0x7f80) {
-        const unsigned r = (id >> 3) / 9;
+        unsigned r, c;
+        lt_what(id, &r, &c);
 #pragma unroll
         for (int y = 0; y < 4; ++y) {
           if ((e[y] & 0x7f80u) == 0x7f80u) e[y] &= 0xffff0000u;
@@ -205,12 +211,13 @@ __device__ __forceinline__ void lt_run(const LtArgs& g, const LtItem& it, LtLds&
     for (int x = 0; x < LT_NK; ++x) st.q[x] = *reinterpret_cast<const lt_bf16x8*>(x < LT_R / 16 ? q + 16 * x : r + 16 * (x - LT_R / 16));
   }
   st.start(lane, first_block);
-  const unsigned off = 16 * ((lane & ~7) + ((lane & 7) ^ lt_key((lane >> 3) + 8 * (wave & 1))));
+  const unsigned off = LT_ROW * wave + 16 * (lane ^ lt_key(wave)), rot = lt_rot_off(lane, wave);
   // 32-key tile n of the split: page n / 2, in slot (n + 2) % 4 of the ring
   auto request = [&](int n) {
     if (n < 2 * n_pages) {
-      const char* const from = pool + (int64_t)__builtin_amdgcn_readlane(page_of, (n >> 1) - page_base) * LT_PAGE + (n & 1) * LT_TILE + wave * 1024;
-      lt_fetch(from, off, lds0 + ((n + 2) & 3) * LT_TILE + wave * 1024, once);
+      const char* const from = pool + (int64_t)__builtin_amdgcn_readlane(page_of, (n >> 1) - page_base) * LT_PAGE + (n & 1) * LT_TILE;
+      const unsigned to = lds0 + ((n + 2) & 3) * LT_TILE + wave * 1024;
+      lt_fetch(from, off, rot, to, to + LT_ROT, once);
     }
   };
   request(0);
