@@ -147,7 +147,7 @@ __device__ __forceinline__ void lt_run(const LtArgs& g, const LtItem& it, LtLds&
   const bool once = rows <= LT_GROUP;  // nobody else reads the pages
   const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
 
-  // ---- requests, in the order in which they are needed: pages' numbers, the tree's last 64 rows that the group sees and the parents, Q, the first page
+  // ---- requests: the numbers of the pages, Q, the tree's last 64 rows that the group sees and the parents, the first page
   int page_base = 0, page_of = 0;  // pages, 64 of them at a time in the lanes
   auto look_up = [&](int t) {      // from the split's page t on
     const int p = t + lane < n_pages ? table[t + lane] : 0;
@@ -197,20 +197,6 @@ __device__ __forceinline__ void lt_run(const LtArgs& g, const LtItem& it, LtLds&
     }
   };
   const int top_tree = (std::min(rows, (it.rg + 1) * LT_GROUP) - 1) / a.Hq / 64;
-  int up[LT_MAX_TREE / LT_THREADS];
-  if (last) {
-    tree_rows(top_tree);
-#pragma unroll
-    for (int x = 0; x < LT_MAX_TREE / LT_THREADS; ++x) up[x] = a.parent[it.n0 + std::min(x * LT_THREADS + tid, it.M - 1)];
-  }
-  LtState<NB> st;
-  {
-    const bf16_t* const q = static_cast<const bf16_t*>(a.q.p) + (it.n0 + i) * a.q.row + h * a.q.head + 8 * half;
-    const bf16_t* const r = static_cast<const bf16_t*>(a.q_rope.p) + (it.n0 + i) * a.q_rope.row + h * a.q_rope.head + 8 * half;
-#pragma unroll
-    for (int x = 0; x < LT_NK; ++x) st.q[x] = *reinterpret_cast<const lt_bf16x8*>(x < LT_R / 16 ? q + 16 * x : r + 16 * (x - LT_R / 16));
-  }
-  st.start(lane, first_block);
   const unsigned off = LT_ROW * wave + 16 * (lane ^ lt_key(wave)), rot = lt_rot_off(lane, wave);
   // 32-key tile n of the split: page n / 2, in slot (n + 2) % 4 of the ring
   auto request = [&](int n) {
@@ -220,8 +206,47 @@ __device__ __forceinline__ void lt_run(const LtArgs& g, const LtItem& it, LtLds&
       lt_fetch(from, off, rot, to, to + LT_ROT, once);
     }
   };
-  request(0);
-  request(1);
+  // Q by way of LDS, laid out like keys: the tile of each row block in the slot of its number, its 36 KB shared out among the waves that have the block.  (A lane
+  // reading its own row from memory takes 16 bytes of a line at a time: 144 such loads a workgroup took 4 us.)
+  LtState<NB> st;
+  st.start(lane, first_block);
+  {
+    constexpr int MINE = 9 * RB;  // KB to a wave
+    const int first_kb = MINE * (RB == 4 ? 0 : RB == 2 ? wave >> 1 : wave);
+    const bf16_t* const q = static_cast<const bf16_t*>(a.q.p) + (it.n0 + i) * a.q.row + h * a.q.head;
+    const bf16_t* const r = static_cast<const bf16_t*>(a.q_rope.p) + (it.n0 + i) * a.q_rope.row + h * a.q_rope.head;
+    const unsigned to = lds0 + rb * LT_TILE;
+#pragma unroll 1
+    for (int x = first_kb; x < first_kb + MINE; ++x) {
+      const int from = x < 32 ? x : 8 * (x - 32) + (lane >> 3);  // whose row
+      const int64_t at = __shfl((int64_t)(uintptr_t)(x < 32 ? q : r), from);
+      lt_fetch_one(reinterpret_cast<const char*>(at) + 16 * (x < 32 ? lane ^ (int)lt_key(x) : (lane & 7) ^ ((from >> 1) & 7)), to + 1024 * x);
+    }
+  }
+  if constexpr (RB == 4) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  } else {
+    request(0);
+    request(1);
+    if (n_pages > 0) asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(2 * LT_LOADS) : "memory");
+    else asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+  }
+  {
+    auto key = st.keys(lds, rb * LT_TILE);
+#pragma unroll
+    for (int n = 0; n < LT_NK; ++n) st.q[st.step(n)] = key(n);
+  }
+  lt_meet();  // (the ring is free, or its first half)
+  int up[LT_MAX_TREE / LT_THREADS];
+  if (last) {
+    tree_rows(top_tree);
+#pragma unroll
+    for (int x = 0; x < LT_MAX_TREE / LT_THREADS; ++x) up[x] = a.parent[it.n0 + std::min(x * LT_THREADS + tid, it.M - 1)];
+  }
+  if constexpr (RB == 4) {
+    request(0);
+    request(1);
+  }
   const float c2 = g.c2;
   if (last) {
     if (tid < 2) mem.odd[tid] = 0u;
@@ -505,31 +530,42 @@ LatPlan lat_tree_plan(const int32_t* no, const int64_t* pl, int32_t B, int32_t H
   int64_t longest = 1;
   for (int s = 0; s < B; ++s)
     if (no[s + 1] > no[s]) longest = std::max(longest, (pl[s] + 63) >> 6);
-  constexpr double FIXED = 6.0, CU = 256.0, REC = 0.0012;  // us of an item without pages, compute units, us a row's record (all together)
-  auto page_us = [](int64_t rows) { return rows > 64 ? 3.0 : rows > 32 ? 1.6 : 1.3; };
+  constexpr double FIXED = 9.0, CU = 256.0, REC = 0.0010;  // us of an item without pages, compute units, us a row's record (all together)
+  auto page_us = [](int64_t rows) { return rows > 64 ? 3.4 : rows > 32 ? 2.6 : 2.4; };
   LatPlan best = {};
   best.sp_max = 1;
   double best_us = 0.0;
-  for (int64_t k = 1; k <= longest; k = k < 4 ? k + 1 : k < 8 ? k + 2 : k + k / 4) {  // splits of the longest sequence
-    const int64_t per = (longest + k - 1) / k;
+  // (whether a sequence's splits fit `per` pages each)
+  auto consider = [&](int64_t per) {
     double sum = 0.0, most = 0.0, records = 0.0;
     int64_t items = 0, sp_max = 1;
     for (int s = 0; s < B; ++s) {
       const int64_t rows = (int64_t)(no[s + 1] - no[s]) * Hq;
       if (rows == 0) continue;
       const int64_t pages = (pl[s] + 63) >> 6, n_sp = lt_splits(pages, (int)per), groups = (rows + LT_GROUP - 1) / LT_GROUP;
-      const double item = FIXED + page_us(rows) * (double)((pages + n_sp - 1) / n_sp);
+      const double item = FIXED + page_us(rows) * ((double)pages / (double)n_sp);
       sum += item * (double)(n_sp * groups);
       most = std::max(most, item);
       items += n_sp * groups;
       sp_max = std::max(sp_max, n_sp);
       if (n_sp > 1) records += (double)(rows * n_sp);
     }
-    const double rounds = std::max(1.0, (double)items / CU);
-    double us = std::max(most, sum / CU + (rounds > 1.0 ? 0.5 * most : 0.0));
+    const double rounds = (double)items / CU;
+    double us = rounds <= 1.0 ? most : std::max(most, sum / CU + 0.5 * most);
     if (sp_max > 1) us += 4.0 + REC * records;
     if (best.per == 0 || us < best_us) best_us = us, best.per = (int)per, best.sp_max = (int)sp_max;
-    if (items > 8 * CU) break;
+    return items;
+  };
+  consider(longest);
+  // the finest cuts whose items fill the compute units once, one and a half times, ...
+  for (int64_t target : {32, 64, 128, 192, 256, 512, 1024}) {
+    int64_t lo = 1, hi = longest;  // items(hi) <= target, or hi is the coarsest
+    while (lo < hi) {
+      const int64_t mid = (lo + hi) / 2;
+      if (consider(mid) <= target) hi = mid;
+      else lo = mid + 1;
+    }
+    if (lo == 1) break;
   }
   // runs of items for the XCDs: equal numbers while each has a compute unit, equal times otherwise
   auto items_of = [&](int s, double* cost) {
