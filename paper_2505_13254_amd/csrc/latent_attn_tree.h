@@ -93,6 +93,11 @@ __device__ __forceinline__ void lt_fetch(const char* from, unsigned off, unsigne
 #undef LT_LOAD
 }
 static_assert(LT_LOADS == 9, "lt_fetch");
+// 16 bytes at `off` behind an address, lane l's to the wave's `to` + 16 l.
+__device__ __forceinline__ void lt_fetch_row(const char* from, unsigned off, unsigned to) {
+  unsigned saved;
+  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3\n\ts_mov_b32 m0, %0" : "=&s"(saved) : "s"(to), "v"(off), "s"(from) : "memory");
+}
 // 16 bytes of each lane's own address, lane l's to the wave's `to` + 16 l.
 __device__ __forceinline__ void lt_fetch_one(const void* from, unsigned to) {
   unsigned saved;

@@ -216,11 +216,17 @@ __device__ __forceinline__ void lt_run(const LtArgs& g, const LtItem& it, LtLds&
     const bf16_t* const q = static_cast<const bf16_t*>(a.q.p) + (it.n0 + i) * a.q.row + h * a.q.head;
     const bf16_t* const r = static_cast<const bf16_t*>(a.q_rope.p) + (it.n0 + i) * a.q_rope.row + h * a.q_rope.head;
     const unsigned to = lds0 + rb * LT_TILE;
-#pragma unroll 1
+#pragma unroll 3
     for (int x = first_kb; x < first_kb + MINE; ++x) {
-      const int from = x < 32 ? x : 8 * (x - 32) + (lane >> 3);  // whose row
-      const int64_t at = __shfl((int64_t)(uintptr_t)(x < 32 ? q : r), from);
-      lt_fetch_one(reinterpret_cast<const char*>(at) + 16 * (x < 32 ? lane ^ (int)lt_key(x) : (lane & 7) ^ ((from >> 1) & 7)), to + 1024 * x);
+      if (x < 32) {
+        const uint64_t from = (uint64_t)(unsigned)__builtin_amdgcn_readlane((int)(uintptr_t)q, x) |
+                              (uint64_t)(unsigned)__builtin_amdgcn_readlane((int)((uintptr_t)q >> 32), x) << 32;
+        lt_fetch_row(reinterpret_cast<const char*>(from), 16 * (lane ^ (int)lt_key(x)), to + 1024 * x);
+      } else {
+        const int row8 = 8 * (x - 32) + (lane >> 3);
+        const int64_t from = __shfl((int64_t)(uintptr_t)r, row8);
+        lt_fetch_one(reinterpret_cast<const char*>(from) + 16 * ((lane & 7) ^ ((row8 >> 1) & 7)), to + 1024 * x);
+      }
     }
   }
   if constexpr (RB == 4) {
