@@ -16,7 +16,7 @@ SOURCES = ["api.cpp", "entropy_topk.hip", "tree_prune.hip", "tree_attention.hip"
            "verify_accept.hip", "tree_expand.hip", "adaptive_control.hip", "kv_commit.hip", "tree_validate.hip",
            "rotary.hip", "kv_cache_mx.hip", "tree_attention_mx.hip",
            "tree_attention_mx_e4m3.hip", "tree_attention_mx_e2m1.hip",
-           "block_tables.hip", "latent_rows.hip", "latent_attention.hip", "latent_attn_any.hip", "latent_attn_tree.hip"]
+           "block_tables.hip", "latent_rows.hip", "latent_attention.hip", "latent_attn_any.hip", "latent_attn_tree.hip", "latent_attn_prompt.hip"]
 FLAGS = ["-O3", "-std=c++17", "-fPIC", "--offload-arch=gfx950", "-x", "hip",
          # packed-fp32 instruction selection is switched off for every device function of the library
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

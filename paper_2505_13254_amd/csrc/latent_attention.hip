@@ -32,6 +32,16 @@ static hs_status lat_tree_hosts(const int32_t* no, const int64_t* pl, int32_t B,
   return HS_OK;
 }
 
+// The same of a call on prompts.
+static hs_status lat_prompt_hosts(const int32_t* qo, const int64_t* ko, int32_t B) {
+  HS_REQUIRE(qo[0] == 0 && ko[0] == 0, HS_ERR_SHAPE, "hs_prompt_attention_latent: offsets must begin with 0");
+  for (int s = 0; s < B; ++s) {
+    HS_REQUIRE(qo[s + 1] >= qo[s] && ko[s + 1] >= ko[s], HS_ERR_SHAPE, "hs_prompt_attention_latent: offsets decrease at %d", s);
+    HS_REQUIRE(ko[s + 1] - ko[s] <= LAT_MAX_TOKENS, HS_ERR_UNSUPPORTED, "hs_prompt_attention_latent: sequence %d has %lld keys", s, (long long)(ko[s + 1] - ko[s]));
+  }
+  return HS_OK;
+}
+
 }  // namespace hs
 
 using namespace hs;
@@ -76,13 +86,19 @@ extern "C" hs_status hs_tree_attention_latent(const void* q, int64_t q_stride, i
                    block_table, max_blocks, n_pages, prefix_lens, B, NN, Hq, R, Dr, scale, o, o_stride, o_head_stride, lse};
   if (!lat_tree_matrix(a, dt)) return lat_tree_any(a, dt, static_cast<hipStream_t>(stream));
   const LatPlan p = lat_tree_plan(host_node_offsets, host_prefix_lens, B, Hq);
+  if (p.grid >= LAT_MAX_GRID) return lat_tree_any(a, dt, static_cast<hipStream_t>(stream));
   const size_t need = lat_tree_bytes(p, (int64_t)NN * Hq);
   HS_REQUIRE(need == 0 || (workspace != nullptr && workspace_bytes >= need && reinterpret_cast<uintptr_t>(workspace) % 256 == 0), HS_ERR_WORKSPACE,
              "hs_tree_attention_latent: needs %zu bytes of workspace, got %zu", need, workspace_bytes);
   return lat_tree_launch(a, p, workspace, static_cast<hipStream_t>(stream));
 }
 
-extern "C" size_t hs_prompt_attention_latent_workspace(const int32_t* host_q_offsets, const int64_t* host_kv_offsets, int32_t B, int32_t H, int32_t Dv) { return 0; }
+extern "C" size_t hs_prompt_attention_latent_workspace(const int32_t* host_q_offsets, const int64_t* host_kv_offsets, int32_t B, int32_t H, int32_t Dv) {
+  clear_error();
+  if (B < 1 || H < 1 || Dv != 128 || host_q_offsets == nullptr || host_kv_offsets == nullptr) return 0;
+  if (lat_prompt_hosts(host_q_offsets, host_kv_offsets, B) != HS_OK || (int64_t)host_q_offsets[B] * H >= LAT_MAX_ROWS) return 0;
+  return lat_prompt_bytes(lat_prompt_plan(host_q_offsets, host_kv_offsets, B, H), (int64_t)host_q_offsets[B] * H);
+}
 
 extern "C" hs_status hs_prompt_attention_latent(const void* q, int64_t q_stride, int64_t q_head_stride, const void* q_rope, int64_t q_rope_stride,
                                                 int64_t q_rope_head_stride, const void* k, int64_t k_stride, int64_t k_head_stride, const void* k_rope,
@@ -97,15 +113,10 @@ extern "C" hs_status hs_prompt_attention_latent(const void* q, int64_t q_stride,
   HS_REQUIRE(Dn <= 1024 && Dr <= 1024 && Dv <= 1024, HS_ERR_UNSUPPORTED, "hs_prompt_attention_latent: Dn, Dr and Dv must be at most 1024");
   if (B == 0) return HS_OK;
   HS_REQUIRE(host_q_offsets && host_kv_offsets, HS_ERR_NULL, "hs_prompt_attention_latent: NULL host array");
-  HS_REQUIRE(host_q_offsets[0] == 0 && host_kv_offsets[0] == 0, HS_ERR_SHAPE, "hs_prompt_attention_latent: offsets must begin with 0");
+  const hs_status st = lat_prompt_hosts(host_q_offsets, host_kv_offsets, B);
+  if (st != HS_OK) return st;
   bool any = false;
-  for (int s = 0; s < B; ++s) {
-    HS_REQUIRE(host_q_offsets[s + 1] >= host_q_offsets[s] && host_kv_offsets[s + 1] >= host_kv_offsets[s], HS_ERR_SHAPE,
-               "hs_prompt_attention_latent: offsets decrease at %d", s);
-    HS_REQUIRE(host_kv_offsets[s + 1] - host_kv_offsets[s] <= LAT_MAX_TOKENS, HS_ERR_UNSUPPORTED, "hs_prompt_attention_latent: sequence %d has %lld keys", s,
-               (long long)(host_kv_offsets[s + 1] - host_kv_offsets[s]));
-    any = any || (host_q_offsets[s + 1] > host_q_offsets[s] && host_kv_offsets[s + 1] > host_kv_offsets[s]);
-  }
+  for (int s = 0; s < B; ++s) any = any || (host_q_offsets[s + 1] > host_q_offsets[s] && host_kv_offsets[s + 1] > host_kv_offsets[s]);
   const int N = host_q_offsets[B];
   if (N == 0) return HS_OK;
   HS_REQUIRE((int64_t)N * H < LAT_MAX_ROWS, HS_ERR_UNSUPPORTED, "hs_prompt_attention_latent: rows times heads must be below 2^24");
@@ -118,5 +129,11 @@ extern "C" hs_status hs_prompt_attention_latent(const void* q, int64_t q_stride,
              (long long)o_stride, (long long)o_head_stride);
   LatPromptArgs a = {{q, q_stride, q_head_stride}, {q_rope, q_rope_stride, q_rope_head_stride}, {k, k_stride, k_head_stride}, {v, v_stride, v_head_stride}, k_rope,
                      k_rope_stride, q_offsets, kv_offsets, B, N, H, Dn, Dr, Dv, scale, o, o_stride, o_head_stride, lse};
-  return lat_prompt_any(a, dt, static_cast<hipStream_t>(stream));
+  if (!lat_prompt_matrix(a, dt)) return lat_prompt_any(a, dt, static_cast<hipStream_t>(stream));
+  const LatPlan p = lat_prompt_plan(host_q_offsets, host_kv_offsets, B, H);
+  if (p.grid >= LAT_MAX_GRID) return lat_prompt_any(a, dt, static_cast<hipStream_t>(stream));
+  const size_t need = lat_prompt_bytes(p, (int64_t)N * H);
+  HS_REQUIRE(need == 0 || (workspace != nullptr && workspace_bytes >= need && reinterpret_cast<uintptr_t>(workspace) % 256 == 0), HS_ERR_WORKSPACE,
+             "hs_prompt_attention_latent: needs %zu bytes of workspace, got %zu", need, workspace_bytes);
+  return lat_prompt_launch(a, p, workspace, static_cast<hipStream_t>(stream));
 }

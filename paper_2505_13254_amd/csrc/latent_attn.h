@@ -55,6 +55,16 @@ LatPlan lat_tree_plan(const int32_t* host_node_offsets, const int64_t* host_pref
 size_t lat_tree_bytes(const LatPlan& p, int64_t rows);
 hs_status lat_tree_launch(const LatTreeArgs& a, const LatPlan& p, void* workspace, hipStream_t stream);
 
+// latent_attn_prompt.hip: bfloat16, Dn = 128, Dr = 64, Dv = 128, everything aligned to 16 bytes, on the matrix cores.  (A plan's `per` are tiles of 64 keys, `grid`
+// the items.)
+bool lat_prompt_matrix(const LatPromptArgs& a, hs_dtype dt);
+LatPlan lat_prompt_plan(const int32_t* host_q_offsets, const int64_t* host_kv_offsets, int32_t B, int32_t H);
+size_t lat_prompt_bytes(const LatPlan& p, int64_t rows);
+hs_status lat_prompt_launch(const LatPromptArgs& a, const LatPlan& p, void* workspace, hipStream_t stream);
+
+// What a launch may have of workgroups (a grid's threads are counted in 32 bits); a call of more, of very many short sequences, takes the other kernel.
+constexpr int64_t LAT_MAX_GRID = (int64_t)1 << 22;
+
 // latent_attn_any.hip: any shape and type, float32 arithmetic throughout.
 hs_status lat_tree_any(const LatTreeArgs& a, hs_dtype dt, hipStream_t stream);
 hs_status lat_prompt_any(const LatPromptArgs& a, hs_dtype dt, hipStream_t stream);
