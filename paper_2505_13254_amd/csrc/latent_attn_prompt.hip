@@ -3,8 +3,8 @@
 // A work item is up to 256 rows of one (sequence, head) and one split of the keys that they see: eight waves of 32 rows each share tiles of 64 keys, which
 // global_load_lds brings into a ring of three.  The products are those of the absorbed form (S^T = K Q^T, O^T += V^T P^T, a lane has a query) on keys of
 // 192 and values of 128 elements; the scores of a 32-key block run beside the softmax of the block before it, and two waves to a SIMD fill each
-// other's waits.  Tiles that some row sees only part of (its own last keys, causally) come last, masked, without that overlap: five of them at most but
-// for sequences with fewer keys than rows.
+// other's waits.  Tiles that some row sees only part of (its own last keys, causally: five tiles at most but for sequences with fewer keys than rows) are
+// masked, and the elements of their values that are no numbers made zero by the wave that fetched them.
 //
 // LDS: a tile is 64 rows of keys (256 bytes), 64 of rotary parts (128) and 64 of values (256); 16-byte chunk c of row r stands at c ^ lt_key(r) (keys, values)
 // or c ^ (r / 2 mod 8), so that fragments' reads fall into different banks.
@@ -37,7 +37,7 @@ struct LpArgs {
 struct LpLds {
   char ring[LP_RING * LP_TILE];
   int64_t out_at[LP_WAVES][32];
-  unsigned odd[2][2];
+  unsigned odd[4][2];  // of the masked tiles: which of their 64 values hold a NaN or an infinity
   int again, found[4];
   int64_t found_wide[2];
   int64_t sums[LP_WAVES];
@@ -232,6 +232,7 @@ __global__ __launch_bounds__(LP_THREADS) void k_lat_prompt(LpArgs gl) {
   __shared__ LpLds mem;
   const LatPromptArgs& a = gl.a;
   LpItem it;
+  if (threadIdx.x < 8) mem.odd[threadIdx.x >> 1][threadIdx.x & 1] = 0u;
   if (!lp_find(gl, it, mem)) return;
   char* const lds = mem.ring;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -287,86 +288,89 @@ __global__ __launch_bounds__(LP_THREADS) void k_lat_prompt(LpArgs gl) {
   }
   st.start(lane);
   const float c2 = gl.c2;
+  // What a wave fetched of a masked tile's values, once it is there: 0 x NaN must not reach rows that do not see them.  (Of keys it does not: masked scores are left
+  // out, whatever they are.)
+  auto mend = [&](int t, unsigned tile) {
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      uint4* const at = reinterpret_cast<uint4*>(lds + tile + LP_VAL + 8192 * x + 1024 * wave + 16 * lane);
+      uint4 w = *at;
+      lt_ushort2 high = {0, 0};
+      unsigned* const e = &w.x;
+#pragma unroll
+      for (int y = 0; y < 4; ++y) high = __builtin_elementwise_max(high, __builtin_bit_cast(lt_ushort2, e[y] & 0x7fff7fffu));
+      if (high[0] >= 0x7f80 || high[1] >= 0x7f80) {
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+          if ((e[y] & 0x7f80u) == 0x7f80u) e[y] &= 0xffff0000u;
+          if ((e[y] & 0x7f800000u) == 0x7f800000u) e[y] &= 0xffffu;
+        }
+        *at = w;
+        atomicOr(&mem.odd[t & 3][x], 1u << r4);
+      }
+    }
+  };
+  // Block b of tile t: scores that the lane's row does not see, and those of values that are no numbers.
+  auto mask = [&](lt_floatx16& S, int t, int b) {
+    if (t < n_un) return;
+    const int sees = vis - 64 * (t_lo + t) - 32 * b - 4 * half;
+    const unsigned odd = mem.odd[t & 3][b] >> (4 * half);
+#pragma unroll
+    for (int v = 0; v < 16; ++v) {
+      const int k = 8 * (v >> 2) + (v & 3);
+      S[v] = k < sees ? S[v] : -HS_INF;
+    }
+    if (odd == 0u) return;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) {
+      const int k = 8 * (v >> 2) + (v & 3);
+      S[v] = k < sees && ((odd >> k) & 1u) ? __builtin_nanf("") : S[v];
+    }
+  };
+  // Into tile t: it is there, whole and mended, and every wave is done with tile t - 2.  (The flags of tile t - 2 are free for t + 2.)
+  auto enter = [&](int t, unsigned tile, bool younger) {
+    if (younger) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LP_LOADS) : "memory");
+    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    if (t >= n_un) mend(t, tile);
+    lt_meet();
+    if (tid < 2) mem.odd[(t + 2) & 3][tid] = 0u;
+  };
   float reference = LT_FLOOR;
 #pragma unroll 1
   for (;;) {
     request(0);
     request(1);
-    if (tid < 4) mem.odd[tid >> 1][tid & 1] = 0u;
     st.clear(reference);
     unsigned here = 0;  // where the tile is in the ring
     auto after = [](unsigned tile) { return tile == (LP_RING - 1) * LP_TILE ? 0u : tile + LP_TILE; };
-    if (n_un > 0) {
-      if (n_all > 1) asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(LP_LOADS) : "memory");
-      else asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+    if (n_all > 0) {
+      enter(0, 0, n_all > 1);
       if (mine_rows > 0) {
         lt_floatx16 S = st.scores(lds, 0, 0), N;
         uint4 P0, P1;
-        for (int t = 0; t + 1 < n_un; ++t) {
+        for (int t = 0; t + 1 < n_all; ++t) {
+          mask(S, t, 0);
           st.ahead(lds, here, 1, S, N, c2, P0, P1);
           st.product(lds, here, 0, P0, P1);
-          asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");  // the next tile is there, every wave is done with the one before this
+          enter(t + 1, after(here), false);
           request(t + 2);
+          mask(N, t, 1);
           st.ahead(lds, after(here), 0, N, S, c2, P0, P1);
           st.product(lds, here, 1, P0, P1);
           here = after(here);
         }
+        mask(S, n_all - 1, 0);
         st.ahead(lds, here, 1, S, N, c2, P0, P1);
         st.product(lds, here, 0, P0, P1);
+        mask(N, n_all - 1, 1);
         st.take(lds, here, 1, N, c2);
       } else {
-        for (int t = 0; t + 1 < n_un; ++t) {
-          asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+        for (int t = 0; t + 1 < n_all; ++t) {
+          enter(t + 1, after(here), false);
           request(t + 2);
           here = after(here);
         }
       }
-      here = after(here);
-    }
-    // ---- tiles that some row sees part of
-#pragma unroll 1
-    for (int t = n_un; t < n_all; ++t) {
-      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-      if (t + 1 > 1 && t + 1 > n_un) request(t + 1);
-      if (tid < 2) mem.odd[(t + 1) & 1][tid] = 0u;
-      // keys and values with a NaN or an infinity are noted, and those elements made zero: 0 x NaN must not reach rows that do not see them
-#pragma unroll
-      for (int x = 0; x < LP_LOADS; ++x) {
-        const int part = x < 2 ? 8192 * x : x == 2 ? LP_ROT : LP_VAL + 8192 * (x - 3);
-        uint4* const at = reinterpret_cast<uint4*>(lds + here + part + 1024 * wave + 16 * lane);
-        uint4 w = *at;
-        lt_ushort2 high = {0, 0};
-        unsigned* const e = &w.x;
-#pragma unroll
-        for (int y = 0; y < 4; ++y) high = __builtin_elementwise_max(high, __builtin_bit_cast(lt_ushort2, e[y] & 0x7fff7fffu));
-        if (high[0] >= 0x7f80 || high[1] >= 0x7f80) {
-          const int r = x == 2 ? r8 : x == 1 || x == 4 ? r4 + 32 : r4;
-#pragma unroll
-          for (int y = 0; y < 4; ++y) {
-            if ((e[y] & 0x7f80u) == 0x7f80u) e[y] &= 0xffff0000u;
-            if ((e[y] & 0x7f800000u) == 0x7f800000u) e[y] &= 0xffffu;
-          }
-          *at = w;
-          atomicOr(&mem.odd[t & 1][r >> 5], 1u << (r & 31));
-        }
-      }
-      lt_meet();
-      if (mine_rows > 0) {
-#pragma unroll 1
-        for (int b = 0; b < 2; ++b) {
-          const int sees = vis - 64 * (t_lo + t) - 32 * b;  // keys of the block that the row sees
-          if (__ballot(sees > 0) == 0ull) continue;
-          const unsigned odd = mem.odd[t & 1][b];
-          lt_floatx16 S = st.scores(lds, here, b);
-#pragma unroll
-          for (int v = 0; v < 16; ++v) {
-            const int k = 8 * (v >> 2) + 4 * half + (v & 3);
-            S[v] = k < sees ? ((odd >> k) & 1u ? __builtin_nanf("") : S[v]) : -HS_INF;
-          }
-          st.take(lds, here, b, S, c2);
-        }
-      }
-      here = after(here);
     }
     // ---- a row whose scores rose too far above its reference?
     if (tid == 0) mem.again = 0;
@@ -375,6 +379,7 @@ __global__ __launch_bounds__(LP_THREADS) void k_lat_prompt(LpArgs gl) {
     lt_meet();
     if (mem.again == 0) break;
     reference = st.seen;
+    if (tid < 8) mem.odd[tid >> 1][tid & 1] = 0u;
     lt_meet();
   }
   if (mine_rows <= 0) return;
@@ -423,41 +428,52 @@ __global__ __launch_bounds__(LP_THREADS) void k_lat_prompt(LpArgs gl) {
   }
 }
 
-// The merge of the splits: a wave to a (row, head), two columns to a lane.
+// The merge of the splits: half a wave to a (row, head), four columns to a lane.
 constexpr int LPM_THREADS = 256;
 __global__ __launch_bounds__(LPM_THREADS) void k_lat_prompt_merge(LpArgs gl) {
   const LatPromptArgs& a = gl.a;
-  const int lane = threadIdx.x & 63;
-  const int64_t row = (int64_t)blockIdx.x * (LPM_THREADS / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if (row >= (int64_t)a.N * a.H) return;
-  const int n = (int)(row / a.H), h = (int)(row - (int64_t)n * a.H);
-  int s = 0;
-  for (int base = 0; base < a.B; base += 64) {
-    const bool below = base + lane < a.B && a.q_offsets[base + lane] <= n;
-    const int c = __builtin_popcountll(__ballot(below));
-    s = base + c - 1;
-    if (c < 64) break;
+  const int lane = threadIdx.x & 31;
+  const unsigned row = (unsigned)blockIdx.x * (LPM_THREADS / 32) + (threadIdx.x >> 5);  // (below 2^24)
+  if (row >= (unsigned)a.N * (unsigned)a.H) return;
+  const int n = (int)(row / (unsigned)a.H), h = (int)(row - (unsigned)n * (unsigned)a.H);
+  int lo = 0, hi = a.B;  // the last sequence that begins at or before the row
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (a.q_offsets[mid] <= n) lo = mid;
+    else hi = mid;
   }
-  s = s < 0 ? 0 : s;
-  const int64_t T = a.kv_offsets[s + 1] - a.kv_offsets[s];
+  const int64_t T = a.kv_offsets[lo + 1] - a.kv_offsets[lo];
   const int n_sp = std::min(lp_splits(T < 0 ? 0 : T, gl.per), gl.sp_max);
   if (n_sp == 1) return;
-  const float* const rec = gl.part + row * gl.sp_max * LP_REC;
-  float m = LT_FLOOR;
-  for (int x = lane; x < n_sp; x += 64) m = fmaxf(m, rec[(int64_t)x * LP_REC + LP_DV]);
-  m = wave_max(m);
-  float total = 0.f, o0 = 0.f, o1 = 0.f;
-#pragma unroll 4
-  for (int x = 0; x < n_sp; ++x) {
-    const float* const r = rec + (int64_t)x * LP_REC;
-    const float w = exp2_fast(r[LP_DV] - m);
-    const float2 v = *reinterpret_cast<const float2*>(r + 2 * lane);
-    total = __builtin_fmaf(w, r[LP_DV + 1], total);
-    o0 = __builtin_fmaf(w, v.x, o0), o1 = __builtin_fmaf(w, v.y, o1);
+  const float* const rec = gl.part + (int64_t)row * gl.sp_max * LP_REC;
+  // (one pass, with the running maximum: the records of four splits at a time)
+  float m = LT_FLOOR, total = 0.f;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int x0 = 0; x0 < n_sp; x0 += 4) {
+    float rm[4], rl[4];
+    float4 v[4];
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      const float* const r = rec + (int64_t)std::min(x0 + x, n_sp - 1) * LP_REC;
+      rm[x] = r[LP_DV];
+      rl[x] = r[LP_DV + 1];
+      v[x] = *reinterpret_cast<const float4*>(r + 4 * lane);
+    }
+    const float up = fmaxf(fmaxf(m, fmaxf(rm[0], rm[1])), fmaxf(rm[2], rm[3])), old = exp2_fast(m - up);
+    total *= old, o.x *= old, o.y *= old, o.z *= old, o.w *= old;
+    m = up;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      const float w = x0 + x < n_sp ? exp2_fast(rm[x] - m) : 0.f;
+      if (x0 + x >= n_sp) break;
+      total = __builtin_fmaf(w, rl[x], total);
+      o.x = __builtin_fmaf(w, v[x].x, o.x), o.y = __builtin_fmaf(w, v[x].y, o.y), o.z = __builtin_fmaf(w, v[x].z, o.z), o.w = __builtin_fmaf(w, v[x].w, o.w);
+    }
   }
   const float inv = total == 0.f ? 0.f : 1.f / total;
-  *reinterpret_cast<unsigned*>(static_cast<bf16_t*>(a.o) + n * a.o_row + h * a.o_head + 2 * lane) =
-      __builtin_bit_cast(unsigned, __builtin_convertvector((lt_floatx2{o0 * inv, o1 * inv}), lt_bf16x2));
+  *reinterpret_cast<uint2*>(static_cast<bf16_t*>(a.o) + n * a.o_row + h * a.o_head + 4 * lane) =
+      make_uint2(__builtin_bit_cast(unsigned, __builtin_convertvector((lt_floatx2{o.x * inv, o.y * inv}), lt_bf16x2)),
+                 __builtin_bit_cast(unsigned, __builtin_convertvector((lt_floatx2{o.z * inv, o.w * inv}), lt_bf16x2)));
   if (lane == 0 && a.lse != nullptr) a.lse[row] = total == 0.f ? -HS_INF : (m + __log2f(total)) * LT_LN2;
 }
 
@@ -519,7 +535,7 @@ hs_status lat_prompt_launch(const LatPromptArgs& a, const LatPlan& p, void* work
   const hs_status st = launch_status("latent prompt attention");
   if (st != HS_OK || p.sp_max == 1) return st;
   const int64_t rows = (int64_t)a.N * a.H;
-  hipLaunchKernelGGL(k_lat_prompt_merge, dim3((unsigned)((rows + LPM_THREADS / 64 - 1) / (LPM_THREADS / 64))), dim3(LPM_THREADS), 0, stream, g);
+  hipLaunchKernelGGL(k_lat_prompt_merge, dim3((unsigned)((rows + LPM_THREADS / 32 - 1) / (LPM_THREADS / 32))), dim3(LPM_THREADS), 0, stream, g);
   return launch_status("latent prompt attention, merge");
 }
 
