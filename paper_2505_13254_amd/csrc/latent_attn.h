@@ -3,6 +3,8 @@
 // Absorbed form: every query head of a tree row scores the same keys, a token's latent c [R] and rotary part r [Dr], and the values
 // are the latents themselves.  Expanded form: every head has keys [Dn] and values [Dv] of its own, the rotary part is shared.
 #pragma once
+#include <string.h>
+
 #include "attn_common.h"
 
 namespace hs {
@@ -47,9 +49,31 @@ struct LatPromptArgs {
 struct LatPlan {
   int per;       // pages of a split at most
   int sp_max;    // splits of a sequence at most
+  int group;     // rows of an item at most
   int64_t first[9];  // the first item of each XCD, and the number of items
   int64_t grid;      // workgroups
 };
+// The last plan of a thread (the layers of a step ask for the same one, and so does a call after its workspace query): of calls of up to 512 sequences.
+template <LatPlan (*PLAN)(const int32_t*, const int64_t*, int32_t, int32_t), int LENS>
+LatPlan lat_remember(const int32_t* rows, const int64_t* lens, int32_t B, int32_t heads) {
+  constexpr int MOST = 512;
+  static thread_local struct {
+    int32_t B = -1, heads;
+    int32_t rows[MOST + 1];
+    int64_t lens[MOST + 1];
+    LatPlan plan;
+  } last;
+  if (B > MOST) return PLAN(rows, lens, B, heads);
+  const size_t n = sizeof(int32_t) * (size_t)(B + 1), m = sizeof(int64_t) * (size_t)(B + LENS);
+  if (last.B != B || last.heads != heads || memcmp(last.rows, rows, n) != 0 || memcmp(last.lens, lens, m) != 0) {
+    last.plan = PLAN(rows, lens, B, heads);
+    last.B = B;
+    last.heads = heads;
+    memcpy(last.rows, rows, n);
+    memcpy(last.lens, lens, m);
+  }
+  return last.plan;
+}
 bool lat_tree_matrix(const LatTreeArgs& a, hs_dtype dt);
 LatPlan lat_tree_plan(const int32_t* host_node_offsets, const int64_t* host_prefix_lens, int32_t B, int32_t Hq);
 size_t lat_tree_bytes(const LatPlan& p, int64_t rows);

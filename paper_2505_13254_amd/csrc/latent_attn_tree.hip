@@ -19,6 +19,7 @@ struct LtArgs {
   float c2;    // scale in octaves
   int per;     // pages of a split at most
   int sp_max;  // splits of a sequence at most; 1: results are written directly
+  int group;   // rows of an item at most: 128, 64 or 32
   float* part;
   int first[LT_XCD + 1];  // the first item of each XCD
 };
@@ -86,7 +87,7 @@ __device__ __forceinline__ bool lt_find(const LtArgs& g, LtItem& it, LtLds& mem)
       M = M < 0 || n0 < 0 ? 0 : std::min(std::min(M, LT_MAX_TREE), a.NN - n0);  // (the host's copies say so)
       M = M < 0 ? 0 : M;
       n_sp = M > 0 ? std::min(lt_splits((L + 63) >> 6, g.per), g.sp_max) : 0;
-      groups = (M * a.Hq + LT_GROUP - 1) / LT_GROUP;
+      groups = (M * a.Hq + g.group - 1) / g.group;
     }
     const int mine = n_sp * groups;
     int to = mine;
@@ -134,7 +135,7 @@ __device__ __forceinline__ void lt_run(const LtArgs& g, const LtItem& it, LtLds&
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane & 31, half = lane >> 5;
   const int rb = RB == 4 ? wave : RB == 2 ? wave & 1 : 0, kh = RB == 4 ? 0 : wave >> 1, first_block = RB == 1 ? 8 * (wave & 1) : 0;
-  const int rows = it.M * a.Hq, row_base = it.rg * LT_GROUP + 32 * rb;
+  const int rows = it.M * a.Hq, row_base = it.rg * g.group + 32 * rb;
   const int row = row_base + col < rows ? row_base + col : rows - 1;  // (rows behind the last repeat it)
   const int i = row / a.Hq, h = row - i * a.Hq;
   const bool last = it.sp == it.n_sp - 1;
@@ -144,7 +145,7 @@ __device__ __forceinline__ void lt_run(const LtArgs& g, const LtItem& it, LtLds&
   const int n_full = n_pages - (rest > 0 ? 1 : 0);
   const int32_t* const table = a.table + (int64_t)it.s * a.max_blocks + p_lo;
   const char* const pool = static_cast<const char*>(a.pool);
-  const bool once = rows <= LT_GROUP;  // nobody else reads the pages
+  const bool once = rows <= g.group;  // nobody else reads the pages
   const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
 
   // ---- requests: the numbers of the pages, Q, the tree's last 64 rows that the group sees and the parents, the first page
@@ -196,7 +197,7 @@ __device__ __forceinline__ void lt_run(const LtArgs& g, const LtItem& it, LtLds&
       }
     }
   };
-  const int top_tree = (std::min(rows, (it.rg + 1) * LT_GROUP) - 1) / a.Hq / 64;
+  const int top_tree = (std::min(rows, (it.rg + 1) * g.group) - 1) / a.Hq / 64;
   const unsigned off = LT_ROW * wave + 16 * (lane ^ lt_key(wave)), rot = lt_rot_off(lane, wave);
   // 32-key tile n of the split: page n / 2, in slot (n + 2) % 4 of the ring
   auto request = [&](int n) {
@@ -474,20 +475,22 @@ __global__ __launch_bounds__(LT_THREADS, 1) void k_lat_tree(LtArgs g) {
   __shared__ LtLds mem;
   LtItem it;
   if (!lt_find(g, it, mem)) return;
-  const int left = it.M * g.a.Hq - it.rg * LT_GROUP;
+  const int left = std::min(g.group, it.M * g.a.Hq - it.rg * g.group);
   if (left > 64) lt_run<4>(g, it, mem);
   else if (left > 32) lt_run<2>(g, it, mem);
   else lt_run<1>(g, it, mem);
 }
 
-// The merge of the splits: a wave to a row.
+// The merge of the splits: SHARE waves to a row, which take its records in turn, four at a time each.
 constexpr int LTM_THREADS = 256;
+template <int SHARE>
 __global__ __launch_bounds__(LTM_THREADS) void k_lat_tree_merge(LtArgs g) {
+  __shared__ float sums[SHARE > 1 ? SHARE : 1][64][10];
   const LatTreeArgs& a = g.a;
-  const int lane = threadIdx.x & 63;
-  const int64_t row = (int64_t)blockIdx.x * (LTM_THREADS / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if (row >= (int64_t)a.NN * a.Hq) return;
-  const int n = (int)(row / a.Hq), h = (int)(row - (int64_t)n * a.Hq);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), way = wave % SHARE;
+  const int64_t row = (int64_t)blockIdx.x * (LTM_THREADS / 64 / SHARE) + wave / SHARE;
+  if (row >= (int64_t)a.NN * a.Hq) return;  // (SHARE > 1: the same for the workgroup)
+  const int n = (int)((unsigned)row / (unsigned)a.Hq), h = (int)row - n * a.Hq;
   int s = 0;
   for (int base = 0; base < a.B; base += 64) {
     const bool below = base + lane < a.B && a.node_offsets[base + lane] <= n;
@@ -502,19 +505,56 @@ __global__ __launch_bounds__(LTM_THREADS) void k_lat_tree_merge(LtArgs g) {
   const int n_sp = std::min(lt_splits((L + 63) >> 6, g.per), g.sp_max);
   if (n_sp == 1) return;
   const float* const rec = g.part + row * g.sp_max * LT_REC;
-  float m = LT_FLOOR;
-  for (int x = lane; x < n_sp; x += 64) m = fmaxf(m, rec[(int64_t)x * LT_REC + LT_R]);
-  m = wave_max(m);
-  float total = 0.f;
+  float m = LT_FLOOR, total = 0.f;
   float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-  for (int x = 0; x < n_sp; ++x) {
-    const float* const r = rec + (int64_t)x * LT_REC;
-    const float w = exp2_fast(r[LT_R] - m);
-    const float4 lo = *reinterpret_cast<const float4*>(r + 8 * lane), hi = *reinterpret_cast<const float4*>(r + 8 * lane + 4);
-    total = __builtin_fmaf(w, r[LT_R + 1], total);
-    acc[0] = __builtin_fmaf(w, lo.x, acc[0]), acc[1] = __builtin_fmaf(w, lo.y, acc[1]), acc[2] = __builtin_fmaf(w, lo.z, acc[2]), acc[3] = __builtin_fmaf(w, lo.w, acc[3]);
-    acc[4] = __builtin_fmaf(w, hi.x, acc[4]), acc[5] = __builtin_fmaf(w, hi.y, acc[5]), acc[6] = __builtin_fmaf(w, hi.z, acc[6]), acc[7] = __builtin_fmaf(w, hi.w, acc[7]);
+  for (int x0 = way; x0 < n_sp; x0 += 4 * SHARE) {
+    float rm[4], rl[4];
+    float4 v[4][2];
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      const float* const r = rec + (int64_t)std::min(x0 + x * SHARE, n_sp - 1) * LT_REC;
+      rm[x] = r[LT_R];
+      rl[x] = r[LT_R + 1];
+      v[x][0] = *reinterpret_cast<const float4*>(r + 8 * lane);
+      v[x][1] = *reinterpret_cast<const float4*>(r + 8 * lane + 4);
+    }
+    const float up = fmaxf(fmaxf(m, fmaxf(rm[0], rm[1])), fmaxf(rm[2], rm[3])), old = exp2_fast(m - up);  // (records that stand for no split repeat the last)
+    total *= old;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) acc[e] *= old;
+    m = up;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      if (x0 + x * SHARE >= n_sp) break;
+      const float w = exp2_fast(rm[x] - m);
+      const float f[8] = {v[x][0].x, v[x][0].y, v[x][0].z, v[x][0].w, v[x][1].x, v[x][1].y, v[x][1].z, v[x][1].w};
+      total = __builtin_fmaf(w, rl[x], total);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) acc[e] = __builtin_fmaf(w, f[e], acc[e]);
+    }
+  }
+  if constexpr (SHARE > 1) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sums[way][lane][e] = acc[e];
+    sums[way][lane][8] = m;
+    sums[way][lane][9] = total;
+    __syncthreads();
+    if (way != 0) return;
+    float up = m;
+#pragma unroll
+    for (int w = 1; w < SHARE; ++w) up = fmaxf(up, sums[w][lane][8]);
+    const float own = exp2_fast(m - up);
+    total *= own;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) acc[e] *= own;
+#pragma unroll
+    for (int w = 1; w < SHARE; ++w) {
+      const float f = exp2_fast(sums[w][lane][8] - up);
+      total = __builtin_fmaf(f, sums[w][lane][9], total);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) acc[e] = __builtin_fmaf(f, sums[w][lane][e], acc[e]);
+    }
+    m = up;
   }
   const float inv = 1.f / total;
   unsigned w[4];
@@ -536,50 +576,63 @@ LatPlan lat_tree_plan(const int32_t* no, const int64_t* pl, int32_t B, int32_t H
   int64_t longest = 1;
   for (int s = 0; s < B; ++s)
     if (no[s + 1] > no[s]) longest = std::max(longest, (pl[s] + 63) >> 6);
-  constexpr double FIXED = 9.0, CU = 256.0, REC = 0.0010;  // us of an item without pages, compute units, us a row's record (all together)
-  auto page_us = [](int64_t rows) { return rows > 64 ? 3.4 : rows > 32 ? 2.6 : 2.4; };
+  constexpr double CU = 256.0, REC = 0.0010, SPLIT = 0.2;  // compute units; us a row's record (all together), and a split in the merge
+  // us of an item without pages, and of a page: by what the waves do with one, or by its share of what is read at a time (pages that several groups share come from
+  // the second-level cache, no faster: 250 items' pages on their way are more than it holds)
+  auto block = [](int64_t rows, int group) { return std::min<int64_t>(rows, group) > 64 ? 2 : std::min<int64_t>(rows, group) > 32 ? 1 : 0; };
+  constexpr double FIXED[3] = {10.0, 12.0, 15.0}, PAGE[3] = {1.3, 1.7, 3.0}, ONCE = 0.0094, SHARED = 0.0129;
+  auto item_us = [&](int64_t rows, int group, double pages, double busy) {
+    const int k = block(rows, group);
+    return FIXED[k] + pages * std::max(PAGE[k], busy * (rows <= group ? ONCE : SHARED));
+  };
   LatPlan best = {};
   best.sp_max = 1;
-  double best_us = 0.0;
-  // (whether a sequence's splits fit `per` pages each)
-  auto consider = [&](int64_t per) {
-    double sum = 0.0, most = 0.0, records = 0.0;
+  double best_us = 0.0, best_busy = CU;
+  auto consider = [&](int64_t per, int group) {
     int64_t items = 0, sp_max = 1;
+    double records = 0.0;
     for (int s = 0; s < B; ++s) {
-      const int64_t rows = (int64_t)(no[s + 1] - no[s]) * Hq;
+      const int64_t rows = (int64_t)(no[s + 1] - no[s]) * Hq, n_sp = lt_splits((pl[s] + 63) >> 6, (int)per);
       if (rows == 0) continue;
-      const int64_t pages = (pl[s] + 63) >> 6, n_sp = lt_splits(pages, (int)per), groups = (rows + LT_GROUP - 1) / LT_GROUP;
-      const double item = FIXED + page_us(rows) * ((double)pages / (double)n_sp);
-      sum += item * (double)(n_sp * groups);
-      most = std::max(most, item);
-      items += n_sp * groups;
+      items += n_sp * ((rows + group - 1) / group);
       sp_max = std::max(sp_max, n_sp);
       if (n_sp > 1) records += (double)(rows * n_sp);
     }
-    const double rounds = (double)items / CU;
-    double us = rounds <= 1.0 ? most : std::max(most, sum / CU + 0.5 * most);
-    if (sp_max > 1) us += 4.0 + REC * records;
-    if (best.per == 0 || us < best_us) best_us = us, best.per = (int)per, best.sp_max = (int)sp_max;
+    const double busy = std::min(CU, (double)items);
+    double sum = 0.0, most = 0.0;
+    for (int s = 0; s < B; ++s) {
+      const int64_t rows = (int64_t)(no[s + 1] - no[s]) * Hq, pages = (pl[s] + 63) >> 6, n_sp = lt_splits(pages, (int)per);
+      if (rows == 0) continue;
+      const double item = item_us(rows, group, (double)pages / (double)n_sp, busy);
+      sum += item * (double)(n_sp * ((rows + group - 1) / group));
+      most = std::max(most, item);
+    }
+    double us = (double)items <= CU ? most : std::max(most, sum / CU + 0.5 * most);
+    if (sp_max > 1) us += 4.0 + REC * records + SPLIT * (double)sp_max;
+    if (best.per == 0 || us < best_us) best_us = us, best_busy = busy, best.per = (int)per, best.sp_max = (int)sp_max, best.group = group;
     return items;
   };
-  consider(longest);
-  // the finest cuts whose items fill the compute units once, one and a half times, ...
-  for (int64_t target : {32, 64, 128, 192, 256, 512, 1024}) {
-    int64_t lo = 1, hi = longest;  // items(hi) <= target, or hi is the coarsest
-    while (lo < hi) {
-      const int64_t mid = (lo + hi) / 2;
-      if (consider(mid) <= target) hi = mid;
-      else lo = mid + 1;
+  for (int group : {LT_GROUP, LT_GROUP / 2, LT_GROUP / 4}) {
+    const bool few = consider(longest, group) <= 128;
+    // the finest cuts whose items fill the compute units once, one and a half times, ...
+    for (int64_t target : {32, 64, 128, 192, 256, 512, 1024}) {
+      int64_t lo = 1, hi = longest;  // items(hi) <= target, or hi is the coarsest
+      while (lo < hi) {
+        const int64_t mid = (lo + hi) / 2;
+        if (consider(mid, group) <= target) hi = mid;
+        else lo = mid + 1;
+      }
+      if (lo == 1) break;
     }
-    if (lo == 1) break;
+    if (!few || (int64_t)no[B] * Hq <= group / 2) break;  // smaller groups are for calls of few items
   }
   // runs of items for the XCDs: equal numbers while each has a compute unit, equal times otherwise
   auto items_of = [&](int s, double* cost) {
     const int64_t rows = (int64_t)(no[s + 1] - no[s]) * Hq;
     if (rows == 0) return (int64_t)0;
     const int64_t pages = (pl[s] + 63) >> 6, n_sp = lt_splits(pages, best.per);
-    *cost = FIXED + page_us(rows) * (double)((pages + n_sp - 1) / n_sp);
-    return n_sp * ((rows + LT_GROUP - 1) / LT_GROUP);
+    *cost = item_us(rows, best.group, (double)pages / (double)n_sp, best_busy);
+    return n_sp * ((rows + best.group - 1) / best.group);
   };
   int64_t items = 0;
   double sum = 0.0, cost = 0.0;
@@ -611,13 +664,14 @@ LatPlan lat_tree_plan(const int32_t* no, const int64_t* pl, int32_t B, int32_t H
 size_t lat_tree_bytes(const LatPlan& p, int64_t rows) { return p.sp_max > 1 ? align_up((size_t)rows * p.sp_max * LT_REC * 4, 256) : 0; }
 
 hs_status lat_tree_launch(const LatTreeArgs& a, const LatPlan& p, void* workspace, hipStream_t stream) {
-  LtArgs g = {a, a.scale * LT_LOG2E, p.per, p.sp_max, static_cast<float*>(workspace), {}};
+  LtArgs g = {a, a.scale * LT_LOG2E, p.per, p.sp_max, p.group, static_cast<float*>(workspace), {}};
   for (int x = 0; x <= LT_XCD; ++x) g.first[x] = (int)p.first[x];
   hipLaunchKernelGGL(k_lat_tree, dim3((unsigned)p.grid), dim3(LT_THREADS), 0, stream, g);
   const hs_status st = launch_status("latent attention");
   if (st != HS_OK || p.sp_max == 1) return st;
   const int64_t rows = (int64_t)a.NN * a.Hq;
-  hipLaunchKernelGGL(k_lat_tree_merge, dim3((unsigned)((rows + LTM_THREADS / 64 - 1) / (LTM_THREADS / 64))), dim3(LTM_THREADS), 0, stream, g);
+  if (p.sp_max > 4) hipLaunchKernelGGL(k_lat_tree_merge<4>, dim3((unsigned)rows), dim3(LTM_THREADS), 0, stream, g);
+  else hipLaunchKernelGGL(k_lat_tree_merge<1>, dim3((unsigned)((rows + 3) / 4)), dim3(LTM_THREADS), 0, stream, g);
   return launch_status("latent attention, merge");
 }
 
