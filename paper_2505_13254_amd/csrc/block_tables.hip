@@ -150,8 +150,11 @@ __global__ __launch_bounds__(BT_THREADS) void k_block_tables(BtArgs a) {
 }
 
 // ------------------------------------------------------------------------------------------------ slots of rows
-// A workgroup takes 1024 rows, the sequences' first rows in LDS where they fit.
-constexpr int SM_THREADS = 256, SM_ROWS = 4, SM_LDS = 4096;
+// A thread takes four neighbouring rows (of accepted paths one, which is scanned), finds the sequence of the first by a binary search and walks on from there; first rows, lengths and page counts of the
+// sequences stand in LDS where they fit, so that a row waits for two trips to memory, these and its page's number (and the path of an accepted row).  (A
+// search a row: 1.5 million rows of 512 sequences 14.8 us.)
+constexpr int SM_THREADS = 256, SM_LDS = 1024;
+constexpr int SM_GRID = 1024;  // workgroups at most: beyond that each takes several runs of rows, and reads the sequences once
 
 struct SmArgs {
   const int32_t* node_offsets;
@@ -166,69 +169,95 @@ struct SmArgs {
   int64_t* slots;
   int64_t* new_lens;
 };
+struct SmLds {
+  int off[SM_LDS + 1], held[SM_LDS], accepted[SM_LDS];
+  int64_t len[SM_LDS];
+};
 
-__device__ __forceinline__ int64_t sm_room(const SmArgs& a, int s) {  // tokens that a sequence's pages hold
-  int h = a.max_blocks;
-  if (a.held != nullptr) {
-    h = a.held[s];
-    h = h < 0 ? 0 : (h > a.max_blocks ? a.max_blocks : h);
-  }
-  return (int64_t)h * a.page_tokens;
+__device__ __forceinline__ int sm_accepted(const SmArgs& a, int n) { return n < 0 ? 0 : (n < a.max_depth ? n : a.max_depth); }
+__device__ __forceinline__ int64_t sm_room(const SmArgs& a, int held) {  // tokens that a sequence's pages hold
+  return (int64_t)(held < 0 ? 0 : (held > a.max_blocks ? a.max_blocks : held)) * a.page_tokens;
 }
 
+template <bool PATH>
+constexpr int SM_ROWS = PATH ? 1 : 4;
+template <bool PATH>
 __global__ __launch_bounds__(SM_THREADS) void k_slot_map(SmArgs a) {
-  __shared__ int off_lds[SM_LDS + 1];
+  constexpr int ROWS = SM_ROWS<PATH>;
+  __shared__ SmLds mem;
   const int tid = threadIdx.x;
   const bool small = a.B <= SM_LDS;
   if (small) {
-    for (int s = tid; s <= a.B; s += SM_THREADS) off_lds[s] = a.node_offsets[s];
+    for (int s = tid; s <= a.B; s += SM_THREADS) {
+      mem.off[s] = a.node_offsets[s];
+      if (s < a.B) {
+        mem.len[s] = a.cache_lens[s];
+        mem.held[s] = a.held != nullptr ? a.held[s] : a.max_blocks;
+        if (PATH) mem.accepted[s] = a.accept_len[s];
+      }
+    }
     __syncthreads();
   }
-  auto off = [&](int s) { return small ? off_lds[s] : a.node_offsets[s]; };
-  const int last = a.B > 0 ? off(a.B) : 0;
-#pragma unroll
-  for (int x = 0; x < SM_ROWS; ++x) {
-    const int64_t row = ((int64_t)blockIdx.x * SM_ROWS + x) * SM_THREADS + tid;
-    if (row >= a.NN) break;
-    int64_t slot = -1;
-    if (row < last) {
-      int lo = 0, hi = a.B;  // the last sequence that begins at or before the row
-      while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (off(mid) <= row) lo = mid;
+  auto off = [&](int s) { return small ? mem.off[s] : a.node_offsets[s]; };
+  auto len = [&](int s) { return small ? mem.len[s] : a.cache_lens[s]; };
+  auto room = [&](int s) { return sm_room(a, small ? mem.held[s] : a.held != nullptr ? a.held[s] : a.max_blocks); };
+  auto accepted = [&](int s) { return sm_accepted(a, small ? mem.accepted[s] : a.accept_len[s]); };
+  const int last = off(a.B);
+  const bool wide = reinterpret_cast<uintptr_t>(a.slots) % 16 == 0;
+  for (int64_t first = ((int64_t)blockIdx.x * SM_THREADS + tid) * ROWS; first < a.NN; first += (int64_t)gridDim.x * SM_THREADS * ROWS) {
+    int64_t slot[ROWS];
+    int s = 0, end = 0;
+    if (first < last) {
+      int hi = a.B;  // the last sequence that begins at or before the row
+      while (hi - s > 1) {
+        const int mid = (s + hi) >> 1;
+        if (off(mid) <= first) s = mid;
         else hi = mid;
       }
-      const int s = lo, local = (int)row - off(s);
+      end = off(s + 1);
+    }
+#pragma unroll
+    for (int x = 0; x < ROWS; ++x) {
+      const int64_t row = first + x;
+      slot[x] = -1;
+      if (row >= last || row >= a.NN) continue;
+      while (row >= end && s + 1 < a.B) end = off(++s + 1);
+      const int local = (int)row - off(s);
       int at = local;
-      if (a.accept_path != nullptr && local > 0) {  // the row's place in the accepted path
-        int n = a.accept_len[s];
-        n = n < a.max_depth ? n : a.max_depth;
+      if (PATH && local > 0) {  // the row's place in the accepted path
+        const int n = accepted(s);
         const int32_t* const path = a.accept_path + (int64_t)s * a.max_depth;
         at = -1;
-        for (int j = 0; j < n; ++j)
-          if (path[j] == local) {
-            at = j + 1;
-            break;
-          }
+        for (int j0 = 0; j0 < n && at < 0; j0 += 8) {
+          int p[8];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) p[j] = path[j0 + j < n ? j0 + j : n - 1];
+#pragma unroll
+          for (int j = 7; j >= 0; --j) at = j0 + j < n && p[j] == local ? j0 + j + 1 : at;  // (the first place that names the row)
+        }
       }
-      const int64_t token = a.cache_lens[s] + at;
-      if (at >= 0 && token >= 0 && token < sm_room(a, s)) {
-        const int64_t block = token >> 32 == 0 ? (int64_t)((unsigned)token / (unsigned)a.page_tokens) : token / a.page_tokens;
-        const int page = a.table[(int64_t)s * a.max_blocks + block];
-        if (page >= 0 && page < a.n_pages) slot = (int64_t)page * a.page_tokens + (token - block * a.page_tokens);
-      }
+      const int64_t token = len(s) + at;
+      if (at < 0 || token < 0 || token >= room(s)) continue;
+      const int64_t block = token >> 32 == 0 ? (int64_t)((unsigned)token / (unsigned)a.page_tokens) : token / a.page_tokens;
+      const int page = a.table[(int64_t)s * a.max_blocks + block];
+      if (page >= 0 && page < a.n_pages) slot[x] = (int64_t)page * a.page_tokens + (token - block * a.page_tokens);
     }
-    a.slots[row] = slot;
+    if (ROWS == 4 && wide && first + 3 < a.NN) {
+      reinterpret_cast<longlong2*>(a.slots + first)[0] = make_longlong2(slot[0], slot[1 % ROWS]);
+      reinterpret_cast<longlong2*>(a.slots + first)[1] = make_longlong2(slot[2 % ROWS], slot[3 % ROWS]);
+      continue;
+    }
+#pragma unroll
+    for (int x = 0; x < ROWS; ++x)
+      if (first + x < a.NN) a.slots[first + x] = slot[x];
   }
   if (a.new_lens == nullptr) return;
-  for (int64_t s = (int64_t)blockIdx.x * SM_THREADS + tid; s < a.B; s += (int64_t)gridDim.x * SM_THREADS) {
-    int64_t n = off((int)s + 1) - off((int)s);
-    if (a.accept_path != nullptr && n > 0) {
-      const int k = a.accept_len[s];
-      n = 1 + (k < 0 ? 0 : (k < a.max_depth ? k : a.max_depth));
-    }
-    const int64_t len = a.cache_lens[s], room = sm_room(a, (int)s);
-    a.new_lens[s] = len + n <= room ? len + n : (len > room ? len : room);
+  for (int64_t i = (int64_t)blockIdx.x * SM_THREADS + tid; i < a.B; i += (int64_t)gridDim.x * SM_THREADS) {
+    const int q = (int)i;
+    int64_t n = off(q + 1) - off(q);
+    if (PATH && n > 0) n = 1 + accepted(q);
+    const int64_t l = len(q), most = room(q);
+    a.new_lens[q] = l + n <= most ? l + n : (l > most ? l : most);
   }
 }
 
@@ -276,8 +305,9 @@ extern "C" hs_status hs_slot_map(const int32_t* node_offsets, int32_t NN, const 
     HS_REQUIRE(x + 8 * (uintptr_t)B <= y || y + 8 * (uintptr_t)B <= x, HS_ERR_SHAPE, "hs_slot_map: new_lens must not overlap cache_lens");
   }
   SmArgs a = {node_offsets, NN, accept_path, accept_len, max_depth, block_table, max_blocks, page_tokens, n_pages, B, held, cache_lens, slots, new_lens};
-  int64_t grid = ((int64_t)NN + SM_THREADS * SM_ROWS - 1) / (SM_THREADS * SM_ROWS);
-  if (grid < 1) grid = 1;
-  hipLaunchKernelGGL(k_slot_map, dim3((unsigned)grid), dim3(SM_THREADS), 0, static_cast<hipStream_t>(stream), a);
+  const int run = SM_THREADS * (accept_path != nullptr ? SM_ROWS<true> : SM_ROWS<false>);
+  const int64_t runs = ((int64_t)NN + run - 1) / run, grid = runs < 1 ? 1 : (runs > SM_GRID ? SM_GRID : runs);
+  if (accept_path != nullptr) hipLaunchKernelGGL(k_slot_map<true>, dim3((unsigned)grid), dim3(SM_THREADS), 0, static_cast<hipStream_t>(stream), a);
+  else hipLaunchKernelGGL(k_slot_map<false>, dim3((unsigned)grid), dim3(SM_THREADS), 0, static_cast<hipStream_t>(stream), a);
   return launch_status("slot map");
 }
