@@ -271,8 +271,8 @@ extern "C" hs_status hs_block_tables(const int64_t* want, int32_t page_tokens, i
   clear_error();
   HS_REQUIRE(B >= 0 && page_tokens >= 1 && max_blocks >= 0 && n_pages >= 0, HS_ERR_SHAPE, "hs_block_tables: B=%d page_tokens=%d max_blocks=%d n_pages=%d", B,
              page_tokens, max_blocks, n_pages);
-  HS_REQUIRE((int64_t)B * (max_blocks > 0 ? max_blocks : 1) < (int64_t)1 << 30 && n_pages < 1 << 30, HS_ERR_UNSUPPORTED,
-             "hs_block_tables: B * max_blocks and n_pages must be below 2^30");
+  HS_REQUIRE((int64_t)B * (max_blocks > 0 ? max_blocks : 1) < (int64_t)1 << 30 && n_pages < 1 << 30 && B <= 1 << 20, HS_ERR_UNSUPPORTED,
+             "hs_block_tables: B * max_blocks and n_pages must be below 2^30, B at most 2^20");
   if (B == 0) return HS_OK;
   HS_REQUIRE(want && held && new_held && free_count && new_free_count && (block_table || max_blocks == 0) && (free_pages || n_pages == 0), HS_ERR_NULL,
              "hs_block_tables: NULL argument");

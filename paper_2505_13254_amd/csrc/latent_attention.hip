@@ -51,7 +51,7 @@ extern "C" size_t hs_tree_attention_latent_workspace(const int32_t* host_node_of
   clear_error();
   if (B < 1 || Hq < 1 || host_node_offsets == nullptr || host_prefix_lens == nullptr || R != 512 || Dr != 64) return 0;
   if (lat_tree_hosts(host_node_offsets, host_prefix_lens, B, 0x7fffffff) != HS_OK || (int64_t)host_node_offsets[B] * Hq >= LAT_MAX_ROWS) return 0;
-  return lat_tree_bytes(lat_remember<lat_tree_plan, 0>(host_node_offsets, host_prefix_lens, B, Hq), (int64_t)host_node_offsets[B] * Hq);
+  return lat_tree_bytes(lat_remember<lat_tree_plan, 0>(host_node_offsets, host_prefix_lens, B, Hq));
 }
 
 extern "C" hs_status hs_tree_attention_latent(const void* q, int64_t q_stride, int64_t q_head_stride, const void* q_rope, int64_t q_rope_stride,
@@ -87,7 +87,7 @@ extern "C" hs_status hs_tree_attention_latent(const void* q, int64_t q_stride, i
   if (!lat_tree_matrix(a, dt)) return lat_tree_any(a, dt, static_cast<hipStream_t>(stream));
   const LatPlan p = lat_remember<lat_tree_plan, 0>(host_node_offsets, host_prefix_lens, B, Hq);
   if (p.grid >= LAT_MAX_GRID) return lat_tree_any(a, dt, static_cast<hipStream_t>(stream));
-  const size_t need = lat_tree_bytes(p, (int64_t)NN * Hq);
+  const size_t need = lat_tree_bytes(p);
   HS_REQUIRE(need == 0 || (workspace != nullptr && workspace_bytes >= need && reinterpret_cast<uintptr_t>(workspace) % 256 == 0), HS_ERR_WORKSPACE,
              "hs_tree_attention_latent: needs %zu bytes of workspace, got %zu", need, workspace_bytes);
   return lat_tree_launch(a, p, workspace, static_cast<hipStream_t>(stream));
@@ -97,7 +97,7 @@ extern "C" size_t hs_prompt_attention_latent_workspace(const int32_t* host_q_off
   clear_error();
   if (B < 1 || H < 1 || Dv != 128 || host_q_offsets == nullptr || host_kv_offsets == nullptr) return 0;
   if (lat_prompt_hosts(host_q_offsets, host_kv_offsets, B) != HS_OK || (int64_t)host_q_offsets[B] * H >= LAT_MAX_ROWS) return 0;
-  return lat_prompt_bytes(lat_remember<lat_prompt_plan, 1>(host_q_offsets, host_kv_offsets, B, H), (int64_t)host_q_offsets[B] * H);
+  return lat_prompt_bytes(lat_remember<lat_prompt_plan, 1>(host_q_offsets, host_kv_offsets, B, H));
 }
 
 extern "C" hs_status hs_prompt_attention_latent(const void* q, int64_t q_stride, int64_t q_head_stride, const void* q_rope, int64_t q_rope_stride,
@@ -132,7 +132,7 @@ extern "C" hs_status hs_prompt_attention_latent(const void* q, int64_t q_stride,
   if (!lat_prompt_matrix(a, dt)) return lat_prompt_any(a, dt, static_cast<hipStream_t>(stream));
   const LatPlan p = lat_remember<lat_prompt_plan, 1>(host_q_offsets, host_kv_offsets, B, H);
   if (p.grid >= LAT_MAX_GRID) return lat_prompt_any(a, dt, static_cast<hipStream_t>(stream));
-  const size_t need = lat_prompt_bytes(p, (int64_t)N * H);
+  const size_t need = lat_prompt_bytes(p);
   HS_REQUIRE(need == 0 || (workspace != nullptr && workspace_bytes >= need && reinterpret_cast<uintptr_t>(workspace) % 256 == 0), HS_ERR_WORKSPACE,
              "hs_prompt_attention_latent: needs %zu bytes of workspace, got %zu", need, workspace_bytes);
   return lat_prompt_launch(a, p, workspace, static_cast<hipStream_t>(stream));

@@ -46,12 +46,14 @@ struct LatPromptArgs {
 };
 
 // latent_attn_tree.hip: bfloat16, R = 512, Dr = 64, everything aligned to 16 bytes, on the matrix cores.
+constexpr int64_t LAT_MAX_RECORDS = (int64_t)1 << 22;  // (8.7 GB of 512 columns)
 struct LatPlan {
   int per;       // pages of a split at most
   int sp_max;    // splits of a sequence at most
   int group;     // rows of an item at most
   int64_t first[9];  // the first item of each XCD, and the number of items
   int64_t grid;      // workgroups
+  int64_t records;   // of the rows of sequences with several splits, one to a split
 };
 // The last plan of a thread (the layers of a step ask for the same one, and so does a call after its workspace query): of calls of up to 512 sequences.
 template <LatPlan (*PLAN)(const int32_t*, const int64_t*, int32_t, int32_t), int LENS>
@@ -76,14 +78,14 @@ LatPlan lat_remember(const int32_t* rows, const int64_t* lens, int32_t B, int32_
 }
 bool lat_tree_matrix(const LatTreeArgs& a, hs_dtype dt);
 LatPlan lat_tree_plan(const int32_t* host_node_offsets, const int64_t* host_prefix_lens, int32_t B, int32_t Hq);
-size_t lat_tree_bytes(const LatPlan& p, int64_t rows);
+size_t lat_tree_bytes(const LatPlan& p);
 hs_status lat_tree_launch(const LatTreeArgs& a, const LatPlan& p, void* workspace, hipStream_t stream);
 
 // latent_attn_prompt.hip: bfloat16, Dn = 128, Dr = 64, Dv = 128, everything aligned to 16 bytes, on the matrix cores.  (A plan's `per` are tiles of 64 keys, `grid`
 // the items.)
 bool lat_prompt_matrix(const LatPromptArgs& a, hs_dtype dt);
 LatPlan lat_prompt_plan(const int32_t* host_q_offsets, const int64_t* host_kv_offsets, int32_t B, int32_t H);
-size_t lat_prompt_bytes(const LatPlan& p, int64_t rows);
+size_t lat_prompt_bytes(const LatPlan& p);
 hs_status lat_prompt_launch(const LatPromptArgs& a, const LatPlan& p, void* workspace, hipStream_t stream);
 
 // What a launch may have of workgroups (a grid's threads are counted in 32 bits); a call of more, of very many short sequences, takes the other kernel.

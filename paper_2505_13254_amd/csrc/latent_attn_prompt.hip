@@ -32,15 +32,16 @@ struct LpArgs {
   int per;     // tiles of a split at most
   int sp_max;
   float* part;
+  int records;  // that part holds
 };
 
 struct LpLds {
   char ring[LP_RING * LP_TILE];
   int64_t out_at[LP_WAVES][32];
   unsigned odd[4][2];  // of the masked tiles: which of their 64 values hold a NaN or an infinity
-  int again, found[4];
+  int again, found[5];
   int64_t found_wide[2];
-  int64_t sums[LP_WAVES];
+  int sums[LP_WAVES][2];
 };
 static_assert(sizeof(LpLds) <= 160 * 1024 && LP_WAVES * 32 * LP_OUT_PITCH <= LP_RING * LP_TILE, "LDS of a compute unit");
 
@@ -54,49 +55,57 @@ __host__ __device__ __forceinline__ int lp_splits(int64_t keys, int per) {
 
 struct LpItem {
   int s, n0, n, h, g, sp, n_sp;
+  int rec0;  // the sequence's first record
   int64_t k0, T;
 };
+
+// What the device's arrays say of sequence s, within what the host's copies said.
+__device__ __forceinline__ void lp_sequence(const LpArgs& gl, int s, int* n0, int* n, int64_t* k0, int64_t* T, int* n_sp) {
+  const LatPromptArgs& a = gl.a;
+  const int from = a.q_offsets[s], to = a.q_offsets[s + 1];
+  *k0 = a.kv_offsets[s];
+  const int64_t keys = a.kv_offsets[s + 1] - *k0;
+  *T = keys < 0 ? 0 : std::min(keys, (int64_t)HS_MX_MAX_TOKENS);
+  *n0 = from;
+  const int rows = from < 0 ? 0 : std::min(to - from, a.N - from);
+  *n = rows < 0 ? 0 : rows;
+  *n_sp = std::min(lp_splits(*T, gl.per), gl.sp_max);
+}
+__device__ __forceinline__ int lp_records(int n, int H, int n_sp) { return n_sp > 1 ? n * H * n_sp : 0; }
 
 __device__ __forceinline__ bool lp_find(const LpArgs& gl, LpItem& it, LpLds& mem) {
   const LatPromptArgs& a = gl.a;
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-  const int64_t item = blockIdx.x;
+  const int item = blockIdx.x;  // (fewer than 2^22)
   if (tid == 0) mem.found[0] = -1;
-  int64_t items = 0;
+  int items = 0, records = 0;
   for (int base = 0; base < a.B && items <= item; base += LP_THREADS) {
     const int s = base + tid;
     int n0 = 0, n = 0, n_sp = 1;
     int64_t k0 = 0, T = 0;
-    if (s < a.B) {
-      n0 = a.q_offsets[s];
-      n = a.q_offsets[s + 1] - n0;
-      k0 = a.kv_offsets[s];
-      T = a.kv_offsets[s + 1] - k0;
-      n = n < 0 || n0 < 0 ? 0 : (n > a.N - n0 ? a.N - n0 : n);  // (the host's copies say so)
-      n = n < 0 ? 0 : n;
-      T = T < 0 ? 0 : T;
-      n_sp = std::min(lp_splits(T, gl.per), gl.sp_max);
-    }
-    const int64_t mine = (int64_t)lp_groups(n) * n_sp * a.H;  // (below 2^31: the launch holds them)
-    int to32 = (int)mine;
-    to32 = wave_prefix_sum(to32);
-    if (lane == 63) mem.sums[wave] = to32;
+    if (s < a.B) lp_sequence(gl, s, &n0, &n, &k0, &T, &n_sp);
+    const int mine = lp_groups(n) * n_sp * a.H, recs = lp_records(n, a.H, n_sp);
+    int to = wave_prefix_sum(mine), rec_to = wave_prefix_sum(recs);
+    if (lane == 63) mem.sums[wave][0] = to, mem.sums[wave][1] = rec_to;
     __syncthreads();
-    int64_t before = 0, all = 0;
+    int all = 0, all_recs = 0;
     for (int w = 0; w < LP_WAVES; ++w) {
-      before += w < wave ? mem.sums[w] : 0;
-      all += mem.sums[w];
+      if (w == wave) to += all, rec_to += all_recs;
+      all += mem.sums[w][0];
+      all_recs += mem.sums[w][1];
     }
-    const int64_t at = item - (items + before + to32 - mine);
-    items += all;
+    const int at = item - (items + to - mine);
     if (at >= 0 && at < mine) {
       mem.found[0] = s;
       mem.found[1] = n0;
       mem.found[2] = n;
-      mem.found[3] = (int)at;
+      mem.found[3] = at;
+      mem.found[4] = records + rec_to - recs;
       mem.found_wide[0] = k0;
       mem.found_wide[1] = T;
     }
+    items += all;
+    records += all_recs;
     __syncthreads();
   }
   auto get = [&](int v) { return __builtin_amdgcn_readfirstlane(v); };
@@ -114,7 +123,8 @@ __device__ __forceinline__ bool lp_find(const LpArgs& gl, LpItem& it, LpLds& mem
   const int g = x / it.n_sp;
   it.sp = x - g * it.n_sp;
   it.g = lp_groups(it.n) - 1 - g;  // (the longest first)
-  return true;
+  it.rec0 = get(mem.found[4]);
+  return it.n_sp == 1 || it.rec0 + lp_records(it.n, a.H, it.n_sp) <= gl.records;  // (always, where the arrays are as the host's copies)
 }
 
 struct LpState {
@@ -406,8 +416,9 @@ __global__ __launch_bounds__(LP_THREADS) void k_lat_prompt(LpArgs gl) {
           *reinterpret_cast<const uint4*>(stage + (x >> 4) * LP_OUT_PITCH + 16 * (x & 15));
     return;
   }
+  const int64_t rec0 = it.rec0 + ((int64_t)(first + 32 * wave) * a.H + it.h) * it.n_sp + it.sp;  // (records: row, head, split)
   if (half == 0 && col < mine_rows) {
-    float* const rec = gl.part + ((row0 + (int64_t)col * a.H) * gl.sp_max + it.sp) * LP_REC;
+    float* const rec = gl.part + (rec0 + (int64_t)col * a.H * it.n_sp) * LP_REC;
     rec[LP_DV] = st.m;
     rec[LP_DV + 1] = total;
   }
@@ -422,7 +433,7 @@ __global__ __launch_bounds__(LP_THREADS) void k_lat_prompt(LpArgs gl) {
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll 4
     for (int x = lane; x < mine_rows * 16; x += 64)
-      *reinterpret_cast<float4*>(gl.part + ((row0 + (int64_t)(x >> 4) * a.H) * gl.sp_max + it.sp) * LP_REC + 32 * x0 + 4 * (x & 15)) =
+      *reinterpret_cast<float4*>(gl.part + (rec0 + (int64_t)(x >> 4) * a.H * it.n_sp) * LP_REC + 32 * x0 + 4 * (x & 15)) =
           *reinterpret_cast<const float4*>(stage + (x >> 4) * LP_OUT_PITCH + 16 * (x & 15));
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   }
@@ -432,20 +443,33 @@ __global__ __launch_bounds__(LP_THREADS) void k_lat_prompt(LpArgs gl) {
 constexpr int LPM_THREADS = 256;
 __global__ __launch_bounds__(LPM_THREADS) void k_lat_prompt_merge(LpArgs gl) {
   const LatPromptArgs& a = gl.a;
-  const int lane = threadIdx.x & 31;
-  const unsigned row = (unsigned)blockIdx.x * (LPM_THREADS / 32) + (threadIdx.x >> 5);  // (below 2^24)
-  if (row >= (unsigned)a.N * (unsigned)a.H) return;
+  const int lane = threadIdx.x & 31, wide = threadIdx.x & 63;
+  const unsigned rows = (unsigned)a.N * (unsigned)a.H;  // (below 2^24)
+  const unsigned at = (unsigned)blockIdx.x * (LPM_THREADS / 32) + (threadIdx.x >> 5), row = std::min(at, rows - 1);
   const int n = (int)(row / (unsigned)a.H), h = (int)(row - (unsigned)n * (unsigned)a.H);
-  int lo = 0, hi = a.B;  // the last sequence that begins at or before the row
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (a.q_offsets[mid] <= n) lo = mid;
-    else hi = mid;
+  // the row's sequence, and its first record (whole waves: 64 sequences at a time)
+  int own = 0, n_sp = 0, n0 = 0, rec0 = 0;
+  bool found = false;
+  for (int base = 0, before = 0; base < a.B; base += 64) {
+    int s_n0 = 0, s_n = 0, s_sp = 0;
+    int64_t k0, T;
+    if (base + wide < a.B) lp_sequence(gl, base + wide, &s_n0, &s_n, &k0, &T, &s_sp);
+    const int recs = lp_records(s_n, a.H, s_sp), upto = wave_prefix_sum(recs);
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {  // the wave's two rows
+      const int want = __builtin_amdgcn_readlane(n, 32 * x);
+      const unsigned long long hit = __ballot(s_n0 <= want && want < s_n0 + s_n);
+      if (hit == 0ull) continue;
+      const int who = __builtin_ctzll(hit);
+      const int t_n = __builtin_amdgcn_readlane(s_n, who), t_sp = __builtin_amdgcn_readlane(s_sp, who), t_n0 = __builtin_amdgcn_readlane(s_n0, who),
+                t_rec = before + __builtin_amdgcn_readlane(upto - recs, who);
+      if (wide >> 5 == x) own = t_n, n_sp = t_sp, n0 = t_n0, rec0 = t_rec, found = true;
+    }
+    if (__ballot(!found) == 0ull) break;
+    before += __builtin_amdgcn_readlane(upto, 63);
   }
-  const int64_t T = a.kv_offsets[lo + 1] - a.kv_offsets[lo];
-  const int n_sp = std::min(lp_splits(T < 0 ? 0 : T, gl.per), gl.sp_max);
-  if (n_sp == 1) return;
-  const float* const rec = gl.part + (int64_t)row * gl.sp_max * LP_REC;
+  if (at >= rows || n_sp <= 1 || rec0 + lp_records(own, a.H, n_sp) > gl.records) return;
+  const float* const rec = gl.part + (rec0 + ((int64_t)(n - n0) * a.H + h) * n_sp) * LP_REC;
   // (one pass, with the running maximum: the records of four splits at a time)
   float m = LT_FLOOR, total = 0.f;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -496,8 +520,8 @@ LatPlan lat_prompt_plan(const int32_t* qo, const int64_t* ko, int32_t B, int32_t
   best.sp_max = 1;
   double best_us = 0.0;
   auto consider = [&](int64_t per) {
-    double sum = 0.0, most = 0.0, records = 0.0;
-    int64_t items = 0, sp_max = 1;
+    double sum = 0.0, most = 0.0;
+    int64_t items = 0, sp_max = 1, records = 0;
     for (int s = 0; s < B; ++s) {
       const int n = qo[s + 1] - qo[s];
       if (n == 0) continue;
@@ -507,11 +531,12 @@ LatPlan lat_prompt_plan(const int32_t* qo, const int64_t* ko, int32_t B, int32_t
       most = std::max(most, FIXED + TILE * last / (double)n_sp);
       items += groups * n_sp * H;
       sp_max = std::max(sp_max, n_sp);
-      if (n_sp > 1) records += (double)n * H * (double)n_sp;
+      if (n_sp > 1) records += (int64_t)n * H * n_sp;
     }
     double us = (double)items <= CU ? most : std::max(most, sum / CU + 0.3 * most);
-    if (sp_max > 1) us += 4.0 + REC * records;
-    if (best.per == 0 || us < best_us) best_us = us, best.per = (int)per, best.sp_max = (int)sp_max, best.grid = items;
+    if (sp_max > 1) us += 4.0 + REC * (double)records;
+    if (best.per == 0 || (us < best_us && records <= 4 * LAT_MAX_RECORDS))
+      best_us = us, best.per = (int)per, best.sp_max = (int)sp_max, best.grid = items, best.records = records;
     return items;
   };
   consider(longest);
@@ -527,10 +552,10 @@ LatPlan lat_prompt_plan(const int32_t* qo, const int64_t* ko, int32_t B, int32_t
   return best;
 }
 
-size_t lat_prompt_bytes(const LatPlan& p, int64_t rows) { return p.sp_max > 1 ? align_up((size_t)rows * p.sp_max * LP_REC * 4, 256) : 0; }
+size_t lat_prompt_bytes(const LatPlan& p) { return align_up((size_t)p.records * LP_REC * 4, 256); }
 
 hs_status lat_prompt_launch(const LatPromptArgs& a, const LatPlan& p, void* workspace, hipStream_t stream) {
-  LpArgs g = {a, a.scale * LT_LOG2E, p.per, p.sp_max, static_cast<float*>(workspace)};
+  LpArgs g = {a, a.scale * LT_LOG2E, p.per, p.sp_max, static_cast<float*>(workspace), (int)p.records};
   hipLaunchKernelGGL(k_lat_prompt, dim3((unsigned)p.grid), dim3(LP_THREADS), 0, stream, g);
   const hs_status st = launch_status("latent prompt attention");
   if (st != HS_OK || p.sp_max == 1) return st;

@@ -21,6 +21,7 @@ struct LtArgs {
   int sp_max;  // splits of a sequence at most; 1: results are written directly
   int group;   // rows of an item at most: 128, 64 or 32
   float* part;
+  int records;            // that part holds: n_sp of every row of a sequence with several splits, sequence by sequence
   int first[LT_XCD + 1];  // the first item of each XCD
 };
 
@@ -34,6 +35,7 @@ __host__ __device__ __forceinline__ int lt_first_page(int sp, int n_sp, int page
 
 struct LtItem {
   int s, n0, M, sp, n_sp, rg;
+  int rec0;  // the sequence's first record
   int64_t L;
 };
 
@@ -45,26 +47,38 @@ struct LtLds {
   unsigned odd[2];
   int again;  // some row's reference was too low
   int found[8];
-  int sums[4];
+  int sums[4][2];
 };
 static_assert(sizeof(LtLds) <= 160 * 1024, "LDS of a compute unit");
 
-// Inclusive prefix sums over the workgroup, and the total.
-__device__ __forceinline__ int lt_scan(int& x, LtLds& mem) {
+// Inclusive prefix sums of two numbers over the workgroup, and the totals.
+__device__ __forceinline__ void lt_scan(int& x, int& y, int* all_x, int* all_y, LtLds& mem) {
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   x = wave_prefix_sum(x);
-  if (lane == 63) mem.sums[wave] = x;
+  y = wave_prefix_sum(y);
+  if (lane == 63) mem.sums[wave][0] = x, mem.sums[wave][1] = y;
   __syncthreads();
-  int before = 0, all = 0;
+  *all_x = *all_y = 0;
 #pragma unroll
   for (int w = 0; w < 4; ++w) {
-    const int v = mem.sums[w];
-    before += w < wave ? v : 0;
-    all += v;
+    if (w == wave) x += *all_x, y += *all_y;
+    *all_x += mem.sums[w][0];
+    *all_y += mem.sums[w][1];
   }
-  x += before;
-  return all;
 }
+
+// What the device's arrays say of sequence s, within what the host's copies said.
+__device__ __forceinline__ void lt_sequence(const LtArgs& g, int s, int* n0, int* M, int64_t* L, int* n_sp) {
+  const LatTreeArgs& a = g.a;
+  const int from = a.node_offsets[s], to = a.node_offsets[s + 1];
+  const int64_t len = a.prefix_lens[s], most = std::min((int64_t)a.max_blocks * 64, (int64_t)HS_MX_MAX_TOKENS);
+  *n0 = from;
+  *L = len < 0 ? 0 : (len > most ? most : len);
+  const int rows = from < 0 ? 0 : std::min(std::min(to - from, LT_MAX_TREE), a.NN - from);
+  *M = rows < 0 ? 0 : rows;
+  *n_sp = rows > 0 ? std::min(lt_splits((*L + 63) >> 6, g.per), g.sp_max) : 0;
+}
+__device__ __forceinline__ int lt_records(int M, int Hq, int n_sp) { return n_sp > 1 ? M * Hq * n_sp : 0; }
 
 // The item of a workgroup: the j-th of XCD x's.
 __device__ __forceinline__ bool lt_find(const LtArgs& g, LtItem& it, LtLds& mem) {
@@ -73,27 +87,16 @@ __device__ __forceinline__ bool lt_find(const LtArgs& g, LtItem& it, LtLds& mem)
   const int item = g.first[x] + j;
   if (item >= g.first[x + 1]) return false;
   if (tid == 0) mem.found[0] = -1;
-  int items = 0;
+  int items = 0, records = 0;
   for (int base = 0; base < a.B && items <= item; base += LT_THREADS) {
     const int s = base + tid;
-    int n0 = 0, M = 0, n_sp = 0, groups = 0;
+    int n0 = 0, M = 0, n_sp = 0;
     int64_t L = 0;
-    if (s < a.B) {
-      n0 = a.node_offsets[s];
-      M = a.node_offsets[s + 1] - n0;
-      L = a.prefix_lens[s];
-      const int64_t most = (int64_t)a.max_blocks * 64;
-      L = L < 0 ? 0 : (L > most ? most : L);
-      M = M < 0 || n0 < 0 ? 0 : std::min(std::min(M, LT_MAX_TREE), a.NN - n0);  // (the host's copies say so)
-      M = M < 0 ? 0 : M;
-      n_sp = M > 0 ? std::min(lt_splits((L + 63) >> 6, g.per), g.sp_max) : 0;
-      groups = (M * a.Hq + g.group - 1) / g.group;
-    }
-    const int mine = n_sp * groups;
-    int to = mine;
-    const int all = lt_scan(to, mem);
+    if (s < a.B) lt_sequence(g, s, &n0, &M, &L, &n_sp);
+    const int groups = (M * a.Hq + g.group - 1) / g.group, mine = n_sp * groups, recs = lt_records(M, a.Hq, n_sp);
+    int to = mine, rec_to = recs, all, all_recs;
+    lt_scan(to, rec_to, &all, &all_recs, mem);
     const int at = item - (items + to - mine);
-    items += all;
     if (at >= 0 && at < mine) {
       const int sp = at / groups;
       mem.found[0] = s;
@@ -103,7 +106,10 @@ __device__ __forceinline__ bool lt_find(const LtArgs& g, LtItem& it, LtLds& mem)
       mem.found[4] = n_sp;
       mem.found[5] = at - sp * groups;
       mem.found[6] = (int)L;
+      mem.found[7] = records + rec_to - recs;
     }
+    items += all;
+    records += all_recs;
     __syncthreads();
   }
   auto get = [&](int k) { return __builtin_amdgcn_readfirstlane(mem.found[k]); };
@@ -115,7 +121,8 @@ __device__ __forceinline__ bool lt_find(const LtArgs& g, LtItem& it, LtLds& mem)
   it.n_sp = get(4);
   it.rg = get(5);
   it.L = get(6);
-  return true;
+  it.rec0 = get(7);
+  return it.n_sp == 1 || it.rec0 + lt_records(it.M, a.Hq, it.n_sp) <= g.records;  // (always, where the arrays are as the host's copies)
 }
 
 // Rows from `first` on of a page in the ring become zero (what lies behind a sequence's last token may be anything, and 0 x NaN is NaN).
@@ -422,7 +429,7 @@ __device__ __forceinline__ void lt_run(const LtArgs& g, const LtItem& it, LtLds&
   if (mine_rows <= 0) return;
   const bool writes_stat = half == 0 && col < mine_rows && out_block == 0;
   char* const stage = lds + wave * 32 * LT_OUT_PITCH;
-  const int64_t row0 = (int64_t)it.n0 * a.Hq + row_base;  // (records: row, then split)
+  const int64_t row0 = (int64_t)it.n0 * a.Hq + row_base, rec0 = it.rec0 + (int64_t)row_base * it.n_sp + it.sp;  // (records: row, then split)
   if (it.n_sp == 1) {
     const float inv = 1.f / total;
     if (writes_stat && a.lse != nullptr) a.lse[row0 + col] = (top + __log2f(total)) * LT_LN2;
@@ -445,7 +452,7 @@ __device__ __forceinline__ void lt_run(const LtArgs& g, const LtItem& it, LtLds&
     }
   } else {
     if (writes_stat) {
-      float* const rec = g.part + ((row0 + col) * g.sp_max + it.sp) * LT_REC;
+      float* const rec = g.part + (rec0 + col * it.n_sp) * LT_REC;
       rec[LT_R] = top;
       rec[LT_R + 1] = total;
     }
@@ -463,7 +470,7 @@ __device__ __forceinline__ void lt_run(const LtArgs& g, const LtItem& it, LtLds&
 #pragma unroll 4
       for (int x = lane; x < mine_rows * PER_ROW; x += 64) {
         const int r = x / PER_ROW, c = x % PER_ROW;
-        *reinterpret_cast<float4*>(g.part + ((row0 + r) * g.sp_max + it.sp) * LT_REC + 32 * (out_block + x0) + 4 * c) =
+        *reinterpret_cast<float4*>(g.part + (rec0 + r * it.n_sp) * LT_REC + 32 * (out_block + x0) + 4 * c) =
             *reinterpret_cast<const float4*>(stage + r * LT_OUT_PITCH + 16 * c);
       }
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -491,20 +498,27 @@ __global__ __launch_bounds__(LTM_THREADS) void k_lat_tree_merge(LtArgs g) {
   const int64_t row = (int64_t)blockIdx.x * (LTM_THREADS / 64 / SHARE) + wave / SHARE;
   if (row >= (int64_t)a.NN * a.Hq) return;  // (SHARE > 1: the same for the workgroup)
   const int n = (int)((unsigned)row / (unsigned)a.Hq), h = (int)row - n * a.Hq;
-  int s = 0;
+  // the row's sequence, and its first record
+  int M = 0, n_sp = 0, n0 = 0, rec0 = 0;
   for (int base = 0; base < a.B; base += 64) {
-    const bool below = base + lane < a.B && a.node_offsets[base + lane] <= n;
-    const int c = __builtin_popcountll(__ballot(below));
-    s = base + c - 1;
-    if (c < 64) break;
+    int own_n0 = 0, own_M = 0, own_sp = 0;
+    int64_t L;
+    const bool there = base + lane < a.B;
+    if (there) lt_sequence(g, base + lane, &own_n0, &own_M, &L, &own_sp);
+    const unsigned long long mine = __ballot(there && own_n0 <= n && n < own_n0 + own_M);
+    const int recs = lt_records(own_M, a.Hq, own_sp), upto = wave_prefix_sum(recs);
+    if (mine != 0ull) {
+      const int who = __builtin_ctzll(mine);
+      M = __builtin_amdgcn_readlane(own_M, who);
+      n_sp = __builtin_amdgcn_readlane(own_sp, who);
+      n0 = __builtin_amdgcn_readlane(own_n0, who);
+      rec0 += __builtin_amdgcn_readlane(upto - recs, who);
+      break;
+    }
+    rec0 += __builtin_amdgcn_readlane(upto, 63);
   }
-  s = s < 0 ? 0 : s;
-  int64_t L = a.prefix_lens[s];
-  const int64_t most = (int64_t)a.max_blocks * 64;
-  L = L < 0 ? 0 : (L > most ? most : L);
-  const int n_sp = std::min(lt_splits((L + 63) >> 6, g.per), g.sp_max);
-  if (n_sp == 1) return;
-  const float* const rec = g.part + row * g.sp_max * LT_REC;
+  if (n_sp <= 1 || rec0 + lt_records(M, a.Hq, n_sp) > g.records) return;
+  const float* const rec = g.part + (rec0 + ((int64_t)(n - n0) * a.Hq + h) * n_sp) * LT_REC;
   float m = LT_FLOOR, total = 0.f;
   float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
   for (int x0 = way; x0 < n_sp; x0 += 4 * SHARE) {
@@ -589,14 +603,13 @@ LatPlan lat_tree_plan(const int32_t* no, const int64_t* pl, int32_t B, int32_t H
   best.sp_max = 1;
   double best_us = 0.0, best_busy = CU;
   auto consider = [&](int64_t per, int group) {
-    int64_t items = 0, sp_max = 1;
-    double records = 0.0;
+    int64_t items = 0, sp_max = 1, records = 0;
     for (int s = 0; s < B; ++s) {
       const int64_t rows = (int64_t)(no[s + 1] - no[s]) * Hq, n_sp = lt_splits((pl[s] + 63) >> 6, (int)per);
       if (rows == 0) continue;
       items += n_sp * ((rows + group - 1) / group);
       sp_max = std::max(sp_max, n_sp);
-      if (n_sp > 1) records += (double)(rows * n_sp);
+      if (n_sp > 1) records += rows * n_sp;
     }
     const double busy = std::min(CU, (double)items);
     double sum = 0.0, most = 0.0;
@@ -608,8 +621,9 @@ LatPlan lat_tree_plan(const int32_t* no, const int64_t* pl, int32_t B, int32_t H
       most = std::max(most, item);
     }
     double us = (double)items <= CU ? most : std::max(most, sum / CU + 0.5 * most);
-    if (sp_max > 1) us += 4.0 + REC * records + SPLIT * (double)sp_max;
-    if (best.per == 0 || us < best_us) best_us = us, best_busy = busy, best.per = (int)per, best.sp_max = (int)sp_max, best.group = group;
+    if (sp_max > 1) us += 4.0 + REC * (double)records + SPLIT * (double)sp_max;
+    if (best.per == 0 || (us < best_us && records <= LAT_MAX_RECORDS))
+      best_us = us, best_busy = busy, best.per = (int)per, best.sp_max = (int)sp_max, best.group = group, best.records = records;
     return items;
   };
   for (int group : {LT_GROUP, LT_GROUP / 2, LT_GROUP / 4}) {
@@ -661,10 +675,10 @@ LatPlan lat_tree_plan(const int32_t* no, const int64_t* pl, int32_t B, int32_t H
   return best;
 }
 
-size_t lat_tree_bytes(const LatPlan& p, int64_t rows) { return p.sp_max > 1 ? align_up((size_t)rows * p.sp_max * LT_REC * 4, 256) : 0; }
+size_t lat_tree_bytes(const LatPlan& p) { return align_up((size_t)p.records * LT_REC * 4, 256); }
 
 hs_status lat_tree_launch(const LatTreeArgs& a, const LatPlan& p, void* workspace, hipStream_t stream) {
-  LtArgs g = {a, a.scale * LT_LOG2E, p.per, p.sp_max, p.group, static_cast<float*>(workspace), {}};
+  LtArgs g = {a, a.scale * LT_LOG2E, p.per, p.sp_max, p.group, static_cast<float*>(workspace), (int)p.records, {}};
   for (int x = 0; x <= LT_XCD; ++x) g.first[x] = (int)p.first[x];
   hipLaunchKernelGGL(k_lat_tree, dim3((unsigned)p.grid), dim3(LT_THREADS), 0, stream, g);
   const hs_status st = launch_status("latent attention");

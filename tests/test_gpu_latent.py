@@ -83,6 +83,68 @@ def test_large_trees_and_chains(hs, n, Hq):
     Tree([n], [1], Hq, seed=n, trees=[star]).check(hs)
 
 
+def _full_chip(Hq, seed=0, B=140):
+    """More items than a launch of small groups is made for: groups of up to 128 rows, with every number of row blocks."""
+    rs = np.random.RandomState(seed)
+    lens = [0, 1, 63, 64, 65, 127, 128, 129, 191, 700, 1500] + [int(v) for v in rs.randint(0, 400, B - 11)]
+    return Tree([int(v) for v in rs.randint(1, 4, B)], lens, Hq, seed=seed)
+
+
+@pytest.mark.parametrize("Hq", [16, 40, 64, 100, 128])
+def test_full_chips(hs, Hq):
+    _full_chip(Hq, seed=Hq).check(hs)
+
+
+@pytest.mark.parametrize("Hq", [16, 64, 128])
+def test_full_chips_scores_that_grow(hs, Hq):
+    t = _full_chip(Hq, seed=1)
+    t.q[:] = 0.0
+    t.q[:, :, 5] = 8.0
+    t.q[:, 1::2, 5] = -8.0
+    for s, (p, l) in enumerate(zip(t.prefix, t.lens)):
+        p[:, 5] = (torch.arange(l, device=DEV) * (2.0 if s % 2 else -1.5)).to(BF)
+        for b in range(-(-l // 64)):
+            part = p[64 * b:64 * b + 64]
+            t.pool[int(t.table_host[s, b]), :part.shape[0]] = part
+    t.check(hs)
+
+
+@pytest.mark.parametrize("Hq", [16, 64, 128])
+def test_full_chips_nan(hs, Hq):
+    from latent_util import ancestors
+    t = _full_chip(Hq, seed=2)
+    want = t.want()
+    first = np.concatenate([[0], np.cumsum(t.sizes)])
+    clean = torch.ones(t.NN, dtype=torch.bool, device=DEV)
+    for s in range(0, t.B, 7):                                            # the last tree row of every seventh sequence
+        row = int(first[s + 1]) - 1
+        t.c_tree[row, 11] = float("nan") if s % 2 else float("inf")
+        clean[int(first[s]):int(first[s + 1])] = dev(~ancestors(t.parents[s])[:, t.sizes[s] - 1])
+    t.pool[int(t.table_host[9, 3]), 17, 570] = float("nan")               # a stored token of the tenth
+    clean[int(first[9]):int(first[10])] = False
+    o, lse = t.call(hs)
+    compare((o[clean], lse[clean]), tuple(w[clean] for w in want))
+    assert (~torch.isfinite(o[~clean])).flatten(1).any(1).all()
+
+
+@pytest.mark.parametrize("B,Hq,long", [(300, 16, 20000), (700, 3, 9000), (257, 128, 3000)])
+def test_many_sequences_and_a_long_one(hs, B, Hq, long):
+    rs = np.random.RandomState(B)
+    lens = [int(v) for v in rs.randint(0, 200, B)]
+    lens[B // 2] = long
+    sizes = [int(v) for v in rs.randint(0, 3, B)]
+    sizes[B // 2] = 2
+    t = Tree(sizes, lens, Hq, seed=B)
+    t.check(hs)
+    ws = hs.hs_tree_attention_latent_workspace(t.host_no, t.host_pl, Hq, 512, 64, DEV)
+    if ws is not None:                                                    # records of the sequences that are cut, not of all
+        assert ws.numel() < 2064 * 2 * Hq * 400
+        with pytest.raises(hs.HsError):
+            t.call(hs, ws=ws[:ws.numel() - 256])
+        with pytest.raises(ValueError):
+            t.call(hs, ws=ws.cpu())
+
+
 def test_long_caches(hs):
     Tree([1, 3, 1], [70000, 33333, 16384], 16, seed=3).check(hs)
     Tree([2], [40001], 128, seed=4).check(hs)
@@ -249,6 +311,21 @@ def test_prompt_attention(hs, rows, keys, H):
                                                         ([70], [70], 2, 128, 0, 128, BF), ([30], [90], 2, 64, 64, 256, BF), ([40], [41], 3, 128, 64, 64, BF)])
 def test_prompt_attention_other_shapes(hs, rows, keys, H, Dn, Dr, Dv, dtype):
     Prompt(rows, keys, H, Dn, Dr, Dv, dtype, seed=Dn).check(hs)
+
+
+@pytest.mark.parametrize("B,H,long", [(600, 4, 9000), (70, 8, 20000)])
+def test_many_prompts_and_a_long_one(hs, B, H, long):
+    rs = np.random.RandomState(B)
+    rows = [int(v) for v in rs.randint(0, 20, B)]
+    keys = [n + int(v) for n, v in zip(rows, rs.randint(0, 100, B))]
+    rows[B // 2], keys[B // 2] = 40, long
+    p = Prompt(rows, keys, H, seed=B)
+    p.check(hs)
+    ws = hs.hs_prompt_attention_latent_workspace(p.host_qo, p.host_ko, H, 128, DEV)
+    if ws is not None:
+        assert ws.numel() < 528 * H * 40 * 400
+        with pytest.raises(hs.HsError):
+            p.call(hs, ws=ws[:ws.numel() - 256])
 
 
 def test_long_prompts(hs):
