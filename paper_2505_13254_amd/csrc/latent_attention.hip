@@ -90,7 +90,7 @@ extern "C" hs_status hs_tree_attention_latent(const void* q, int64_t q_stride, i
   const size_t need = lat_tree_bytes(p);
   HS_REQUIRE(need == 0 || (workspace != nullptr && workspace_bytes >= need && reinterpret_cast<uintptr_t>(workspace) % 256 == 0), HS_ERR_WORKSPACE,
              "hs_tree_attention_latent: needs %zu bytes of workspace, got %zu", need, workspace_bytes);
-  return lat_tree_launch(a, p, workspace, static_cast<hipStream_t>(stream));
+  return lat_tree_launch(a, p, (int)host_prefix_lens[0], workspace, static_cast<hipStream_t>(stream));
 }
 
 extern "C" size_t hs_prompt_attention_latent_workspace(const int32_t* host_q_offsets, const int64_t* host_kv_offsets, int32_t B, int32_t H, int32_t Dv) {

@@ -79,7 +79,7 @@ LatPlan lat_remember(const int32_t* rows, const int64_t* lens, int32_t B, int32_
 bool lat_tree_matrix(const LatTreeArgs& a, hs_dtype dt);
 LatPlan lat_tree_plan(const int32_t* host_node_offsets, const int64_t* host_prefix_lens, int32_t B, int32_t Hq);
 size_t lat_tree_bytes(const LatPlan& p);
-hs_status lat_tree_launch(const LatTreeArgs& a, const LatPlan& p, void* workspace, hipStream_t stream);
+hs_status lat_tree_launch(const LatTreeArgs& a, const LatPlan& p, int one_len, void* workspace, hipStream_t stream);  // one_len: B == 1, the stored tokens
 
 // latent_attn_prompt.hip: bfloat16, Dn = 128, Dr = 64, Dv = 128, everything aligned to 16 bytes, on the matrix cores.  (A plan's `per` are tiles of 64 keys, `grid`
 // the items.)

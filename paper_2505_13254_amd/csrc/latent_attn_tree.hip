@@ -21,6 +21,7 @@ struct LtArgs {
   int sp_max;  // splits of a sequence at most; 1: results are written directly
   int group;   // rows of an item at most: 128, 64 or 32
   float* part;
+  int one_rows, one_len;  // B == 1: the tree's rows and the stored tokens
   int records;            // that part holds: n_sp of every row of a sequence with several splits, sequence by sequence
   int first[LT_XCD + 1];  // the first item of each XCD
 };
@@ -86,6 +87,16 @@ __device__ __forceinline__ bool lt_find(const LtArgs& g, LtItem& it, LtLds& mem)
   const int x = (int)(blockIdx.x & (LT_XCD - 1)), j = (int)(blockIdx.x / LT_XCD), tid = threadIdx.x;
   const int item = g.first[x] + j;
   if (item >= g.first[x + 1]) return false;
+  if (a.B == 1) {  // (no trip to memory)
+    it.s = it.n0 = it.rec0 = 0;
+    it.M = g.one_rows;
+    it.L = g.one_len;
+    it.n_sp = lt_splits((it.L + 63) >> 6, g.per);
+    const int groups = (it.M * a.Hq + g.group - 1) / g.group;
+    it.sp = item / groups;
+    it.rg = item - it.sp * groups;
+    return true;
+  }
   if (tid == 0) mem.found[0] = -1;
   int items = 0, records = 0;
   for (int base = 0; base < a.B && items <= item; base += LT_THREADS) {
@@ -252,23 +263,25 @@ __device__ __forceinline__ void lt_run(const LtArgs& g, const LtItem& it, LtLds&
   }
   lt_meet();  // (the ring is free, or its first half)
   int up[LT_MAX_TREE / LT_THREADS];
-  if (last) {
-    tree_rows(top_tree);
-#pragma unroll
-    for (int x = 0; x < LT_MAX_TREE / LT_THREADS; ++x) up[x] = a.parent[it.n0 + std::min(x * LT_THREADS + tid, it.M - 1)];
-  }
-  if constexpr (RB == 4) {
-    request(0);
-    request(1);
-  }
-  const float c2 = g.c2;
-  if (last) {
+  auto tree_there = [&]() {
     if (tid < 2) mem.odd[tid] = 0u;
 #pragma unroll
     for (int x = 0; x < LT_MAX_TREE / LT_THREADS; ++x) mem.parent[x * LT_THREADS + tid] = up[x];
     lt_meet();
     mend_tree();  // (the parents were requested behind the tree's rows, and are there)
+  };
+  if (last) {
+    tree_rows(top_tree);
+#pragma unroll
+    for (int x = 0; x < LT_MAX_TREE / LT_THREADS; ++x) up[x] = a.parent[it.n0 + std::min(x * LT_THREADS + tid, it.M - 1)];
+    if constexpr (RB < 4) tree_there();  // (in one branch with the loads: to the compiler they are on their way behind any other, and it waits for all in the page loop)
   }
+  if constexpr (RB == 4) {
+    request(0);
+    request(1);
+    if (last) tree_there();
+  }
+  const float c2 = g.c2;
   float reference = LT_FLOOR;
 #pragma unroll 1
   for (bool first = true;; first = false) {
@@ -478,14 +491,21 @@ __device__ __forceinline__ void lt_run(const LtArgs& g, const LtItem& it, LtLds&
   }
 }
 
+// MOST: row blocks of an item at most.  (A kernel of its own for each: of groups of 32 rows a third of the code is fetched, and there is no scratch memory to set
+// up: one token of 16 heads on 2048 18.5 -> 17.3 us, 64 sequences 66.6 -> 64.9 us.)
+template <int MOST>
 __global__ __launch_bounds__(LT_THREADS, 1) void k_lat_tree(LtArgs g) {
   __shared__ LtLds mem;
   LtItem it;
   if (!lt_find(g, it, mem)) return;
   const int left = std::min(g.group, it.M * g.a.Hq - it.rg * g.group);
-  if (left > 64) lt_run<4>(g, it, mem);
-  else if (left > 32) lt_run<2>(g, it, mem);
-  else lt_run<1>(g, it, mem);
+  if constexpr (MOST == 4) {
+    if (left > 64) return lt_run<4>(g, it, mem);
+  }
+  if constexpr (MOST >= 2) {
+    if (left > 32) return lt_run<2>(g, it, mem);
+  }
+  lt_run<1>(g, it, mem);
 }
 
 // The merge of the splits: SHARE waves to a row, which take its records in turn, four at a time each.
@@ -587,9 +607,9 @@ bool lat_tree_matrix(const LatTreeArgs& a, hs_dtype dt) {
 
 // Pages of a split, by estimated times.
 LatPlan lat_tree_plan(const int32_t* no, const int64_t* pl, int32_t B, int32_t Hq) {
-  int64_t longest = 1;
+  int64_t longest = 1, widest = 0;
   for (int s = 0; s < B; ++s)
-    if (no[s + 1] > no[s]) longest = std::max(longest, (pl[s] + 63) >> 6);
+    if (no[s + 1] > no[s]) longest = std::max(longest, (pl[s] + 63) >> 6), widest = std::max(widest, (int64_t)(no[s + 1] - no[s]) * Hq);
   constexpr double CU = 256.0, REC = 0.0010, SPLIT = 0.2;  // compute units; us a row's record (all together), and a split in the merge
   // us of an item without pages, and of a page: by what the waves do with one, or by its share of what is read at a time (pages that several groups share come from
   // the second-level cache, no faster: 250 items' pages on their way are more than it holds)
@@ -627,6 +647,7 @@ LatPlan lat_tree_plan(const int32_t* no, const int64_t* pl, int32_t B, int32_t H
     return items;
   };
   for (int group : {LT_GROUP, LT_GROUP / 2, LT_GROUP / 4}) {
+    if (group > LT_GROUP / 4 && widest <= group / 2) continue;  // (no group has so many rows)
     const bool few = consider(longest, group) <= 128;
     // the finest cuts whose items fill the compute units once, one and a half times, ...
     for (int64_t target : {32, 64, 128, 192, 256, 512, 1024}) {
@@ -638,7 +659,7 @@ LatPlan lat_tree_plan(const int32_t* no, const int64_t* pl, int32_t B, int32_t H
       }
       if (lo == 1) break;
     }
-    if (!few || (int64_t)no[B] * Hq <= group / 2) break;  // smaller groups are for calls of few items
+    if (!few) break;  // smaller groups are for calls of few items
   }
   // runs of items for the XCDs: equal numbers while each has a compute unit, equal times otherwise
   auto items_of = [&](int s, double* cost) {
@@ -677,10 +698,12 @@ LatPlan lat_tree_plan(const int32_t* no, const int64_t* pl, int32_t B, int32_t H
 
 size_t lat_tree_bytes(const LatPlan& p) { return align_up((size_t)p.records * LT_REC * 4, 256); }
 
-hs_status lat_tree_launch(const LatTreeArgs& a, const LatPlan& p, void* workspace, hipStream_t stream) {
-  LtArgs g = {a, a.scale * LT_LOG2E, p.per, p.sp_max, p.group, static_cast<float*>(workspace), (int)p.records, {}};
+hs_status lat_tree_launch(const LatTreeArgs& a, const LatPlan& p, int one_len, void* workspace, hipStream_t stream) {
+  LtArgs g = {a, a.scale * LT_LOG2E, p.per, p.sp_max, p.group, static_cast<float*>(workspace), a.NN, one_len, (int)p.records, {}};
   for (int x = 0; x <= LT_XCD; ++x) g.first[x] = (int)p.first[x];
-  hipLaunchKernelGGL(k_lat_tree, dim3((unsigned)p.grid), dim3(LT_THREADS), 0, stream, g);
+  if (p.group > 64) hipLaunchKernelGGL(k_lat_tree<4>, dim3((unsigned)p.grid), dim3(LT_THREADS), 0, stream, g);
+  else if (p.group > 32) hipLaunchKernelGGL(k_lat_tree<2>, dim3((unsigned)p.grid), dim3(LT_THREADS), 0, stream, g);
+  else hipLaunchKernelGGL(k_lat_tree<1>, dim3((unsigned)p.grid), dim3(LT_THREADS), 0, stream, g);
   const hs_status st = launch_status("latent attention");
   if (st != HS_OK || p.sp_max == 1) return st;
   const int64_t rows = (int64_t)a.NN * a.Hq;
