@@ -135,5 +135,5 @@ extern "C" hs_status hs_prompt_attention_latent(const void* q, int64_t q_stride,
   const size_t need = lat_prompt_bytes(p);
   HS_REQUIRE(need == 0 || (workspace != nullptr && workspace_bytes >= need && reinterpret_cast<uintptr_t>(workspace) % 256 == 0), HS_ERR_WORKSPACE,
              "hs_prompt_attention_latent: needs %zu bytes of workspace, got %zu", need, workspace_bytes);
-  return lat_prompt_launch(a, p, workspace, static_cast<hipStream_t>(stream));
+  return lat_prompt_launch(a, p, (int)host_kv_offsets[1], workspace, static_cast<hipStream_t>(stream));
 }

@@ -86,7 +86,7 @@ hs_status lat_tree_launch(const LatTreeArgs& a, const LatPlan& p, int one_len, v
 bool lat_prompt_matrix(const LatPromptArgs& a, hs_dtype dt);
 LatPlan lat_prompt_plan(const int32_t* host_q_offsets, const int64_t* host_kv_offsets, int32_t B, int32_t H);
 size_t lat_prompt_bytes(const LatPlan& p);
-hs_status lat_prompt_launch(const LatPromptArgs& a, const LatPlan& p, void* workspace, hipStream_t stream);
+hs_status lat_prompt_launch(const LatPromptArgs& a, const LatPlan& p, int one_len, void* workspace, hipStream_t stream);  // one_len: B == 1, the keys
 
 // What a launch may have of workgroups (a grid's threads are counted in 32 bits); a call of more, of very many short sequences, takes the other kernel.
 constexpr int64_t LAT_MAX_GRID = (int64_t)1 << 22;

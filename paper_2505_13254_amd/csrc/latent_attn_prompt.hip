@@ -33,6 +33,7 @@ struct LpArgs {
   int sp_max;
   float* part;
   int records;  // that part holds
+  int one_len;  // B == 1: the keys (its rows are N)
 };
 
 struct LpLds {
@@ -62,6 +63,12 @@ struct LpItem {
 // What the device's arrays say of sequence s, within what the host's copies said.
 __device__ __forceinline__ void lp_sequence(const LpArgs& gl, int s, int* n0, int* n, int64_t* k0, int64_t* T, int* n_sp) {
   const LatPromptArgs& a = gl.a;
+  if (a.B == 1) {  // (no trip to memory)
+    *n0 = 0, *k0 = 0;
+    *n = a.N, *T = gl.one_len;
+    *n_sp = lp_splits(*T, gl.per);
+    return;
+  }
   const int from = a.q_offsets[s], to = a.q_offsets[s + 1];
   *k0 = a.kv_offsets[s];
   const int64_t keys = a.kv_offsets[s + 1] - *k0;
@@ -77,6 +84,20 @@ __device__ __forceinline__ bool lp_find(const LpArgs& gl, LpItem& it, LpLds& mem
   const LatPromptArgs& a = gl.a;
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   const int item = blockIdx.x;  // (fewer than 2^22)
+  auto place = [&](int at) {
+    it.n_sp = std::min(lp_splits(it.T, gl.per), gl.sp_max);
+    const int x = at / a.H;
+    it.h = at - x * a.H;
+    const int g = x / it.n_sp;
+    it.sp = x - g * it.n_sp;
+    it.g = lp_groups(it.n) - 1 - g;  // (the longest first)
+  };
+  if (a.B == 1) {
+    it.s = it.rec0 = 0;
+    lp_sequence(gl, 0, &it.n0, &it.n, &it.k0, &it.T, &it.n_sp);
+    place(item);
+    return true;
+  }
   if (tid == 0) mem.found[0] = -1;
   int items = 0, records = 0;
   for (int base = 0; base < a.B && items <= item; base += LP_THREADS) {
@@ -116,13 +137,7 @@ __device__ __forceinline__ bool lp_find(const LpArgs& gl, LpItem& it, LpLds& mem
   auto wide = [&](int64_t v) { return (int64_t)(uint32_t)get((int)v) | (int64_t)get((int)(v >> 32)) << 32; };
   it.k0 = wide(mem.found_wide[0]);
   it.T = wide(mem.found_wide[1]);
-  const int at = get(mem.found[3]);
-  it.n_sp = std::min(lp_splits(it.T, gl.per), gl.sp_max);
-  const int x = at / a.H;
-  it.h = at - x * a.H;
-  const int g = x / it.n_sp;
-  it.sp = x - g * it.n_sp;
-  it.g = lp_groups(it.n) - 1 - g;  // (the longest first)
+  place(get(mem.found[3]));
   it.rec0 = get(mem.found[4]);
   return it.n_sp == 1 || it.rec0 + lp_records(it.n, a.H, it.n_sp) <= gl.records;  // (always, where the arrays are as the host's copies)
 }
@@ -449,8 +464,12 @@ __global__ __launch_bounds__(LPM_THREADS) void k_lat_prompt_merge(LpArgs gl) {
   const int n = (int)(row / (unsigned)a.H), h = (int)(row - (unsigned)n * (unsigned)a.H);
   // the row's sequence, and its first record (whole waves: 64 sequences at a time)
   int own = 0, n_sp = 0, n0 = 0, rec0 = 0;
-  bool found = false;
-  for (int base = 0, before = 0; base < a.B; base += 64) {
+  bool found = a.B == 1;
+  if (found) {
+    int64_t k0, T;
+    lp_sequence(gl, 0, &n0, &own, &k0, &T, &n_sp);
+  }
+  for (int base = 0, before = 0; base < a.B && a.B > 1; base += 64) {
     int s_n0 = 0, s_n = 0, s_sp = 0;
     int64_t k0, T;
     if (base + wide < a.B) lp_sequence(gl, base + wide, &s_n0, &s_n, &k0, &T, &s_sp);
@@ -554,8 +573,8 @@ LatPlan lat_prompt_plan(const int32_t* qo, const int64_t* ko, int32_t B, int32_t
 
 size_t lat_prompt_bytes(const LatPlan& p) { return align_up((size_t)p.records * LP_REC * 4, 256); }
 
-hs_status lat_prompt_launch(const LatPromptArgs& a, const LatPlan& p, void* workspace, hipStream_t stream) {
-  LpArgs g = {a, a.scale * LT_LOG2E, p.per, p.sp_max, static_cast<float*>(workspace), (int)p.records};
+hs_status lat_prompt_launch(const LatPromptArgs& a, const LatPlan& p, int one_len, void* workspace, hipStream_t stream) {
+  LpArgs g = {a, a.scale * LT_LOG2E, p.per, p.sp_max, static_cast<float*>(workspace), (int)p.records, one_len};
   hipLaunchKernelGGL(k_lat_prompt, dim3((unsigned)p.grid), dim3(LP_THREADS), 0, stream, g);
   const hs_status st = launch_status("latent prompt attention");
   if (st != HS_OK || p.sp_max == 1) return st;

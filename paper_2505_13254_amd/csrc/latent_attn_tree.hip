@@ -520,7 +520,8 @@ __global__ __launch_bounds__(LTM_THREADS) void k_lat_tree_merge(LtArgs g) {
   const int n = (int)((unsigned)row / (unsigned)a.Hq), h = (int)row - n * a.Hq;
   // the row's sequence, and its first record
   int M = 0, n_sp = 0, n0 = 0, rec0 = 0;
-  for (int base = 0; base < a.B; base += 64) {
+  if (a.B == 1) M = g.one_rows, n_sp = lt_splits((g.one_len + 63) >> 6, g.per);
+  for (int base = 0; base < a.B && a.B > 1; base += 64) {
     int own_n0 = 0, own_M = 0, own_sp = 0;
     int64_t L;
     const bool there = base + lane < a.B;
