@@ -1,6 +1,6 @@
 // Expanded latent attention of prompt rows on the matrix cores: bfloat16, Dn = 128, Dr = 64, Dv = 128.
 //
-// A work item is up to 256 rows of one (sequence, head) and one split of the keys that they see: eight waves of 32 rows each share tiles of 64 keys, which
+// A work item is up to 256 (or 128) rows of one (sequence, head) and one split of the keys that they see: eight waves of 32 rows each share tiles of 64 keys, which
 // global_load_lds brings into a ring of three.  The products are those of the absorbed form (S^T = K Q^T, O^T += V^T P^T, a lane has a query) on keys of
 // 192 and values of 128 elements; the scores of a 32-key block run beside the softmax of the block before it, and two waves to a SIMD fill each
 // other's waits.  Tiles that some row sees only part of (its own last keys, causally: five tiles at most but for sequences with fewer keys than rows) are
@@ -31,6 +31,7 @@ struct LpArgs {
   float c2;
   int per;     // tiles of a split at most
   int sp_max;
+  int group;   // rows of an item at most: 256, or 128 (four waves only move tiles)
   float* part;
   int records;  // that part holds
   int one_len;  // B == 1: the keys (its rows are N)
@@ -46,9 +47,12 @@ struct LpLds {
 };
 static_assert(sizeof(LpLds) <= 160 * 1024 && LP_WAVES * 32 * LP_OUT_PITCH <= LP_RING * LP_TILE, "LDS of a compute unit");
 
-// Groups of n rows, their size (equal ones, whole blocks of 32), tiles of `keys` keys, splits of a sequence.
-__host__ __device__ __forceinline__ int lp_groups(int n) { return (n + LP_GROUP - 1) / LP_GROUP; }
-__host__ __device__ __forceinline__ int lp_size(int n) { return n <= 0 ? 32 : 32 * ((n + 32 * lp_groups(n) - 1) / (32 * lp_groups(n))); }
+// Groups of n rows where they have `group` at most, their size (equal ones, whole blocks of 32), tiles of `keys` keys, splits of a sequence.
+__host__ __device__ __forceinline__ int lp_groups(int n, int group) { return (n + group - 1) / group; }
+__host__ __device__ __forceinline__ int lp_size(int n, int group) {
+  const int all = 32 * lp_groups(n, group);
+  return n <= 0 ? 32 : 32 * ((n + all - 1) / all);
+}
 __host__ __device__ __forceinline__ int lp_splits(int64_t keys, int per) {
   const int64_t tiles = (keys + 63) >> 6;
   return tiles <= per ? 1 : (int)((tiles + per - 1) / per);
@@ -90,7 +94,7 @@ __device__ __forceinline__ bool lp_find(const LpArgs& gl, LpItem& it, LpLds& mem
     it.h = at - x * a.H;
     const int g = x / it.n_sp;
     it.sp = x - g * it.n_sp;
-    it.g = lp_groups(it.n) - 1 - g;  // (the longest first)
+    it.g = lp_groups(it.n, gl.group) - 1 - g;  // (the longest first)
   };
   if (a.B == 1) {
     it.s = it.rec0 = 0;
@@ -105,7 +109,7 @@ __device__ __forceinline__ bool lp_find(const LpArgs& gl, LpItem& it, LpLds& mem
     int n0 = 0, n = 0, n_sp = 1;
     int64_t k0 = 0, T = 0;
     if (s < a.B) lp_sequence(gl, s, &n0, &n, &k0, &T, &n_sp);
-    const int mine = lp_groups(n) * n_sp * a.H, recs = lp_records(n, a.H, n_sp);
+    const int mine = lp_groups(n, gl.group) * n_sp * a.H, recs = lp_records(n, a.H, n_sp);
     int to = wave_prefix_sum(mine), rec_to = wave_prefix_sum(recs);
     if (lane == 63) mem.sums[wave][0] = to, mem.sums[wave][1] = rec_to;
     __syncthreads();
@@ -262,7 +266,7 @@ __global__ __launch_bounds__(LP_THREADS) void k_lat_prompt(LpArgs gl) {
   char* const lds = mem.ring;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane & 31, half = lane >> 5;
-  const int size = lp_size(it.n), first = it.g * size, rows = std::min(size, it.n - first);  // rows first .. first + rows - 1 of the sequence
+  const int size = lp_size(it.n, gl.group), first = it.g * size, rows = std::min(size, it.n - first);  // rows first .. first + rows - 1 of the sequence
   const int mine_rows = std::min(32, rows - 32 * wave);                                      // <= 0: none, the wave only moves tiles
   const int row = first + std::min(32 * wave + col, rows - 1);                               // (rows behind the last repeat it)
   // row i of the sequence sees T - n + i + 1 keys
@@ -529,22 +533,24 @@ bool lat_prompt_matrix(const LatPromptArgs& a, hs_dtype dt) {
          a.v.row < FAR && a.k_rope_row < FAR;
 }
 
-// Tiles of a split, by estimated times.
+// Rows of a group and tiles of a split, by estimated times.  (Groups of 128 for calls of few items: 660 rows of 20 heads 29.6 -> 19.1 us, 3468 of 16 heads
+// 106 -> 76; where the items fill the chip, groups of 256: 8192 rows of 32 heads 640 us, of 128 724.)
 LatPlan lat_prompt_plan(const int32_t* qo, const int64_t* ko, int32_t B, int32_t H) {
   int64_t longest = 1;
   for (int s = 0; s < B; ++s)
     if (qo[s + 1] > qo[s]) longest = std::max(longest, (ko[s + 1] - ko[s] + 63) >> 6);
-  constexpr double FIXED = 8.0, TILE = 2.0, CU = 256.0, REC = 0.0003;  // us of an item without tiles, of a tile, compute units, us a row's record
+  constexpr double FIXED = 8.0, CU = 256.0, REC = 0.0002;  // us of an item without tiles, compute units, us a row's record
   LatPlan best = {};
   best.sp_max = 1;
   double best_us = 0.0;
-  auto consider = [&](int64_t per) {
+  auto consider = [&](int64_t per, int group) {
+    const double TILE = group == LP_GROUP ? 1.7 : 1.15;  // us: one wave to a SIMD has fewer products to do, and nobody who fills its waits
     double sum = 0.0, most = 0.0;
     int64_t items = 0, sp_max = 1, records = 0;
     for (int s = 0; s < B; ++s) {
       const int n = qo[s + 1] - qo[s];
       if (n == 0) continue;
-      const int64_t T = ko[s + 1] - ko[s], n_sp = lp_splits(T, (int)per), groups = lp_groups(n);
+      const int64_t T = ko[s + 1] - ko[s], n_sp = lp_splits(T, (int)per), groups = lp_groups(n, group);
       const double last = (double)((T + 63) >> 6), first = std::max(0.0, (double)(T - n) / 64.0);  // tiles of the last group, about those of the first
       sum += (double)groups * H * ((double)n_sp * FIXED + TILE * (last + first) / 2);
       most = std::max(most, FIXED + TILE * last / (double)n_sp);
@@ -555,18 +561,20 @@ LatPlan lat_prompt_plan(const int32_t* qo, const int64_t* ko, int32_t B, int32_t
     double us = (double)items <= CU ? most : std::max(most, sum / CU + 0.3 * most);
     if (sp_max > 1) us += 4.0 + REC * (double)records;
     if (best.per == 0 || (us < best_us && records <= 4 * LAT_MAX_RECORDS))
-      best_us = us, best.per = (int)per, best.sp_max = (int)sp_max, best.grid = items, best.records = records;
+      best_us = us, best.per = (int)per, best.sp_max = (int)sp_max, best.group = group, best.grid = items, best.records = records;
     return items;
   };
-  consider(longest);
-  for (int64_t target : {64, 128, 192, 256, 384, 512, 1024, 2048}) {
-    int64_t lo = 1, hi = longest;
-    while (lo < hi) {
-      const int64_t mid = (lo + hi) / 2;
-      if (consider(mid) <= target) hi = mid;
-      else lo = mid + 1;
+  for (int group : {LP_GROUP, LP_GROUP / 2}) {
+    consider(longest, group);
+    for (int64_t target : {64, 128, 192, 256, 384, 512, 1024, 2048}) {
+      int64_t lo = 1, hi = longest;
+      while (lo < hi) {
+        const int64_t mid = (lo + hi) / 2;
+        if (consider(mid, group) <= target) hi = mid;
+        else lo = mid + 1;
+      }
+      if (lo == 1) break;
     }
-    if (lo == 1) break;
   }
   return best;
 }
@@ -574,7 +582,7 @@ LatPlan lat_prompt_plan(const int32_t* qo, const int64_t* ko, int32_t B, int32_t
 size_t lat_prompt_bytes(const LatPlan& p) { return align_up((size_t)p.records * LP_REC * 4, 256); }
 
 hs_status lat_prompt_launch(const LatPromptArgs& a, const LatPlan& p, int one_len, void* workspace, hipStream_t stream) {
-  LpArgs g = {a, a.scale * LT_LOG2E, p.per, p.sp_max, static_cast<float*>(workspace), (int)p.records, one_len};
+  LpArgs g = {a, a.scale * LT_LOG2E, p.per, p.sp_max, p.group, static_cast<float*>(workspace), (int)p.records, one_len};
   hipLaunchKernelGGL(k_lat_prompt, dim3((unsigned)p.grid), dim3(LP_THREADS), 0, stream, g);
   const hs_status st = launch_status("latent prompt attention");
   if (st != HS_OK || p.sp_max == 1) return st;

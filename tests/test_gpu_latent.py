@@ -328,6 +328,36 @@ def test_many_prompts_and_a_long_one(hs, B, H, long):
             p.call(hs, ws=ws[:ws.numel() - 256])
 
 
+
+WIDE = [([257] * 9, [300] * 9, 64), ([700, 1, 257, 40, 0, 33], [900, 500, 257, 20, 100, 33], 96), ([300, 900], [20000, 5000], 24), ([513], [3001], 96)]
+
+
+@pytest.mark.parametrize("rows,keys,H", WIDE)
+def test_prompts_that_fill_the_chip(hs, rows, keys, H):
+    """Eight waves with rows of their own, where the calls of few heads have four."""
+    Prompt(rows, keys, H, seed=H).check(hs)
+
+
+def test_prompts_that_fill_the_chip_with_nan(hs):
+    p = Prompt([300, 260], [513, 260], 128, seed=13)
+    want = p.want()
+    p.v[500, :, 3], p.k[700, :, 5] = float("nan"), float("nan")
+    o, lse = p.call(hs)
+    clean = torch.ones(560, dtype=torch.bool, device=DEV)
+    clean[500 - 213:300] = False
+    clean[300 + 700 - 513:] = False
+    compare((o[clean], lse[clean]), tuple(w[clean] for w in want))
+    assert torch.isnan(o[~clean]).any(-1).all()
+
+
+def test_prompts_that_fill_the_chip_with_scores_that_grow(hs):
+    p = Prompt([300], [513], 256, seed=14)
+    p.q[:] = 0.0
+    p.q[:, :, 5] = 8.0
+    p.k[:, :, 5] = torch.linspace(0, 900, 513).to(DEV).to(BF)[:, None]
+    p.check(hs)
+
+
 def test_long_prompts(hs):
     Prompt([2500], [2500], 8, seed=3).check(hs)
     Prompt([300, 900], [20000, 5000], 2, seed=4).check(hs)
