@@ -665,9 +665,12 @@ hs_status hs_latent_read(const void* pool, int64_t n_slots, const int64_t* slots
  *   second product and the output once.
  *   parent, node_offsets, host_node_offsets, block_table, prefix_lens, host_prefix_lens as in hs_tree_attention_paged; lse [NN,Hq] dense, may be NULL.
  *   The launch is planned from the host copies: they must equal the device arrays, and a captured launch keeps them.
- * A NaN or an infinity in a token reaches the rows that see it and no others: they are NaN, as a whole or in some columns.  Weights are relative to a
- * running maximum, values may have any magnitude below 2^90.  Block-table entries behind a sequence's last token are not looked at.  The same call gives the
- * same bits.
+ * A NaN or an infinity in a token reaches the rows that see it and no others: they are NaN, as a whole or in some columns.  Scores may have any
+ * magnitude that float32 holds, values any below 2^78 (a row's weights are relative to one of its first scores and at most 2^24; where a later score is higher than that, its
+ * group of rows is computed once more, with the maximum).  Block-table entries behind a sequence's last token are not looked at.  The same call gives the same bits.
+ * HS_BF16 with R = 512, Dr = 64, pointers at multiples of 16 bytes and strides of multiples of 8 elements runs on the matrix cores; every other call takes a kernel for any
+ * shape, which reads the tokens again for each row and head (tens to hundreds of times slower).  The former needs the workspace of the query (0 bytes: none), at a multiple of 256:
+ * 2064 bytes for each row, head and split of the sequences that the plan cuts, or the call returns HS_ERR_WORKSPACE.
  * Requires R <= 1024, Dr <= 1024, at most 1024 tree rows and HS_MX_MAX_TOKENS stored tokens per sequence, NN * Hq < 2^24, scale > 0, output rows that do not overlap.
  */
 size_t hs_tree_attention_latent_workspace(const int32_t* host_node_offsets, const int64_t* host_prefix_lens, int32_t B, int32_t Hq, int32_t R,
@@ -687,6 +690,9 @@ hs_status hs_tree_attention_latent(const void* q, int64_t q_stride, int64_t q_he
  *   o[i,h,:] = softmax_j( scale * (<q[i,h,:], k[j,h,:]> + <q_rope[i,h,:], k_rope[j,:]>) ) . v[j,h,:]
  *   q [N,H,Dn], q_rope [N,H,Dr], k [T,H,Dn], v [T,H,Dv], o [N,H,Dv]: row n, head h at base + n * stride + h * head_stride (elements; k and v may be
  *   slices of one product's result).  k_rope [T,Dr]: rows with a stride.  Types, sums, NaN, magnitudes and the host copies as in hs_tree_attention_latent.
+ * HS_BF16 with Dn = 128, Dr = 64, Dv = 128, pointers at multiples of 16 bytes, strides of multiples of 8 elements and rows of k, v and k_rope less than 2^23 elements
+ * apart runs on the matrix cores and needs the workspace of the query, 528 bytes for each row, head and split of the sequences that the plan cuts, as above; every
+ * other call takes the kernel for any shape.
  * Requires Dn, Dr, Dv <= 1024, at most HS_MX_MAX_TOKENS keys per sequence, N * H < 2^24, scale > 0, output rows that do not overlap.
  */
 size_t hs_prompt_attention_latent_workspace(const int32_t* host_q_offsets, const int64_t* host_kv_offsets, int32_t B, int32_t H, int32_t Dv);

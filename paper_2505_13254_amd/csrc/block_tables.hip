@@ -1,7 +1,7 @@
 // hs_block_tables, hs_slot_map: which pages a sequence has, and where in the pool its rows go.
 //
 // A few bytes a sequence, a page's number an entry that changes hands and 8 bytes a row: bound by the launch and by chains of
-// trips to memory, not by bandwidth, up to some 10^5 entries.
+// trips to memory, not by bandwidth, up to some 10^5 entries: tables 3.4 us for 16 sequences, 4.5 for 512; slots 4 us for 1000 rows, 12 for 1.5 million.
 //
 // hs_block_tables.  Free pages are a stack.  With F pages on it, R pages going back in this call and, in the order of
 // sequences, released page t at place F + t, the k-th page taken is entry F + R - 1 - k of that row of pages.  Entries below F are

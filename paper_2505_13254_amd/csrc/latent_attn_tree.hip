@@ -1,7 +1,7 @@
 // Absorbed attention over latents on the matrix cores (see latent_attn_tree.h).
 //
 // A work item is a group of up to 128 rows of one sequence and one split of its pages; the last split also takes the tree's own rows. The
-// host chooses how many pages a split has at most (lt_plan); everything else of an item is found on the device, from the offsets and
+// host chooses how many pages a split has at most (lat_tree_plan); everything else of an item is found on the device, from the offsets and
 // lengths.  Items are numbered by sequence, split and group, and each XCD has a run of neighbouring ones: the groups of a (sequence, split) find its pages in one L2.
 // Splits hand over sums (records of R + 4 floats: O, reference, denominator), which a second launch merges.
 #include <algorithm>
