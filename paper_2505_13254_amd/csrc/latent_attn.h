@@ -55,10 +55,10 @@ struct LatPlan {
   int64_t grid;      // workgroups
   int64_t records;   // of the rows of sequences with several splits, one to a split
 };
-// The last plan of a thread (the layers of a step ask for the same one, and so does a call after its workspace query): of calls of up to 512 sequences.
+// The last plan of a thread (the layers of a step ask for the same one, and so does a call after its workspace query): of calls of up to 4096 sequences.
 template <LatPlan (*PLAN)(const int32_t*, const int64_t*, int32_t, int32_t), int LENS>
 LatPlan lat_remember(const int32_t* rows, const int64_t* lens, int32_t B, int32_t heads) {
-  constexpr int MOST = 512;
+  constexpr int MOST = 4096;
   static thread_local struct {
     int32_t B = -1, heads;
     int32_t rows[MOST + 1];

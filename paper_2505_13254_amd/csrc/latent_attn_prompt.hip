@@ -566,8 +566,9 @@ LatPlan lat_prompt_plan(const int32_t* qo, const int64_t* ko, int32_t B, int32_t
     return items;
   };
   for (int group : {LP_GROUP, LP_GROUP / 2}) {
-    consider(longest, group);
-    for (int64_t target : {64, 128, 192, 256, 384, 512, 1024, 2048}) {
+    const int64_t whole = consider(longest, group);
+    for (int64_t target : {(int64_t)64, (int64_t)128, (int64_t)192, (int64_t)256, (int64_t)384, (int64_t)512, (int64_t)1024, (int64_t)2048, whole + 256}) {
+      if (target <= whole) continue;
       int64_t lo = 1, hi = longest;
       while (lo < hi) {
         const int64_t mid = (lo + hi) / 2;

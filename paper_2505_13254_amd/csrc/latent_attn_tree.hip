@@ -649,9 +649,11 @@ LatPlan lat_tree_plan(const int32_t* no, const int64_t* pl, int32_t B, int32_t H
   };
   for (int group : {LT_GROUP, LT_GROUP / 2, LT_GROUP / 4}) {
     if (group > LT_GROUP / 4 && widest <= group / 2) continue;  // (no group has so many rows)
-    const bool few = consider(longest, group) <= 128;
-    // the finest cuts whose items fill the compute units once, one and a half times, ...
-    for (int64_t target : {32, 64, 128, 192, 256, 512, 1024}) {
+    const int64_t whole = consider(longest, group);
+    const bool few = whole <= 128;
+    // the finest cuts whose items fill the compute units once, one and a half times, ..., and those of the longest sequences among very many
+    for (int64_t target : {(int64_t)32, (int64_t)64, (int64_t)128, (int64_t)192, (int64_t)256, (int64_t)512, (int64_t)1024, whole + 256}) {
+      if (target <= whole) continue;
       int64_t lo = 1, hi = longest;  // items(hi) <= target, or hi is the coarsest
       while (lo < hi) {
         const int64_t mid = (lo + hi) / 2;

@@ -145,6 +145,16 @@ def test_many_sequences_and_a_long_one(hs, B, Hq, long):
             t.call(hs, ws=ws.cpu())
 
 
+def test_a_long_sequence_among_more_than_fill_the_chip(hs):
+    rs = np.random.RandomState(5)
+    lens = [int(v) for v in rs.randint(0, 130, 1500)]
+    lens[700] = 60000
+    Tree([1] * 1500, lens, 16, seed=5).check(hs)
+    keys = [int(v) for v in rs.randint(1, 70, 1500)]
+    keys[3] = 30000
+    Prompt([1] * 1500, keys, 2, seed=6).check(hs)
+
+
 def test_long_caches(hs):
     Tree([1, 3, 1], [70000, 33333, 16384], 16, seed=3).check(hs)
     Tree([2], [40001], 128, seed=4).check(hs)
