@@ -180,8 +180,9 @@ __device__ __forceinline__ void lt_run(const LtArgs& g, const LtItem& it, LtLds&
     const int left = std::min(64, it.M - 64 * t);
     int id0 = tid;
     asm volatile("" : "+v"(id0));  // (no address of these is kept in registers through the pages)
+    const int pieces = left > 32 ? PIECES : PIECES / 2;  // (of 32 rows or fewer nobody looks at the second tile)
 #pragma unroll 1
-    for (int x = 0; x < PIECES; ++x) {
+    for (int x = 0; x < pieces; ++x) {
       unsigned r, c;
       lt_what(x * LT_THREADS + id0, &r, &c);
       const int64_t from = it.n0 + 64 * t + ((int)r < left ? (int)r : left - 1);
@@ -191,11 +192,12 @@ __device__ __forceinline__ void lt_run(const LtArgs& g, const LtItem& it, LtLds&
   };
   // What a thread fetched, once it is there: rows with a NaN or an infinity are noted, and those elements made zero: 0 x NaN must not reach rows that do not
   // see them.
-  auto mend_tree = [&]() {
+  auto mend_tree = [&](int t) {
     int id0 = tid;
     asm volatile("" : "+v"(id0));
-#pragma unroll 6
-    for (int x = 0; x < PIECES; ++x) {
+    const int pieces = it.M - 64 * t > 32 ? PIECES : PIECES / 2;
+#pragma unroll 3
+    for (int x = 0; x < pieces; ++x) {
       const unsigned id = x * LT_THREADS + id0;
       uint4 w = *reinterpret_cast<const uint4*>(lds + 16 * id);
       lt_ushort2 most = {0, 0};
@@ -268,7 +270,7 @@ __device__ __forceinline__ void lt_run(const LtArgs& g, const LtItem& it, LtLds&
 #pragma unroll
     for (int x = 0; x < LT_MAX_TREE / LT_THREADS; ++x) mem.parent[x * LT_THREADS + tid] = up[x];
     lt_meet();
-    mend_tree();  // (the parents were requested behind the tree's rows, and are there)
+    mend_tree(top_tree);  // (the parents were requested behind the tree's rows, and are there)
   };
   if (last) {
     tree_rows(top_tree);
@@ -298,7 +300,7 @@ __device__ __forceinline__ void lt_run(const LtArgs& g, const LtItem& it, LtLds&
         lt_meet();
         tree_rows(t);
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        mend_tree();
+        mend_tree(t);
       }
       lt_meet();
 #pragma unroll 1
