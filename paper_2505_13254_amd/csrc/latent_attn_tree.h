@@ -11,7 +11,7 @@
 //   RB = 1 (up to 32)        four waves a block: a half of the page and a half of the columns (scores computed twice)
 // The latter two are bound by the stream of pages, not by what the waves do.
 // Measured: RB = 4, 4 x 97 rows of 64 heads on 8192 tokens, 1.06 to 1.1 PFLOP/s, the chip's power (a product of 8192^3 by the library: 1.22); RB = 1, 64 rows of
-// 16 heads on 4451 pages, 5.0 TB/s over the whole call (a copy of 4 GiB: 4.8); one row of 16 heads on 2048 tokens 13 us, of which 4 until the last workgroup starts,
+// 16 heads on 4451 pages, 5.0 TB/s over the whole call (a copy of 4 GiB: 4.8); one row of 16 heads on 2048 tokens 12 us, of which 4 until the last workgroup starts,
 // 6 until Q and the first page are there, and 4 for two pages.
 //
 // LDS: a ring of four 32-key tiles, which global_load_lds fills.  A tile is its rows' latents, 1024 bytes each, and behind them their rotary parts, 128 bytes
