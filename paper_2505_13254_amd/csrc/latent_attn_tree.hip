@@ -608,16 +608,17 @@ bool lat_tree_matrix(const LatTreeArgs& a, hs_dtype dt) {
          fits(a.pool, 0, 0) && fits(a.c_tree, a.c_stride, 0) && fits(a.r_tree, a.r_stride, 0) && fits(a.o, a.o_row, a.o_head);
 }
 
-// Pages of a split, by estimated times.
+// Pages of a split, by estimated times.  (Constants fitted to calls with the group size forced: 100 rows of 16 heads on 8414 tokens 128 rows 56 us, 64 rows 69, 32 rows 129; 50 rows
+// of 20 heads on 102 tokens 24, 21 and 18.)
 LatPlan lat_tree_plan(const int32_t* no, const int64_t* pl, int32_t B, int32_t Hq) {
   int64_t longest = 1, widest = 0;
   for (int s = 0; s < B; ++s)
     if (no[s + 1] > no[s]) longest = std::max(longest, (pl[s] + 63) >> 6), widest = std::max(widest, (int64_t)(no[s + 1] - no[s]) * Hq);
-  constexpr double CU = 256.0, REC = 0.0010, SPLIT = 0.2;  // compute units; us a row's record (all together), and a split in the merge
+  constexpr double CU = 256.0, REC = 0.0006, SPLIT = 0.1;  // compute units; us a row's record (all together), and a split in the merge
   // us of an item without pages, and of a page: by what the waves do with one, or by its share of what is read at a time (pages that several groups share come from
   // the second-level cache, no faster: 250 items' pages on their way are more than it holds)
   auto block = [](int64_t rows, int group) { return std::min<int64_t>(rows, group) > 64 ? 2 : std::min<int64_t>(rows, group) > 32 ? 1 : 0; };
-  constexpr double FIXED[3] = {10.0, 12.0, 15.0}, PAGE[3] = {1.3, 1.7, 3.0}, ONCE = 0.0094, SHARED = 0.0129;
+  constexpr double FIXED[3] = {10.0, 11.0, 15.0}, PAGE[3] = {1.3, 2.0, 3.0}, ONCE = 0.0094, SHARED = 0.0129;
   auto item_us = [&](int64_t rows, int group, double pages, double busy) {
     const int k = block(rows, group);
     return FIXED[k] + pages * std::max(PAGE[k], busy * (rows <= group ? ONCE : SHARED));
