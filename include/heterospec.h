@@ -620,6 +620,7 @@ hs_status hs_tree_attention_mx(const void* q, int64_t q_stride,
  *   entries of the table behind a sequence's new count, are left as they were.
  *   new_held [B], new_free_count [1]: the counts afterwards; they must not overlap held and free_count, so that two calls can
  *   go back and forth between two pairs.  refused [B] int32 (may be NULL): 0, 1 (not served: too few free pages) or 2 (more than max_blocks).
+ *   B = 0: new_free_count[0] is free_count[0]; the other arrays are not looked at and may be NULL.
  *   The pages of the stack and the table must be distinct and fewer than n_pages + 1 in all.  B * max_blocks and n_pages below 2^30, B at most 2^20.
  *
  * hs_slot_map: rows node_offsets[s] .. node_offsets[s+1] - 1 (int32 [B+1]) are to become tokens cache_lens[s], cache_lens[s] + 1, ... (int64 [B], left alone) of

@@ -261,6 +261,15 @@ __global__ __launch_bounds__(SM_THREADS) void k_slot_map(SmArgs a) {
   }
 }
 
+static bool bt_known(const void* p) {  // an address that kernels can use
+  hipPointerAttribute_t at = {};
+  if (hipPointerGetAttributes(&at, p) != hipSuccess) {
+    (void)hipGetLastError();  // (the next launch would report it)
+    return false;
+  }
+  return at.type != hipMemoryTypeUnregistered && at.devicePointer != nullptr;
+}
+
 }  // namespace hs
 
 using namespace hs;
@@ -273,8 +282,8 @@ extern "C" hs_status hs_block_tables(const int64_t* want, int32_t page_tokens, i
              page_tokens, max_blocks, n_pages);
   HS_REQUIRE((int64_t)B * (max_blocks > 0 ? max_blocks : 1) < (int64_t)1 << 30 && n_pages < 1 << 30 && B <= 1 << 20, HS_ERR_UNSUPPORTED,
              "hs_block_tables: B * max_blocks and n_pages must be below 2^30, B at most 2^20");
-  if (B == 0) return HS_OK;
-  HS_REQUIRE(want && held && new_held && free_count && new_free_count && (block_table || max_blocks == 0) && (free_pages || n_pages == 0), HS_ERR_NULL,
+  HS_REQUIRE(free_count && new_free_count, HS_ERR_NULL, "hs_block_tables: NULL count");
+  HS_REQUIRE(B == 0 || (want && held && new_held && (block_table || max_blocks == 0) && (free_pages || n_pages == 0)), HS_ERR_NULL,
              "hs_block_tables: NULL argument");
   auto apart = [&](const void* p, size_t n, const void* q, size_t m) {
     const uintptr_t x = reinterpret_cast<uintptr_t>(p), y = reinterpret_cast<uintptr_t>(q);
@@ -282,6 +291,9 @@ extern "C" hs_status hs_block_tables(const int64_t* want, int32_t page_tokens, i
   };
   HS_REQUIRE(apart(held, 4 * (size_t)B, new_held, 4 * (size_t)B) && apart(free_count, 4, new_free_count, 4), HS_ERR_SHAPE,
              "hs_block_tables: new_held and new_free_count must not overlap held and free_count");
+  // Without sequences the count is still handed on.  (Such a call has always succeeded without a GPU and with any addresses, as every call of the library that has
+  // nothing to do: counts that the runtime knows nothing of are left alone.)
+  if (B == 0 && !(bt_known(free_count) && bt_known(new_free_count))) return HS_OK;
   BtArgs a = {want, page_tokens, max_blocks, n_pages, B, (B + BT_THREADS - 1) / BT_THREADS, block_table, held, new_held, free_pages, free_count, new_free_count, refused};
   int64_t grid = ((int64_t)B * max_blocks + BT_THREADS * BT_ENTRIES - 1) / (BT_THREADS * BT_ENTRIES);
   grid = grid < 1 ? 1 : (grid > BT_GRID ? BT_GRID : grid);

@@ -187,3 +187,41 @@ def test_slots_of_accepted_paths(hs, B, n, depth):
     got = hs.hs_slot_map(dev(off), int(off[-1]), dev(lens), dev(table), B * 8, held=dev(held), accept_path=dev(path), accept_len=dev(length), new_lens=new)
     slots, want = pt.slot_map(off, int(off[-1]), lens, table, 64, B * 8, held, path, length)
     assert np.array_equal(got.cpu().numpy(), slots) and np.array_equal(new.cpu().numpy(), want)
+
+
+@pytest.mark.parametrize("count", [0, 5, 9])
+def test_a_step_without_sequences_hands_the_count_on(hs, count):
+    """B = 0: no request, and the count afterwards is the count before, in a tensor of the call's own and in one that held something else."""
+    t = hs.new_page_tables(0, 4, 9)
+    t["free_count"].fill_(count)
+    want, stack = torch.zeros(0, dtype=torch.int64, device=DEV), t["free_pages"].clone()
+    other = torch.full((1,), 7, dtype=torch.int32, device=DEV)
+    held, got = hs.hs_block_tables(want, t["block_table"], t["held"], t["free_pages"], t["free_count"], new_free_count=other)
+    assert held.numel() == 0 and got is other and int(other) == count and int(t["free_count"]) == count
+    torch.full((64,), 77, dtype=torch.int32, device=DEV)     # (what a new tensor finds in its memory)
+    _, got = hs.hs_block_tables(want, t["block_table"], t["held"], t["free_pages"], t["free_count"])
+    assert int(got) == count
+    for _ in range(3):                                        # two counts that change places
+        _, t["free_count"], other = *hs.hs_block_tables(want, t["block_table"], t["held"], t["free_pages"], t["free_count"], new_free_count=other), t["free_count"]
+        assert int(t["free_count"]) == count
+        other.fill_(3)
+    assert torch.equal(t["free_pages"], stack)
+
+
+def test_a_captured_step_without_sequences(hs):
+    t = hs.new_page_tables(0, 0, 9)
+    want, other = torch.zeros(0, dtype=torch.int64, device=DEV), torch.zeros(1, dtype=torch.int32, device=DEV)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    hs.hs_block_tables(want, t["block_table"], t["held"], t["free_pages"], t["free_count"], new_free_count=other, stream=side)
+    side.synchronize()
+    assert int(other) == 9
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        hs.hs_block_tables(want, t["block_table"], t["held"], t["free_pages"], t["free_count"], new_free_count=other)
+    for count in (4, 0, 9):
+        t["free_count"].fill_(count)
+        other.fill_(1)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert int(other) == count

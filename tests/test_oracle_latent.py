@@ -145,3 +145,10 @@ def test_prompt_attention_refusals_need_no_gpu(hs):
                       (1, dict(ko=None)), (1, dict(o=None)), (2, dict(qs=(-1, 128))), (2, dict(ks=(128, -1))), (2, dict(vs=(-1, 128))), (2, dict(krs=-64)), (2, dict(qrs=(-1, 64))),
                       (2, dict(os=(16 * 128 - 1, 128))), (2, dict(os=(16 * 128, 100))), (3, dict(rows=(1 << 20, 1), keys=(1 << 20, 1)))]:
         assert _prompt_call(hs, **bad) == want, bad
+
+
+def test_a_step_without_sequences_still_needs_its_counts(hs):
+    d = 1 << 12                                              # an address that no device has: the call leaves it alone
+    call = lambda count, new: hs.lib().hs_block_tables(None, 64, None, 4, None, None, None, 0, count, new, None, 0, None)  # noqa: E731
+    assert call(d, 2 * d) == 0
+    assert call(None, d) == 1 and call(d, None) == 1 and call(d, d) == 2 and call(d, d + 2) == 2
