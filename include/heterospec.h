@@ -666,7 +666,9 @@ hs_status hs_latent_read(const void* pool, int64_t n_slots, const int64_t* slots
  *   second product and the output once.
  *   parent, node_offsets, host_node_offsets, block_table, prefix_lens, host_prefix_lens as in hs_tree_attention_paged; lse [NN,Hq] dense, may be NULL.
  *   The launch is planned from the host copies: they must equal the device arrays, and a captured launch keeps them.
- * A NaN or an infinity in a token reaches the rows that see it and no others: they are NaN, as a whole or in some columns.  Scores may have any
+ * A NaN in a token, or an infinity in a latent or an expanded value, reaches the rows that see it and no others: they are not finite, as a whole or in some columns.  An
+ * infinity in a rotary part or an expanded key counts by the score that it makes: with -infinity the token has a weight of zero (or is as a NaN, where it is one of the
+ * tree's own rows), otherwise the row is NaN.  A row whose scores are all -infinity is NaN.  Scores may have any
  * magnitude that float32 holds, values any below 2^78 (a row's weights are relative to one of its first scores and at most 2^24; where a later score is higher than that, its
  * group of rows is computed once more, with the maximum).  Block-table entries behind a sequence's last token are not looked at.  The same call gives the same bits.
  * HS_BF16 with R = 512, Dr = 64, pointers at multiples of 16 bytes and strides of multiples of 8 elements runs on the matrix cores; every other call takes a kernel for any

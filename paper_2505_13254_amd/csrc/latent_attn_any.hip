@@ -3,7 +3,8 @@
 // o = softmax_j(scale (q . k_j + q_rope . r_j)) . v_j in float32, one pass over the keys with the running maximum and sum of a
 // softmax.  A workgroup of four waves has one (row, query head); each wave takes every fourth 64 keys.  A lane has a key for the
 // scores (the query stands in LDS, one broadcast read to 64 products) and every 64th column for the values.  Keys that a row does not
-// see are skipped, not multiplied by zero, so that nothing in them reaches it.  The waves' sums meet in LDS.
+// see are skipped, not multiplied by zero, so that nothing in them reaches it; a score of -infinity is a weight of zero that is multiplied, so that an infinity
+// in its value does.  The waves' sums meet in LDS.
 //
 // Bound by the vector pipe and by reads of a key a lane: what float32, and shapes without matrix-core kernels, take.
 // (bfloat16, one row of 16 heads on 2048 tokens of 512 + 64: 664 us, where the matrix cores take 15.)
@@ -27,15 +28,18 @@ __device__ __forceinline__ float la_at<bf16_t>(const bf16_t* p, int64_t i) { ret
 template <typename T, typename Seen, typename Key>
 __device__ __forceinline__ void la_row(const T* q, int a_n, const T* qr, int b_n, int v_n, int64_t tiles, float scale, T* o, float* lse, Seen seen, Key key) {
   __shared__ float q_lds[2 * LA_MOST], p_lds[LA_WAVES][64], out[LA_WAVES][LA_MOST], stat[LA_WAVES][2];
+  __shared__ int some[LA_WAVES];
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   for (int x = tid; x < a_n + b_n; x += LA_THREADS) q_lds[x] = x < a_n ? la_at(q, x) : la_at(qr, x - a_n);
   __syncthreads();
   float acc[LA_MOST / 64], m = LA_FLOOR, l = 0.f;
+  bool any = false;  // the wave's keys that the row sees: is there one?
 #pragma unroll
   for (int x = 0; x < LA_MOST / 64; ++x) acc[x] = 0.f;
   for (int64_t t = wave; t < tiles; t += LA_WAVES) {
     const unsigned long long bits = seen(t);
     if (bits == 0ull) continue;
+    any = true;
     const bool on = (bits >> lane) & 1ull;
     float s = -HS_INF;
     if (on) {
@@ -65,7 +69,7 @@ __device__ __forceinline__ void la_row(const T* q, int a_n, const T* qr, int b_n
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   }
-  if (lane == 0) stat[wave][0] = m, stat[wave][1] = l;
+  if (lane == 0) stat[wave][0] = m, stat[wave][1] = l, some[wave] = any;
 #pragma unroll
   for (int x = 0; x < LA_MOST / 64; ++x)
     if (64 * x + lane < v_n) out[wave][64 * x + lane] = acc[x];
@@ -75,11 +79,13 @@ __device__ __forceinline__ void la_row(const T* q, int a_n, const T* qr, int b_n
   for (int w = 1; w < LA_WAVES; ++w) top = fmaxf(top, stat[w][0]);
 #pragma unroll
   for (int w = 0; w < LA_WAVES; ++w) f[w] = __expf(stat[w][0] - top), total += f[w] * stat[w][1];
-  const bool none = top == LA_FLOOR && total == 0.f;  // no key at all
+  bool none = true;  // no key at all.  (Keys whose scores are all -infinity have no weight either: they give 0 / 0.)
+#pragma unroll
+  for (int w = 0; w < LA_WAVES; ++w) none = none && !some[w];
   for (int x = tid; x < v_n; x += LA_THREADS) {
     float y = 0.f;
 #pragma unroll
-    for (int w = 0; w < LA_WAVES; ++w) y += stat[w][1] == 0.f ? 0.f : f[w] * out[w][x];
+    for (int w = 0; w < LA_WAVES; ++w) y = __builtin_fmaf(f[w], out[w][x], y);  // (of a wave without keys 0; of scores of -infinity 0 too, or the NaN of 0 x infinity)
     store_elem(o + x, none ? 0.f : y / total);
   }
   if (tid == 0 && lse != nullptr) *lse = none ? -HS_INF : top + __logf(total);

@@ -528,3 +528,144 @@ def test_a_request_from_prompt_to_accepted_drafts(hs):
         lens = new
         assert lens.tolist() == [len(k) for k in kept]
         assert t["held"].tolist() == [-(-len(k) // 64) for k in kept] and int(t["free_count"]) == 14 - sum(t["held"].tolist())
+
+
+# ------------------------------------------------------------------------------------------------ scores of -infinity
+# By the definition such a score is a weight of zero, 0 x infinity is NaN, and a row that sees no other score is 0 / 0: NaN, with a logarithm of -infinity.  A row
+# that sees no key is 0.
+OTHER = [(96, 32, F32), (100, 20, BF), (512, 64, F32), (512, 0, BF)]
+
+
+@pytest.mark.parametrize("R,Dr,dtype", OTHER)
+@pytest.mark.parametrize("L,n", [(5, 1), (70, 1), (200, 1), (300, 1), (0, 3), (5, 3), (300, 3)])
+def test_other_shapes_a_latent_that_scores_minus_infinity(hs, L, n, R, Dr, dtype):
+    """The tree's last row holds an infinity against which its own query points; no other row sees it."""
+    t = Tree([n, 2], [L, 70], 3, R, Dr, dtype, seed=L + R, trees=[np.array([-1, 0, 0], np.int32)[:n], np.array([-1, 0], np.int32)])
+    want = t.want()
+    row, clean = n - 1, [x for x in range(n + 2) if x != n - 1]
+    t.q[row, :, 0] = 1.0
+    t.c_tree[row, 0] = float("-inf")
+    o, lse = t.call(hs)
+    compare((o[clean], lse[clean]), tuple(w[clean] for w in want))
+    assert torch.isnan(o[row, :, 0]).all()
+    rest = torch.cat([t.prefix[0], torch.cat([t.c_tree, t.r_tree], 1)[:min(row, 1)]])  # what the row sees besides: the prefix and the root
+    compare((o[row:row + 1, :, 1:], lse[row:row + 1]), Rest(t, row, rest).want(slice(1, None)))
+
+
+class Rest:
+    """One tree row's attention over given tokens alone."""
+
+    def __init__(self, t, row, tokens):
+        self.t, self.q, self.tokens = t, torch.cat([t.q[row], t.q_rope[row]], 1).double(), tokens.double()
+
+    def want(self, columns=slice(None)):
+        from latent_util import fill
+        H, R = self.t.Hq, self.t.R
+        o, lse = torch.zeros((H, R), dtype=torch.float64, device=DEV), torch.zeros(H, dtype=torch.float64, device=DEV)
+        bo, bl = torch.zeros_like(o), torch.zeros_like(lse)
+        fill(self.q, self.tokens, self.tokens[:, :R], torch.zeros((H, len(self.tokens)), dtype=torch.bool, device=DEV), self.t.scale, self.t.dtype, o, lse, bo, bl)
+        return o[None, :, columns], lse[None], bo[None, :, columns], bl[None]
+
+
+@pytest.mark.parametrize("R,Dr,dtype", OTHER + [(512, 64, BF)])
+def test_tree_rows_that_see_scores_of_minus_infinity_alone(hs, R, Dr, dtype):
+    """A root without a prefix, and a root whose whole prefix scores -infinity too."""
+    t = Tree([2, 1], [0, 150], 3, R, Dr, dtype, seed=R)
+    want = t.want()
+    t.q[0, :, 0], t.q[2, :, 0] = 1.0, 1.0
+    t.c_tree[0, 0] = t.c_tree[2, 0] = float("-inf")
+    for b in range(3):
+        t.pool[int(t.table_host[1, b]), :, 0] = float("-inf")
+    o, lse = t.call(hs)
+    for row in (0, 2):
+        assert torch.isnan(o[row]).all()
+        assert not torch.isfinite(lse[row]).any() and not (lse[row] > 0).any()
+    assert want is not None
+
+
+@pytest.mark.parametrize("R,Dr,dtype", [(96, 32, F32), (100, 20, BF), (512, 64, F32), (512, 64, BF)])
+def test_a_stored_rotary_part_of_minus_infinity_is_a_weight_of_zero(hs, R, Dr, dtype):
+    t = Tree([2, 1], [130, 70], 3, R, Dr, dtype, seed=R + 1)
+    t.q_rope[:2, :, 1] = 1.0
+    t.pool[int(t.table_host[0, 1]), 9, R + 1] = float("-inf")             # token 73 of the first sequence
+    whole = t.prefix[0]
+    t.prefix[0] = torch.cat([whole[:73], whole[74:]])
+    t.lens[0] = 129
+    want = t.want()
+    compare(t.call(hs), want)
+
+
+@pytest.mark.parametrize("R,Dr,dtype", OTHER)
+def test_other_shapes_nan_reaches_the_rows_that_see_it_alone(hs, R, Dr, dtype):
+    from latent_util import ancestors
+    t = Tree([70, 5], [100, 70], 2, R, Dr, dtype, seed=R + 2)
+    want = t.want()
+    for row, at, value in ((7, 3, float("nan")), (66, R - 1, float("inf")), (30, 2, float("-inf"))):
+        keep = t.c_tree.clone()
+        t.c_tree[row, at] = value
+        o, lse = t.call(hs)
+        clean = torch.ones(75, dtype=torch.bool, device=DEV)
+        clean[:70] = ~dev(ancestors(t.parents[0])[:, row])
+        compare((o[clean], lse[clean]), tuple(w[clean] for w in want))
+        assert (~torch.isfinite(o[~clean])).flatten(2).any(2).all()
+        t.c_tree = keep
+    t.pool[int(t.table_host[1, 0]), 3, 5] = float("nan")
+    o, lse = t.call(hs)
+    compare((o[:70], lse[:70]), tuple(w[:70] for w in want))
+    assert torch.isnan(o[70:]).all()
+
+
+PROMPT_OTHER = [(96, 32, 64, F32), (100, 20, 36, BF), (128, 64, 128, F32)]
+
+
+def _keys_of_minus_infinity(hs, Dn, Dr, Dv, dtype, rows, keys, H, cut):
+    """The first sequence's keys all score -infinity, as does the first key of the second and a later one; the third has rows in front of its keys."""
+    p = Prompt(rows, keys, H, Dn, Dr, Dv, dtype, seed=Dn + sum(rows))
+    if cut:
+        assert hs.hs_prompt_attention_latent_workspace(p.host_qo, p.host_ko, H, Dv, DEV) is not None
+    qo, ko = p.host_qo.tolist(), p.host_ko.tolist()
+    p.q[:, :, 1] = 1.0
+    later = (ko[1] + ko[2]) // 2                                          # seen by some rows of the second sequence, or all
+    p.k[:, :, 1] = 0.0
+    want = p.want()
+    p.k[:ko[1], :, 1] = float("-inf")
+    p.k[ko[1], :, 1] = p.k[later, :, 1] = float("-inf")
+    o, lse = p.call(hs)
+    none = torch.tensor([keys[0] - rows[0] + i + 1 <= 0 for i in range(rows[0])], device=DEV)
+    first, lone = slice(0, qo[1]), keys[1] - rows[1] == 0
+    assert (o[first][none] == 0).all() and torch.isnan(o[first][~none]).all() and torch.isneginf(lse[first]).all()
+    if lone:                                                              # the row that sees the first key alone
+        assert torch.isnan(o[qo[1]]).all() and torch.isneginf(lse[qo[1]]).all()
+    compare((o[qo[2]:], lse[qo[2]:]), tuple(w[qo[2]:] for w in want))
+    # the others, as if those keys were not there: their weights are zero
+    a, b, k0, k1 = qo[1], qo[2], ko[1], ko[2]
+    hide = torch.arange(k1 - k0, device=DEV)[None] > (torch.arange(b - a, device=DEV) + (k1 - k0) - (b - a))[:, None]
+    hide[:, 0] = hide[:, later - k0] = True
+    from latent_util import fill
+    p.k[:, :, 1] = 0.0
+    skip = 1 if lone else 0
+    for h in range(H):
+        part = [torch.zeros(b - a, Dv, dtype=torch.float64, device=DEV), torch.zeros(b - a, dtype=torch.float64, device=DEV)]
+        more = [torch.zeros_like(x) for x in part]
+        fill(torch.cat([p.q[a:b, h], p.q_rope[a:b, h]], 1).double(), torch.cat([p.k[k0:k1, h], p.k_rope[k0:k1]], 1).double(), p.v[k0:k1, h].double(), hide, p.scale, dtype,
+             part[0], part[1], more[0], more[1])
+        compare((o[a + skip:b, h], lse[a + skip:b, h]), (part[0][skip:], part[1][skip:], more[0][skip:], more[1][skip:]))
+
+
+@pytest.mark.parametrize("Dn,Dr,Dv,dtype", PROMPT_OTHER)
+@pytest.mark.parametrize("rows,keys", [([3, 9, 4], [3, 9, 2]), ([70, 150, 30], [40, 150, 20]), ([5, 3, 1], [300, 200, 1])])
+def test_prompts_of_other_shapes_keys_that_score_minus_infinity(hs, rows, keys, Dn, Dr, Dv, dtype):
+    _keys_of_minus_infinity(hs, Dn, Dr, Dv, dtype, rows, keys, 3, False)
+
+
+@pytest.mark.parametrize("Dn,Dr,Dv,dtype", PROMPT_OTHER)
+def test_prompts_of_other_shapes_nan_reaches_the_rows_that_see_it_alone(hs, Dn, Dr, Dv, dtype):
+    for at, value in ((90, float("nan")), (130, float("inf")), (199, float("-inf"))):
+        p = Prompt([150, 20], [200, 30], 2, Dn, Dr, Dv, dtype, seed=at)
+        want = p.want()
+        p.v[at, :, 2] = value
+        o, lse = p.call(hs)
+        clean = torch.ones(170, dtype=torch.bool, device=DEV)
+        clean[at - 50:150] = False
+        compare((o[clean], lse[clean]), tuple(w[clean] for w in want))
+        assert (~torch.isfinite(o[~clean, :, 2])).all()
