@@ -417,9 +417,9 @@ __global__ __launch_bounds__(LP_THREADS) void k_lat_prompt(LpArgs gl) {
   const int64_t row0 = (int64_t)(it.n0 + first + 32 * wave) * a.H + it.h;  // of rows a.H apart
   char* const stage = lds + wave * 32 * LP_OUT_PITCH;
   if (it.n_sp == 1) {
-    const float inv = total == 0.f ? 0.f : 1.f / total;  // (0: a row that sees nothing)
+    const float inv = vis == 0 ? 0.f : 1.f / total;  // (a row that sees keys of score -infinity alone is 0 / 0, its logarithm -infinity)
     if (half == 0 && col < mine_rows && a.lse != nullptr)
-      a.lse[row0 + (int64_t)col * a.H] = total == 0.f ? -HS_INF : (st.m + __log2f(total)) * LT_LN2;
+      a.lse[row0 + (int64_t)col * a.H] = (st.m + __log2f(total)) * LT_LN2;
     if (half == 0) mem.out_at[wave][col] = (int64_t)(it.n0 + row) * a.o_row + it.h * a.o_head;
 #pragma unroll
     for (int t = 0; t < LP_NB; ++t)
@@ -468,15 +468,16 @@ __global__ __launch_bounds__(LPM_THREADS) void k_lat_prompt_merge(LpArgs gl) {
   const unsigned at = (unsigned)blockIdx.x * (LPM_THREADS / 32) + (threadIdx.x >> 5), row = std::min(at, rows - 1);
   const int n = (int)(row / (unsigned)a.H), h = (int)(row - (unsigned)n * (unsigned)a.H);
   // the row's sequence, and its first record (whole waves: 64 sequences at a time)
-  int own = 0, n_sp = 0, n0 = 0, rec0 = 0;
+  int own = 0, n_sp = 0, n0 = 0, rec0 = 0, keys = 0;
   bool found = a.B == 1;
   if (found) {
     int64_t k0, T;
     lp_sequence(gl, 0, &n0, &own, &k0, &T, &n_sp);
+    keys = (int)T;
   }
   for (int base = 0, before = 0; base < a.B && a.B > 1; base += 64) {
     int s_n0 = 0, s_n = 0, s_sp = 0;
-    int64_t k0, T;
+    int64_t k0, T = 0;
     if (base + wide < a.B) lp_sequence(gl, base + wide, &s_n0, &s_n, &k0, &T, &s_sp);
     const int recs = lp_records(s_n, a.H, s_sp), upto = wave_prefix_sum(recs);
 #pragma unroll
@@ -486,8 +487,8 @@ __global__ __launch_bounds__(LPM_THREADS) void k_lat_prompt_merge(LpArgs gl) {
       if (hit == 0ull) continue;
       const int who = __builtin_ctzll(hit);
       const int t_n = __builtin_amdgcn_readlane(s_n, who), t_sp = __builtin_amdgcn_readlane(s_sp, who), t_n0 = __builtin_amdgcn_readlane(s_n0, who),
-                t_rec = before + __builtin_amdgcn_readlane(upto - recs, who);
-      if (wide >> 5 == x) own = t_n, n_sp = t_sp, n0 = t_n0, rec0 = t_rec, found = true;
+                t_rec = before + __builtin_amdgcn_readlane(upto - recs, who), t_keys = __builtin_amdgcn_readlane((int)T, who);
+      if (wide >> 5 == x) own = t_n, n_sp = t_sp, n0 = t_n0, rec0 = t_rec, keys = t_keys, found = true;
     }
     if (__ballot(!found) == 0ull) break;
     before += __builtin_amdgcn_readlane(upto, 63);
@@ -518,11 +519,11 @@ __global__ __launch_bounds__(LPM_THREADS) void k_lat_prompt_merge(LpArgs gl) {
       o.x = __builtin_fmaf(w, v[x].x, o.x), o.y = __builtin_fmaf(w, v[x].y, o.y), o.z = __builtin_fmaf(w, v[x].z, o.z), o.w = __builtin_fmaf(w, v[x].w, o.w);
     }
   }
-  const float inv = total == 0.f ? 0.f : 1.f / total;
+  const float inv = keys - own + (n - n0) < 0 ? 0.f : 1.f / total;  // (0: a row that sees no key)
   *reinterpret_cast<uint2*>(static_cast<bf16_t*>(a.o) + n * a.o_row + h * a.o_head + 4 * lane) =
       make_uint2(__builtin_bit_cast(unsigned, __builtin_convertvector((lt_floatx2{o.x * inv, o.y * inv}), lt_bf16x2)),
                  __builtin_bit_cast(unsigned, __builtin_convertvector((lt_floatx2{o.z * inv, o.w * inv}), lt_bf16x2)));
-  if (lane == 0 && a.lse != nullptr) a.lse[row] = total == 0.f ? -HS_INF : (m + __log2f(total)) * LT_LN2;
+  if (lane == 0 && a.lse != nullptr) a.lse[row] = (m + __log2f(total)) * LT_LN2;
 }
 
 // ------------------------------------------------------------------------------------------------ the host's part

@@ -669,3 +669,9 @@ def test_prompts_of_other_shapes_nan_reaches_the_rows_that_see_it_alone(hs, Dn, 
         clean[at - 50:150] = False
         compare((o[clean], lse[clean]), tuple(w[clean] for w in want))
         assert (~torch.isfinite(o[~clean, :, 2])).all()
+
+
+@pytest.mark.parametrize("rows,keys,H,cut", [([3, 9, 4], [3, 9, 2], 3, False), ([70, 150, 30], [40, 150, 20], 16, False), ([257, 300, 90], [300, 300, 50], 3, False),
+                                             ([5, 3, 1], [3000, 2500, 1], 3, True), ([700, 650, 300], [640, 2000, 40], 1, True), ([300, 257, 3], [400, 257, 2], 128, False)])
+def test_prompt_keys_that_score_minus_infinity(hs, rows, keys, H, cut):
+    _keys_of_minus_infinity(hs, 128, 64, 128, BF, rows, keys, H, cut)
