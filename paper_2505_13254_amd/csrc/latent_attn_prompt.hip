@@ -371,6 +371,7 @@ __global__ __launch_bounds__(LP_THREADS) void k_lat_prompt(LpArgs gl) {
     request(0);
     request(1);
     st.clear(reference);
+    lt_meet();  // (the flags are cleared: of a lone sequence no barrier stood in front of this one, and tile 0 may be a masked one)
     unsigned here = 0;  // where the tile is in the ring
     auto after = [](unsigned tile) { return tile == (LP_RING - 1) * LP_TILE ? 0u : tile + LP_TILE; };
     if (n_all > 0) {
@@ -410,7 +411,6 @@ __global__ __launch_bounds__(LP_THREADS) void k_lat_prompt(LpArgs gl) {
     if (mem.again == 0) break;
     reference = st.seen;
     if (tid < 8) mem.odd[tid >> 1][tid & 1] = 0u;
-    lt_meet();
   }
   if (mine_rows <= 0) return;
   const float total = lt_half_sum(st.l);

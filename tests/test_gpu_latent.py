@@ -675,3 +675,29 @@ def test_prompts_of_other_shapes_nan_reaches_the_rows_that_see_it_alone(hs, Dn, 
                                              ([5, 3, 1], [3000, 2500, 1], 3, True), ([700, 650, 300], [640, 2000, 40], 1, True), ([300, 257, 3], [400, 257, 2], 128, False)])
 def test_prompt_keys_that_score_minus_infinity(hs, rows, keys, H, cut):
     _keys_of_minus_infinity(hs, 128, 64, 128, BF, rows, keys, H, cut)
+
+
+@pytest.mark.parametrize("rows,keys", [(64, 64), (300, 300), (200, 210), (700, 700)])
+@pytest.mark.parametrize("H", [3, 64])
+def test_a_lone_prompt_nan_among_its_first_keys(hs, rows, keys, H):
+    """One sequence, whose first tile is masked: what is found in its values has to reach the rows that see it, and only those."""
+    for at, column, value in ((0, 3, float("nan")), (5, 127, float("inf")), (40, 0, float("-inf")), (63, 64, float("nan"))):
+        p = Prompt([rows], [keys], H, seed=at)
+        want = p.want()
+        p.v[at, :, column] = value
+        for _ in range(3):
+            o, lse = p.call(hs)
+            clean = torch.ones(rows, dtype=torch.bool, device=DEV)
+            clean[max(0, at - (keys - rows)):] = False
+            compare((o[clean], lse[clean]), tuple(w[clean] for w in want))
+            assert (~torch.isfinite(o[~clean])).any(-1).all()
+
+
+def test_a_lone_prompt_of_more_rows_than_keys_that_is_cut(hs):
+    p = Prompt([700], [640], 1, seed=5)
+    assert hs.hs_prompt_attention_latent_workspace(p.host_qo, p.host_ko, 1, 128, DEV) is not None
+    p.check(hs)
+    p.k[:, :, 1] = float("-inf")
+    p.q[:, :, 1] = 1.0
+    o, lse = p.call(hs)
+    assert (o[:60] == 0).all() and torch.isnan(o[60:]).all() and torch.isneginf(lse).all()
