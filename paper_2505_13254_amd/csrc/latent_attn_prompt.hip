@@ -186,13 +186,14 @@ struct LpState {
     }
     return f;
   }
-  __device__ __forceinline__ void refer(float top, float c2) {  // (as LtState's)
-    const float up = lt_half_max(top) * c2;
-    seen = fmaxf(seen, up);
+  __device__ __forceinline__ void refer(float top) {  // (this and the next three as LtState's)
+    seen = fmaxf(seen, lt_half_max(top));
     m = m == LT_FLOOR ? seen : m;
   }
+  __device__ __forceinline__ bool rose(float c2) const { return (seen - m) * c2 > LT_RISE; }
+  __device__ __forceinline__ float octaves(float c2) const { return fmaxf(m * c2, LT_FLOOR); }
   __device__ __forceinline__ unsigned pair(const lt_floatx16& S, float c2, int e) {
-    const lt_floatx2 p = {exp2_fast(__builtin_fmaf(S[2 * e], c2, -m)), exp2_fast(__builtin_fmaf(S[2 * e + 1], c2, -m))};
+    const lt_floatx2 p = {exp2_fast((S[2 * e] - m) * c2), exp2_fast((S[2 * e + 1] - m) * c2)};
     l += p[0] + p[1];
     return __builtin_bit_cast(unsigned, __builtin_convertvector(p, lt_bf16x2));
   }
@@ -227,7 +228,7 @@ struct LpState {
     float top = fmaxf(S[0], S[1]);
 #pragma unroll
     for (int v = 2; v < 16; ++v) top = fmaxf(top, S[v]);
-    refer(top, c2);
+    refer(top);
     uint4 P0, P1;
     P0.x = pair(S, c2, 0), P0.y = pair(S, c2, 1), P0.z = pair(S, c2, 2), P0.w = pair(S, c2, 3);
     P1.x = pair(S, c2, 4), P1.y = pair(S, c2, 5), P1.z = pair(S, c2, 6), P1.w = pair(S, c2, 7);
@@ -249,7 +250,7 @@ struct LpState {
 #pragma unroll
         for (int v = 5 * n + 1; v < 5 * n + 6; ++v) top = fmaxf(top, S[v]);
       }
-      if (n == 2) refer(top, c2);
+      if (n == 2) refer(top);
       if (n >= 3 && n < 11) w[n - 3] = pair(S, c2, n - 3);
       __builtin_amdgcn_sched_barrier(0);
     }
@@ -406,7 +407,7 @@ __global__ __launch_bounds__(LP_THREADS) void k_lat_prompt(LpArgs gl) {
     // ---- a row whose scores rose too far above its reference?
     if (tid == 0) mem.again = 0;
     lt_meet();
-    if (__ballot(st.seen > st.m + LT_RISE) != 0ull && lane == 0) mem.again = 1;
+    if (__ballot(st.rose(c2)) != 0ull && lane == 0) mem.again = 1;
     lt_meet();
     if (mem.again == 0) break;
     reference = st.seen;
@@ -419,7 +420,7 @@ __global__ __launch_bounds__(LP_THREADS) void k_lat_prompt(LpArgs gl) {
   if (it.n_sp == 1) {
     const float inv = vis == 0 ? 0.f : 1.f / total;  // (a row that sees keys of score -infinity alone is 0 / 0, its logarithm -infinity)
     if (half == 0 && col < mine_rows && a.lse != nullptr)
-      a.lse[row0 + (int64_t)col * a.H] = (st.m + __log2f(total)) * LT_LN2;
+      a.lse[row0 + (int64_t)col * a.H] = (st.octaves(c2) + __log2f(total)) * LT_LN2;
     if (half == 0) mem.out_at[wave][col] = (int64_t)(it.n0 + row) * a.o_row + it.h * a.o_head;
 #pragma unroll
     for (int t = 0; t < LP_NB; ++t)
@@ -439,7 +440,7 @@ __global__ __launch_bounds__(LP_THREADS) void k_lat_prompt(LpArgs gl) {
   const int64_t rec0 = it.rec0 + ((int64_t)(first + 32 * wave) * a.H + it.h) * it.n_sp + it.sp;  // (records: row, head, split)
   if (half == 0 && col < mine_rows) {
     float* const rec = gl.part + (rec0 + (int64_t)col * a.H * it.n_sp) * LP_REC;
-    rec[LP_DV] = st.m;
+    rec[LP_DV] = st.octaves(c2);
     rec[LP_DV + 1] = total;
   }
 #pragma unroll

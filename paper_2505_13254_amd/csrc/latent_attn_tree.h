@@ -41,7 +41,7 @@ constexpr int LT_GROUP = 128;                 // rows of a work item
 constexpr int LT_NK = (LT_R + LT_DR) / 16;    // steps of the first product
 constexpr int LT_MAX_TREE = 1024;
 constexpr float LT_FLOOR = -3e38f;
-constexpr float LT_RISE = 24.f;               // octaves that a score may rise above the reference
+constexpr float LT_RISE = 24.f;               // octaves that a weight may rise above the reference's
 constexpr float LT_LN2 = 0.6931471805599453f, LT_LOG2E = 1.4426950408889634f;
 
 constexpr int LT_ROT = 32 * 2 * LT_R;  // where a tile's rotary parts begin
@@ -123,7 +123,7 @@ template <int NB>
 struct LtState {
   lt_bf16x8 q[LT_NK];  // element 16 i + 8 half + j of step i
   lt_floatx16 acc[NB]; // O^T: column 32 t + 8 (v / 4) + 4 half + v % 4
-  float m, l, seen;    // reference of the scores (octaves), sum of the weights relative to it (of this half-wave's keys), largest score
+  float m, l, seen;    // reference of the scores (products, not scaled yet), sum of the weights relative to it (of this half-wave's keys), largest score
   unsigned k_at, r_at, v_at;  // the lane's places in a tile: of its K row's first chunk, of its rotary part's, of its V rows' (the wave's first column on)
 
   __device__ __forceinline__ void clear(float reference) {
@@ -194,9 +194,8 @@ struct LtState {
   }
   // A row's reference is the largest score of the first tile in which it sees a key, and stays: a weight may be as large as 2^LT_RISE.  `seen` is the
   // largest score so far; where it has risen further, the item is done again with it as the reference.
-  __device__ __forceinline__ void refer(float top, float c2) {
-    const float up = lt_half_max(top) * c2;
-    seen = fmaxf(seen, up);
+  __device__ __forceinline__ void refer(float top) {
+    seen = fmaxf(seen, lt_half_max(top));
     m = m == LT_FLOOR ? seen : m;
   }
   __device__ __forceinline__ float top_of(const lt_floatx16& S) const {
@@ -205,14 +204,18 @@ struct LtState {
     for (int v = 2; v < 16; ++v) top = fmaxf(top, S[v]);
     return top;
   }
-  __device__ __forceinline__ unsigned pair(const lt_floatx16& S, float c2, int e) {  // weights 2 e, 2 e + 1
-    const lt_floatx2 p = {exp2_fast(__builtin_fmaf(S[2 * e], c2, -m)), exp2_fast(__builtin_fmaf(S[2 * e + 1], c2, -m))};
+  __device__ __forceinline__ bool rose(float c2) const { return (seen - m) * c2 > LT_RISE; }
+  __device__ __forceinline__ float octaves(float c2) const { return fmaxf(m * c2, LT_FLOOR); }  // the reference, scaled
+  // Weights 2 e, 2 e + 1.  (The difference comes first: of scores as large as 2^30 octaves a scaled reference is off by the rounding of a product, more octaves
+  // than float32 has, and a fused multiplication would keep them: weights would be infinite, or all zero.)
+  __device__ __forceinline__ unsigned pair(const lt_floatx16& S, float c2, int e) {
+    const lt_floatx2 p = {exp2_fast((S[2 * e] - m) * c2), exp2_fast((S[2 * e + 1] - m) * c2)};
     l += p[0] + p[1];
     return __builtin_bit_cast(unsigned, __builtin_convertvector(p, lt_bf16x2));
   }
   // A tile by itself: its scores (masked ones at -infinity) are S.
   __device__ __forceinline__ void take(char* lds, unsigned tile, const lt_floatx16& S, float c2) {
-    refer(top_of(S), c2);
+    refer(top_of(S));
     uint4 P0, P1;
     P0.x = pair(S, c2, 0), P0.y = pair(S, c2, 1), P0.z = pair(S, c2, 2), P0.w = pair(S, c2, 3);
     P1.x = pair(S, c2, 4), P1.y = pair(S, c2, 5), P1.z = pair(S, c2, 6), P1.w = pair(S, c2, 7);
@@ -250,7 +253,7 @@ struct LtState {
 #pragma unroll
         for (int v = 3 * n + 1; v < 3 * n + 4; ++v) top = fmaxf(top, S[v]);
       }
-      if (n == 5) refer(top, c2);
+      if (n == 5) refer(top);
       if (n >= 8 && n < 32 && (n - 8) % 3 == 0) w[(n - 8) / 3] = pair(S, c2, (n - 8) / 3);
       __builtin_amdgcn_sched_barrier(0);
     }

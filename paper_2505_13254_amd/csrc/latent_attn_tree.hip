@@ -392,7 +392,7 @@ __device__ __forceinline__ void lt_run(const LtArgs& g, const LtItem& it, LtLds&
   // ---- a row whose scores rose too far above its reference?
   if (tid == 0) mem.again = 0;
   lt_meet();
-  if (__ballot(st.seen > st.m + LT_RISE) != 0ull && lane == 0) mem.again = 1;
+  if (__ballot(st.rose(c2)) != 0ull && lane == 0) mem.again = 1;
   lt_meet();
   if (mem.again == 0) break;
   reference = st.seen;
@@ -403,7 +403,7 @@ __device__ __forceinline__ void lt_run(const LtArgs& g, const LtItem& it, LtLds&
 
   // ---- out: the halves of the keys meet, then rows leave by way of LDS
   lt_meet();
-  float total = lt_half_sum(st.l), top = st.m;
+  float total = lt_half_sum(st.l), top = st.octaves(c2);
   constexpr int KEEP = RB == 4 ? NB : NB / 2;  // blocks that the wave writes
   int out_block = first_block;
   if constexpr (RB != 4) {
@@ -414,8 +414,9 @@ __device__ __forceinline__ void lt_run(const LtArgs& g, const LtItem& it, LtLds&
     }
     lt_meet();
     const float m2 = mem.stat[other][0][col], l2 = mem.stat[other][1][col];
-    top = fmaxf(st.m, m2);
-    const float mine = exp2_fast(st.m - top), theirs = exp2_fast(m2 - top);
+    const float own = top;
+    top = fmaxf(own, m2);
+    const float mine = exp2_fast(own - top), theirs = exp2_fast(m2 - top);
     total = total * mine + l2 * theirs;
     float4* const to = reinterpret_cast<float4*>(lds) + wave * (KEEP * 4 * 64) + lane;
     const float4* const from = reinterpret_cast<const float4*>(lds) + other * (KEEP * 4 * 64) + lane;

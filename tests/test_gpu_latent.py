@@ -701,3 +701,55 @@ def test_a_lone_prompt_of_more_rows_than_keys_that_is_cut(hs):
     p.q[:, :, 1] = 1.0
     o, lse = p.call(hs)
     assert (o[:60] == 0).all() and torch.isnan(o[60:]).all() and torch.isneginf(lse).all()
+
+
+# ------------------------------------------------------------------------------------------------ scores of any magnitude
+@pytest.mark.parametrize("power", [20, 30, 33, 40, 60, 100])
+@pytest.mark.parametrize("Hq,sizes,lens", [(16, [1, 1], [0, 64]), (3, [40, 2], [0, 200]), (128, [3, 2], [70, 513])])
+def test_scores_of_any_magnitude(hs, Hq, sizes, lens, power):
+    """Scores far above 2^24 are one-hot: every row's own token has the largest, by a factor, and is the result."""
+    NN = sum(sizes)
+    t = Tree(sizes, lens, Hq, seed=power)
+    t.pool[..., 512:], t.q[:], t.q_rope[:], t.r_tree[:] = 0.0, 0.0, 0.0, 0.0
+    t.q_rope[:, :, 7] = 2.0 ** (power // 2) * 1.3
+    depth = torch.zeros(NN)
+    at = 0
+    for n, parent in zip(sizes, t.parents):
+        for i in range(1, n):
+            depth[at + i] = depth[at + int(parent[i])] + 1
+        at += n
+    t.r_tree[:, 7] = ((1.0 + depth).to(DEV) * 2.0 ** (power - power // 2) * 1.7).to(BF)
+    o, lse = t.call(hs)
+    assert torch.equal(o, t.c_tree[:, None].expand(-1, Hq, -1))
+    x = (t.q_rope.double()[:, :, 7] * t.r_tree.double()[:, None, 7]) * t.scale
+    assert ((lse.double() - x).abs() <= 8 * 2.0 ** -24 * x).all()
+    t.q_rope.neg_()                                       # all scores far below zero: the least of them, the root's, or the prefix's zeros
+    o, lse = t.call(hs)
+    at = 0
+    for s, (n, L) in enumerate(zip(sizes, lens)):
+        if L == 0:
+            assert torch.equal(o[at:at + n], t.c_tree[at:at + 1, None].expand(n, Hq, -1))
+        else:
+            mean = t.prefix[s][:, :512].double().mean(0)
+            size = t.prefix[s][:, :512].double().abs().mean(0)
+            assert ((o[at:at + n].double() - mean).abs() <= 2.0 ** -8 * mean.abs() + (2.0 ** -8 + 2.0 ** -17) * size).all()
+            assert ((lse[at:at + n] - float(np.log(L))).abs() <= 1e-5).all()
+        at += n
+
+
+@pytest.mark.parametrize("power", [20, 30, 33, 40, 60, 100])
+@pytest.mark.parametrize("rows,keys,H", [([1, 64], [1, 64], 3), ([100, 300], [130, 300], 16), ([5, 3], [3000, 2000], 2), ([300, 257], [300, 300], 128)])
+def test_prompt_scores_of_any_magnitude(hs, rows, keys, H, power):
+    """The last key that a row sees has the largest score by 1/64 of it at least: the result is its value."""
+    p = Prompt(rows, keys, H, seed=power)
+    p.q[:], p.q_rope[:], p.k[:], p.k_rope[:] = 0.0, 0.0, 0.0, 0.0
+    p.q[:, :, 9] = 2.0 ** (power // 2) * 1.3
+    ko, qo = p.host_ko.tolist(), p.host_qo.tolist()
+    own = torch.cat([torch.arange(n) + ko[s + 1] - n for s, n in enumerate(rows)]).to(DEV)
+    for s in range(2):                                    # rising in steps that bfloat16 holds: 64 of them to an octave
+        i = torch.arange(keys[s], device=DEV).double()
+        p.k[ko[s]:ko[s + 1], :, 9] = (2.0 ** (power - power // 2 - (keys[s] >> 6) + torch.floor(i / 64)) * (1.0 + (i % 64) / 64)).to(BF)[:, None]
+    o, lse = p.call(hs)
+    assert torch.equal(o, p.v[own])
+    x = p.q.double()[:, :, 9] * p.k.double()[own, :, 9] * p.scale
+    assert ((lse.double() - x).abs() <= 8 * 2.0 ** -24 * x).all()
