@@ -40,7 +40,8 @@
  *
  * Conventions that hold for every call
  *   - Pointers are DEVICE pointers unless the parameter name starts with host_.  The caller owns
- *     every buffer; the library allocates and frees nothing, and keeps nothing after a call.
+ *     every buffer; the library allocates and frees nothing, and keeps nothing after a call but the
+ *     last launch plans of a host thread (where a call plans from host copies; its section says so).
  *   - Scratch memory comes from the caller: `workspace` must be 256-byte aligned, and the bytes the
  *     matching *_workspace query returns for the same shape arguments are always enough (row scan and
  *     accept walk: for calls of fewer rows too).  A call may need less than its query says; a workspace
@@ -665,7 +666,9 @@ hs_status hs_latent_read(const void* pool, int64_t n_slots, const int64_t* slots
  *   with a stride.  pool [n_pages, 64, R + Dr] dense.  All of type dt; float32 sums and softmax, with HS_BF16 P is rounded to bfloat16 for the
  *   second product and the output once.
  *   parent, node_offsets, host_node_offsets, block_table, prefix_lens, host_prefix_lens as in hs_tree_attention_paged; lse [NN,Hq] dense, may be NULL.
- *   The launch is planned from the host copies: they must equal the device arrays, and a captured launch keeps them.
+ *   The launch is planned from the host copies: they must equal the device arrays, and a captured launch keeps them.  Lengths that hs_slot_map left on
+ *   the device have to be read back for them.  Each host thread keeps the last plan of this call and of hs_prompt_attention_latent, by its whole input, for up to 4096
+ *   sequences: a model's layers and a workspace query share it; two batches in turn are planned again each time (2 us for one sequence to 0.2 ms for 4000).
  * A NaN in a token, or an infinity in a latent or an expanded value, reaches the rows that see it and no others: they are not finite, as a whole or in some columns.  An
  * infinity in a rotary part or an expanded key counts by the score that it makes: with -infinity the token has a weight of zero (or is as a NaN, where it is one of the
  * tree's own rows), otherwise the row is NaN.  A row whose scores are all -infinity is NaN.  Scores may have any
@@ -692,7 +695,7 @@ hs_status hs_tree_attention_latent(const void* q, int64_t q_stride, int64_t q_he
  * own.  Row i of n sees the keys 0 .. T - n + i of its T (none where that is negative: o = 0, lse = -infinity):
  *   o[i,h,:] = softmax_j( scale * (<q[i,h,:], k[j,h,:]> + <q_rope[i,h,:], k_rope[j,:]>) ) . v[j,h,:]
  *   q [N,H,Dn], q_rope [N,H,Dr], k [T,H,Dn], v [T,H,Dv], o [N,H,Dv]: row n, head h at base + n * stride + h * head_stride (elements; k and v may be
- *   slices of one product's result).  k_rope [T,Dr]: rows with a stride.  Types, sums, NaN, magnitudes and the host copies as in hs_tree_attention_latent.
+ *   slices of one product's result).  k_rope [T,Dr]: rows with a stride.  Types, sums, NaN, magnitudes, the host copies and the plan as in hs_tree_attention_latent.
  * HS_BF16 with Dn = 128, Dr = 64, Dv = 128, pointers at multiples of 16 bytes, strides of multiples of 8 elements and rows of k, v and k_rope less than 2^23 elements
  * apart runs on the matrix cores and needs the workspace of the query, 528 bytes for each row, head and split of the sequences that the plan cuts, as above; every
  * other call takes the kernel for any shape.

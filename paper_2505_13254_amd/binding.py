@@ -607,7 +607,8 @@ def new_page_tables(B: int, max_blocks: int, n_pages: int, device="cuda:0") -> D
 def hs_block_tables(want, block_table, held, free_pages, free_count, *, page_tokens: int = HS_MX_PAGE, new_held=None, new_free_count=None, refused=None,
                     stream=None):
     """Pages for want[s] tokens (int64 [B], GPU) of every sequence: block_table int32 [B, max_blocks] and free_pages int32 [n_pages] are updated in
-    place, held int32 [B] and free_count int32 [1] are left alone.  refused: int32 [B] or None.  Returns (new_held, new_free_count)."""
+    place, held int32 [B] and free_count int32 [1] are left alone.  refused: int32 [B] or None.  Returns (new_held, new_free_count); of no
+    sequences the count as it was."""
     B = want.numel()
     if block_table.dim() != 2 or block_table.shape[0] != B or held.numel() != B:
         raise ValueError("block_table must be [B, max_blocks], held [B]")

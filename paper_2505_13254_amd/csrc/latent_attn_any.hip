@@ -7,7 +7,7 @@
 // in its value does.  The waves' sums meet in LDS.
 //
 // Bound by the vector pipe and by reads of a key a lane: what float32, and shapes without matrix-core kernels, take.
-// (bfloat16, one row of 16 heads on 2048 tokens of 512 + 64: 664 us, where the matrix cores take 15.)
+// (bfloat16, one row of 16 heads on 2048 tokens of 512 + 64: 642 us, where the matrix cores take 15.)
 #include "latent_attn.h"
 
 namespace hs {

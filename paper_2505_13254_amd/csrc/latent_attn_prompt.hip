@@ -536,8 +536,8 @@ bool lat_prompt_matrix(const LatPromptArgs& a, hs_dtype dt) {
          a.v.row < FAR && a.k_rope_row < FAR;
 }
 
-// Rows of a group and tiles of a split, by estimated times.  (Groups of 128 for calls of few items: 660 rows of 20 heads 29.6 -> 19.1 us, 3468 of 16 heads
-// 106 -> 76; where the items fill the chip, groups of 256: 8192 rows of 32 heads 640 us, of 128 724.)
+// Rows of a group and tiles of a split, by estimated times.  (Groups of 128 for calls of few items: 660 rows of 20 heads 29.6 -> 19.3 us, 3468 of 16 heads
+// 106 -> 82; where the items fill the chip, groups of 256: 8192 rows of 32 heads 640 us, of 128 724.)
 LatPlan lat_prompt_plan(const int32_t* qo, const int64_t* ko, int32_t B, int32_t H) {
   int64_t longest = 1;
   for (int s = 0; s < B; ++s)

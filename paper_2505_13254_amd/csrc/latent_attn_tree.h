@@ -5,13 +5,13 @@
 // lane and its other half, and P is born in the layout that the second product takes).
 //
 // A workgroup has four waves, one to a SIMD with all of its 512 registers: 32 queries a wave take 144 registers for Q and 256 for O.  Rows (a
-// sequence's tree row and head) are dealt in groups of 128.  What a group's waves share depends on how many 32-row blocks it has:
+// sequence's tree row and head) are dealt in groups of 128, or of 64 or 32 where a call has few items.  What a group's waves share depends on how many 32-row blocks it has:
 //   RB = 4 (65 .. 128 rows)  a block each, every key; the scores of the next tile run beside the softmax of this one
 //   RB = 2 (33 .. 64)        two waves a block, each with one half of every 64-key page
 //   RB = 1 (up to 32)        four waves a block: a half of the page and a half of the columns (scores computed twice)
 // The latter two are bound by the stream of pages, not by what the waves do.
 // Measured: RB = 4, 4 x 97 rows of 64 heads on 8192 tokens, 1.06 to 1.1 PFLOP/s, the chip's power (a product of 8192^3 by the library: 1.22); RB = 1, 64 rows of
-// 16 heads on 4451 pages, 5.0 TB/s over the whole call (a copy of 4 GiB: 4.8); one row of 16 heads on 2048 tokens 12 us, of which 4 until the last workgroup starts,
+// 16 heads on 4451 pages, 5.1 TB/s over the whole call (a kernel that only reads: 6.4); one row of 16 heads on 2048 tokens 12 us, of which 4 until the last workgroup starts,
 // 6 until Q and the first page are there, and 4 for two pages.
 //
 // LDS: a ring of four 32-key tiles, which global_load_lds fills.  A tile is its rows' latents, 1024 bytes each, and behind them their rotary parts, 128 bytes

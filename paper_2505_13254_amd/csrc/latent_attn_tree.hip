@@ -609,7 +609,7 @@ bool lat_tree_matrix(const LatTreeArgs& a, hs_dtype dt) {
          fits(a.pool, 0, 0) && fits(a.c_tree, a.c_stride, 0) && fits(a.r_tree, a.r_stride, 0) && fits(a.o, a.o_row, a.o_head);
 }
 
-// Pages of a split, by estimated times.  (Constants fitted to calls with the group size forced: 100 rows of 16 heads on 8414 tokens 128 rows 56 us, 64 rows 69, 32 rows 129; 50 rows
+// Pages of a split, by estimated times.  (Constants fitted to calls with the group size forced: 100 rows of 16 heads on 8414 tokens 128 rows 56 to 58 us, 64 rows 69, 32 rows 129; 50 rows
 // of 20 heads on 102 tokens 24, 21 and 18.)
 LatPlan lat_tree_plan(const int32_t* no, const int64_t* pl, int32_t B, int32_t Hq) {
   int64_t longest = 1, widest = 0;

@@ -1,8 +1,8 @@
 // hs_latent_store, hs_latent_read: rows of latents into and out of a pool, by slots.
 //
 // A row is R + Dr elements, which come from (go to) two tensors: the latent and the rotary part.  Copies of 16 bytes a thread:
-// bound by memory, each row's bytes once in and once out: 30528 rows of 1152 bytes go in in 13.4 us and out in 13.2
-// (5.3 TB/s, counting both sides).
+// bound by memory, each row's bytes once in and once out: 30528 rows of 1152 bytes go in in 14.2 us and out in 13.5
+// (5.0 and 5.2 TB/s, counting both sides).
 #include "attn_common.h"
 
 namespace hs {

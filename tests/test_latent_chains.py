@@ -55,3 +55,48 @@ def test_no_copy_between_the_steps_of_a_chain(tmp_path):
     subprocess.check_call([exe] + B.FLAGS + ["--cuda-device-only", "-S", os.path.join(B.CSRC, "latent_attn_tree.hip"), "-o", out], stderr=subprocess.DEVNULL)
     chains, bad = _broken_chains(open(out).read())
     assert chains >= 6 and not bad, bad[:3]
+
+
+def _in_loops(assembly, kernel, wanted):
+    """Lines with `wanted` that lie on a cycle of the kernel's control flow: they are reached again from themselves."""
+    lines = assembly.split("\n")
+    start = next(n for n, line in enumerate(lines) if re.match(r"^\S*%s\S*:" % kernel, line))
+    end = next(n for n in range(start, len(lines)) if ".Lfunc_end" in lines[n])
+    code = [line.split(";")[0].strip() for line in lines[start:end]]
+    label = {c[:-1]: n for n, c in enumerate(code) if c.endswith(":")}
+
+    def after(n):
+        jump = re.match(r"(s_c?branch\w*)\s+(\S+)", code[n])
+        to = [label[jump.group(2)]] if jump else []
+        return to + ([n + 1] if n + 1 < len(code) and not code[n].startswith(("s_endpgm", "s_branch")) else [])
+
+    bad = []
+    for n in [n for n, c in enumerate(code) if wanted in c]:
+        seen, todo = set(), after(n)
+        while todo:
+            x = todo.pop()
+            if x not in seen:
+                seen.add(x)
+                todo += after(x)
+        if n in seen:
+            bad.append(code[n])
+    return bad
+
+
+def test_the_check_sees_a_loop():
+    text = "k_x:\n\tscratch_load_dword v1, off, off\n.LBB0_1:\n\tv_mov_b32 v0, v1\n\ts_cbranch_scc1 .LBB0_1\n\ts_endpgm\n.Lfunc_end0:\n"
+    assert not _in_loops(text, "k_x", "scratch_")
+    assert _in_loops(text.replace("v_mov_b32 v0, v1", "scratch_store_dword off, v1, off"), "k_x", "scratch_")
+
+
+def test_no_register_is_kept_in_memory_inside_a_loop(tmp_path):
+    """A load from there would wait for every tile on its way."""
+    try:
+        exe = B.hipcc()
+    except RuntimeError:
+        pytest.skip("no hipcc")
+    out = str(tmp_path / "a.s")
+    subprocess.check_call([exe] + B.FLAGS + ["--cuda-device-only", "-S", os.path.join(B.CSRC, "latent_attn_tree.hip"), "-o", out], stderr=subprocess.DEVNULL)
+    text = open(out).read()
+    for most in (1, 2, 4):
+        assert not _in_loops(text, "k_lat_treeILi%dE" % most, "scratch_"), most
