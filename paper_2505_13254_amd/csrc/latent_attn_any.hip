@@ -14,7 +14,7 @@ namespace hs {
 
 constexpr int LA_THREADS = 256, LA_WAVES = 4;
 constexpr int LA_MOST = 1024;  // columns of a value
-constexpr float LA_FLOOR = -3e38f;
+constexpr float LA_FLOOR = -__FLT_MAX__;
 
 template <typename T>
 __device__ __forceinline__ float la_at(const T* p, int64_t i);

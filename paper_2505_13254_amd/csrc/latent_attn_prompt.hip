@@ -186,12 +186,11 @@ struct LpState {
     }
     return f;
   }
-  __device__ __forceinline__ void refer(float top) {  // (this and the next three as LtState's)
+  __device__ __forceinline__ void refer(float top) {  // (this and the next two as LtState's)
     seen = fmaxf(seen, lt_half_max(top));
     m = m == LT_FLOOR ? seen : m;
   }
   __device__ __forceinline__ bool rose(float c2) const { return (seen - m) * c2 > LT_RISE; }
-  __device__ __forceinline__ float octaves(float c2) const { return fmaxf(m * c2, LT_FLOOR); }
   __device__ __forceinline__ unsigned pair(const lt_floatx16& S, float c2, int e) {
     const lt_floatx2 p = {exp2_fast((S[2 * e] - m) * c2), exp2_fast((S[2 * e + 1] - m) * c2)};
     l += p[0] + p[1];
@@ -420,7 +419,7 @@ __global__ __launch_bounds__(LP_THREADS) void k_lat_prompt(LpArgs gl) {
   if (it.n_sp == 1) {
     const float inv = vis == 0 ? 0.f : 1.f / total;  // (a row that sees keys of score -infinity alone is 0 / 0, its logarithm -infinity)
     if (half == 0 && col < mine_rows && a.lse != nullptr)
-      a.lse[row0 + (int64_t)col * a.H] = (st.octaves(c2) + __log2f(total)) * LT_LN2;
+      a.lse[row0 + (int64_t)col * a.H] = st.m * a.scale + __log2f(total) * LT_LN2;
     if (half == 0) mem.out_at[wave][col] = (int64_t)(it.n0 + row) * a.o_row + it.h * a.o_head;
 #pragma unroll
     for (int t = 0; t < LP_NB; ++t)
@@ -440,7 +439,7 @@ __global__ __launch_bounds__(LP_THREADS) void k_lat_prompt(LpArgs gl) {
   const int64_t rec0 = it.rec0 + ((int64_t)(first + 32 * wave) * a.H + it.h) * it.n_sp + it.sp;  // (records: row, head, split)
   if (half == 0 && col < mine_rows) {
     float* const rec = gl.part + (rec0 + (int64_t)col * a.H * it.n_sp) * LP_REC;
-    rec[LP_DV] = st.octaves(c2);
+    rec[LP_DV] = st.m;
     rec[LP_DV + 1] = total;
   }
 #pragma unroll
@@ -509,12 +508,12 @@ __global__ __launch_bounds__(LPM_THREADS) void k_lat_prompt_merge(LpArgs gl) {
       rl[x] = r[LP_DV + 1];
       v[x] = *reinterpret_cast<const float4*>(r + 4 * lane);
     }
-    const float up = fmaxf(fmaxf(m, fmaxf(rm[0], rm[1])), fmaxf(rm[2], rm[3])), old = exp2_fast(m - up);
+    const float up = fmaxf(fmaxf(m, fmaxf(rm[0], rm[1])), fmaxf(rm[2], rm[3])), old = exp2_fast((m - up) * gl.c2);
     total *= old, o.x *= old, o.y *= old, o.z *= old, o.w *= old;
     m = up;
 #pragma unroll
     for (int x = 0; x < 4; ++x) {
-      const float w = x0 + x < n_sp ? exp2_fast(rm[x] - m) : 0.f;
+      const float w = x0 + x < n_sp ? exp2_fast((rm[x] - m) * gl.c2) : 0.f;
       if (x0 + x >= n_sp) break;
       total = __builtin_fmaf(w, rl[x], total);
       o.x = __builtin_fmaf(w, v[x].x, o.x), o.y = __builtin_fmaf(w, v[x].y, o.y), o.z = __builtin_fmaf(w, v[x].z, o.z), o.w = __builtin_fmaf(w, v[x].w, o.w);
@@ -524,7 +523,7 @@ __global__ __launch_bounds__(LPM_THREADS) void k_lat_prompt_merge(LpArgs gl) {
   *reinterpret_cast<uint2*>(static_cast<bf16_t*>(a.o) + n * a.o_row + h * a.o_head + 4 * lane) =
       make_uint2(__builtin_bit_cast(unsigned, __builtin_convertvector((lt_floatx2{o.x * inv, o.y * inv}), lt_bf16x2)),
                  __builtin_bit_cast(unsigned, __builtin_convertvector((lt_floatx2{o.z * inv, o.w * inv}), lt_bf16x2)));
-  if (lane == 0 && a.lse != nullptr) a.lse[row] = (m + __log2f(total)) * LT_LN2;
+  if (lane == 0 && a.lse != nullptr) a.lse[row] = m * a.scale + __log2f(total) * LT_LN2;
 }
 
 // ------------------------------------------------------------------------------------------------ the host's part

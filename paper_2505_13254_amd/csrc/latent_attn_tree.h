@@ -40,7 +40,7 @@ constexpr int LT_LOADS = LT_TILE / 1024 / 4;  // to a wave, for a tile
 constexpr int LT_GROUP = 128;                 // rows of a work item
 constexpr int LT_NK = (LT_R + LT_DR) / 16;    // steps of the first product
 constexpr int LT_MAX_TREE = 1024;
-constexpr float LT_FLOOR = -3e38f;
+constexpr float LT_FLOOR = -__FLT_MAX__;  // no score yet
 constexpr float LT_RISE = 24.f;               // octaves that a weight may rise above the reference's
 constexpr float LT_LN2 = 0.6931471805599453f, LT_LOG2E = 1.4426950408889634f;
 
@@ -205,9 +205,8 @@ struct LtState {
     return top;
   }
   __device__ __forceinline__ bool rose(float c2) const { return (seen - m) * c2 > LT_RISE; }
-  __device__ __forceinline__ float octaves(float c2) const { return fmaxf(m * c2, LT_FLOOR); }  // the reference, scaled
-  // Weights 2 e, 2 e + 1.  (The difference comes first: of scores as large as 2^30 octaves a scaled reference is off by the rounding of a product, more octaves
-  // than float32 has, and a fused multiplication would keep them: weights would be infinite, or all zero.)
+  // Weights 2 e, 2 e + 1.  (The difference comes first, here and in the merges: of scores as large as 2^30 octaves a scaled reference is off by the rounding of a product, more
+  // octaves than float32 has, and a fused multiplication would keep them: weights would be infinite, or all zero.  Still larger ones have no octaves in float32.)
   __device__ __forceinline__ unsigned pair(const lt_floatx16& S, float c2, int e) {
     const lt_floatx2 p = {exp2_fast((S[2 * e] - m) * c2), exp2_fast((S[2 * e + 1] - m) * c2)};
     l += p[0] + p[1];

@@ -403,7 +403,7 @@ __device__ __forceinline__ void lt_run(const LtArgs& g, const LtItem& it, LtLds&
 
   // ---- out: the halves of the keys meet, then rows leave by way of LDS
   lt_meet();
-  float total = lt_half_sum(st.l), top = st.octaves(c2);
+  float total = lt_half_sum(st.l), top = st.m;
   constexpr int KEEP = RB == 4 ? NB : NB / 2;  // blocks that the wave writes
   int out_block = first_block;
   if constexpr (RB != 4) {
@@ -416,7 +416,7 @@ __device__ __forceinline__ void lt_run(const LtArgs& g, const LtItem& it, LtLds&
     const float m2 = mem.stat[other][0][col], l2 = mem.stat[other][1][col];
     const float own = top;
     top = fmaxf(own, m2);
-    const float mine = exp2_fast(own - top), theirs = exp2_fast(m2 - top);
+    const float mine = exp2_fast((own - top) * c2), theirs = exp2_fast((m2 - top) * c2);
     total = total * mine + l2 * theirs;
     float4* const to = reinterpret_cast<float4*>(lds) + wave * (KEEP * 4 * 64) + lane;
     const float4* const from = reinterpret_cast<const float4*>(lds) + other * (KEEP * 4 * 64) + lane;
@@ -448,7 +448,7 @@ __device__ __forceinline__ void lt_run(const LtArgs& g, const LtItem& it, LtLds&
   const int64_t row0 = (int64_t)it.n0 * a.Hq + row_base, rec0 = it.rec0 + (int64_t)row_base * it.n_sp + it.sp;  // (records: row, then split)
   if (it.n_sp == 1) {
     const float inv = 1.f / total;
-    if (writes_stat && a.lse != nullptr) a.lse[row0 + col] = (top + __log2f(total)) * LT_LN2;
+    if (writes_stat && a.lse != nullptr) a.lse[row0 + col] = top * a.scale + __log2f(total) * LT_LN2;
 #pragma unroll
     for (int t = 0; t < KEEP; ++t)
 #pragma unroll
@@ -556,7 +556,7 @@ __global__ __launch_bounds__(LTM_THREADS) void k_lat_tree_merge(LtArgs g) {
       v[x][0] = *reinterpret_cast<const float4*>(r + 8 * lane);
       v[x][1] = *reinterpret_cast<const float4*>(r + 8 * lane + 4);
     }
-    const float up = fmaxf(fmaxf(m, fmaxf(rm[0], rm[1])), fmaxf(rm[2], rm[3])), old = exp2_fast(m - up);  // (records that stand for no split repeat the last)
+    const float up = fmaxf(fmaxf(m, fmaxf(rm[0], rm[1])), fmaxf(rm[2], rm[3])), old = exp2_fast((m - up) * g.c2);  // (records that stand for no split repeat the last)
     total *= old;
 #pragma unroll
     for (int e = 0; e < 8; ++e) acc[e] *= old;
@@ -564,7 +564,7 @@ __global__ __launch_bounds__(LTM_THREADS) void k_lat_tree_merge(LtArgs g) {
 #pragma unroll
     for (int x = 0; x < 4; ++x) {
       if (x0 + x * SHARE >= n_sp) break;
-      const float w = exp2_fast(rm[x] - m);
+      const float w = exp2_fast((rm[x] - m) * g.c2);
       const float f[8] = {v[x][0].x, v[x][0].y, v[x][0].z, v[x][0].w, v[x][1].x, v[x][1].y, v[x][1].z, v[x][1].w};
       total = __builtin_fmaf(w, rl[x], total);
 #pragma unroll
@@ -581,13 +581,13 @@ __global__ __launch_bounds__(LTM_THREADS) void k_lat_tree_merge(LtArgs g) {
     float up = m;
 #pragma unroll
     for (int w = 1; w < SHARE; ++w) up = fmaxf(up, sums[w][lane][8]);
-    const float own = exp2_fast(m - up);
+    const float own = exp2_fast((m - up) * g.c2);
     total *= own;
 #pragma unroll
     for (int e = 0; e < 8; ++e) acc[e] *= own;
 #pragma unroll
     for (int w = 1; w < SHARE; ++w) {
-      const float f = exp2_fast(sums[w][lane][8] - up);
+      const float f = exp2_fast((sums[w][lane][8] - up) * g.c2);
       total = __builtin_fmaf(f, sums[w][lane][9], total);
 #pragma unroll
       for (int e = 0; e < 8; ++e) acc[e] = __builtin_fmaf(f, sums[w][lane][e], acc[e]);
@@ -599,7 +599,7 @@ __global__ __launch_bounds__(LTM_THREADS) void k_lat_tree_merge(LtArgs g) {
 #pragma unroll
   for (int x = 0; x < 4; ++x) w[x] = __builtin_bit_cast(unsigned, __builtin_convertvector((lt_floatx2{acc[2 * x] * inv, acc[2 * x + 1] * inv}), lt_bf16x2));
   *reinterpret_cast<uint4*>(static_cast<bf16_t*>(a.o) + n * a.o_row + h * a.o_head + 8 * lane) = make_uint4(w[0], w[1], w[2], w[3]);
-  if (lane == 0 && a.lse != nullptr) a.lse[row] = (m + __log2f(total)) * LT_LN2;
+  if (lane == 0 && a.lse != nullptr) a.lse[row] = m * a.scale + __log2f(total) * LT_LN2;
 }
 
 // ------------------------------------------------------------------------------------------------ the host's part

@@ -753,3 +753,32 @@ def test_prompt_scores_of_any_magnitude(hs, rows, keys, H, power):
     assert torch.equal(o, p.v[own])
     x = p.q.double()[:, :, 9] * p.k.double()[own, :, 9] * p.scale
     assert ((lse.double() - x).abs() <= 8 * 2.0 ** -24 * x).all()
+
+
+@pytest.mark.parametrize("sign", [-1.0, 1.0])
+@pytest.mark.parametrize("R,Dr,dtype", [(512, 64, BF), (96, 32, F32)])
+@pytest.mark.parametrize("L", [0, 70])
+def test_scores_next_to_the_largest_float(hs, L, R, Dr, dtype, sign):
+    """Products of 1.9 * 2^127, with a scale of 1: a row that sees nothing else is its own token, and one that sees a prefix of zero scores the prefix's mean or its own token."""
+    t = Tree([1, 1], [L, L], 3, R, Dr, dtype, seed=L)
+    t.pool[..., R:], t.q[:], t.q_rope[:], t.r_tree[:] = 0.0, 0.0, 0.0, 0.0
+    t.q_rope[:, :, 7], t.r_tree[:, 7], t.scale = 2.0 ** 64, sign * 1.8984375 * 2.0 ** 63, 0.25
+    o, lse = t.call(hs)
+    t.scale = 1.0
+    for got, scale in ((o, 0.25), (t.call(hs)[0], 1.0)):
+        if L == 0 or sign > 0:
+            assert torch.equal(got, t.c_tree[:, None].expand(-1, 3, -1)), scale
+        else:
+            for s in range(2):
+                x = t.prefix[s][:, :R].double()
+                assert ((got[s].double() - x.mean(0)).abs() <= 2.0 ** -8 * x.mean(0).abs() + 2.0 ** -7 * x.abs().mean(0)).all(), scale
+    x = sign * 1.8984375 * 2.0 ** 125 if L == 0 or sign > 0 else float(np.log(L))
+    assert ((lse.double() - x).abs() <= 8 * 2.0 ** -24 * abs(x)).all()
+
+
+def test_prompt_scores_next_to_the_largest_float(hs):
+    p = Prompt([3, 1], [3, 1], 3, seed=1)
+    p.q[:], p.q_rope[:], p.k[:], p.k_rope[:] = 0.0, 0.0, 0.0, 0.0
+    p.q[:, :, 9], p.k[:, :, 9], p.scale = 2.0 ** 64, -1.8984375 * 2.0 ** 63, 1.0
+    o, _ = p.call(hs)
+    assert torch.equal(o[[0, 3]], p.v[[0, 3]]) and torch.isfinite(o).all()
